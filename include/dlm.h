@@ -352,6 +352,233 @@ dlm_status dlm_cascade(dlm_model* drafter, dlm_model* refiner, int32_t batch, in
                        size_t workspace_bytes, void* hip_stream, dlm_cascade_stats* h_stats);
 
 /*
+ * Rotary positions.
+ *
+ * A head of head_dim values holds rot_dim / 2 pairs (a, b) in its first
+ * rot_dim values; the others pass through.  The pair i of a row at position p
+ * (int32, any sign) becomes
+ *     a' = scale * (a cos(p w_i) - b sin(p w_i)),
+ *     b' = scale * (b cos(p w_i) + a sin(p w_i)),
+ * with pairs of values i and i + rot_dim / 2 (interleaved == 0) or 2 i and
+ * 2 i + 1 (interleaved != 0).  w_i = theta^(-2 i / rot_dim), changed for
+ * contexts `factor` times as long as original_len by
+ *   DLM_ROPE_LINEAR  w_i / factor;
+ *   DLM_ROPE_NTK     theta * factor^(rot_dim / (rot_dim - 2)) in place of
+ *                    theta (rot_dim >= 4);
+ *   DLM_ROPE_YARN    by parts (YaRN, Peng et al. 2023): with r_i =
+ *                    original_len w_i / (2 pi) turns in the original context
+ *                    and g_i = clamp((r_i - beta_slow) / (beta_fast -
+ *                    beta_slow), 0, 1), w_i becomes g_i w_i + (1 - g_i) w_i /
+ *                    factor, and scale is 0.1 ln(factor) + 1 unless given.
+ * scale 0 in the spec stands for that default (1 for the other kinds).
+ *
+ * dlm_rope_init fills *out, a plain host structure without pointers, that the
+ * caller keeps and passes on; no device memory belongs to it.  phase[i] is w_i
+ * / (2 pi) as a fraction of 2^64: a position times it, modulo 2^64, is the
+ * angle's fraction of a turn exactly, so far positions lose nothing.
+ *
+ * dlm_rope_apply: rows x heads x head_dim values of `dtype` at d_x (element
+ * (r, h, c) at r * x_row_stride + h * x_head_stride + c, strides in elements),
+ * rotated into d_y with its own strides; d_y may be d_x with the same strides.
+ * d_pos int32 [rows].  transpose != 0 turns the other way (scale and all): the
+ * gradient with respect to x of a rotation, given that of its result.
+ * Computed in float32, rounded once.  Strides are not negative; rows and heads
+ * of y must not overlap, those of x may (stride 0: one row for all).
+ */
+typedef enum { DLM_BF16 = 0, DLM_F16 = 1, DLM_F32 = 2 } dlm_dtype;
+typedef enum { DLM_ROPE_PLAIN = 0, DLM_ROPE_LINEAR = 1, DLM_ROPE_NTK = 2, DLM_ROPE_YARN = 3 } dlm_rope_scaling;
+#define DLM_ROPE_MAX_PAIRS 128
+
+typedef struct dlm_rope_spec {
+    int32_t head_dim;          /* 2 .. 256                                       */
+    int32_t rot_dim;           /* even, 2 .. head_dim                            */
+    int32_t interleaved;
+    int32_t scaling;           /* dlm_rope_scaling                               */
+    int32_t original_len;      /* DLM_ROPE_YARN: > 0                             */
+    float scale;               /* >= 0; 0 = the kind's own                       */
+    double theta;              /* > 0                                            */
+    double factor;             /* >= 1 unless DLM_ROPE_PLAIN                     */
+    double beta_slow;          /* DLM_ROPE_YARN: 0 <= beta_slow < beta_fast      */
+    double beta_fast;
+} dlm_rope_spec;
+
+typedef struct dlm_rope {
+    int32_t head_dim;
+    int32_t rot_dim;
+    int32_t interleaved;
+    float scale;
+    uint64_t phase[DLM_ROPE_MAX_PAIRS];
+} dlm_rope;
+
+dlm_status dlm_rope_init(const dlm_rope_spec* spec, dlm_rope* out);
+dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int32_t heads, const void* d_x,
+                          int64_t x_row_stride, int64_t x_head_stride, void* d_y, int64_t y_row_stride,
+                          int64_t y_head_stride, const int32_t* d_pos, int32_t transpose, void* hip_stream);
+
+/*
+ * A paged key/value cache, shared by sequences and by alternative drafts.
+ *
+ * The caller owns every buffer; dlm_cache is a host structure that names them.
+ * Pages hold page_len tokens; d_k and d_v (dtype DLM_BF16 or DLM_F16, 256-byte
+ * aligned) are [n_layers][n_pages][n_kv_heads][page_len][head_dim].  Row s of
+ * d_table lists the pages of sequence s in order (-1: none), d_len[s] counts
+ * its tokens, d_ref[p] the table entries that name page p (0: free).  Token t
+ * of a sequence sits in entry t / page_len, place t % page_len.
+ *
+ * A window is the rows that a pass works on behind a sequence's d_len tokens:
+ * one token, a prompt, a block, a tree of drafted tokens, or several drafts of
+ * a block side by side.  Windows of a batch are packed: row i of sequence s is
+ * row d_row_start[s] + i of the row tensors (d_row_start int32 [n_seqs + 1],
+ * not decreasing, within 0 .. total_rows; at most max_rows rows per sequence,
+ * none for a sequence that sits the pass out).  A pass is
+ *   dlm_cache_reserve   room for every window, pages of its own to write to;
+ *   per layer: dlm_cache_append (window row i becomes token d_len + i, not yet
+ *                        counted) and dlm_cache_attend;
+ *   dlm_cache_commit    the rows to keep move to the front of the window and
+ *                        count; the pages behind them are freed.
+ * dlm_cache_step is such a pass (without the first and the last) of a model.
+ *
+ * Nothing waits for the device, so lengths and tables are the device's, and
+ * cannot be checked by the host.  The kernels never touch memory outside the
+ * buffers whatever they hold: rows, lengths and entries out of range are cut
+ * off, keys in an entry that names no page of the pool are seen by no row, and
+ * rows appended there are dropped.  d_ok outputs (int32, may be NULL) say per
+ * sequence or pair whether an operation took place (1) or was left out whole
+ * (0).  All calls that share a cache or a workspace must be ordered on one
+ * stream (or by events); they may be captured in a HIP graph.
+ * d_workspace: dlm_cache_workspace_bytes(cache, max total_rows, max_rows,
+ * n_heads) bytes, 256-byte aligned; it keeps nothing between calls.
+ *
+ * Limits: head_dim 64 or 128; page_len 16, 32, 64 or 128; n_pages <= 2^20;
+ * n_seqs <= 1024; max_pages * page_len <= 2^26; n_kv_heads <= 128.
+ */
+typedef struct dlm_cache {
+    int32_t dtype;
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t page_len;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t n_seqs;
+    int32_t max_pages;         /* entries of a table row                         */
+    void* d_k;
+    void* d_v;
+    int32_t* d_ref;            /* [n_pages]                                      */
+    int32_t* d_len;            /* [n_seqs]                                       */
+    int32_t* d_table;          /* [n_seqs][max_pages]                            */
+} dlm_cache;
+
+size_t dlm_cache_workspace_bytes(const dlm_cache* cache, int32_t total_rows, int32_t max_rows, int32_t n_heads);
+
+/* Empty every sequence and free every page. */
+dlm_status dlm_cache_reset(const dlm_cache* cache, void* hip_stream);
+
+/*
+ * Room for the windows: entries of tokens d_len .. d_len + rows - 1 that name
+ * no page get one, and those that name a page with more than one reference get
+ * one of their own in its place (its tokens below d_len copied, in every
+ * layer).  Sequences are served in order, each with the free pages of lowest
+ * id; the first that no longer fits, and all after it that need a page, are
+ * left as they were, as is one whose tokens would pass its table row.  A page
+ * whose last reference goes with the call is free for the next one.
+ */
+dlm_status dlm_cache_reserve(const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows, int32_t* d_ok,
+                             void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Keys and values of the windows' rows into their pages in one layer, keys (and
+ * the queries that come with them) rotated.  d_k / d_v: row r, head h at r *
+ * stride + h * head_dim (strides in elements), of src_dtype: the cache's dtype
+ * or DLM_F32.  rope NULL: no rotation.  d_pos int32 [total_rows]: positions for
+ * the rotation, NULL for d_len + i (a tree's tokens pass their own depth).
+ * d_q (may be NULL): n_heads queries per row, of src_dtype, rotated into
+ * d_q_out of the cache's dtype (may be d_q if the types are equal).  Computed in
+ * float32, rounded once.
+ */
+dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                            int32_t max_rows, int32_t src_dtype, const void* d_k, int64_t k_stride, const void* d_v,
+                            int64_t v_stride, const dlm_rope* rope, const int32_t* d_pos, int32_t n_heads,
+                            const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, void* hip_stream);
+
+/*
+ * Attention of the windows' rows in one layer: a row sees its sequence's d_len
+ * tokens and those rows j of its own window whose bit is set (bit j % 32 of word
+ * j / 32 of its mask_words words, mask_words * 32 >= max_rows; d_mask NULL:
+ * every row of the window).  d_q, d_o: row r, head h at r * stride + h *
+ * head_dim, of the cache's dtype, 16-byte aligned, strides in elements and
+ * multiples of 8; d_o may be d_q.  n_heads a multiple of n_kv_heads: query head
+ * h reads key head h / (n_heads / n_kv_heads).  scale > 0, or 0 for 1 /
+ * sqrt(head_dim).  max_keys: an upper bound of d_len + rows that the caller
+ * vouches for (later keys are not read), or 0 for what a table row can hold; the
+ * work is spread by it.  d_lse float [total_rows][n_heads] (may be NULL): log
+ * of the sum of exp(scale * q . k).  A row that sees no key gives zeros and
+ * -infinity.  What a row does not see does not change it, whatever it holds.
+ * Rows of d_o behind the last window keep their values.  Scores, softmax and
+ * sums are float32, probabilities are rounded to the cache's dtype for the
+ * product with V.
+ */
+dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                            int32_t max_rows, int32_t max_keys, int32_t n_heads, const void* d_q, int64_t q_stride,
+                            const uint32_t* d_mask, int32_t mask_words, float scale, void* d_o, int64_t o_stride,
+                            float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * End of a pass: of a sequence's window the rows d_keep[d_keep_start[s]] ..
+ * (rising, d_keep_start int32 [n_seqs + 1] within 0 .. total_keep) become its
+ * next tokens, in every layer, and the pages behind them are freed.  d_keep and
+ * d_keep_start NULL: every row.  Left out whole (ok 0): a list that does not rise
+ * within the window, a window without its pages, tokens that would move into a
+ * page with other references.  A sequence without rows is left as it is (ok 1).
+ */
+dlm_status dlm_cache_commit(const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                            const int32_t* d_keep, const int32_t* d_keep_start, int32_t total_keep, int32_t* d_ok,
+                            void* hip_stream);
+
+/*
+ * Sequence d_dst[i] becomes a copy of d_src[i] that shares its pages (those of
+ * its d_len tokens; what d_dst[i] held is freed first).  Left out (ok 0): an
+ * index out of range, a d_dst that is also some pair's d_src or another pair's
+ * d_dst.  n_pairs <= 1024.
+ */
+dlm_status dlm_cache_fork(const dlm_cache* cache, int32_t n_pairs, const int32_t* d_src, const int32_t* d_dst,
+                          int32_t* d_ok, void* hip_stream);
+
+/*
+ * Sequence s keeps at most d_new_len[s] tokens; its pages behind them, and those
+ * reserved and not used, are freed.  A negative length leaves it alone.
+ * d_new_len NULL: 0 for every sequence.
+ */
+dlm_status dlm_cache_truncate(const dlm_cache* cache, const int32_t* d_new_len, void* hip_stream);
+
+/*
+ * The pages in use move to the lowest ids (those with an id past their number,
+ * in order, into the free ones below it, in order), in every layer, and tables
+ * and references follow.  d_n_used int32 (may be NULL): their number.
+ */
+dlm_status dlm_cache_compact(const dlm_cache* cache, int32_t* d_n_used, void* d_workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/*
+ * A model's pass over windows behind a cache: the refiner's forward on
+ * total_rows packed rows, whose keys and values go into the reserved places and
+ * whose queries see what dlm_cache_attend says, then the vocabulary reduction of
+ * every row.  d_tokens int32 [total_rows] ([MASK] allowed); d_pos, d_mask,
+ * mask_words, max_keys as above; a window with d_mask NULL is a block that sees
+ * itself and everything before it, so a prompt, then blocks, is block-AR
+ * drafting's visibility.  The cache has the model's layers and key heads, and
+ * dtype DLM_BF16.  Rows that no window covers are computed without meaning.
+ * d_top1 int32, d_conf float, d_max_logit float [total_rows] as
+ * dlm_draft_step, each may be NULL.  d_n_invalid int32 (may be NULL): token ids
+ * outside [0, vocab); they are read as a valid one.
+ */
+size_t dlm_cache_step_workspace_bytes(const dlm_config* cfg, const dlm_cache* cache, int32_t total_rows,
+                                      int32_t max_rows);
+dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                          int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                          const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                          void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid);
+
+/*
  * Test hooks (same kernels as dlm_refine_step, intermediate results exposed).
  *
  * dlm_debug_forward: forward over d_tokens without the reduction; writes the

@@ -3,13 +3,14 @@
 One refinement pass: a non-causal transformer forward over prompt+draft, a
 fused per-position top-1/confidence reduction over the vocabulary, and the
 threshold edit/unmask rule -- all in hand-written HIP kernels behind the C ABI
-of include/dlm.h (libdlm.so); also block-AR drafting and the two-model
-draft-then-refine cascade.  PyTorch supplies device memory and streams.
+of include/dlm.h (libdlm.so); also block-AR drafting, the two-model
+draft-then-refine cascade, and a paged key/value cache with rotary positions
+and attention of windows (tokens, trees and blocks of drafted tokens) over it.  PyTorch supplies device memory and streams.
 """
 
 from ._lib import DlmConfig, DlmError, DlmStats, LIB_PATH, load  # noqa: F401
 
-__all__ = ["DlmConfig", "DlmError", "DlmStats", "LIB_PATH", "load", "Refiner", "cascade"]
+__all__ = ["DlmConfig", "DlmError", "DlmStats", "LIB_PATH", "load", "PagedCache", "Refiner", "Rope", "cascade"]
 
 
 def __getattr__(name):
@@ -19,4 +20,7 @@ def __getattr__(name):
     if name == "cascade":
         from .model import cascade
         return cascade
+    if name in ("PagedCache", "Rope"):
+        from . import cache
+        return getattr(cache, name)
     raise AttributeError(name)

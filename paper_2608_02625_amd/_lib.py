@@ -57,11 +57,34 @@ class DlmCascadeStats(ctypes.Structure):
                 "refine_ms": float(self.refine_ms)}
 
 
+class DlmRopeSpec(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("original_len", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("theta", ctypes.c_double), ("factor", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("beta_fast", ctypes.c_double)]
+
+
+class DlmRope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("phase", ctypes.c_uint64 * 128)]
+
+
+class DlmCache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_len", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("d_k", ctypes.c_void_p),
+                ("d_v", ctypes.c_void_p), ("d_ref", ctypes.c_void_p), ("d_len", ctypes.c_void_p),
+                ("d_table", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _F = ctypes.c_float
 _SZ = ctypes.c_size_t
+_L = ctypes.c_int64
 _CFG = ctypes.POINTER(DlmConfig)
+_CACHE = ctypes.POINTER(DlmCache)
+_ROPE = ctypes.POINTER(DlmRope)
 SIGNATURES = [
     ("dlm_weights_bytes", _SZ, [_CFG]),
     ("dlm_workspace_bytes", _SZ, [_CFG, _I, _I, _I]),
@@ -83,6 +106,19 @@ SIGNATURES = [
     ("dlm_cascade_workspace_bytes", _SZ, [_CFG, _CFG, _I, _I, _I, _I]),
     ("dlm_cascade", _I, [_P, _P, _I, _I, _I, _P, _P, _I, _I, _F, _I, ctypes.POINTER(DlmEditRule), _P, _SZ, _P,
                          ctypes.POINTER(DlmCascadeStats)]),
+    ("dlm_rope_init", _I, [ctypes.POINTER(DlmRopeSpec), _ROPE]),
+    ("dlm_rope_apply", _I, [_ROPE, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _I, _P]),
+    ("dlm_cache_workspace_bytes", _SZ, [_CACHE, _I, _I, _I]),
+    ("dlm_cache_reset", _I, [_CACHE, _P]),
+    ("dlm_cache_reserve", _I, [_CACHE, _P, _I, _P, _P, _SZ, _P]),
+    ("dlm_cache_append", _I, [_CACHE, _I, _P, _I, _I, _I, _P, _L, _P, _L, _ROPE, _P, _I, _P, _L, _P, _L, _P]),
+    ("dlm_cache_attend", _I, [_CACHE, _I, _P, _I, _I, _I, _I, _P, _L, _P, _I, _F, _P, _L, _P, _P, _SZ, _P]),
+    ("dlm_cache_commit", _I, [_CACHE, _P, _I, _P, _P, _I, _P, _P]),
+    ("dlm_cache_fork", _I, [_CACHE, _I, _P, _P, _P, _P]),
+    ("dlm_cache_truncate", _I, [_CACHE, _P, _P]),
+    ("dlm_cache_compact", _I, [_CACHE, _P, _P, _SZ, _P]),
+    ("dlm_cache_step_workspace_bytes", _SZ, [_CFG, _CACHE, _I, _I]),
+    ("dlm_cache_step", _I, [_P, _CACHE, _P, _I, _I, _I, _P, _P, _P, _I, _P, _SZ, _P, _P, _P, _P, _P]),
     ("dlm_debug_forward", _I, [_P, _I, _I, _I, _P, _P, _SZ, _P, _P, _P, _P, _P, _P, _P, _P]),
     ("dlm_debug_layer", _I, [_P, _I, _I, _I, _P, _P, _P, _SZ, _P, _P, _P]),
     ("dlm_debug_head", _I, [_P, _I, _I, _I, _P, _P, _SZ, _P, _P, _P, _P]),

@@ -11,7 +11,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdlm.so")
 BUILD = os.path.join(HERE, "_build")
-SOURCES = ["init.hip", "gemm.hip", "attention.hip", "elementwise.hip", "moe.hip", "engine.hip"]
+SOURCES = ["init.hip", "gemm.hip", "attention.hip", "elementwise.hip", "moe.hip", "rope.hip", "pages.hip",
+           "paged_attention.hip", "cache.hip", "engine.hip"]
+HOST_SOURCES = ["cache.hip", "engine.hip"]     # the C ABI's host code: what build_host_sanitized() instruments
 ARCH = os.environ.get("DLM_OFFLOAD_ARCH", "gfx950")
 
 CFLAGS = [
@@ -80,7 +82,7 @@ def _clangxx() -> str:
 
 
 def build_host_sanitized() -> str:
-    """The library with the host code of its C ABI (engine.hip: argument
+    """The library with the host code of its C ABI (HOST_SOURCES: argument
     validation, planning, error paths) under AddressSanitizer and
     UndefinedBehaviorSanitizer; the kernel sources' objects are those of
     build(), and device code is never instrumented.  For CPU checks of the
@@ -90,17 +92,18 @@ def build_host_sanitized() -> str:
     os.makedirs(out_dir, exist_ok=True)
     objs = []
     for src in SOURCES:
-        if src != "engine.hip":
+        if src not in HOST_SOURCES:
             obj = os.path.join(BUILD, src.replace(".hip", ".o"))
             if not os.path.exists(obj):
                 _compile(src)
             objs.append(obj)
-    obj = os.path.join(out_dir, "engine.o")
-    cmd = [_hipcc(), *CFLAGS, *SANITIZE, "-c", os.path.join(CSRC, "engine.hip"), "-o", obj]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"sanitized host build failed:\n{r.stderr}")
-    objs.append(obj)
+    for src in HOST_SOURCES:
+        obj = os.path.join(out_dir, src.replace(".hip", ".o"))
+        cmd = [_hipcc(), *CFLAGS, *SANITIZE, "-c", os.path.join(CSRC, src), "-o", obj]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"sanitized host build failed for {src}:\n{r.stderr}")
+        objs.append(obj)
     out = os.path.join(out_dir, "libdlm_hostsan.so")
     rocm = os.path.realpath(os.path.join(os.path.dirname(os.path.realpath(_hipcc())), ".."))
     # The sanitizer runtime is not linked in: the loading process preloads it,

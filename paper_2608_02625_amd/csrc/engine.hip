@@ -24,7 +24,9 @@
 #include <vector>
 
 #include "../../include/dlm.h"
+#include "cache.h"
 #include "kernels.h"
+#include "status.h"
 #include "tiling.h"
 
 namespace {
@@ -61,6 +63,13 @@ dlm_status caught_exception() noexcept {
     }
     return DLM_ERR_INTERNAL;
 }
+
+}  // namespace
+
+dlm_status dlm_internal_fail(dlm_status s, const std::string& msg) { return fail(s, msg); }
+dlm_status dlm_internal_caught() noexcept { return caught_exception(); }
+
+namespace {
 
 // Test hook: the n-th pass through a host allocation point from now throws
 // std::bad_alloc (0: never).
@@ -304,6 +313,17 @@ struct dlm_model {
 
 namespace {
 
+// What dlm_cache_step adds to a pass.
+struct PagedStep {
+    CacheArgs cache;
+    const dlm_rope* rope;
+    const int32_t *row_start, *pos;
+    const uint32_t* mask;
+    int total_rows, max_rows, max_keys, mask_words;
+    float* qkv;                         // [T][(H + 2 KV) * hd]
+    void* attend_ws;
+};
+
 struct Ctx {
     dlm_model* m;
     const dlm_config& c;
@@ -327,6 +347,9 @@ struct Ctx {
     int att_block = 0;                  // > 0: the window's rows are blocks that see no later one
     bool head_next = false;             // the head follows the last block
     bool hfin_ready = false;            // hfin already holds the head's normalised rows
+    // Windows behind a paged cache (dlm_cache_step): the T packed rows' K and V go
+    // into their pages and the attention reads them there.
+    const PagedStep* paged = nullptr;
     float* dbg_router_logits = nullptr;  // test hook: router logits [T][E] of the layer run
     // Only the draft rows leave the last block (the head reads nothing else):
     // its MoE FFN then runs on the B*D draft rows alone.  Their K / V for the
@@ -404,6 +427,32 @@ GemmArgs gemm_args(const bf16_t* A, int64_t lda, const bf16_t* B, int64_t ldb, i
         if (_s != DLM_OK) return _s;     \
     } while (0)
 
+// QKV projection, K / V into the pages, attention over them.  The projection
+// leaves float32, so that keys and queries are rounded once, after the rotation.
+dlm_status run_paged_attention(Ctx& x, int l, const bf16_t* h, bf16_t* q, bf16_t* attn) {
+    const dlm_config& c = x.c;
+    const PagedStep& p = *x.paged;
+    const int hd = c.head_dim, H = c.n_heads, KV = c.n_kv_heads, N = (H + 2 * KV) * hd;
+    GemmArgs a = gemm_args(h, c.d_model, x.wt(x.m->plan.layers[l].wqkv), c.d_model, x.T, N, c.d_model);
+    a.out = p.qkv;
+    a.ldo = N;
+    const GemmTile t = resid_tile(x.T, N, c.d_model);
+    a.variant = t.variant;
+    TRY(gemm(x, "gemm_qkv", a, EPI_F32, false, t.bm, t.bn, 0));
+    prof_begin(x, "cache_append");
+    hipError_t e = launch_append(p.cache, DLM_BF16, l, p.row_start, p.total_rows, p.max_rows, DLM_F32,
+                                 p.qkv + (size_t)H * hd, N, p.qkv + (size_t)(H + KV) * hd, N, p.rope, p.pos, H, p.qkv, N,
+                                 q, (int64_t)H * hd, x.st);
+    prof_end(x, "cache_append");
+    if (e != hipSuccess) return fail(DLM_ERR_HIP, std::string("cache_append: ") + hipGetErrorString(e));
+    prof_begin(x, "cache_attend");
+    e = launch_attend(p.cache, DLM_BF16, l, p.row_start, p.total_rows, p.max_rows, p.max_keys, H, q, (int64_t)H * hd,
+                      p.mask, p.mask_words, 1.f / sqrtf((float)hd), attn, (int64_t)H * hd, nullptr, p.attend_ws, x.st);
+    prof_end(x, "cache_attend");
+    if (e != hipSuccess) return fail(DLM_ERR_HIP, std::string("cache_attend: ") + hipGetErrorString(e));
+    return DLM_OK;
+}
+
 // One transformer block on the fp32 residual stream x (in place).
 dlm_status run_layer(Ctx& x, int l) {
     const dlm_config& c = x.c;
@@ -419,7 +468,9 @@ dlm_status run_layer(Ctx& x, int l) {
 
     if (!x.h_ready) LAUNCH(x, "rmsnorm", launch_rmsnorm(xs, x.wt(L.g1), h, x.T, d, c.norm_eps, x.st));
     x.h_ready = false;
-    {
+    if (x.paged) {
+        TRY(run_paged_attention(x, l, h, q, attn));
+    } else {
         // Transposed: rows = the (H + 2 KV) * hd output features, columns = tokens.
         const int N = (H + 2 * KV) * hd;
         GemmArgs a = gemm_args(x.wt(L.wqkv), d, h, d, N, x.T, d);
@@ -438,7 +489,7 @@ dlm_status run_layer(Ctx& x, int l) {
         TRY(gemm(x, "gemm_qkv", a, EPI_QKV, false, t.bm, t.bn, 0));
     }
     if (x.kv_only && l + 1 == c.n_layers) return DLM_OK;    // the cache holds this window's K/V now
-    {
+    if (!x.paged) {
         prof_begin(x, "attention");
         hipError_t e = launch_attention(q, k, v, attn, x.B, x.S, kvS, x.q0 + x.S, H, KV, hd, x.st, x.att_split,
                                         x.att_keys_lo, x.att_block);
@@ -814,6 +865,35 @@ struct Drafter {
         return DLM_OK;
     }
 };
+
+// ------------------------------------------------------------ windows behind a paged cache
+// Workspace: a pass over one sequence of T rows, the projection's float32 rows,
+// the attention's parts.
+struct StepPlan {
+    Workspace w;
+    size_t qkv = 0, attend = 0, total = 0;
+};
+
+StepPlan plan_step(const dlm_config& c, const dlm_cache& cache, int T, int max_rows) {
+    StepPlan p;
+    p.w = plan_workspace(c, 1, 0, T);
+    p.qkv = p.w.total;
+    p.attend = align_up(p.qkv + (size_t)T * (c.n_heads + 2 * c.n_kv_heads) * c.head_dim * 4);
+    p.total = align_up(p.attend + attend_workspace_bytes(cache.n_seqs, c.n_kv_heads, c.head_dim, T, max_rows,
+                                                         c.n_heads / c.n_kv_heads));
+    return p;
+}
+
+std::string check_step(const dlm_config& c, const dlm_cache* cache, int T, int max_rows) {
+    if (!cache) return "cache is NULL";
+    if (cache->dtype != DLM_BF16) return "the cache's dtype must be DLM_BF16";
+    if (cache->n_layers != c.n_layers || cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim)
+        return "the cache's layers, key heads and head_dim must be the model's";
+    if (max_rows < 1) return "max_rows must be >= 1";
+    std::string e = check_shape(1, 0, T);
+    if (e.empty()) e = check_offsets(c, T);
+    return e;
+}
 
 dlm_status fail_invalid_tokens(int n) {
     return fail(DLM_ERR_INVALID_ARG, std::to_string(n) + " token id(s) outside [0, vocab) or [MASK] id(s) in the "
@@ -1273,6 +1353,76 @@ dlm_status dlm_cascade(dlm_model* drafter, dlm_model* refiner, int32_t batch, in
         cs.draft_ms = std::chrono::duration<double, std::milli>(t1 - t0).count();
         cs.refine_ms = std::chrono::duration<double, std::milli>(t2 - t1).count();
         if (h_stats) *h_stats = cs;
+        return DLM_OK;
+    } catch (...) {
+        return caught_exception();
+    }
+}
+
+size_t dlm_cache_step_workspace_bytes(const dlm_config* cfg, const dlm_cache* cache, int32_t total_rows,
+                                      int32_t max_rows) {
+    try {
+        if (!validate(cfg).empty() || !check_step(*cfg, cache, total_rows, max_rows).empty()) return 0;
+        if (dlm_cache_workspace_bytes(cache, total_rows, max_rows, cfg->n_heads) == 0) return 0;
+        return plan_step(*cfg, *cache, total_rows, std::min(max_rows, total_rows)).total;
+    } catch (...) {
+        caught_exception();
+        return 0;
+    }
+}
+
+dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                          int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                          const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                          void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid) {
+    try {
+        if (!m) return fail(DLM_ERR_INVALID_ARG, "model handle is NULL");
+        const dlm_config& c = m->cfg;
+        const std::string bad = check_step(c, cache, total_rows, max_rows);
+        if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
+        TRY(dlm_internal_check_cache(cache));
+        if (!d_row_start || !d_tokens) return fail(DLM_ERR_INVALID_ARG, "row_start or tokens is NULL");
+        if (max_keys < 0) return fail(DLM_ERR_INVALID_ARG, "max_keys must be >= 0");
+        const int rows = std::min(max_rows, total_rows);
+        if (d_mask && (int64_t)mask_words * 32 < rows) return fail(DLM_ERR_INVALID_ARG, "mask must hold max_rows bits per row");
+        const StepPlan plan = plan_step(c, *cache, total_rows, rows);
+        if (!d_workspace) return fail(DLM_ERR_INVALID_ARG, "workspace is NULL");
+        if (workspace_bytes < plan.total)
+            return fail(DLM_ERR_WORKSPACE, "workspace too small: need " + std::to_string(plan.total) + " bytes, got " +
+                                               std::to_string(workspace_bytes));
+        if (((uintptr_t)d_workspace) % kAlign) return fail(DLM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+        dlm_rope_spec spec{};
+        spec.head_dim = spec.rot_dim = c.head_dim;
+        spec.theta = c.rope_theta;
+        dlm_rope rope;
+        TRY(dlm_rope_init(&spec, &rope));
+        const int64_t room = (int64_t)cache->max_pages * cache->page_len;
+        PagedStep step{};
+        step.cache = cache_args(*cache);
+        step.rope = &rope;
+        step.row_start = d_row_start;
+        step.pos = d_pos;
+        step.mask = d_mask;
+        step.total_rows = total_rows;
+        step.max_rows = rows;
+        step.max_keys = (int)std::min<int64_t>(max_keys ? max_keys : room, room);
+        step.mask_words = d_mask ? mask_words : 0;
+        Ctx x = ctx_for(m, 1, 0, total_rows, d_workspace, plan.w, hip_stream);
+        step.qkv = x.at<float>(plan.qkv);
+        step.attend_ws = x.at<char>(plan.attend);
+        x.paged = &step;
+        x.head_next = true;
+        int32_t* counters = x.at<int32_t>(plan.w.counters);
+        launch_zero_i32(counters, CNT_WORDS, x.st);
+        run_embed(x, d_tokens, 0, counters + CNT_INVALID);
+        for (int l = 0; l < c.n_layers; ++l) TRY(run_layer(x, l));
+        int32_t* top1 = d_top1 ? d_top1 : x.at<int32_t>(plan.w.top1);
+        float* conf = d_conf ? d_conf : x.at<float>(plan.w.conf);
+        float* mx = d_max_logit ? d_max_logit : x.at<float>(plan.w.maxlogit);
+        TRY(run_head(x, top1, conf, mx, nullptr));
+        if (d_n_invalid)
+            HIP_TRY(hipMemcpyAsync(d_n_invalid, counters + CNT_INVALID, 4, hipMemcpyDeviceToDevice, x.st));
+        HIP_TRY(hipGetLastError());
         return DLM_OK;
     } catch (...) {
         return caught_exception();

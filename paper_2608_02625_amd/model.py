@@ -12,6 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import DlmConfig, DlmStats, check
+from .cache import PagedCache
 
 CONFIG_FIELDS = [f for f, _ in DlmConfig._fields_]
 
@@ -236,6 +237,47 @@ class Refiner:
                                       float(threshold), tokens.data_ptr(), ws.data_ptr(), ws.numel(), self.stream,
                                       _ptr(top1), _ptr(conf), _ptr(max_logit), _ptr(stats)), "dlm_draft_step")
         return tokens
+
+    # ------------------------------------------------- windows behind a paged cache
+    def cache(self, n_pages: int, page_len: int, n_seqs: int, max_pages: int) -> "PagedCache":
+        """An empty paged cache of this model's layers and key heads."""
+        return PagedCache(self.cfg.n_layers, n_pages, page_len, self.cfg.n_kv_heads, self.cfg.head_dim, n_seqs,
+                          max_pages, device=self.device)
+
+    def cache_step(self, cache: "PagedCache", tokens: torch.Tensor, row_start: torch.Tensor, max_rows: int,
+                   positions: torch.Tensor | None = None, mask: torch.Tensor | None = None, max_keys: int = 0,
+                   n_invalid: torch.Tensor | None = None):
+        """Forward of the packed window rows tokens (int32 [rows]) behind the cache, whose
+        reserved places take their keys and values.  row_start int32 [n_seqs + 1];
+        positions int32 [rows] (default: the tokens' places); mask int32 [rows, words]:
+        the window rows that a row sees (default: all of its window's).  Returns (top-1
+        int32, confidence float, max logit float), each [rows]."""
+        T = tokens.numel()
+        for t, name, n in ((tokens, "tokens", T), (positions, "positions", T),
+                           (row_start, "row_start", cache.n_seqs + 1), (n_invalid, "n_invalid", 1)):
+            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
+                raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values")
+        words = 0
+        if mask is not None:
+            if mask.dtype != torch.int32 or mask.dim() != 2 or mask.shape[0] != T or not mask.is_contiguous():
+                raise ValueError("mask must be a contiguous int32 tensor [rows, words]")
+            words = mask.shape[1]
+        key = ("cache", T, min(int(max_rows), T), cache.n_seqs)
+        ws = self._ws.get(key)
+        if ws is None:
+            n = self.lib.dlm_cache_step_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(cache.c), T, int(max_rows))
+            if n == 0:
+                raise ValueError(f"invalid window shape ({T} rows, {max_rows} at most) or a cache of another model")
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            self._ws[key] = ws
+        top1 = torch.empty(T, dtype=torch.int32, device=self.device)
+        conf = torch.empty(T, dtype=torch.float32, device=self.device)
+        mx = torch.empty(T, dtype=torch.float32, device=self.device)
+        check(self.lib.dlm_cache_step(self._handle, ctypes.byref(cache.c), row_start.data_ptr(), T, int(max_rows),
+                                      int(max_keys), tokens.data_ptr(), _ptr(positions), _ptr(mask), words,
+                                      ws.data_ptr(), ws.numel(), self.stream, top1.data_ptr(), conf.data_ptr(),
+                                      mx.data_ptr(), _ptr(n_invalid)), "dlm_cache_step")
+        return top1, conf, mx
 
     def debug_forward(self, tokens: torch.Tensor, prompt_len: int, want_logits: bool = False,
                       want_routes: bool = False):
