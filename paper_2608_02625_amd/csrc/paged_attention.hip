@@ -370,46 +370,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
         for (int e = 0; e < 16; ++e) oacc[n][e] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;                 // m_run in units of the scores
 
-    const int kfrag = j * ROW, kkey = k_key<CPR>(j);
-    // Transposing reads: lane i of 16 hands in 4 values of row i / 4.
+    // Fragments.  A stage starts at a multiple of a row and a chunk's number is the
+    // only thing in the address bits that it takes up, so the k-th chunk pair of K
+    // (2 k + g, with the row's key) and the n-th four chunks of V are one base each
+    // with a constant xor-ed in.
+    const int kfrag = j * ROW + ((g ^ k_key<CPR>(j)) << 4);
+    // Transposing reads: lane i of 16 hands in 4 values of row i / 4; rows 8 apart
+    // have the same key.
     const int vrow = 4 * g + ((lane & 15) >> 2);
-    const int vfrag = HALF + vrow * ROW + (lane & 1) * 8;
-    const int vchunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-    const int vkey = v_key<CPR>(vrow);                    // rows vrow + 8 i have the same key
+    const int vfrag = HALF + vrow * ROW + (lane & 1) * 8 +
+                      (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ v_key<CPR>(vrow)) << 4);
     const uint32_t* mrow = a.mask ? a.mask + t * a.mask_words : nullptr;
 
-    // Tiles of this wave group: t0 + wk, t0 + wk + WK, ...  Copies past the last
-    // one repeat it into a stage that is not read again.
-    const int mine = (u.t1 - u.t0 - wk + WK - 1) / WK;    // may be <= 0
-    const int last = u.t0 + wk + (mine - 1) * WK;
-    Pages next{};
-    if (mine > 0) {
-#pragma unroll
-        for (int s = 0; s < NS - 1; ++s) {
-            const int kt = min(u.t0 + wk + s * WK, last);
-            issue(kt, s, pages_of(kt));
-        }
-        next = pages_of(min(u.t0 + wk + (NS - 1) * WK, last));
-    }
-    // The queries' loads end here and not inside the loop, where their wait would
-    // take the copies in flight with it.
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
-#endif
-    int stage = 0;
-    for (int it = 0; it < mine; ++it) {
-        const int kt = u.t0 + wk + it * WK;
-        wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
-        tile_barrier<WM>();                        // the group's have; the stage before is free
-        issue(min(kt + (NS - 1) * WK, last), stage == 0 ? NS - 1 : stage - 1, next);
-        next = pages_of(min(kt + NS * WK, last));
-        const int sb = ring + stage * STAGE;
-        const uint32_t gone = (missing >> (2 * stage)) & 3;
-        stage = stage + 1 == NS ? 0 : stage + 1;
-        if (!busy) continue;
-        const int k0 = kt * kTile;
+    // One tile's scores, softmax and products; masked: some row does not see all of
+    // it.  One path with scalar branches around what masks need: two copies of the
+    // products would hold the accumulators twice.
+    auto tile = [&](bool masked, int k0, int sb, uint32_t gone) {
 
+        const int ka = sb + kfrag, va = sb + vfrag;
         f32x16 st;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = 0.f;
@@ -418,16 +396,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
             s16x8 kf[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-                kf[x] = *(__attribute__((address_space(3))) const s16x8*)((lds_char*)lds + sb + kfrag +
-                                                                          (((2 * (k4 + x) + g) ^ kkey) << 4));
+                kf[x] = *(__attribute__((address_space(3))) const s16x8*)((lds_char*)lds + (ka ^ ((k4 + x) << 5)));
             sched_fence();
 #pragma unroll
             for (int x = 0; x < 4; ++x) st = mfma<F16>(kf[x], qf[k4 + x], st);
         }
 
-        uint32_t wild = 0;                                // keys with an infinity or NaN in V that some row must not see
-        uint32_t see = 0xffffffffu;
-        if (k0 + kTile > u.s.len || gone) {
+        uint32_t see = 0xffffffffu;                       // keys that the row sees
+        if (__builtin_expect(masked, 0)) {
             const int rel = k0 - u.s.len;                 // first key's place in the window
             if (mrow) {
                 const int w = rel >> 5, sh = rel & 31;
@@ -444,21 +420,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 if (!((mine_see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
-            if (mrow) {
-                uint32_t hi = 0, lo = 0;                  // largest exponents among the values
-#pragma unroll
-                for (int x = 0; x < CPR / 2; ++x) {
-                    const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)((lds_char*)lds + sb + HALF + j * ROW +
-                                                                                     (g * (CPR / 2) + x) * 16);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        hi = max(hi, w[i] & 0x7fffffffu);
-                        lo = max(lo, (w[i] << 16) & 0x7fffffffu);
-                    }
-                }
-                const uint64_t votes = __ballot(is_wild<F16>(max(hi, lo) >> 16));
-                wild = uniform((int)((uint32_t)votes | (uint32_t)(votes >> 32)));
-            }
         }
         float mt = st[0];
 #pragma unroll
@@ -495,38 +456,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
 
         // V^T fragments of 16 keys: two transposing reads of 4 keys each.
         auto v_frag = [&](int n, int s2) {
-            const int c = ((4 * n + vchunk) ^ vkey) << 4;
-            const s16x4 lo = lds_transpose((lds_ptr_t)((lds_char*)lds + sb + vfrag + (16 * s2) * ROW + c));
-            const s16x4 hi = lds_transpose((lds_ptr_t)((lds_char*)lds + sb + vfrag + (16 * s2 + 8) * ROW + c));
+            const int at = va ^ (n << 6);
+            const s16x4 lo = lds_transpose((lds_ptr_t)((lds_char*)lds + at + (16 * s2) * ROW));
+            const s16x4 hi = lds_transpose((lds_ptr_t)((lds_char*)lds + at + (16 * s2 + 8) * ROW));
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
-        wild = uniform((int)wild);                        // scalar: a branch, not a mask over the products
-        if (!wild) {
+        // Keys with an infinity or NaN in V, of a tile that some row does not see whole.
+        uint32_t wild = 0;
+        if (__builtin_expect(masked, 0)) {
+            uint32_t hi = 0, lo = 0;                      // largest magnitudes among a key's values
 #pragma unroll
-            for (int n2 = 0; n2 < NB; n2 += 2) {
-                s16x8 vf[2][2];
+            for (int x = 0; x < CPR / 2; ++x) {
+                const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)((lds_char*)lds + sb + HALF + j * ROW +
+                                                                                 (g * (CPR / 2) + x) * 16);
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int s2 = 0; s2 < 2; ++s2) vf[n][s2] = v_frag(n2 + n, s2);
-                sched_fence();
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) oacc[n2 + n] = mfma<F16>(vf[n][s2], pf[s2], oacc[n2 + n]);
-            }
-        } else {
-            // Rare: finite values by their probabilities, then the others, whatever
-            // their probability, into the rows that see their keys.
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    s16x8 v = v_frag(n, s2);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = is_wild<F16>((uint16_t)v[i]) ? (short)0 : v[i];
-                    oacc[n] = mfma<F16>(v, pf[s2], oacc[n]);
+                for (int i = 0; i < 4; ++i) {
+                    hi = max(hi, w[i] & 0x7fffffffu);
+                    lo = max(lo, (w[i] << 16) & 0x7fffffffu);
                 }
+                if (x % 2) sched_fence();                 // few registers at a time
+            }
+            const uint64_t votes = __ballot(is_wild<F16>(max(hi, lo) >> 16));
+            wild = uniform((int)((uint32_t)votes | (uint32_t)(votes >> 32)));
+        }
+#pragma unroll
+        for (int n2 = 0; n2 < NB; n2 += 2) {
+            s16x8 vf[2][2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) vf[n][s2] = v_frag(n2 + n, s2);
+            sched_fence();
+            if (__builtin_expect(wild, 0)) {              // finite values only; the others follow
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        short& v = reinterpret_cast<short(&)[8]>(vf[x >> 1][x & 1])[i];
+                        v = is_wild<F16>((uint16_t)v) ? (short)0 : v;
+                    }
+            }
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) oacc[n2 + n] = mfma<F16>(vf[n][s2], pf[s2], oacc[n2 + n]);
+        }
+        if (__builtin_expect(wild, 0)) {
+            // Rare: infinities and NaN, whatever their probability, into the rows that
+            // see their keys.
             for (uint32_t left = wild; left; left &= left - 1) {
                 const int key = __builtin_ctz(left);
                 const bool sees = (see >> key) & 1;
@@ -542,9 +519,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
                             const uint32_t bits = (x & 1 ? w[x >> 1] >> 16 : w[x >> 1]) & 0xffffu;
                             if (sees && is_wild<F16>(bits)) oacc[n][4 * i + x] += widen<F16>(bits);
                         }
+                        sched_fence();
                     }
             }
         }
+    };
+
+    // Tiles of this wave group: t0 + wk, t0 + wk + WK, ...  Copies past the last
+    // one repeat it into a stage that is not read again.
+    const int mine = (u.t1 - u.t0 - wk + WK - 1) / WK;    // may be <= 0
+    const int last = u.t0 + wk + (mine - 1) * WK;
+    Pages next{};
+    if (mine > 0) {
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s) {
+            const int kt = min(u.t0 + wk + s * WK, last);
+            issue(kt, s, pages_of(kt));
+        }
+        next = pages_of(min(u.t0 + wk + (NS - 1) * WK, last));
+    }
+    // The queries' loads end here and not inside the loop, where their wait would
+    // take the copies in flight with it.
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
+#endif
+    const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
+    int stage = 0;
+    for (int it = 0; it < mine; ++it) {
+        const int kt = u.t0 + wk + it * WK;
+        wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
+        tile_barrier<WM>();                        // the group's have; the stage before is free
+        issue(min(kt + (NS - 1) * WK, last), stage == 0 ? NS - 1 : stage - 1, next);
+        next = pages_of(min(kt + NS * WK, last));
+        const int sb = ring + stage * STAGE;
+        const uint32_t gone = (missing >> (2 * stage)) & 3;
+        stage = stage + 1 == NS ? 0 : stage + 1;
+        if (!busy) continue;
+        const int k0 = kt * kTile;
+        tile(k0 + kTile > clear || gone, k0, sb, gone);
     }
 
     wait_all_memory();                                    // no copy may still land in LDS
