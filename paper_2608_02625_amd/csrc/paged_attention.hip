@@ -82,11 +82,24 @@ __device__ __forceinline__ float widen(uint32_t bits16) {
     else return __uint_as_float(bits16 << 16);
 }
 
-__device__ __forceinline__ s16x4 lds_transpose(lds_ptr_t p) {
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+// The pointer is restrict so that the read carries alias information of its own:
+// without any, the compiler lets it wait for every copy into LDS in flight, of other
+// tiles too (the copies that it needs are awaited by count).
+__device__ __forceinline__ s16x4 transposed_read(lds_s16x4* __restrict__ p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
 #else
     return s16x4{};
+#endif
+}
+__device__ __forceinline__ s16x4 lds_transpose(lds_ptr_t p) { return transposed_read((lds_s16x4*)p); }
+
+// lds_dma16_buf, past the caches' replacement (ONCE: nobody else reads the bytes).
+template <bool ONCE>
+__device__ __forceinline__ void copy16(buf_rsrc_t r, uint32_t voffset, lds_ptr_t lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, (int)voffset, 0, 0, ONCE ? 2 : 0);
 #endif
 }
 
@@ -139,7 +152,7 @@ struct AttnArgs {
     int rows_per_wg;                          // packed rows of a workgroup
     int step;                                 // keys of a step
     int min_steps;                            // least steps of a unit
-    int units;                                // units aimed at
+    int units;                                // units aimed at: the workgroups that the chip holds at once
     float* part_o;                            // [slots][rows_per_wg][head_dim]
     float2* part_ml;                          // [slots][rows_per_wg]
 };
@@ -167,13 +180,27 @@ struct Unit {
     int slot, parts;                          // workspace slot of this part; parts of its item
 };
 
-__device__ __forceinline__ int wave_scan(int v, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(v, o, 64);
-        if (lane >= o) v += y;
-    }
+// Inclusive prefix sum over the wave by lane moves (a shuffle through LDS each would
+// cost a call of few keys more than its products): within rows of 16, then the totals
+// of rows 0 and 2 into the next, then of lane 31 into the upper half.
+__device__ __forceinline__ int wave_scan(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // row_bcast:15
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);     // row_bcast:31
+#endif
     return v;
+}
+// Value of lane l, the same for the whole wave.
+__device__ __forceinline__ int from_lane(int v, int l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_readlane(v, l);
+#else
+    return v;
+#endif
 }
 
 // The index-th unit (or, with `items`, the index-th item of several parts) in the
@@ -187,38 +214,40 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
         tiles = (s.n * a.group + per_tile - 1) / per_tile;
         steps = max((s.keys + a.step - 1) / a.step, 1);
     };
-    int sum = 0;                                          // steps of all items (fits: checked by the host)
+    const Seq first = sequence(a, lane);
+    int sum = 0, items = 0;                               // steps of all items (fit: checked by the host)
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
-        shape(sequence(a, b0 + lane), tiles, steps);
-        int w = tiles * steps * a.c.n_kv;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o, 64);
-        sum += w;
+        shape(b0 ? sequence(a, b0 + lane) : first, tiles, steps);
+        sum += from_lane(wave_scan(tiles * steps * a.c.n_kv), 63);
+        items += from_lane(wave_scan(tiles * a.c.n_kv), 63);
     }
-    const int most = max(a.min_steps, (sum + a.units - 1) / a.units);
+    // Cut into runs of sum / n steps an item's last one is half empty on average, so
+    // this aims at `units` of them together.
+    const int n = max(a.units - items / 2, a.units / 2);
+    const int most = max(a.min_steps, (sum + n - 1) / n);
     int before = 0, slots_before = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
-        const Seq s = sequence(a, b0 + lane);
+        const Seq s = b0 ? sequence(a, b0 + lane) : first;
         shape(s, tiles, steps);
         const int parts = (steps + most - 1) / most;
         const int all = tiles * a.c.n_kv * parts, split = parts > 1 ? all : 0;
         const int count = ITEMS ? (parts > 1 ? tiles * a.c.n_kv : 0) : all;
-        const int end = before + wave_scan(count, lane), slot_end = slots_before + wave_scan(split, lane);
+        const int end = before + wave_scan(count), slot_end = slots_before + wave_scan(split);
         const uint64_t hit = __ballot(index < end && index >= end - count);
         if (hit) {
-            const int l = __ffsll((unsigned long long)hit) - 1;
+            const int l = __builtin_ctzll(hit);
             u.b = uniform(b0 + l);
-            u.s.n = uniform(__shfl(s.n, l, 64));
-            u.s.start = uniform(__shfl(s.start, l, 64));
-            u.s.len = uniform(__shfl(s.len, l, 64));
-            u.s.keys = uniform(__shfl(s.keys, l, 64));
-            u.parts = uniform(__shfl(parts, l, 64));
-            const int n_tiles = uniform(__shfl(tiles, l, 64));
-            const int all_steps = uniform(__shfl(steps, l, 64));
-            int i = index - uniform(__shfl(end - count, l, 64));
-            const int slot0 = uniform(__shfl(slot_end - split, l, 64));
+            u.s.n = from_lane(s.n, l);
+            u.s.start = from_lane(s.start, l);
+            u.s.len = from_lane(s.len, l);
+            u.s.keys = from_lane(s.keys, l);
+            u.parts = from_lane(parts, l);
+            const int n_tiles = from_lane(tiles, l);
+            const int all_steps = from_lane(steps, l);
+            int i = index - from_lane(end - count, l);
+            const int slot0 = from_lane(slot_end - split, l);
             u.row_tile = uniform(i % n_tiles);
             i /= n_tiles;
             int part = 0;
@@ -234,25 +263,275 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             u.t1 = uniform(min(u.t0 + each, (u.s.keys + kTile - 1) / kTile));
             return true;
         }
-        before = __shfl(end, 63, 64);
-        slots_before = __shfl(slot_end, 63, 64);
+        before = from_lane(end, 63);
+        slots_before = from_lane(slot_end, 63);
     }
     return false;
 }
 
-// ------------------------------------------------------------------ the kernel
+// ------------------------------------------------------------------ tiles
 
-// Between a tile's copies having landed for this wave and its use: the waves that
-// share the tile meet, a wave of its own only has its earlier LDS reads behind it.
-template <int WAVES>
-__device__ __forceinline__ void tile_barrier() {
-    if constexpr (WAVES > 1) {
-        lds_barrier();
-    } else {
-        wait_lgkmcnt<0>();
+template <int HD>
+struct Dims {
+    static constexpr int CPR = HD / 8;                    // 16-byte chunks of a row
+    static constexpr int ROW = HD * 2;
+    static constexpr int HALF = kTile * ROW;              // bytes of a K or V tile
+    static constexpr int NB = HD / 32, NKS = HD / 16;     // 32-feature blocks; 16-feature steps
+    static constexpr int ROWS_PER_COPY = 64 / CPR;        // rows of a 1 KB copy
+};
+
+// Where the keys of one (sequence, key head) lie.  Everything here is scalar but the
+// table entries, of which lane i keeps number base + i: a tile's come from there by a
+// lane index, without a load in front of its copies.
+template <int HD>
+struct Keys {
+    const char *k, *v;
+    const int32_t* table;
+    uint32_t page_bytes;
+    int keys, n_pages, max_pages, page_log2, page_mask, base, held;
+
+    __device__ __forceinline__ Keys(const AttnArgs& a, const Unit& u) {
+        const uint32_t head = (uint32_t)a.c.page_len * Dims<HD>::ROW;
+        k = a.c.k + a.layer_base + (int64_t)u.kvh * head;
+        v = a.c.v + a.layer_base + (int64_t)u.kvh * head;
+        page_bytes = head * a.c.n_kv;                     // at most 4 MB
+        table = a.c.table + (int64_t)u.b * a.c.max_pages;
+        keys = u.s.keys;
+        n_pages = a.c.n_pages;
+        max_pages = a.c.max_pages;
+        page_log2 = a.c.page_log2;
+        page_mask = a.c.page_len - 1;
+        fetch((u.t0 * kTile) >> page_log2);
+    }
+    // Entries past the row's end are read as its last one, whose keys then lie behind
+    // the last token.
+    __device__ __forceinline__ void fetch(int first) {
+        base = first;
+        held = table[min(first + (int)(threadIdx.x & 63), max_pages - 1)];
 #if defined(__HIP_DEVICE_COMPILE__)
-        asm volatile("" ::: "memory");
+        asm volatile("" : "+v"(held));                    // waited for here, not wherever it is used
 #endif
+    }
+    // Entries of the two groups of 16 keys of a tile.
+    __device__ __forceinline__ int2 entries(int kt) {
+        const int e0 = (kt * kTile) >> page_log2, e1 = (kt * kTile + 16) >> page_log2;
+        if (__builtin_expect((uint32_t)(e0 - base) > 62u, 0)) fetch(e0);
+        return int2{from_lane(held, e0 - base), from_lane(held, e1 - base)};
+    }
+    __device__ __forceinline__ bool is_page(int page) const { return (uint32_t)page < (uint32_t)n_pages; }
+    // Bit s: group s of the tile has no page.
+    __device__ __forceinline__ uint32_t missing(const int2& e) const {
+        return (is_page(e.x) ? 0u : 1u) | (is_page(e.y) ? 0u : 2u);
+    }
+    // Byte offset in the pools, and bytes that hold tokens, of the 16 keys of group s.
+    __device__ __forceinline__ int64_t offset(int page, int kt, int s) const {
+        return (int64_t)((uint64_t)(uint32_t)(is_page(page) ? page : 0) * page_bytes) +
+               ((kt * kTile + s * 16) & page_mask) * Dims<HD>::ROW;
+    }
+    __device__ __forceinline__ int bytes(int page, int kt, int s) const {
+        const int g = kt * 2 + s, full = keys >> 4;
+        const int n = g < full ? 16 : g == full ? keys & 15 : 0;
+        return is_page(page) ? n * Dims<HD>::ROW : 0;
+    }
+};
+
+// Word w of a row's mask (0 outside of it).  Scalar w: a branch.
+__device__ __forceinline__ uint32_t mask_word(const AttnArgs& a, const uint32_t* mask_row, int w) {
+    return w >= 0 && w < a.mask_words ? mask_row[w] : 0;
+}
+// Which keys of the tile from k0 on a row sees; lo, hi: words (k0 - len) / 32, rounded
+// down, and the next one of its mask.
+__device__ __forceinline__ uint32_t seen_keys(const AttnArgs& a, const Seq& s, uint32_t lo, uint32_t hi, int k0,
+                                              uint32_t gone) {
+    uint32_t see = 0xffffffffu;
+    if (a.mask) {
+        const int rel = k0 - s.len, sh = rel & 31;        // first key's place in the window
+        see = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+        if (rel < 0) see |= rel <= -32 ? 0xffffffffu : (1u << -rel) - 1;      // tokens before the window
+    }
+    const int left = s.keys - k0;
+    if (left < 32) see &= left <= 0 ? 0 : (1u << left) - 1;
+    if (gone & 1) see &= 0xffff0000u;
+    if (gone & 2) see &= 0x0000ffffu;
+    return see;
+}
+
+// 32 rows: lane (j, g) holds row j, keys 8 (e / 4) + 4 g + e % 4 of a tile's scores
+// and features 32 n + 8 (e / 4) + 4 g + e % 4 of the output.
+template <bool F16, int HD>
+struct RowTile {
+    using D = Dims<HD>;
+    f32x16 o[D::NB];
+    float m, l;                                           // m in units of the scores
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < D::NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
+    }
+    __device__ __forceinline__ static void hide(f32x16& st, uint32_t see, int g) {
+        see >>= 4 * g;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (!((see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
+    }
+    // Scores to probabilities, the B operand of O^T = V^T P^T.
+    __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, s16x8 (&pf)[2]) {
+        float mt = st[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mt = fmaxf(mt, st[e]);
+        mt = both_max(mt);
+        // Each row by its own scores alone, so that its bits do not depend on others'.
+        const bool move = (mt - m) * scale_log2 > 8.f;
+        if (__any(move)) {
+            const float m_new = move ? mt : m;
+            const float alpha = move ? __builtin_amdgcn_exp2f((m - m_new) * scale_log2) : 1.f;
+            l *= alpha;
+#pragma unroll
+            for (int n = 0; n < D::NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[n][e] *= alpha;
+            m = m_new;
+        }
+        const float nb = m == -INFINITY ? 0.f : -m * scale_log2;
+        float sum = 0.f;
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i], scale_log2, nb));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i + 1], scale_log2, nb));
+                sum += p0 + p1;
+                w[i] = pack2<F16>(p0, p1);
+            }
+            pf[s2] = __builtin_bit_cast(s16x8, w);
+        }
+        l += sum;
+    }
+};
+
+// LDS byte addresses of V fragments of a tile.  A stage starts at a multiple of a row
+// and a chunk's number is the only thing in the address bits that it takes up, so the
+// n-th four chunks are one base with a constant xor-ed in.  Transposing reads: lane i
+// of 16 hands in 4 values of row i / 4; rows 8 apart have the same key.
+template <int HD>
+__device__ __forceinline__ int v_base(int lane) {
+    const int row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    return row * Dims<HD>::ROW + (lane & 1) * 8 +
+           (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ v_key<Dims<HD>::CPR>(row)) << 4);
+}
+
+// V^T fragments of two 32-feature blocks (n2, n2 + 1) of a tile; va: LDS byte address of
+// its V rows plus v_base.
+template <int HD>
+__device__ __forceinline__ void read_values(s16x8 (&vf)[2][2], lds_ptr_t lds, int va, int n2) {
+    using D = Dims<HD>;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+            const int at = (va ^ ((n2 + n) << 6)) + 16 * s2 * D::ROW;
+            const s16x4 lo = lds_transpose((lds_ptr_t)((lds_char*)lds + at));
+            const s16x4 hi = lds_transpose((lds_ptr_t)((lds_char*)lds + at + 8 * D::ROW));
+            vf[n][s2] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+}
+
+// O^T += V^T P^T of RT row tiles; v: LDS byte address of the V tile, vf: its first
+// fragments (asked for before the softmax, which hides their latency).  `masked`: some
+// row does not see all of it, so that infinities and NaN are looked for and, if there
+// are any (the result), left out.  One path with scalar branches: two copies of the
+// products would hold the accumulators twice.
+template <bool F16, int HD, int RT>
+__device__ __forceinline__ bool add_values(RowTile<F16, HD> (&rt)[RT], const s16x8 (&pf)[RT][2], s16x8 (&vf)[2][2],
+                                           lds_ptr_t lds, int v, int lane, int base, bool masked) {
+    using D = Dims<HD>;
+    const int g = lane >> 5, j = lane & 31;
+    uint32_t wild = 0;                                    // keys with an infinity or NaN
+    if (__builtin_expect(masked, 0)) {
+        uint32_t hi = 0, lo = 0;                          // largest magnitudes among a key's values
+#pragma unroll
+        for (int x = 0; x < D::CPR / 2; ++x) {
+            // a row's chunks in an order of its own: rows lie a multiple of all banks apart
+            const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)((lds_char*)lds + v + j * D::ROW +
+                                                                             (g * (D::CPR / 2) + (x ^ (j & (D::CPR / 2 - 1)))) * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi = max(hi, w[i] & 0x7fffffffu);
+                lo = max(lo, (w[i] << 16) & 0x7fffffffu);
+            }
+            if (x % 2) sched_fence();                     // few registers at a time
+        }
+        const uint64_t votes = __ballot(is_wild<F16>(max(hi, lo) >> 16));
+        wild = uniform((int)((uint32_t)votes | (uint32_t)(votes >> 32)));
+    }
+#pragma unroll
+    for (int n2 = 0; n2 < D::NB; n2 += 2) {
+        if (n2) {
+            read_values<HD>(vf, lds, v + base, n2);
+            sched_fence();
+        }
+        if (__builtin_expect(wild, 0)) {                  // finite values only
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const short y = vf[x >> 1][x & 1][i];
+                    vf[x >> 1][x & 1][i] = is_wild<F16>((uint16_t)y) ? (short)0 : y;
+                }
+        }
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) rt[r].o[n2 + n] = mfma<F16>(vf[n][s2], pf[r][s2], rt[r].o[n2 + n]);
+    }
+    return wild != 0;
+}
+
+// Rare: the infinities and NaN that add_values left out, whatever their probability,
+// into the rows that see their keys; straight from the pages, once, after the last
+// tile.  Tiles first, first + step, ... below end; `clear`: keys that every row sees.
+template <bool F16, int HD, int RT>
+__device__ __forceinline__ void add_wild(RowTile<F16, HD> (&rt)[RT], const AttnArgs& a, const Unit& u, Keys<HD>& keys,
+                                         const uint32_t* const (&mrow)[RT], int first, int end, int step, int clear, int g) {
+    using D = Dims<HD>;
+#pragma unroll 1
+    for (int kt = first; kt < end; kt += step) {
+        const int2 e = keys.entries(kt);
+        const uint32_t gone = keys.missing(e);
+        if (kt * kTile + kTile <= clear && !gone) continue;
+        uint32_t see[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int w = (kt * kTile - u.s.len) >> 5;
+            see[r] = seen_keys(a, u.s, a.mask ? mask_word(a, mrow[r], w) : 0, a.mask ? mask_word(a, mrow[r], w + 1) : 0,
+                               kt * kTile, gone);
+        }
+#pragma unroll 1
+        for (int i = 0; i < kTile; ++i) {
+            if ((gone >> (i >> 4)) & 1 || kt * kTile + i >= keys.keys) continue;
+            const char* row = keys.v + keys.offset(i < 16 ? e.x : e.y, kt, i >> 4) + (i & 15) * D::ROW + 8 * g;
+#pragma unroll
+            for (int n = 0; n < D::NB; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(row + (n * 32 + 8 * q) * 2);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const uint32_t bits = (x & 1 ? w[x >> 1] >> 16 : w[x >> 1]) & 0xffffu;
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+                            if (((see[r] >> i) & 1) && is_wild<F16>(bits)) rt[r].o[n][4 * q + x] += widen<F16>(bits);
+                    }
+                    sched_fence();
+                }
+        }
     }
 }
 
@@ -267,132 +546,118 @@ __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
     return l == 0.f ? -INFINITY : (m * a.scale_log2 + __builtin_amdgcn_logf(l)) * 0.69314718f;
 }
 
-// WK groups of waves of a workgroup take its tiles in turn, each with NS stages
-// of its own; the 4 / WK waves of a group share the tiles and take 32 rows each.
-template <bool F16, int HD, int WK, int NS, int WPE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void attend_kernel(const AttnArgs a) {
-    constexpr int WM = 4 / WK;
-    constexpr int CPR = HD / 8;                           // 16-byte chunks of a row
-    constexpr int ROW = HD * 2;
-    constexpr int HALF = kTile * ROW;                     // bytes of a K or V tile
-    constexpr int STAGE = 2 * HALF;
-    constexpr int COPIES = HALF / 1024 / WM;              // 1 KB copies per wave of a K or V tile
-    constexpr int NB = HD / 32, NKS = HD / 16;
-    static_assert(COPIES >= 1 && NS >= 2, "stages");
+// ------------------------------------------------------------------ many rows
+
+// More than 64 packed rows: 4 waves of 32 rows share tiles of K and V in LDS, three
+// stages of them, copied by all.  164 VGPRs at head_dim 128, so three workgroups (12
+// waves) share a CU, 48 KB of LDS each.
+constexpr int kManyRows = 128, kManyStages = 3;
+
+template <bool F16, int HD, bool ONCE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attend_many_kernel(const AttnArgs a) {
+    using D = Dims<HD>;
+    constexpr int NS = kManyStages, STAGE = 2 * D::HALF;
+    constexpr int COPIES = D::HALF / 1024 / 4;            // 1 KB copies per wave of a K or V tile
     // The kernel's only LDS variable: with a second one the compiler tells the two
     // apart, takes a fragment read to depend on every copy in flight into this one,
     // and waits for them all.
-    __shared__ __attribute__((aligned(16))) char smem[WK * NS * STAGE];
+    __shared__ __attribute__((aligned(16))) char smem[NS * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int g = lane >> 5, j = lane & 31;
-    const int wm = wave % WM, wk = wave / WM;
     Unit u;
     // Neighbouring units share their keys (row tiles): workgroups go to the 8 XCDs
     // in turn, so each XCD takes runs of 8 units.
     const int wg = blockIdx.x;
-    const int index = WK == 1 ? (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7) : wg;
-    if (!find_unit<false>(a, index, u)) return;
-    const int rows = min(u.s.n * a.group - u.row_tile * a.rows_per_wg, a.rows_per_wg);   // of this workgroup
-    const bool busy = wm * 32 < rows;                     // this wave has rows
-    const int r = min(wm * 32 + j, rows - 1) + u.row_tile * a.rows_per_wg;
-    const int node = r / a.group, head = u.kvh * a.group + r % a.group;
-    const int64_t t = (int64_t)u.s.start + node;          // packed row
+    if (!find_unit<false>(a, (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7), u)) return;
+    const int rows = min(u.s.n * a.group - u.row_tile * kManyRows, kManyRows);           // of this workgroup
+    const bool busy = wave * 32 < rows;                   // this wave has rows
+    const int r = min(wave * 32 + j, rows - 1) + u.row_tile * kManyRows;
+    const int head = u.kvh * a.group + r % a.group;
+    const int64_t t = (int64_t)u.s.start + r / a.group;   // packed row
+    Keys<HD> keys(a, u);
 
-    const lds_ptr_t lds = (lds_ptr_t)smem;
-    const int ring = wk * NS * STAGE;
-    // Copies: lane L of copy p reads the chunk that belongs at byte 16 L of its
-    // 1 KB block; the block's rows lie within one group of 16 keys, which lie in one
-    // page.
-    constexpr int ROWS_PER_COPY = 64 / CPR;
+    // Copies: lane L of copy p reads the chunk that belongs at byte 16 L of its 1 KB
+    // block; a wave's blocks of a tile lie within one group of 16 keys.
     uint32_t k_off[COPIES], v_off[COPIES];
 #pragma unroll
     for (int p = 0; p < COPIES; ++p) {
-        const int row = (wm * COPIES + p) * ROWS_PER_COPY + lane / CPR, pc = lane % CPR;
-        k_off[p] = (uint32_t)((row & 15) * ROW + ((pc ^ k_key<CPR>(row)) << 4));
-        v_off[p] = (uint32_t)((row & 15) * ROW + ((pc ^ v_key<CPR>(row)) << 4));
+        const int row = (wave * COPIES + p) * D::ROWS_PER_COPY + lane / D::CPR, pc = lane % D::CPR;
+        k_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ k_key<D::CPR>(row)) << 4));
+        v_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ v_key<D::CPR>(row)) << 4));
     }
-    const int64_t head_bytes = (int64_t)a.c.page_len * ROW;
-    const char* kp = a.c.k + a.layer_base + u.kvh * head_bytes;
-    const char* vp = a.c.v + a.layer_base + u.kvh * head_bytes;
-    const int64_t page_bytes = head_bytes * a.c.n_kv;
-    const int32_t* table = a.c.table + (int64_t)u.b * a.c.max_pages;
-    // Pages of the two groups of 16 keys of a tile.  Entries past the row's end are
-    // read as its last one, whose keys then lie behind the last token.
-    struct Pages {
-        int p[2];
-    };
-    auto pages_of = [&](int kt) {
-        Pages x;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            x.p[s] = uniform(ld_const(table + min((kt * kTile + s * 16) >> a.c.page_log2, a.c.max_pages - 1)));
-        return x;
-    };
-    auto held = [&](int page) { return page >= 0 && page < a.c.n_pages; };
-    constexpr int SUBS = COPIES * ROWS_PER_COPY > 16 ? 2 : 1;   // groups of 16 keys that a wave copies from
+    const lds_ptr_t lds = (lds_ptr_t)smem;
+    const int sub = wave * COPIES * D::ROWS_PER_COPY / 16;
     uint32_t missing = 0;                                 // two bits per stage: groups without a page
-    auto issue = [&](int kt, int stage, const Pages& pages) {
-        const int kd = ring + stage * STAGE + wm * COPIES * 1024;
-        missing &= ~(3u << (2 * stage));
-        missing |= (uint32_t)uniform((held(pages.p[0]) ? 0 : 1) | (held(pages.p[1]) ? 0 : 2)) << (2 * stage);
+    auto issue = [&](int kt, int stage) {
+        const int2 e = keys.entries(kt);
+        missing = (missing & ~(3u << (2 * stage))) | keys.missing(e) << (2 * stage);
+        const int page = sub ? e.y : e.x, bytes = keys.bytes(page, kt, sub);
+        const int64_t at = keys.offset(page, kt, sub);
+        const buf_rsrc_t kr = make_rsrc(keys.k + at, bytes), vr = make_rsrc(keys.v + at, bytes);
+        const int d = stage * STAGE + wave * COPIES * 1024;
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) {
-            const int sub = SUBS == 2 ? s : wm * COPIES * ROWS_PER_COPY / 16;
-            const int key = kt * kTile + sub * 16;
-            const int page = uniform(sub ? pages.p[1] : pages.p[0]);
-            const int bytes = uniform(held(page) ? min(max(u.s.keys - key, 0), 16) * ROW : 0);
-            const int64_t at = uniform(held(page) ? page : 0) * page_bytes + (key & (a.c.page_len - 1)) * ROW;
-            const buf_rsrc_t kr = make_rsrc(kp + at, bytes), vr = make_rsrc(vp + at, bytes);
+        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(kr, k_off[p], (lds_ptr_t)((lds_char*)lds + d + p * 1024));
 #pragma unroll
-            for (int p = 0; p < COPIES / SUBS; ++p) {
-                const int c = s * (COPIES / SUBS) + p;
-                lds_dma16_buf(kr, k_off[c], 0, (lds_ptr_t)((lds_char*)lds + kd + c * 1024));
-            }
-#pragma unroll
-            for (int p = 0; p < COPIES / SUBS; ++p) {
-                const int c = s * (COPIES / SUBS) + p;
-                lds_dma16_buf(vr, v_off[c], 0, (lds_ptr_t)((lds_char*)lds + kd + HALF + c * 1024));
-            }
-        }
+        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(vr, v_off[p], (lds_ptr_t)((lds_char*)lds + d + D::HALF + p * 1024));
     };
 
-    s16x8 qf[NKS];
+    s16x8 qf[D::NKS];
     {
         const uint16_t* qp = a.q + t * a.q_stride + head * HD + g * 8;
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) qf[ks] = *reinterpret_cast<const s16x8*>(qp + ks * 16);
+        for (int ks = 0; ks < D::NKS; ++ks) qf[ks] = *reinterpret_cast<const s16x8*>(qp + ks * 16);
     }
-    f32x16 oacc[NB];
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[n][e] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;                 // m_run in units of the scores
-
-    // Fragments.  A stage starts at a multiple of a row and a chunk's number is the
-    // only thing in the address bits that it takes up, so the k-th chunk pair of K
-    // (2 k + g, with the row's key) and the n-th four chunks of V are one base each
-    // with a constant xor-ed in.
-    const int kfrag = j * ROW + ((g ^ k_key<CPR>(j)) << 4);
-    // Transposing reads: lane i of 16 hands in 4 values of row i / 4; rows 8 apart
-    // have the same key.
-    const int vrow = 4 * g + ((lane & 15) >> 2);
-    const int vfrag = HALF + vrow * ROW + (lane & 1) * 8 +
-                      (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ v_key<CPR>(vrow)) << 4);
+    RowTile<F16, HD> rt[1];
+    rt[0].clear();
+    const int kfrag = j * D::ROW + ((g ^ k_key<D::CPR>(j)) << 4);      // chunk 2 ks + g: xor ks << 5
+    const int vfrag = v_base<HD>(lane);
     const uint32_t* mrow = a.mask ? a.mask + t * a.mask_words : nullptr;
+    const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
 
-    // One tile's scores, softmax and products; masked: some row does not see all of
-    // it.  One path with scalar branches around what masks need: two copies of the
-    // products would hold the accumulators twice.
-    auto tile = [&](bool masked, int k0, int sb, uint32_t gone) {
+    // Copies past the last tile repeat it into a stage that is not read again.
+    const int last = u.t1 - 1;
+    if (u.t0 < u.t1) {
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s) issue(min(u.t0 + s, last), s);
+    }
+    // The queries' loads end here and not inside the loop, where their wait would
+    // take the copies in flight with it.
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int ks = 0; ks < D::NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
+#endif
+    // Words of the row's mask for this tile and the next one, read a tile ahead: in
+    // front of that tile's copies, so that waiting for them does not wait for those.
+    const int w0 = ((u.t0 * kTile) - u.s.len) >> 5;
+    uint32_t word0 = 0, word1 = 0, word2 = 0;
+    if (a.mask) {
+        word0 = mask_word(a, mrow, w0);
+        word1 = mask_word(a, mrow, w0 + 1);
+    }
+    int stage = 0;
+    bool wild = false;
+    for (int kt = u.t0; kt < u.t1; ++kt) {
+        wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
+        lds_barrier();                                    // everyone's have; the stage before is free
+        if (a.mask) word2 = mask_word(a, mrow, w0 + kt - u.t0 + 2);
+        issue(min(kt + NS - 1, last), stage == 0 ? NS - 1 : stage - 1);
+        const int sb = stage * STAGE;
+        const uint32_t gone = (missing >> (2 * stage)) & 3;
+        stage = stage + 1 == NS ? 0 : stage + 1;
+        const uint32_t lo = word0, hi = word1;
+        word0 = word1;
+        word1 = word2;
+        if (!busy) continue;
+        const int k0 = kt * kTile;
+        const bool masked = k0 + kTile > clear || gone;
 
-        const int ka = sb + kfrag, va = sb + vfrag;
+        const int ka = sb + kfrag;
         f32x16 st;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = 0.f;
 #pragma unroll
-        for (int k4 = 0; k4 < NKS; k4 += 4) {
+        for (int k4 = 0; k4 < D::NKS; k4 += 4) {
             s16x8 kf[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x)
@@ -401,289 +666,333 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE))) void
 #pragma unroll
             for (int x = 0; x < 4; ++x) st = mfma<F16>(kf[x], qf[k4 + x], st);
         }
-
-        uint32_t see = 0xffffffffu;                       // keys that the row sees
-        if (__builtin_expect(masked, 0)) {
-            const int rel = k0 - u.s.len;                 // first key's place in the window
-            if (mrow) {
-                const int w = rel >> 5, sh = rel & 31;
-                const uint32_t lo = w >= 0 && w < a.mask_words ? mrow[w] : 0;
-                const uint32_t hi = w + 1 >= 0 && w + 1 < a.mask_words ? mrow[w + 1] : 0;
-                see = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
-                if (rel < 0) see |= rel <= -32 ? 0xffffffffu : (1u << -rel) - 1;      // tokens before the window
-            }
-            const int left = u.s.keys - k0;
-            if (left < 32) see &= left <= 0 ? 0 : (1u << left) - 1;
-            if (gone & 1) see &= 0xffff0000u;
-            if (gone & 2) see &= 0x0000ffffu;
-            const uint32_t mine_see = see >> (4 * g);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (!((mine_see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
-        }
-        float mt = st[0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) mt = fmaxf(mt, st[e]);
-        mt = both_max(mt);
-        // Each row by its own scores alone, so that its bits do not depend on others'.
-        const bool move = (mt - m_run) * a.scale_log2 > 8.f;
-        if (__any(move)) {
-            const float m_new = move ? mt : m_run;
-            const float alpha = move ? __builtin_amdgcn_exp2f((m_run - m_new) * a.scale_log2) : 1.f;
-            l_run *= alpha;
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) oacc[n][e] *= alpha;
-            m_run = m_new;
-        }
-        const float nb = m_run == -INFINITY ? 0.f : -m_run * a.scale_log2;
-        float lt = 0.f;
-        s16x8 pf[2];
-#pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i], a.scale_log2, nb));
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i + 1], a.scale_log2, nb));
-                lt += p0 + p1;
-                w[i] = pack2<F16>(p0, p1);
-            }
-            pf[s2] = __builtin_bit_cast(s16x8, w);
-        }
-        l_run += lt;
-
-        // V^T fragments of 16 keys: two transposing reads of 4 keys each.
-        auto v_frag = [&](int n, int s2) {
-            const int at = va ^ (n << 6);
-            const s16x4 lo = lds_transpose((lds_ptr_t)((lds_char*)lds + at + (16 * s2) * ROW));
-            const s16x4 hi = lds_transpose((lds_ptr_t)((lds_char*)lds + at + (16 * s2 + 8) * ROW));
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        // Keys with an infinity or NaN in V, of a tile that some row does not see whole.
-        uint32_t wild = 0;
-        if (__builtin_expect(masked, 0)) {
-            uint32_t hi = 0, lo = 0;                      // largest magnitudes among a key's values
-#pragma unroll
-            for (int x = 0; x < CPR / 2; ++x) {
-                const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)((lds_char*)lds + sb + HALF + j * ROW +
-                                                                                 (g * (CPR / 2) + x) * 16);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    hi = max(hi, w[i] & 0x7fffffffu);
-                    lo = max(lo, (w[i] << 16) & 0x7fffffffu);
-                }
-                if (x % 2) sched_fence();                 // few registers at a time
-            }
-            const uint64_t votes = __ballot(is_wild<F16>(max(hi, lo) >> 16));
-            wild = uniform((int)((uint32_t)votes | (uint32_t)(votes >> 32)));
-        }
-#pragma unroll
-        for (int n2 = 0; n2 < NB; n2 += 2) {
-            s16x8 vf[2][2];
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) vf[n][s2] = v_frag(n2 + n, s2);
-            sched_fence();
-            if (__builtin_expect(wild, 0)) {              // finite values only; the others follow
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        short& v = reinterpret_cast<short(&)[8]>(vf[x >> 1][x & 1])[i];
-                        v = is_wild<F16>((uint16_t)v) ? (short)0 : v;
-                    }
-            }
-#pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) oacc[n2 + n] = mfma<F16>(vf[n][s2], pf[s2], oacc[n2 + n]);
-        }
-        if (__builtin_expect(wild, 0)) {
-            // Rare: infinities and NaN, whatever their probability, into the rows that
-            // see their keys.
-            for (uint32_t left = wild; left; left &= left - 1) {
-                const int key = __builtin_ctz(left);
-                const bool sees = (see >> key) & 1;
-                const int at = sb + HALF + key * ROW + 8 * g;
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const u32x2 w = *(__attribute__((address_space(3))) const u32x2*)((lds_char*)lds + at +
-                                                                                         (((4 * n + i) ^ v_key<CPR>(key)) << 4));
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const uint32_t bits = (x & 1 ? w[x >> 1] >> 16 : w[x >> 1]) & 0xffffu;
-                            if (sees && is_wild<F16>(bits)) oacc[n][4 * i + x] += widen<F16>(bits);
-                        }
-                        sched_fence();
-                    }
-            }
-        }
-    };
-
-    // Tiles of this wave group: t0 + wk, t0 + wk + WK, ...  Copies past the last
-    // one repeat it into a stage that is not read again.
-    const int mine = (u.t1 - u.t0 - wk + WK - 1) / WK;    // may be <= 0
-    const int last = u.t0 + wk + (mine - 1) * WK;
-    Pages next{};
-    if (mine > 0) {
-#pragma unroll
-        for (int s = 0; s < NS - 1; ++s) {
-            const int kt = min(u.t0 + wk + s * WK, last);
-            issue(kt, s, pages_of(kt));
-        }
-        next = pages_of(min(u.t0 + wk + (NS - 1) * WK, last));
-    }
-    // The queries' loads end here and not inside the loop, where their wait would
-    // take the copies in flight with it.
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
-#endif
-    const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
-    int stage = 0;
-    for (int it = 0; it < mine; ++it) {
-        const int kt = u.t0 + wk + it * WK;
-        wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
-        tile_barrier<WM>();                        // the group's have; the stage before is free
-        issue(min(kt + (NS - 1) * WK, last), stage == 0 ? NS - 1 : stage - 1, next);
-        next = pages_of(min(kt + NS * WK, last));
-        const int sb = ring + stage * STAGE;
-        const uint32_t gone = (missing >> (2 * stage)) & 3;
-        stage = stage + 1 == NS ? 0 : stage + 1;
-        if (!busy) continue;
-        const int k0 = kt * kTile;
-        tile(k0 + kTile > clear || gone, k0, sb, gone);
+        s16x8 vf[2][2];
+        read_values<HD>(vf, lds, sb + D::HALF + vfrag, 0);
+        sched_fence();
+        if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, lo, hi, k0, gone), g);
+        s16x8 pf[1][2];
+        rt[0].softmax(st, a.scale_log2, pf[0]);
+        wild |= add_values<F16, HD, 1>(rt, pf, vf, lds, sb + D::HALF, lane, vfrag, masked);
     }
 
     wait_all_memory();                                    // no copy may still land in LDS
-    l_run = both_sum(l_run);
-
-    if constexpr (WK == 1) {
-        if (!busy) return;
-        const int row = wm * 32 + j;
-        if (u.parts > 1) {                                // what is left of a row until its parts are joined
-            if (row < rows) {
-                float* p = a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + 4 * g;
+    if (!busy) return;
+    if (__builtin_expect(wild, 0)) add_wild<F16, HD, 1>(rt, a, u, keys, {mrow}, u.t0, u.t1, 1, clear, g);
+    const f32x16* o = rt[0].o;
+    const float l = both_sum(rt[0].l), m = rt[0].m;
+    const int row = wave * 32 + j;
+    if (u.parts > 1) {                                    // what is left of a row until its parts are joined
+        if (row < rows) {
+            float* p = a.part_o + ((int64_t)u.slot * kManyRows + row) * HD + 4 * g;
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < D::NB; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32x4*>(p + n * 32 + 8 * i) =
-                            f32x4{oacc[n][4 * i], oacc[n][4 * i + 1], oacc[n][4 * i + 2], oacc[n][4 * i + 3]};
-                if (g == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m_run, l_run};
-            }
-            return;
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<f32x4*>(p + n * 32 + 8 * i) =
+                        f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+            if (g == 0) a.part_ml[(int64_t)u.slot * kManyRows + row] = float2{m, l};
         }
-        // Rows that saw nothing: the sum is 0 and so is every product.
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-        uint16_t* orow = a.o + t * a.o_stride + head * HD;
+        return;
+    }
+    // Rows that saw nothing: the sum is 0 and so is every product.
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* orow = a.o + t * a.o_stride + head * HD;
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            uint32_t p[4][2];
+    for (int n = 0; n < D::NB; ++n) {
+        uint32_t p[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i][0] = pack2<F16>(o[n][4 * i] * inv, o[n][4 * i + 1] * inv);
+            p[i][1] = pack2<F16>(o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv);
+        }
+        swap_halves16(p);
+        if (row < rows) {
+            uint16_t* dst = orow + n * 32 + 16 * g;
+            *reinterpret_cast<u32x4*>(dst) = u32x4{p[0][0], p[0][1], p[2][0], p[2][1]};
+            *reinterpret_cast<u32x4*>(dst + 8) = u32x4{p[1][0], p[1][1], p[3][0], p[3][1]};
+        }
+    }
+    if (a.lse && g == 0 && row < rows) a.lse[t * a.n_heads + head] = log_sum(a, m, l);
+}
+
+// ------------------------------------------------------------------ few rows
+
+// Up to 64 packed rows (RT row tiles per wave): bound by the bytes of K and V, each
+// read once, so what counts is how many are in flight.  Every wave takes tiles of its
+// own (every WAVES-th of the unit), without barriers, through S stages of its own:
+// keys of the next tile are asked for as soon as the products with this one's have
+// read them, and values likewise.  Up to 32 rows: one stage, so that a workgroup's 64
+// KB (66 with the join's sums) leave room for a second one, which works while the first
+// starts or ends; 64 rows hold twice the accumulators (420 VGPRs, one wave per SIMD):
+// two stages.  All of the 128 KB per CU are in flight but for the tiles at work.
+template <bool F16, int HD, int RT, int S>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 && RT == 1 ? 4 : RT == 1 ? 2 : 1))) void
+attend_few_kernel(const AttnArgs a) {
+    using D = Dims<HD>;
+    constexpr int WAVES = 4;
+    constexpr int COPIES = D::HALF / 1024;                // 1 KB copies of a V tile
+    constexpr int C4 = HD / 4;
+    constexpr int RING = 2 * S * D::HALF;                 // a wave's stages: S tiles of K, then of V
+    constexpr int OUT = 32 * RT * HD * 4;                 // a wave's outputs in the end, then maxima and sums
+    constexpr int OWN = RING > OUT + 32 * RT * 8 ? RING : OUT + 32 * RT * 8;
+    __shared__ __attribute__((aligned(16))) char smem[WAVES * OWN];   // the only LDS variable, as above
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int g = lane >> 5, j = lane & 31;
+    Unit u;
+    if (!find_unit<false>(a, blockIdx.x, u)) return;
+    const int rows = u.s.n * a.group;                     // one row tile: all rows of (sequence, key head)
+    Keys<HD> keys(a, u);
+    const lds_ptr_t lds = (lds_ptr_t)smem;
+    const int ring = wave * OWN;
+
+    s16x8 qf[RT][D::NKS];
+    const uint32_t* mrow[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int r = min(x * 32 + j, rows - 1);
+        const int64_t t = (int64_t)u.s.start + r / a.group;
+        const uint16_t* qp = a.q + t * a.q_stride + (u.kvh * a.group + r % a.group) * HD + g * 8;
+#pragma unroll
+        for (int ks = 0; ks < D::NKS; ++ks) qf[x][ks] = *reinterpret_cast<const s16x8*>(qp + ks * 16);
+        mrow[x] = a.mask ? a.mask + t * a.mask_words : nullptr;
+    }
+    uint32_t k_off[COPIES], v_off[COPIES];                // within a group of 16 keys, as above
+#pragma unroll
+    for (int p = 0; p < COPIES; ++p) {
+        const int row = p * D::ROWS_PER_COPY + lane / D::CPR, pc = lane % D::CPR;
+        k_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ k_key<D::CPR>(row)) << 4));
+        v_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ v_key<D::CPR>(row)) << 4));
+    }
+    auto issue = [&](const char* pool, const uint32_t (&off)[COPIES], int kt, int dst, const int2& e) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int page = s ? e.y : e.x;
+            const buf_rsrc_t r = make_rsrc(pool + keys.offset(page, kt, s), keys.bytes(page, kt, s));
+#pragma unroll
+            for (int p = s * (COPIES / 2); p < (s + 1) * (COPIES / 2); ++p)
+                copy16<true>(r, off[p], (lds_ptr_t)((lds_char*)lds + dst + p * 1024));
+        }
+    };
+    RowTile<F16, HD> rt[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) rt[x].clear();
+    const int kfrag = j * D::ROW + ((g ^ k_key<D::CPR>(j)) << 4);
+    const int vfrag = v_base<HD>(lane);
+    const int clear = a.mask ? u.s.len : u.s.keys;
+
+    // Tiles u.t0 + wave + WAVES i, i < n.  Copies past the last one repeat it.
+    const int n = (u.t1 - u.t0 - wave + WAVES - 1) / WAVES;           // may be <= 0
+    auto tile_at = [&](int i) { return u.t0 + wave + min(i, n - 1) * WAVES; };
+    // This wave's LDS reads are behind: their stage may be copied into.
+    auto reads_done = [&]() {
+        wait_lgkmcnt<0>();
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" ::: "memory");
+#endif
+    };
+    auto landed = [&]() {                                 // all but what was asked for after the oldest tile
+        wait_vmcnt<COPIES * (2 * S - 1)>();
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" ::: "memory");
+#endif
+    };
+    bool wild = false;
+    if (n > 0) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int2 e = keys.entries(tile_at(i));
+            issue(keys.k, k_off, tile_at(i), ring + i * D::HALF, e);
+            issue(keys.v, v_off, tile_at(i), ring + (S + i) * D::HALF, e);
+        }
+        int2 now = keys.entries(tile_at(0)), next = keys.entries(tile_at(S));
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+        for (int x = 0; x < RT; ++x)                      // as above: the queries' loads end here
+#pragma unroll
+            for (int ks = 0; ks < D::NKS; ++ks) asm volatile("" ::"v"(qf[x][ks]));
+#endif
+        // Mask words of a tile, read a tile ahead as above.
+        uint32_t lo[RT], hi[RT];
+        auto words = [&](int kt, uint32_t (&l)[RT], uint32_t (&h)[RT]) {
+            const int w = (kt * kTile - u.s.len) >> 5;
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                l[x] = a.mask ? mask_word(a, mrow[x], w) : 0;
+                h[x] = a.mask ? mask_word(a, mrow[x], w + 1) : 0;
+            }
+        };
+        words(tile_at(0), lo, hi);
+        int stage = 0;
+        for (int i = 0; i < n; ++i) {
+            const int k0 = tile_at(i) * kTile;
+            const int ks_at = ring + stage * D::HALF, vs_at = ks_at + S * D::HALF;
+            landed();
+            f32x16 st[RT];
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) st[x][e] = 0.f;
+            const int ka = ks_at + kfrag;
+#pragma unroll
+            for (int k4 = 0; k4 < D::NKS; k4 += 4) {
+                s16x8 kf[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    kf[y] = *(__attribute__((address_space(3))) const s16x8*)((lds_char*)lds + (ka ^ ((k4 + y) << 5)));
+                sched_fence();
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) st[x] = mfma<F16>(kf[y], qf[x][k4 + y], st[x]);
+            }
+            uint32_t lo_next[RT], hi_next[RT];
+            words(tile_at(i + 1), lo_next, hi_next);
+            reads_done();
+            issue(keys.k, k_off, tile_at(i + S), ks_at, next);
+            const uint32_t gone = keys.missing(now);
+            const bool masked = k0 + kTile > clear || gone;
+            s16x8 pf[RT][2];
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                if (__builtin_expect(masked, 0)) rt[x].hide(st[x], seen_keys(a, u.s, lo[x], hi[x], k0, gone), g);
+                rt[x].softmax(st[x], a.scale_log2, pf[x]);
+            }
+            landed();
+            s16x8 vf[2][2];
+            read_values<HD>(vf, lds, vs_at + vfrag, 0);
+            sched_fence();
+            wild |= add_values<F16, HD, RT>(rt, pf, vf, lds, vs_at, lane, vfrag, masked);
+            reads_done();
+            issue(keys.v, v_off, tile_at(i + S), vs_at, next);
+            now = S == 1 ? next : keys.entries(tile_at(i + 1));
+            next = keys.entries(tile_at(i + 1 + S));
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                lo[x] = lo_next[x];
+                hi[x] = hi_next[x];
+            }
+            stage = stage + 1 == S ? 0 : stage + 1;
+        }
+    }
+    wait_all_memory();                                    // no copy may still land in LDS
+    if (__builtin_expect(wild, 0)) add_wild<F16, HD, RT>(rt, a, u, keys, mrow, u.t0 + wave, u.t1, WAVES, clear, g);
+
+    // The waves' shares of the rows, joined through LDS: each wave's outputs in its
+    // own stages, 16-byte chunks turned by the row against bank conflicts.
+    auto ml = [&](int w, int row) -> float2& { return reinterpret_cast<float2*>(smem + w * OWN + OUT)[row]; };
+    float* own = reinterpret_cast<float*>(smem + ring);
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const float l = both_sum(rt[x].l);
+#pragma unroll
+        for (int nb = 0; nb < D::NB; ++nb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[i][0] = pack2<F16>(oacc[n][4 * i] * inv, oacc[n][4 * i + 1] * inv);
-                p[i][1] = pack2<F16>(oacc[n][4 * i + 2] * inv, oacc[n][4 * i + 3] * inv);
+                const f32x16& o = rt[x].o[nb];
+                *reinterpret_cast<f32x4*>(own + (x * 32 + j) * HD + (((nb * 8 + 2 * i + g) ^ (j & (C4 - 1))) << 2)) =
+                    f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
             }
-            swap_halves16(p);
-            if (row < rows) {
-                uint16_t* dst = orow + n * 32 + 16 * g;
-                *reinterpret_cast<u32x4*>(dst) = u32x4{p[0][0], p[0][1], p[2][0], p[2][1]};
-                *reinterpret_cast<u32x4*>(dst + 8) = u32x4{p[1][0], p[1][1], p[3][0], p[3][1]};
-            }
+        if (g == 0) ml(wave, x * 32 + j) = float2{rt[x].m, l};
+    }
+    __syncthreads();
+    for (int x = tid; x < rows * C4; x += 256) {
+        const int row = x / C4, c4 = x % C4;
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) m = fmaxf(m, ml(w, row).x);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float2 part = ml(w, row);
+            const float f = part.x == m ? 1.f : __builtin_amdgcn_exp2f((part.x - m) * a.scale_log2);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(smem + w * OWN + (row * HD + ((c4 ^ (row & 31 & (C4 - 1))) << 2)) * 4);
+            l += part.y * f;
+            o += v * f;
         }
-        if (a.lse && g == 0 && row < rows) a.lse[t * a.n_heads + head] = log_sum(a, m_run, l_run);
-    } else {
-        // The wave groups' shares of the 32 rows, joined through LDS: each wave's
-        // outputs in its own stages, 16-byte chunks turned by the row against bank
-        // conflicts.
-        constexpr int C4 = HD / 4;
-        constexpr int ML = 32 * HD * 4;                   // maxima and sums behind the outputs
-        static_assert(ML + 32 * 8 <= NS * STAGE, "a wave's outputs fit its stages");
-        float* own = reinterpret_cast<float*>(smem + ring);
-        auto ml = [&](int w, int row) -> float2& { return reinterpret_cast<float2*>(smem + w * NS * STAGE + ML)[row]; };
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4*>(own + j * HD + (((n * 8 + 2 * i + g) ^ (j & (C4 - 1))) << 2)) =
-                    f32x4{oacc[n][4 * i], oacc[n][4 * i + 1], oacc[n][4 * i + 2], oacc[n][4 * i + 3]};
-        if (g == 0) ml(wk, j) = float2{m_run, l_run};
-        __syncthreads();
-        for (int x = tid; x < rows * C4; x += 256) {
-            const int row = x / C4, c4 = x % C4;
-            float m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) m = fmaxf(m, ml(w, row).x);
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                const float2 part = ml(w, row);
-                const float f = part.x == m ? 1.f : __builtin_amdgcn_exp2f((part.x - m) * a.scale_log2);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(smem + w * NS * STAGE + (row * HD + ((c4 ^ (row & (C4 - 1))) << 2)) * 4);
-                l += part.y * f;
-                o += v * f;
-            }
-            if (u.parts > 1) {
-                *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
-                if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
-            } else {
-                const int pr = row + u.row_tile * a.rows_per_wg;
-                const int64_t to = (int64_t)u.s.start + pr / a.group;
-                const int h = u.kvh * a.group + pr % a.group;
-                store_out<F16>(a, to, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-                if (a.lse && c4 == 0) a.lse[to * a.n_heads + h] = log_sum(a, m, l);
-            }
+        if (u.parts > 1) {
+            *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
+            if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
+        } else {
+            const int64_t t = (int64_t)u.s.start + row / a.group;
+            const int h = u.kvh * a.group + row % a.group;
+            store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
+            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
         }
     }
 }
 
 // The parts of an item's rows, joined in order: blockIdx.x the item, blockIdx.y a
-// group of rows; a thread takes 4 features of a row.
+// group of rows (every gridDim.y-th).  A thread takes 4 features of a row, and of
+// the parts a run of a quarter, so that their loads are in flight together.
+constexpr int kJoinRuns = 4;
+
 template <bool F16, int HD>
 __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
-    constexpr int C4 = HD / 4;
+    constexpr int C4 = HD / 4, ROWS = 256 / (C4 * kJoinRuns);
+    __shared__ f32x4 run_o[kJoinRuns][ROWS][C4];
+    __shared__ float2 run_ml[kJoinRuns][ROWS];
     Unit u;
     if (!find_unit<true>(a, blockIdx.x, u)) return;
     const int rows = min(u.s.n * a.group - u.row_tile * a.rows_per_wg, a.rows_per_wg);
-    const int row = blockIdx.y * (256 / C4) + threadIdx.x / C4, c4 = threadIdx.x % C4;
-    if (row >= rows) return;
-    const float2* ml = a.part_ml + (int64_t)u.slot * a.rows_per_wg + row;
-    const float* po = a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int p = 0; p < u.parts; ++p) m = fmaxf(m, ml[(int64_t)p * a.rows_per_wg].x);
-    float l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int p = 0; p < u.parts; ++p) {
-        const float2 part = ml[(int64_t)p * a.rows_per_wg];
-        const f32x4 v = *reinterpret_cast<const f32x4*>(po + (int64_t)p * a.rows_per_wg * HD);
-        const float f = part.x == m ? 1.f : __builtin_amdgcn_exp2f((part.x - m) * a.scale_log2);
-        l += part.y * f;
-        o += v * f;
+    const int c4 = threadIdx.x % C4, local = threadIdx.x / C4 % ROWS, run = threadIdx.x / (C4 * ROWS);
+    const int each = (u.parts + kJoinRuns - 1) / kJoinRuns;
+    const int p0 = min(run * each, u.parts), p1 = min(p0 + each, u.parts);
+    for (int r0 = blockIdx.y * ROWS; r0 < rows; r0 += gridDim.y * ROWS) {
+        const int row = min(r0 + local, rows - 1);
+        const float2* ml = a.part_ml + (int64_t)u.slot * a.rows_per_wg + row;
+        const float* po = a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4;
+        float m = -INFINITY, l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        auto add = [&](const float2& part, const f32x4& v) {
+            const float mn = fmaxf(m, part.x);
+            const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
+            const float f1 = part.x == mn ? 1.f : __builtin_amdgcn_exp2f((part.x - mn) * a.scale_log2);
+            l = l * f0 + part.y * f1;
+            o = o * f0 + v * f1;
+            m = mn;
+        };
+        int p = p0;
+        for (; p + 8 <= p1; p += 8) {
+            float2 part[8];
+            f32x4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                part[i] = ml[(int64_t)(p + i) * a.rows_per_wg];
+                v[i] = *reinterpret_cast<const f32x4*>(po + (int64_t)(p + i) * a.rows_per_wg * HD);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) add(part[i], v[i]);
+        }
+        for (; p < p1; ++p) add(ml[(int64_t)p * a.rows_per_wg], *reinterpret_cast<const f32x4*>(po + (int64_t)p * a.rows_per_wg * HD));
+        run_o[run][local][c4] = o;
+        if (c4 == 0) run_ml[run][local] = float2{m, l};
+        __syncthreads();
+        if (run == 0 && r0 + local < rows) {
+#pragma unroll
+            for (int i = 1; i < kJoinRuns; ++i) add(run_ml[i][local], run_o[i][local][c4]);
+            const int pr = row + u.row_tile * a.rows_per_wg;
+            const int64_t t = (int64_t)u.s.start + pr / a.group;
+            const int h = u.kvh * a.group + pr % a.group;
+            store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
+            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
+        }
+        __syncthreads();
     }
-    const int pr = row + u.row_tile * a.rows_per_wg;
-    const int64_t t = (int64_t)u.s.start + pr / a.group;
-    const int h = u.kvh * a.group + pr % a.group;
-    store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-    if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
 }
 
-// How a call is laid out: packed rows of a workgroup, keys of a step, units.
+// How a call is laid out: packed rows of a workgroup, keys of a step, units.  A second
+// kernel that joins parts costs about 5 us, so short sequences are not split: up to
+// 1024 keys a unit of few rows takes them whole (641 keys, head_dim 64: 8.5 us, split
+// 6.3 + 3.8 and a launch), up to 256 one of many rows.
 struct Shape {
     int rows_per_wg, step, units, min_steps;
 };
-Shape shape_for(int max_rows, int group) {
-    // Up to 32 packed rows: one wave's worth, so the four waves of a workgroup take
-    // different keys.  More: 32 rows per wave, keys shared.
-    if ((int64_t)max_rows * group <= 32) return {32, 4 * kTile, 256, 2};
-    return {128, kTile, 512, 4};
+Shape shape_for(int max_rows, int group, int max_keys) {
+    const int64_t rows = (int64_t)max_rows * group;
+    if (rows <= 32) return {32, 4 * kTile, 512, max_keys <= 1024 ? 8 : 2};
+    if (rows <= 64) return {64, 4 * kTile, 256, max_keys <= 1024 ? 8 : 2};
+    return {kManyRows, kTile, 512, 8};
 }
 int64_t item_bound(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int rows_per_wg) {
     const int64_t per_seq = ((int64_t)max_rows * group + rows_per_wg - 1) / rows_per_wg;
@@ -695,14 +1004,22 @@ template <bool F16, int HD>
 hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t st) {
     const int64_t wgs = (items + (may_split ? a.units : 0) + 63) / 64 * 64;
     if (wgs > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)wgs), block(256);
     if (a.rows_per_wg == 32)
-        hipLaunchKernelGGL((attend_kernel<F16, HD, 4, HD == 128 ? 2 : 4, 1>), dim3((unsigned)wgs), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 1, 1>), grid, block, 0, st, a);
+    else if (a.rows_per_wg == 64)
+        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 2, 2>), grid, block, 0, st, a);
+    else if ((int64_t)a.max_rows * a.group <= kManyRows)          // one row tile: each key is read once
+        hipLaunchKernelGGL((attend_many_kernel<F16, HD, true>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((attend_kernel<F16, HD, 1, 3, 3>), dim3((unsigned)wgs), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((attend_many_kernel<F16, HD, false>), grid, block, 0, st, a);
     if (may_split) {
-        const int rows = (int)std::min<int64_t>(a.rows_per_wg, (int64_t)a.max_rows * a.group), per = 256 / (HD / 4);
-        hipLaunchKernelGGL((join_kernel<F16, HD>), dim3((unsigned)std::min<int64_t>(items, a.units), (rows + per - 1) / per),
-                           dim3(256), 0, st, a);
+        // Where there are many items few of them are split: a workgroup then walks rows.
+        const int rows = (int)std::min<int64_t>(a.rows_per_wg, (int64_t)a.max_rows * a.group);
+        const int per = 256 / (HD / 4 * kJoinRuns);
+        const int64_t x = std::min<int64_t>(items, a.units);
+        const int64_t y = std::min<int64_t>((rows + per - 1) / per, std::max<int64_t>(1, 2048 / x));
+        hipLaunchKernelGGL((join_kernel<F16, HD>), dim3((unsigned)x, (unsigned)y), dim3(256), 0, st, a);
     }
     return hipGetLastError();
 }
@@ -713,7 +1030,7 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
 // at most twice the units aimed at.
 size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
     (void)n_seqs, (void)n_kv, (void)total_rows;
-    const Shape s = shape_for(max_rows, group);
+    const Shape s = shape_for(max_rows, group, 0);
     const size_t rows = (size_t)2 * s.units * s.rows_per_wg;
     return round256(rows * head_dim * 4) + round256(rows * 8);
 }
@@ -739,7 +1056,7 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.o = (uint16_t*)o;
     a.o_stride = o_stride;
     a.lse = lse;
-    const Shape s = shape_for(max_rows, a.group);
+    const Shape s = shape_for(max_rows, a.group, max_keys);
     a.rows_per_wg = s.rows_per_wg;
     a.step = s.step;
     a.units = s.units;
