@@ -6,7 +6,6 @@ libdlm.so's HIP kernels through the C ABI.  Nothing here waits for the device.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
@@ -18,43 +17,46 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _SCALINGS = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
-def _ptr(t: torch.Tensor | None) -> int | None:
-    return None if t is None else t.data_ptr()
+# A call is a few microseconds of work on the device: what happens on the host is
+# kept to what checks and passes on the arguments.
+_raw_stream = torch._C._cuda_getCurrentRawStream      # (device index) -> hipStream_t
+_current_device = torch._C._cuda_getDevice
 
 
-def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+def _launch(fn, name: str, index: int, *args):
+    """fn(*args, stream) with device `index` current; its refusals raise."""
+    if _current_device() == index:
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status:
+        check(status, name)
 
 
-def _on(device: torch.device):
-    """The device current for the call, if it is not yet."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-
-def _ints(t: torch.Tensor | None, name: str, n: int | None, device: torch.device) -> torch.Tensor | None:
-    """t checked: a contiguous int32 tensor of n elements on the device."""
+def _ints(t: torch.Tensor | None, name: str, n: int | None, device: torch.device) -> int | None:
+    """Address of t, a contiguous int32 tensor of n elements on the device."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+    if t.dtype is not torch.int32 or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
     if n is not None and t.numel() != n:
         raise ValueError(f"{name} must hold {n} values, has {t.numel()}")
-    return t
+    return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, name: str, heads: int | None, head_dim: int, device: torch.device) -> torch.Tensor:
-    """t checked: [rows, heads, head_dim] whose heads lie next to each other."""
-    if t.dim() != 3 or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads) or t.device != device:
+def _rows(t: torch.Tensor, name: str, heads: int | None, head_dim: int, device: torch.device):
+    """(rows, heads, elements from row to row) of t [rows, heads, head_dim], whose heads
+    lie next to each other."""
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != head_dim or (heads is not None and shape[1] != heads) or t.device != device:
         raise ValueError(f"{name} must be [rows, {heads if heads is not None else 'heads'}, {head_dim}] on {device}, "
-                         f"is {tuple(t.shape)} on {t.device}")
-    if (head_dim > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != head_dim):
+                         f"is {tuple(shape)} on {t.device}")
+    n, h, _ = shape
+    row, head, one = t.stride()
+    if one != 1 or (h > 1 and head != head_dim):
         raise ValueError(f"the heads of {name} must lie next to each other")
-    return t
-
-
-def _stride(t: torch.Tensor) -> int:
-    """Elements from row to row (a single row's own length where torch gives any)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return n, h, row if n > 1 else h * head_dim           # a single row has any stride
 
 
 class Rope:
@@ -78,29 +80,31 @@ class Rope:
                            float(beta_slow), float(beta_fast))
         self.c = DlmRope()
         check(self.lib.dlm_rope_init(ctypes.byref(spec), ctypes.byref(self.c)), "dlm_rope_init")
+        self._ref = ctypes.byref(self.c)
+        self._head_dim = int(self.c.head_dim)
 
     @property
     def head_dim(self) -> int:
-        return int(self.c.head_dim)
+        return self._head_dim
 
     def apply(self, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None,
               transpose: bool = False) -> torch.Tensor:
         """x [rows, heads, head_dim] (any row and head strides) rotated to `positions`
         (int32 [rows]); into `out` (may be x).  transpose: the gradient with respect
         to x, given the gradient x of a rotation's result."""
-        if x.dim() != 3 or x.shape[2] != self.head_dim or x.dtype not in _DTYPES or not x.is_cuda:
-            raise ValueError(f"x must be a bfloat16, float16 or float32 device tensor [rows, heads, {self.head_dim}]")
+        shape, kind, device = x.shape, _DTYPES.get(x.dtype), x.device
+        if len(shape) != 3 or shape[2] != self._head_dim or kind is None or device.type != "cuda":
+            raise ValueError(f"x must be a bfloat16, float16 or float32 device tensor [rows, heads, {self._head_dim}]")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+            out = torch.empty(shape, dtype=x.dtype, device=device)
+        elif out.shape != shape or out.dtype is not x.dtype or out.device != device:
             raise ValueError("out must have x's shape, type and device")
-        if x.stride(2) != 1 or out.stride(2) != 1:
+        xs, ys = x.stride(), out.stride()
+        if xs[2] != 1 or ys[2] != 1:
             raise ValueError("the values of a head must lie next to each other")
-        _ints(positions, "positions", x.shape[0], x.device)
-        with _on(x.device):
-            check(self.lib.dlm_rope_apply(ctypes.byref(self.c), _DTYPES[x.dtype], x.shape[0], x.shape[1], x.data_ptr(),
-                                          x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
-                                          positions.data_ptr(), int(transpose), _stream(x.device)), "dlm_rope_apply")
+        pos = _ints(positions, "positions", shape[0], device)
+        _launch(self.lib.dlm_rope_apply, "dlm_rope_apply", device.index, self._ref, kind, shape[0], shape[1],
+                x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0], ys[1], pos, 1 if transpose else 0)
         return out
 
 
@@ -146,31 +150,35 @@ class PagedCache:
         c.d_k, c.d_v = self.k.data_ptr(), self.v.data_ptr()
         c.d_ref, c.d_len, c.d_table = self.ref.data_ptr(), self.len.data_ptr(), self.table.data_ptr()
         self.c = c
-        self._ws = {}
+        self._ref = ctypes.byref(c)
+        self._n_seqs, self._kv, self._hd, self._kind = int(n_seqs), int(n_kv_heads), int(head_dim), _DTYPES[dtype]
+        self._ws, self._by_size = {}, {}
         self.reset()
 
     # -------------------------------------------------------------- plumbing
     @property
     def n_seqs(self) -> int:
-        return int(self.c.n_seqs)
+        return self._n_seqs
 
     def workspace(self, total_rows: int = 0, max_rows: int = 0, n_heads: int = 0) -> torch.Tensor:
         """Workspace of calls with these sizes; kept, so that captured graphs stay valid."""
-        n = self.lib.dlm_cache_workspace_bytes(ctypes.byref(self.c), total_rows, max_rows, n_heads)
-        if n == 0:
-            raise ValueError(f"invalid sizes: {total_rows} rows, {max_rows} at most, {n_heads} heads")
-        ws = self._ws.get(n)
+        key = (total_rows, max_rows, n_heads)
+        ws = self._ws.get(key)
         if ws is None:
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            self._ws[n] = ws
+            n = self.lib.dlm_cache_workspace_bytes(self._ref, total_rows, max_rows, n_heads)
+            if n == 0:
+                raise ValueError(f"invalid sizes: {total_rows} rows, {max_rows} at most, {n_heads} heads")
+            ws = self._by_size.get(n)
+            if ws is None:
+                ws = self._by_size[n] = torch.empty(n, dtype=torch.uint8, device=self.device)
+            self._ws[key] = ws
         return ws
 
     def _call(self, name: str, *args):
-        with _on(self.device):
-            check(getattr(self.lib, name)(ctypes.byref(self.c), *args, _stream(self.device)), name)
+        _launch(getattr(self.lib, name), name, self.device.index, self._ref, *args)
 
-    def _starts(self, row_start: torch.Tensor) -> torch.Tensor:
-        return _ints(row_start, "row_start", self.n_seqs + 1, self.device)
+    def _starts(self, row_start: torch.Tensor) -> int:
+        return _ints(row_start, "row_start", self._n_seqs + 1, self.device)
 
     # -------------------------------------------------------------- pages
     def reset(self):
@@ -180,40 +188,39 @@ class PagedCache:
     def reserve(self, row_start: torch.Tensor, total_rows: int | None = None) -> torch.Tensor:
         """Room for the windows' rows; ok int32 [n_seqs].  total_rows: rows that count
         (default: no bound but row_start's own)."""
-        self._starts(row_start)
-        ok = torch.empty(self.n_seqs, dtype=torch.int32, device=self.device)
+        starts = self._starts(row_start)
+        ok = torch.empty(self._n_seqs, dtype=torch.int32, device=self.device)
         ws = self.workspace()
-        self._call("dlm_cache_reserve", row_start.data_ptr(), 1 << 24 if total_rows is None else int(total_rows),
-                   ok.data_ptr(), ws.data_ptr(), ws.numel())
+        self._call("dlm_cache_reserve", starts, 1 << 24 if total_rows is None else int(total_rows), ok.data_ptr(),
+                   ws.data_ptr(), ws.numel())
         return ok
 
     def commit(self, row_start: torch.Tensor, keep: torch.Tensor | None = None, keep_start: torch.Tensor | None = None,
                total_rows: int | None = None) -> torch.Tensor:
         """The kept rows of each window (default all) become its sequence's next tokens;
         ok int32 [n_seqs]."""
-        self._starts(row_start)
-        _ints(keep, "keep", None, self.device)
-        _ints(keep_start, "keep_start", self.n_seqs + 1, self.device)
-        ok = torch.empty(self.n_seqs, dtype=torch.int32, device=self.device)
+        starts = self._starts(row_start)
+        kept = _ints(keep, "keep", None, self.device)
+        kept_start = _ints(keep_start, "keep_start", self._n_seqs + 1, self.device)
+        ok = torch.empty(self._n_seqs, dtype=torch.int32, device=self.device)
         n_keep = 0 if keep is None else keep.numel()
         if keep is not None and n_keep == 0:
-            keep = row_start                              # an empty list has no address; nothing of it is read
-        self._call("dlm_cache_commit", row_start.data_ptr(), 1 << 24 if total_rows is None else int(total_rows),
-                   _ptr(keep), _ptr(keep_start), n_keep, ok.data_ptr())
+            kept = starts                                 # an empty list has no address; nothing of it is read
+        self._call("dlm_cache_commit", starts, 1 << 24 if total_rows is None else int(total_rows), kept, kept_start,
+                   n_keep, ok.data_ptr())
         return ok
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor) -> torch.Tensor:
         """Sequences dst become copies of src that share their pages; ok int32 [pairs]."""
-        _ints(src, "src", None, self.device)
-        _ints(dst, "dst", src.numel(), self.device)
-        ok = torch.empty(src.numel(), dtype=torch.int32, device=self.device)
-        self._call("dlm_cache_fork", src.numel(), src.data_ptr(), dst.data_ptr(), ok.data_ptr())
+        n = src.numel()
+        a, b = _ints(src, "src", None, self.device), _ints(dst, "dst", n, self.device)
+        ok = torch.empty(n, dtype=torch.int32, device=self.device)
+        self._call("dlm_cache_fork", n, a, b, ok.data_ptr())
         return ok
 
     def truncate(self, new_len: torch.Tensor | None = None):
         """Keep at most new_len[s] tokens of sequence s (negative: leave it; None: 0 for all)."""
-        _ints(new_len, "new_len", self.n_seqs, self.device)
-        self._call("dlm_cache_truncate", _ptr(new_len))
+        self._call("dlm_cache_truncate", _ints(new_len, "new_len", self._n_seqs, self.device))
 
     def compact(self) -> torch.Tensor:
         """Move the pages in use to the lowest ids; int32 [1], how many there are."""
@@ -229,30 +236,28 @@ class PagedCache:
         """Keys and values [rows, n_kv_heads, head_dim] of the windows into their reserved
         places; keys and queries rotated by `rope` to `positions` (default: the tokens'
         places).  Returns the rotated queries (in q_out if given)."""
-        KV, hd, T = int(self.c.n_kv_heads), int(self.c.head_dim), k.shape[0]
-        self._starts(row_start)
-        _rows(k, "k", KV, hd, self.device)
-        _rows(v, "v", KV, hd, self.device)
-        if v.shape[0] != T or v.dtype != k.dtype or k.dtype not in _DTYPES:
+        device, kind = self.device, k.dtype
+        starts = self._starts(row_start)
+        T, _, ks = _rows(k, "k", self._kv, self._hd, device)
+        Tv, _, vs = _rows(v, "v", self._kv, self._hd, device)
+        if Tv != T or v.dtype is not kind or kind not in _DTYPES:
             raise ValueError("k and v must have the same rows and a floating type of 16 or 32 bits")
-        _ints(positions, "positions", T, self.device)
-        heads = 0
+        pos = _ints(positions, "positions", T, device)
+        heads = qs = qos = 0
+        qp = qop = None
         if q is not None:
-            _rows(q, "q", None, hd, self.device)
-            heads = q.shape[1]
-            if q.shape[0] != T or q.dtype != k.dtype:
+            Tq, heads, qs = _rows(q, "q", None, self._hd, device)
+            if Tq != T or q.dtype is not kind:
                 raise ValueError("q must have the rows and the type of k")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-            _rows(q_out, "q_out", heads, hd, self.device)
-            if q_out.shape[0] != T or q_out.dtype != self.dtype:
+                q_out = torch.empty(q.shape, dtype=self.dtype, device=device)
+            To, _, qos = _rows(q_out, "q_out", heads, self._hd, device)
+            if To != T or q_out.dtype is not self.dtype:
                 raise ValueError("q_out must have q's rows and the cache's type")
-        if T == 0:
-            return q_out
-        self._call("dlm_cache_append", int(layer), row_start.data_ptr(), T, int(max_rows), _DTYPES[k.dtype],
-                   k.data_ptr(), _stride(k), v.data_ptr(), _stride(v), None if rope is None else ctypes.byref(rope.c),
-                   _ptr(positions), heads, _ptr(q), 0 if q is None else _stride(q), _ptr(q_out),
-                   0 if q is None else _stride(q_out))
+            qp, qop = q.data_ptr(), q_out.data_ptr()
+        if T:
+            self._call("dlm_cache_append", layer, starts, T, max_rows, _DTYPES[kind], k.data_ptr(), ks, v.data_ptr(), vs,
+                       None if rope is None else rope._ref, pos, heads, qp, qs, qop, qos)
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int,
@@ -261,27 +266,25 @@ class PagedCache:
         """Attention of the windows' rows q [rows, heads, head_dim] over their sequences'
         tokens and the window rows whose bits are set in mask (int32 [rows, words];
         None: all of them)."""
-        hd, T = int(self.c.head_dim), q.shape[0]
-        self._starts(row_start)
-        _rows(q, "q", None, hd, self.device)
+        device = self.device
+        starts = self._starts(row_start)
+        T, heads, qs = _rows(q, "q", None, self._hd, device)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-        _rows(out, "out", q.shape[1], hd, self.device)
-        if q.dtype != self.dtype or out.dtype != self.dtype or out.shape[0] != T:
+            out = torch.empty(q.shape, dtype=q.dtype, device=device)
+        To, _, os = _rows(out, "out", heads, self._hd, device)
+        if q.dtype is not self.dtype or out.dtype is not self.dtype or To != T:
             raise ValueError("q and out must have the cache's type and the same rows")
         words = 0
         if mask is not None:
             if mask.dim() != 2 or mask.shape[0] != T:
                 raise ValueError("mask must be int32 [rows, words]")
-            _ints(mask, "mask", None, self.device)
             words = mask.shape[1]
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (T, q.shape[1])
-                                or not lse.is_contiguous() or lse.device != self.device):
+        bits = _ints(mask, "mask", None, device)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, heads) or not lse.is_contiguous()
+                                or lse.device != device):
             raise ValueError("lse must be a contiguous float32 tensor [rows, heads]")
-        if T == 0:
-            return out
-        ws = self.workspace(T, int(max_rows), q.shape[1])
-        self._call("dlm_cache_attend", int(layer), row_start.data_ptr(), T, int(max_rows), int(max_keys), q.shape[1],
-                   q.data_ptr(), _stride(q), _ptr(mask), words, float(scale), out.data_ptr(), _stride(out), _ptr(lse),
-                   ws.data_ptr(), ws.numel())
+        if T:
+            ws = self.workspace(T, max_rows, heads)
+            self._call("dlm_cache_attend", layer, starts, T, max_rows, max_keys, heads, q.data_ptr(), qs, bits, words, scale,
+                       out.data_ptr(), os, None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel())
         return out
