@@ -156,21 +156,6 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_plan_kernel(CacheArgs c,
     for (int i = threadIdx.x; i < n_given; i += kPlanThreads) atomicSub(&c.ref[ws.given_up[i]], 1);
 }
 
-// Bytes from one place to another, 16 at a time, by a workgroup.
-__device__ __forceinline__ void copy_bytes(const char* src, char* dst, int bytes) {
-    constexpr int kUnroll = 4;
-    const int step = blockDim.x * 16;
-    int o = threadIdx.x * 16;
-    for (; o + (kUnroll - 1) * step < bytes; o += kUnroll * step) {
-        u32x4 x[kUnroll];
-#pragma unroll
-        for (int i = 0; i < kUnroll; ++i) x[i] = *reinterpret_cast<const u32x4*>(src + o + i * step);
-#pragma unroll
-        for (int i = 0; i < kUnroll; ++i) *reinterpret_cast<u32x4*>(dst + o + i * step) = x[i];
-    }
-    for (; o < bytes; o += step) *reinterpret_cast<u32x4*>(dst + o) = *reinterpret_cast<const u32x4*>(src + o);
-}
-
 // Tokens of the last, partly filled page of each sequence that got a page of its
 // own: one workgroup per (sequence, layer, K or V).
 __global__ __launch_bounds__(256) void reserve_copy_kernel(CacheArgs c, const int2* __restrict__ copy) {
@@ -180,7 +165,19 @@ __global__ __launch_bounds__(256) void reserve_copy_kernel(CacheArgs c, const in
     const int bytes = (c.len[b] & (c.page_len - 1)) * c.head_dim * 2;
     const int64_t head = (int64_t)c.page_len * c.head_dim * 2, page = head * c.n_kv;
     char* pool = (blockIdx.x & 1 ? c.v : c.k) + (int64_t)(blockIdx.x >> 1) * c.n_pages * page;
-    for (int h = 0; h < c.n_kv; ++h) copy_bytes(pool + move.x * page + h * head, pool + move.y * page + h * head, bytes);
+    const char* src = pool + move.x * page;
+    char* dst = pool + move.y * page;
+    constexpr int kHeads = 4;                         // at a time, their loads in flight together
+    for (int o = threadIdx.x * 16; o < bytes; o += blockDim.x * 16)
+        for (int h = 0; h < c.n_kv; h += kHeads) {
+            u32x4 x[kHeads];
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i)
+                if (h + i < c.n_kv) x[i] = *reinterpret_cast<const u32x4*>(src + (h + i) * head + o);
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i)
+                if (h + i < c.n_kv) *reinterpret_cast<u32x4*>(dst + (h + i) * head + o) = x[i];
+        }
 }
 
 // ------------------------------------------------------------------ commit
@@ -228,40 +225,53 @@ __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start
     return k;
 }
 
-// Kept rows to the front of the window: one workgroup per (layer, K or V, key
-// head) and sequence.  A chunk of rows is read whole before it is written; later
-// rows lie behind every place already written (the list rises, so its i-th row
-// is never in front of place i).
+// Kept rows to the front of the window: one workgroup per (layer, K or V, key head)
+// and sequence.  A chunk of rows is read whole before it is written; later rows lie
+// behind every place already written (the list rises, so its i-th row is never in
+// front of place i).  The first chunk is read before the list has been checked, since
+// the checks are a chain of loads themselves: from places cut to the window's pages,
+// and not written if the list fails.
 constexpr int kMoveLoads = 4;
 
 __global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
                                                           int total_rows, const int32_t* __restrict__ keep,
                                                           const int32_t* __restrict__ keep_start, int total_keep) {
     const int b = blockIdx.y;
-    const Kept k = check_commit(c, b, row_start, total_rows, keep, keep_start, total_keep);
-    if (!k.ok || !k.moves) return;
     const int chunks = c.head_dim / 8, rows_at_once = 256 * kMoveLoads / chunks;
     const int h = blockIdx.x % c.n_kv, lk = blockIdx.x / c.n_kv;
     const int64_t head = (int64_t)c.page_len * c.head_dim * 2, page = head * c.n_kv;
     char* pool = (lk & 1 ? c.v : c.k) + (int64_t)(lk >> 1) * c.n_pages * page + h * head;
+    const int len = max(c.len[b], 0), first = max(keep_start[b], 0);
+    const int listed = min(max(keep_start[b + 1] - first, 0), total_keep - min(first, total_keep));
+    const int n = window_rows(row_start, b, total_rows);
+    if (n == 0) return;
+    // Place of a token (chunk threadIdx % chunks of it), in some page whatever the table holds.
     auto place = [&](int64_t t) {
-        const int p = c.table[(int64_t)b * c.max_pages + (t >> c.page_log2)];
-        return pool + p * page + (t & (c.page_len - 1)) * c.head_dim * 2 + (threadIdx.x % chunks) * 16;
+        const int e = (int)min(t >> c.page_log2, (int64_t)c.max_pages - 1);
+        const int p = c.table[(int64_t)b * c.max_pages + e];
+        return pool + (names_page(p, c) ? p : 0) * page + (t & (c.page_len - 1)) * c.head_dim * 2 +
+               (threadIdx.x % chunks) * 16;
     };
-    for (int r0 = 0; r0 < k.m; r0 += rows_at_once) {
-        u32x4 x[kMoveLoads];
-        int from[kMoveLoads];
+    u32x4 x[kMoveLoads];
+    int from[kMoveLoads];
+    auto read = [&](int r0) {
 #pragma unroll
         for (int i = 0; i < kMoveLoads; ++i) {
             const int r = r0 + (i * 256 + (int)threadIdx.x) / chunks;
-            from[i] = r < k.m ? keep[k.first + r] : r;
-            if (from[i] != r) x[i] = *reinterpret_cast<const u32x4*>(place((int64_t)k.len + from[i]));
+            from[i] = r < listed ? min(max(keep[first + r], 0), n - 1) : r;
+            if (from[i] != r) x[i] = *reinterpret_cast<const u32x4*>(place((int64_t)len + from[i]));
         }
+    };
+    read(0);
+    const Kept k = check_commit(c, b, row_start, total_rows, keep, keep_start, total_keep);
+    if (!k.ok || !k.moves) return;                    // else k.m is `listed`, and no row was cut
+    for (int r0 = 0; r0 < k.m; r0 += rows_at_once) {
+        if (r0) read(r0);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kMoveLoads; ++i) {
             const int r = r0 + (i * 256 + (int)threadIdx.x) / chunks;
-            if (from[i] != r) *reinterpret_cast<u32x4*>(place((int64_t)k.len + r)) = x[i];
+            if (from[i] != r) *reinterpret_cast<u32x4*>(place((int64_t)len + r)) = x[i];
         }
         __syncthreads();
     }
@@ -366,19 +376,31 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CacheArgs c,
     }
 }
 
-// Pages to their new places.  The work list (page, layer, K or V) is walked by a
-// fixed grid, since only the device knows its length; the last `table_blocks`
-// workgroups bring tables and references in line meanwhile, which the copies do
-// not read.
+// Pages to their new places.  The work list (page, layer, K or V, piece of 16 KB) is
+// walked by a fixed grid, since only the device knows its length; the last workgroups
+// bring tables and references in line meanwhile, which the copies do not read.  More
+// than the caches hold in general, so past their replacement.
+constexpr int kPiece = 16384;                         // 4 accesses of 16 bytes per thread
+
 __global__ __launch_bounds__(256) void compact_move_kernel(CacheArgs c, CompactPlan ws, int copy_blocks) {
     const int n = *ws.n_moves;
     if ((int)blockIdx.x < copy_blocks) {
-        const int64_t page = (int64_t)c.n_kv * c.page_len * c.head_dim * 2;
-        const int64_t units = (int64_t)n * c.n_layers * 2;
+        const int page = c.n_kv * c.page_len * c.head_dim * 2;            // at most 4 MB, a multiple of 2 KB
+        const int pieces = (page + kPiece - 1) / kPiece, per_page = 2 * c.n_layers * pieces;
+        const int64_t units = (int64_t)n * per_page;
         for (int64_t u = blockIdx.x; u < units; u += copy_blocks) {
-            const int i = (int)(u / (2 * c.n_layers)), lk = (int)(u % (2 * c.n_layers));
+            const int i = (int)(u / per_page), rest = (int)(u % per_page);
+            const int lk = rest / pieces, o0 = rest % pieces * kPiece + (int)threadIdx.x * 16;
             char* pool = (lk & 1 ? c.v : c.k) + (int64_t)(lk >> 1) * c.n_pages * page;
-            copy_bytes(pool + ws.src[i] * page, pool + ws.dst[i] * page, (int)page);
+            const char* src = pool + (int64_t)ws.src[i] * page;
+            char* dst = pool + (int64_t)ws.dst[i] * page;
+            u32x4 x[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (o0 + q * 4096 < page) x[q] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + o0 + q * 4096));
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (o0 + q * 4096 < page) __builtin_nontemporal_store(x[q], reinterpret_cast<u32x4*>(dst + o0 + q * 4096));
         }
         return;
     }

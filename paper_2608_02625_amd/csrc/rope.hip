@@ -11,6 +11,8 @@
 //
 // Bound by the bytes of the rows: a thread takes one vector of pairs of a row,
 // computes its sines and cosines once and walks heads with them.
+#include <algorithm>
+
 #include "common.h"
 #include "cache.h"
 
@@ -42,24 +44,36 @@ template <typename T, int N>
 struct alignas(sizeof(T) * N) Vec {
     T v[N];
 };
+// One access; STREAM: past the caches' replacement.
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load(const void* p) {
+    if constexpr (STREAM && sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_nontemporal_load((const u32x4*)p));
+    else if constexpr (STREAM && sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_nontemporal_load((const u32x2*)p));
+    else return *(const V*)p;
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store(void* p, const V& v) {
+    if constexpr (STREAM && sizeof(V) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+    else if constexpr (STREAM && sizeof(V) == 8) __builtin_nontemporal_store(__builtin_bit_cast(u32x2, v), (u32x2*)p);
+    else *(V*)p = v;
+}
 
 // V pairs of a head: from src to dst (rotated by (c, s) where `rotate`), the
 // pairs being values at offsets o .. o + V - 1 and o + half .. (INTER: at 2 o ..
 // 2 (o + V) - 1).
-template <typename S, typename D, int V, bool INTER>
+template <typename S, typename D, int V, bool INTER, bool STREAM>
 __device__ __forceinline__ void turn_pairs(const S* src, D* dst, int o, int half, const float (&c)[V],
                                            const float (&s)[V], bool rotate) {
     float a[V], b[V];
     if constexpr (INTER) {
-        const Vec<S, 2 * V> x = *reinterpret_cast<const Vec<S, 2 * V>*>(src + 2 * o);
+        const auto x = load<STREAM, Vec<S, 2 * V>>(src + 2 * o);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             a[i] = to_f32(x.v[2 * i]);
             b[i] = to_f32(x.v[2 * i + 1]);
         }
     } else {
-        const Vec<S, V> x = *reinterpret_cast<const Vec<S, V>*>(src + o);
-        const Vec<S, V> y = *reinterpret_cast<const Vec<S, V>*>(src + o + half);
+        const auto x = load<STREAM, Vec<S, V>>(src + o), y = load<STREAM, Vec<S, V>>(src + o + half);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             a[i] = to_f32(x.v[i]);
@@ -81,7 +95,7 @@ __device__ __forceinline__ void turn_pairs(const S* src, D* dst, int o, int half
             x.v[2 * i] = (D)a[i];
             x.v[2 * i + 1] = (D)b[i];
         }
-        *reinterpret_cast<Vec<D, 2 * V>*>(dst + 2 * o) = x;
+        store<STREAM>(dst + 2 * o, x);
     } else {
         Vec<D, V> x, y;
 #pragma unroll
@@ -89,17 +103,17 @@ __device__ __forceinline__ void turn_pairs(const S* src, D* dst, int o, int half
             x.v[i] = (D)a[i];
             y.v[i] = (D)b[i];
         }
-        *reinterpret_cast<Vec<D, V>*>(dst + o) = x;
-        *reinterpret_cast<Vec<D, V>*>(dst + o + half) = y;
+        store<STREAM>(dst + o, x);
+        store<STREAM>(dst + o + half, y);
     }
 }
-template <typename S, typename D, int V>
+template <typename S, typename D, int V, bool STREAM>
 __device__ __forceinline__ void pass_values(const S* src, D* dst) {
-    const Vec<S, V> x = *reinterpret_cast<const Vec<S, V>*>(src);
+    const auto x = load<STREAM, Vec<S, V>>(src);
     Vec<D, V> y;
 #pragma unroll
     for (int i = 0; i < V; ++i) y.v[i] = (D)to_f32(x.v[i]);
-    *reinterpret_cast<Vec<D, V>*>(dst) = y;
+    store<STREAM>(dst, y);
 }
 
 // How a workgroup's threads are laid over a head, the heads and the rows:
@@ -120,7 +134,7 @@ __device__ __forceinline__ void angles(const uint64_t* phase, float scale, int64
     }
 }
 
-template <typename T, int V, bool INTER>
+template <typename T, int V, bool INTER, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T* x, int64_t x_row, int64_t x_head, T* y,
                                                    int64_t y_row, int64_t y_head, const int32_t* __restrict__ pos,
                                                    int rows, int heads, Lanes ln, bool back) {
@@ -134,20 +148,20 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
     if (lane < ln.turn) {
         float c[V], s[V];
         angles<V>(rope.phase, rope.scale, pos[r], lane * V, back, c, s);
-#pragma unroll 2
+#pragma unroll 4
         for (int h = h0; h < heads; h += ln.slots)
-            turn_pairs<T, T, V, INTER>(x + h * x_head, y + h * y_head, lane * V, rope.rot_dim / 2, c, s, true);
+            turn_pairs<T, T, V, INTER, STREAM>(x + h * x_head, y + h * y_head, lane * V, rope.rot_dim / 2, c, s, true);
     } else {
         const int o = rope.rot_dim + (lane - ln.turn) * V;
 #pragma unroll 2
-        for (int h = h0; h < heads; h += ln.slots) pass_values<T, T, V>(x + h * x_head + o, y + h * y_head + o);
+        for (int h = h0; h < heads; h += ln.slots) pass_values<T, T, V, STREAM>(x + h * x_head + o, y + h * y_head + o);
     }
 }
 
 // Keys, values and queries of the rows of sequence blockIdx.y.  Head indexes run
 // over the keys, the values, then the queries.  Values take the keys' lanes
 // without a rotation.
-template <typename S, typename D, int V, bool INTER>
+template <typename S, typename D, int V, bool INTER, bool STREAM>
 __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheArgs c, int64_t layer_base,
                                                      const int32_t* __restrict__ row_start, int total_rows,
                                                      int max_rows, const S* k, int64_t k_stride, const S* v,
@@ -176,7 +190,7 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
     float co[V], si[V];
     const bool rotate = rope.scale != 0.f;                    // 0: no rotation asked for
     if (turns && rotate) angles<V>(rope.phase, rope.scale, pos ? pos[r] : t, o, false, co, si);
-#pragma unroll 2
+#pragma unroll 4
     for (int h = h0; h < n_all; h += ln.slots) {
         const S* src;
         D* dst;
@@ -192,9 +206,9 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
         }
         if (h < 2 * c.n_kv && !held) continue;
         if (turns)
-            turn_pairs<S, D, V, INTER>(src, dst, o, rope.rot_dim / 2, co, si, rotate && (h < c.n_kv || h >= 2 * c.n_kv));
+            turn_pairs<S, D, V, INTER, STREAM>(src, dst, o, rope.rot_dim / 2, co, si, rotate && (h < c.n_kv || h >= 2 * c.n_kv));
         else
-            pass_values<S, D, V>(src + o, dst + o);
+            pass_values<S, D, V, STREAM>(src + o, dst + o);
     }
 }
 
@@ -203,6 +217,10 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
 bool fits(const void* p, int elem, int n, int64_t stride) {
     return (uintptr_t)p % ((size_t)n * elem) == 0 && stride % n == 0;
 }
+// Whether a call's bytes are too many for the 256 MB memory-side cache to keep any for
+// the next kernel: then they go past it.  A copy of 2 x 160 MB runs at 5.6 TB/s, past
+// the caches at 6.2; one of 2 x 32 MB (which stays cached) at 6.8 and 5.7.
+bool streams(int64_t bytes) { return bytes >= (int64_t)128 << 20; }
 // Most pairs per access: V values (half layout) or 2 V (interleaved) make at most
 // 16 bytes of the wider type; `aligned(n)` tells whether accesses of n values are.
 template <typename F>
@@ -213,27 +231,38 @@ int pairs_per_access(const dlm_rope& r, int elem, F aligned) {
     }
     return 1;
 }
-// Few rows: a thread per (row, head, vector of pairs), so that the whole chip
-// has work; many: threads walk heads and reuse their sines and cosines.
+// A thread walks heads with its sines and cosines.  How many heads a workgroup takes at
+// a time: the number that leaves the fewest threads and turns idle, the largest of
+// those (4099 rows of 16 heads of 20 lanes: 9.0 us, where 8 heads of one row leave a
+// third of the workgroup idle, 11.0; 20000 rows of 24 heads of 16 lanes: 8 heads of 2
+// rows 65 us, 2 heads of 8 rows 78).
 Lanes lay_out(const dlm_rope& r, int V, int64_t rows, int heads) {
-    Lanes ln{r.rot_dim / 2 / V, (r.head_dim - r.rot_dim) / V, heads, 1};
-    const int lanes = ln.turn + ln.pass, most = 256 / lanes;
-    while (ln.slots > 1 && rows * lanes * ln.slots > (1 << 20)) ln.slots = (ln.slots + 1) / 2;
-    if (ln.slots > most) ln.slots = most;
-    ln.rows = most / ln.slots;
-    return ln;
+    const int turn = r.rot_dim / 2 / V, pass = (r.head_dim - r.rot_dim) / V;
+    const int most = 256 / (turn + pass);
+    Lanes best{turn, pass, 1, 1};
+    double best_use = 0.;
+    for (int s = 1; s <= heads && s <= most; ++s) {
+        const int rows_at_once = (int)std::min<int64_t>(most / s, rows);
+        const double use = (double)(s * rows_at_once) / most * heads / (s * ((heads + s - 1) / s));
+        if (use >= best_use) {
+            best_use = use;
+            best.slots = s;
+            best.rows = rows_at_once;
+        }
+    }
+    return best;
 }
 
-template <typename T, int V>
+template <typename T, int V, bool STREAM = false>
 hipError_t rope_layout(const dlm_rope& r, int rows, int heads, const void* x, int64_t xr, int64_t xh, void* y,
                        int64_t yr, int64_t yh, const int32_t* pos, bool back, hipStream_t st) {
     const Lanes ln = lay_out(r, V, rows, heads);
     const dim3 grid((rows + ln.rows - 1) / ln.rows);
     if (r.interleaved)
-        hipLaunchKernelGGL((rope_kernel<T, V, true>), grid, dim3(256), 0, st, r, (const T*)x, xr, xh, (T*)y, yr, yh, pos,
+        hipLaunchKernelGGL((rope_kernel<T, V, true, STREAM>), grid, dim3(256), 0, st, r, (const T*)x, xr, xh, (T*)y, yr, yh, pos,
                            rows, heads, ln, back);
     else
-        hipLaunchKernelGGL((rope_kernel<T, V, false>), grid, dim3(256), 0, st, r, (const T*)x, xr, xh, (T*)y, yr, yh, pos,
+        hipLaunchKernelGGL((rope_kernel<T, V, false, STREAM>), grid, dim3(256), 0, st, r, (const T*)x, xr, xh, (T*)y, yr, yh, pos,
                            rows, heads, ln, back);
     return hipGetLastError();
 }
@@ -244,6 +273,12 @@ hipError_t rope_type(const dlm_rope& r, int rows, int heads, const void* x, int6
         return fits(x, sizeof(T), n, xr) && fits(x, sizeof(T), n, xh) && fits(y, sizeof(T), n, yr) &&
                fits(y, sizeof(T), n, yh);
     });
+    // Widest accesses: 8 pairs of two bytes, 4 of four; interleaved ones half as many.
+    constexpr int W = 16 / sizeof(T);
+    const bool stream = streams(2 * (int64_t)rows * heads * r.head_dim * sizeof(T));
+    if (V == W && stream) return rope_layout<T, W, true>(r, rows, heads, x, xr, xh, y, yr, yh, pos, back, st);
+    if (r.interleaved && V == W / 2 && stream)
+        return rope_layout<T, W / 2, true>(r, rows, heads, x, xr, xh, y, yr, yh, pos, back, st);
     if constexpr (sizeof(T) == 2)
         if (V == 8) return rope_layout<T, 8>(r, rows, heads, x, xr, xh, y, yr, yh, pos, back, st);
     if (V == 4) return rope_layout<T, 4>(r, rows, heads, x, xr, xh, y, yr, yh, pos, back, st);
@@ -265,18 +300,18 @@ struct AppendCall {
     int64_t q_out_stride;
     hipStream_t st;
 };
-template <typename S, typename D, int V>
+template <typename S, typename D, int V, bool STREAM = false>
 hipError_t append_layout(const AppendCall& a) {
     const int n_all = 2 * a.c.n_kv + (a.q ? a.n_heads : 0);
-    const Lanes ln = lay_out(a.rope, V, a.total_rows, n_all);
+    const Lanes ln = lay_out(a.rope, V, a.max_rows, n_all);
     const dim3 grid((a.max_rows + ln.rows - 1) / ln.rows, a.c.n_seqs);
     const int64_t layer_base = (int64_t)a.layer * a.c.n_pages * a.c.n_kv * a.c.page_len * a.c.head_dim;
     if (a.rope.interleaved)
-        hipLaunchKernelGGL((append_kernel<S, D, V, true>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base,
+        hipLaunchKernelGGL((append_kernel<S, D, V, true, STREAM>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base,
                            a.row_start, a.total_rows, a.max_rows, (const S*)a.k, a.k_stride, (const S*)a.v, a.v_stride,
                            a.pos, a.n_heads, (const S*)a.q, a.q_stride, (D*)a.q_out, a.q_out_stride, ln);
     else
-        hipLaunchKernelGGL((append_kernel<S, D, V, false>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base,
+        hipLaunchKernelGGL((append_kernel<S, D, V, false, STREAM>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base,
                            a.row_start, a.total_rows, a.max_rows, (const S*)a.k, a.k_stride, (const S*)a.v, a.v_stride,
                            a.pos, a.n_heads, (const S*)a.q, a.q_stride, (D*)a.q_out, a.q_out_stride, ln);
     return hipGetLastError();
@@ -287,6 +322,11 @@ hipError_t append_type(const AppendCall& a) {
         return fits(a.k, sizeof(S), n, a.k_stride) && fits(a.v, sizeof(S), n, a.v_stride) &&
                (!a.q || (fits(a.q, sizeof(S), n, a.q_stride) && fits(a.q_out, sizeof(D), n, a.q_out_stride)));
     });
+    constexpr int W = 16 / sizeof(S);
+    const int64_t width = (int64_t)(2 * a.c.n_kv + (a.q ? a.n_heads : 0)) * a.c.head_dim;
+    const bool stream = streams(a.total_rows * width * (int64_t)(sizeof(S) + sizeof(D)));
+    if (V == W && stream) return append_layout<S, D, W, true>(a);
+    if (a.rope.interleaved && V == W / 2 && stream) return append_layout<S, D, W / 2, true>(a);
     if constexpr (sizeof(S) == 2)
         if (V == 8) return append_layout<S, D, 8>(a);
     if (V == 4) return append_layout<S, D, 4>(a);
