@@ -549,21 +549,24 @@ __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
 // ------------------------------------------------------------------ many rows
 
 // More than 64 packed rows: 4 waves of 32 rows share tiles of K and V in LDS, three
-// stages of them, copied by all.  164 VGPRs at head_dim 128, so three workgroups (12
-// waves) share a CU, 48 KB of LDS each.
+// stages of them, copied by all.  WK = 1: 168 VGPRs at head_dim 128, so three
+// workgroups (12 waves) share a CU, 48 KB of LDS each.  WK = 2, for calls with too few
+// rows to fill the chip: two such groups of waves take tiles in turn and add up in the
+// end, half the steps and half the parts to join for the same split.
 constexpr int kManyRows = 128, kManyStages = 3;
 
-template <bool F16, int HD, bool ONCE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attend_many_kernel(const AttnArgs a) {
+template <bool F16, int HD, bool ONCE, int WK>
+__global__ __launch_bounds__(256 * WK) __attribute__((amdgpu_waves_per_eu(WK == 1 ? 3 : 2))) void
+attend_many_kernel(const AttnArgs a) {
     using D = Dims<HD>;
     constexpr int NS = kManyStages, STAGE = 2 * D::HALF;
     constexpr int COPIES = D::HALF / 1024 / 4;            // 1 KB copies per wave of a K or V tile
     // The kernel's only LDS variable: with a second one the compiler tells the two
     // apart, takes a fragment read to depend on every copy in flight into this one,
     // and waits for them all.
-    __shared__ __attribute__((aligned(16))) char smem[NS * STAGE];
+    __shared__ __attribute__((aligned(16))) char smem[WK * NS * STAGE];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform((tid >> 6) & 3), wk = uniform(tid >> 8);
     const int g = lane >> 5, j = lane & 31;
     Unit u;
     // Neighbouring units share their keys (row tiles): workgroups go to the 8 XCDs
@@ -587,6 +590,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
         v_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ v_key<D::CPR>(row)) << 4));
     }
     const lds_ptr_t lds = (lds_ptr_t)smem;
+    const int ring = wk * NS * STAGE;
     const int sub = wave * COPIES * D::ROWS_PER_COPY / 16;
     uint32_t missing = 0;                                 // two bits per stage: groups without a page
     auto issue = [&](int kt, int stage) {
@@ -595,7 +599,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
         const int page = sub ? e.y : e.x, bytes = keys.bytes(page, kt, sub);
         const int64_t at = keys.offset(page, kt, sub);
         const buf_rsrc_t kr = make_rsrc(keys.k + at, bytes), vr = make_rsrc(keys.v + at, bytes);
-        const int d = stage * STAGE + wave * COPIES * 1024;
+        const int d = ring + stage * STAGE + wave * COPIES * 1024;
 #pragma unroll
         for (int p = 0; p < COPIES; ++p) copy16<ONCE>(kr, k_off[p], (lds_ptr_t)((lds_char*)lds + d + p * 1024));
 #pragma unroll
@@ -615,11 +619,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
     const uint32_t* mrow = a.mask ? a.mask + t * a.mask_words : nullptr;
     const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
 
-    // Copies past the last tile repeat it into a stage that is not read again.
-    const int last = u.t1 - 1;
-    if (u.t0 < u.t1) {
+    // Tiles u.t0 + wk + WK i, i < n, the same n for all waves (they meet at every one):
+    // copies past the last tile repeat it, and a step on it is one that no row sees.
+    const int n = (u.t1 - u.t0 + WK - 1) / WK;
+    auto tile_at = [&](int i) { return min(u.t0 + wk + i * WK, u.t1 - 1); };
+    if (n > 0) {
 #pragma unroll
-        for (int s = 0; s < NS - 1; ++s) issue(min(u.t0 + s, last), s);
+        for (int s = 0; s < NS - 1; ++s) issue(tile_at(s), s);
     }
     // The queries' loads end here and not inside the loop, where their wait would
     // take the copies in flight with it.
@@ -627,27 +633,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
 #pragma unroll
     for (int ks = 0; ks < D::NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
 #endif
-    // Words of the row's mask for this tile and the next one, read a tile ahead: in
-    // front of that tile's copies, so that waiting for them does not wait for those.
-    const int w0 = ((u.t0 * kTile) - u.s.len) >> 5;
-    uint32_t word0 = 0, word1 = 0, word2 = 0;
-    if (a.mask) {
-        word0 = mask_word(a, mrow, w0);
-        word1 = mask_word(a, mrow, w0 + 1);
+    // Words of the row's mask for this tile, read a tile ahead: in front of that tile's
+    // copies, so that waiting for them does not wait for those.
+    uint32_t lo = 0, hi = 0;
+    auto word_of = [&](int kt) { return (kt * kTile - u.s.len) >> 5; };
+    if (a.mask && n > 0) {
+        lo = mask_word(a, mrow, word_of(tile_at(0)));
+        hi = mask_word(a, mrow, word_of(tile_at(0)) + 1);
     }
     int stage = 0;
     bool wild = false;
-    for (int kt = u.t0; kt < u.t1; ++kt) {
+    for (int i = 0; i < n; ++i) {
         wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
         lds_barrier();                                    // everyone's have; the stage before is free
-        if (a.mask) word2 = mask_word(a, mrow, w0 + kt - u.t0 + 2);
-        issue(min(kt + NS - 1, last), stage == 0 ? NS - 1 : stage - 1);
-        const int sb = stage * STAGE;
-        const uint32_t gone = (missing >> (2 * stage)) & 3;
+        uint32_t lo_next = 0, hi_next = 0;
+        if (a.mask) {
+            lo_next = mask_word(a, mrow, word_of(tile_at(i + 1)));
+            hi_next = mask_word(a, mrow, word_of(tile_at(i + 1)) + 1);
+        }
+        issue(tile_at(i + NS - 1), stage == 0 ? NS - 1 : stage - 1);
+        const int kt = u.t0 + wk + i * WK, sb = ring + stage * STAGE;
+        const uint32_t gone = kt < u.t1 ? (missing >> (2 * stage)) & 3 : 3;
         stage = stage + 1 == NS ? 0 : stage + 1;
-        const uint32_t lo = word0, hi = word1;
-        word0 = word1;
-        word1 = word2;
+        const uint32_t w0 = lo, w1 = hi;
+        lo = lo_next;
+        hi = hi_next;
         if (!busy) continue;
         const int k0 = kt * kTile;
         const bool masked = k0 + kTile > clear || gone;
@@ -669,27 +679,54 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
         s16x8 vf[2][2];
         read_values<HD>(vf, lds, sb + D::HALF + vfrag, 0);
         sched_fence();
-        if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, lo, hi, k0, gone), g);
+        if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, w0, w1, k0, gone), g);
         s16x8 pf[1][2];
         rt[0].softmax(st, a.scale_log2, pf[0]);
         wild |= add_values<F16, HD, 1>(rt, pf, vf, lds, sb + D::HALF, lane, vfrag, masked);
     }
 
     wait_all_memory();                                    // no copy may still land in LDS
-    if (!busy) return;
-    if (__builtin_expect(wild, 0)) add_wild<F16, HD, 1>(rt, a, u, keys, {mrow}, u.t0, u.t1, 1, clear, g);
-    const f32x16* o = rt[0].o;
-    const float l = both_sum(rt[0].l), m = rt[0].m;
+    if (__builtin_expect(wild, 0)) add_wild<F16, HD, 1>(rt, a, u, keys, {mrow}, u.t0 + wk, u.t1, WK, clear, g);
+    f32x16* o = rt[0].o;
+    float l = both_sum(rt[0].l), m = rt[0].m;
     const int row = wave * 32 + j;
+    if constexpr (WK == 2) {
+        // The second group's outputs through LDS, lane by lane: both hold the same rows
+        // and features in the same registers.
+        static_assert(4 * (D::NB * 16 + 2) * 64 * 4 <= WK * NS * STAGE, "the outputs fit the stages");
+        float* slot = reinterpret_cast<float*>(smem) + wave * ((D::NB * 16 + 2) * 64) + lane;
+        __syncthreads();
+        if (wk == 1) {
+#pragma unroll
+            for (int nb = 0; nb < D::NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) slot[(nb * 16 + e) * 64] = o[nb][e];
+            slot[D::NB * 16 * 64] = m;
+            slot[(D::NB * 16 + 1) * 64] = l;
+        }
+        __syncthreads();
+        if (wk == 1) return;
+        const float m1 = slot[D::NB * 16 * 64], l1 = slot[(D::NB * 16 + 1) * 64];
+        const float mn = fmaxf(m, m1);
+        const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
+        const float f1 = m1 == mn ? 1.f : __builtin_amdgcn_exp2f((m1 - mn) * a.scale_log2);
+#pragma unroll
+        for (int nb = 0; nb < D::NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[nb][e] = o[nb][e] * f0 + slot[(nb * 16 + e) * 64] * f1;
+        l = l * f0 + l1 * f1;
+        m = mn;
+    }
+    if (!busy) return;
     if (u.parts > 1) {                                    // what is left of a row until its parts are joined
         if (row < rows) {
             float* p = a.part_o + ((int64_t)u.slot * kManyRows + row) * HD + 4 * g;
 #pragma unroll
-            for (int n = 0; n < D::NB; ++n)
+            for (int nb = 0; nb < D::NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<f32x4*>(p + n * 32 + 8 * i) =
-                        f32x4{o[n][4 * i], o[n][4 * i + 1], o[n][4 * i + 2], o[n][4 * i + 3]};
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<f32x4*>(p + nb * 32 + 8 * e) =
+                        f32x4{o[nb][4 * e], o[nb][4 * e + 1], o[nb][4 * e + 2], o[nb][4 * e + 3]};
             if (g == 0) a.part_ml[(int64_t)u.slot * kManyRows + row] = float2{m, l};
         }
         return;
@@ -698,16 +735,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
     const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t* orow = a.o + t * a.o_stride + head * HD;
 #pragma unroll
-    for (int n = 0; n < D::NB; ++n) {
+    for (int nb = 0; nb < D::NB; ++nb) {
         uint32_t p[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            p[i][0] = pack2<F16>(o[n][4 * i] * inv, o[n][4 * i + 1] * inv);
-            p[i][1] = pack2<F16>(o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv);
+            p[i][0] = pack2<F16>(o[nb][4 * i] * inv, o[nb][4 * i + 1] * inv);
+            p[i][1] = pack2<F16>(o[nb][4 * i + 2] * inv, o[nb][4 * i + 3] * inv);
         }
         swap_halves16(p);
         if (row < rows) {
-            uint16_t* dst = orow + n * 32 + 16 * g;
+            uint16_t* dst = orow + nb * 32 + 16 * g;
             *reinterpret_cast<u32x4*>(dst) = u32x4{p[0][0], p[0][1], p[2][0], p[2][1]};
             *reinterpret_cast<u32x4*>(dst + 8) = u32x4{p[1][0], p[1][1], p[3][0], p[3][1]};
         }
@@ -981,17 +1018,22 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
     }
 }
 
-// How a call is laid out: packed rows of a workgroup, keys of a step, units.  A second
-// kernel that joins parts costs about 5 us, so short sequences are not split: up to
-// 1024 keys a unit of few rows takes them whole (641 keys, head_dim 64: 8.5 us, split
-// 6.3 + 3.8 and a launch), up to 256 one of many rows.
+// How a call is laid out: packed rows of a workgroup, keys of a step, units, least
+// steps of a unit.  A second kernel that joins parts costs about 5 us, so short
+// sequences are not split: up to 1024 keys a unit of few rows takes them whole (641
+// keys, head_dim 64: 8.5 us, split 6.3 + 3.8 and a launch), up to 256 one of many rows.
+// Many rows: with no more row tiles than CUs two wave groups each (8 trees of up to 64
+// rows over 512 to 4096 keys: 18.0 + 7.6 us with the join, one group 20.7 + 9.0); with
+// more of them one group, three workgroups per CU (8 x 1024 rows: 87 us, two groups
+// 107).
 struct Shape {
     int rows_per_wg, step, units, min_steps;
 };
-Shape shape_for(int max_rows, int group, int max_keys) {
+Shape shape_for(int max_rows, int group, int64_t many_items, int max_keys) {
     const int64_t rows = (int64_t)max_rows * group;
     if (rows <= 32) return {32, 4 * kTile, 512, max_keys <= 1024 ? 8 : 2};
     if (rows <= 64) return {64, 4 * kTile, 256, max_keys <= 1024 ? 8 : 2};
+    if (many_items <= 256) return {kManyRows, 2 * kTile, 256, 4};
     return {kManyRows, kTile, 512, 8};
 }
 int64_t item_bound(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int rows_per_wg) {
@@ -1009,10 +1051,18 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
         hipLaunchKernelGGL((attend_few_kernel<F16, HD, 1, 1>), grid, block, 0, st, a);
     else if (a.rows_per_wg == 64)
         hipLaunchKernelGGL((attend_few_kernel<F16, HD, 2, 2>), grid, block, 0, st, a);
-    else if ((int64_t)a.max_rows * a.group <= kManyRows)          // one row tile: each key is read once
-        hipLaunchKernelGGL((attend_many_kernel<F16, HD, true>), grid, block, 0, st, a);
-    else
-        hipLaunchKernelGGL((attend_many_kernel<F16, HD, false>), grid, block, 0, st, a);
+    else {
+        const bool once = (int64_t)a.max_rows * a.group <= kManyRows;     // one row tile: each key is read once
+        const bool two = a.step == 2 * kTile;
+        if (two && once)
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 2>), grid, dim3(512), 0, st, a);
+        else if (two)
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 2>), grid, dim3(512), 0, st, a);
+        else if (once)
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 1>), grid, block, 0, st, a);
+        else
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 1>), grid, block, 0, st, a);
+    }
     if (may_split) {
         // Where there are many items few of them are split: a workgroup then walks rows.
         const int rows = (int)std::min<int64_t>(a.rows_per_wg, (int64_t)a.max_rows * a.group);
@@ -1029,8 +1079,7 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
 // Split items have at least two parts of which all but one are full, so they make
 // at most twice the units aimed at.
 size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
-    (void)n_seqs, (void)n_kv, (void)total_rows;
-    const Shape s = shape_for(max_rows, group, 0);
+    const Shape s = shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), 0);
     const size_t rows = (size_t)2 * s.units * s.rows_per_wg;
     return round256(rows * head_dim * 4) + round256(rows * 8);
 }
@@ -1056,7 +1105,8 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.o = (uint16_t*)o;
     a.o_stride = o_stride;
     a.lse = lse;
-    const Shape s = shape_for(max_rows, a.group, max_keys);
+    const Shape s = shape_for(max_rows, a.group, item_bound(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, kManyRows),
+                              max_keys);
     a.rows_per_wg = s.rows_per_wg;
     a.step = s.step;
     a.units = s.units;
