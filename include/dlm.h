@@ -450,7 +450,8 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
  * n_heads) bytes, 256-byte aligned; it keeps nothing between calls.
  *
  * Limits: head_dim 64 or 128; page_len 16, 32, 64 or 128; n_pages <= 2^20;
- * n_seqs <= 1024; max_pages * page_len <= 2^26; n_kv_heads <= 128.
+ * n_seqs <= 1024; max_pages * page_len <= 2^26; n_kv_heads <= 128; total_rows <=
+ * 2^24; n_seqs * n_heads * max_rows <= 2^33.
  */
 typedef struct dlm_cache {
     int32_t dtype;

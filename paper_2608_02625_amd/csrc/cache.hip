@@ -256,6 +256,8 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
         if ((int64_t)rows * group > (1 << 28)) return fail(DLM_ERR_INVALID_ARG, "max_rows times query heads per key head too large");
         TRY(check_workspace(d_workspace, workspace_bytes,
                             attend_workspace_bytes(cache->n_seqs, cache->n_kv_heads, cache->head_dim, total_rows, rows, group)));
+        if ((int64_t)cache->n_seqs * n_heads * rows > ((int64_t)1 << 33))
+            return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
         const int keys = (int)std::min<int64_t>(max_keys ? max_keys : capacity(*cache), capacity(*cache));
         return launched(launch_attend(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows, rows, keys, n_heads,
                                       d_q, q_stride, d_mask, d_mask ? mask_words : 0,

@@ -153,8 +153,9 @@ struct AttnArgs {
     int step;                                 // keys of a step
     int min_steps;                            // least steps of a unit
     int units;                                // units aimed at: the workgroups that the chip holds at once
-    float* part_o;                            // [slots][rows_per_wg][head_dim]
-    float2* part_ml;                          // [slots][rows_per_wg]
+    int max_slots;                            // places for parts; enough for any sound row starts
+    float* part_o;                            // [max_slots][rows_per_wg][head_dim]
+    float2* part_ml;                          // [max_slots][rows_per_wg]
 };
 
 struct Seq {
@@ -215,17 +216,20 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
         steps = max((s.keys + a.step - 1) / a.step, 1);
     };
     const Seq first = sequence(a, lane);
-    int sum = 0, items = 0;                               // steps of all items (fit: checked by the host)
+    // Steps of all items: float32, since row starts that overlap may make more of them
+    // than an int holds, and what follows needs no more than its bound (max_slots).
+    float sum = 0.f;
+    int items = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
         shape(b0 ? sequence(a, b0 + lane) : first, tiles, steps);
-        sum += from_lane(wave_scan(tiles * steps * a.c.n_kv), 63);
+        sum += wave_sum_dpp((float)tiles * (float)steps * (float)a.c.n_kv);
         items += from_lane(wave_scan(tiles * a.c.n_kv), 63);
     }
     // Cut into runs of sum / n steps an item's last one is half empty on average, so
     // this aims at `units` of them together.
     const int n = max(a.units - items / 2, a.units / 2);
-    const int most = max(a.min_steps, (sum + n - 1) / n);
+    const int most = max(a.min_steps, (int)fminf(ceilf(sum / (float)n), 0x1p30f));
     int before = 0, slots_before = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
@@ -261,7 +265,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             const int each = (all_steps + u.parts - 1) / u.parts * (a.step / kTile);
             u.t0 = uniform(part * each);
             u.t1 = uniform(min(u.t0 + each, (u.s.keys + kTile - 1) / kTile));
-            return true;
+            return u.parts == 1 || u.slot + u.parts - part <= a.max_slots;
         }
         before = from_lane(end, 63);
         slots_before = from_lane(slot_end, 63);
@@ -1036,6 +1040,9 @@ Shape shape_for(int max_rows, int group, int64_t many_items, int max_keys) {
     if (many_items <= 256) return {kManyRows, 2 * kTile, 256, 4};
     return {kManyRows, kTile, 512, 8};
 }
+// Split items have at least two parts of which all but one are full, so they make
+// at most twice the units aimed at (and a few for the sum's rounding).
+int slots_for(const Shape& s) { return 2 * s.units + 8; }
 int64_t item_bound(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int rows_per_wg) {
     const int64_t per_seq = ((int64_t)max_rows * group + rows_per_wg - 1) / rows_per_wg;
     return n_kv * std::min<int64_t>(n_seqs * per_seq, (int64_t)total_rows * group / rows_per_wg + n_seqs);
@@ -1076,11 +1083,9 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
 
 }  // namespace
 
-// Split items have at least two parts of which all but one are full, so they make
-// at most twice the units aimed at.
 size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
     const Shape s = shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), 0);
-    const size_t rows = (size_t)2 * s.units * s.rows_per_wg;
+    const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
     return round256(rows * head_dim * 4) + round256(rows * 8);
 }
 
@@ -1111,12 +1116,15 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.step = s.step;
     a.units = s.units;
     a.min_steps = s.min_steps;
-    const size_t rows = (size_t)2 * s.units * s.rows_per_wg;
+    const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
+    a.max_slots = slots_for(s);
     a.part_o = (float*)ws;
     a.part_ml = (float2*)((char*)ws + round256(rows * c.head_dim * 4));
     const int64_t items = item_bound(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, s.rows_per_wg);
     const int64_t steps = ((int64_t)max_keys + s.step - 1) / s.step;
-    if (items * std::max<int64_t>(steps, 1) > 0x3fffffff) return hipErrorInvalidValue;    // the units' counts are 32-bit
+    // The list's counts are 32-bit, whatever the row starts.
+    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)max_rows * a.group + s.rows_per_wg - 1) / s.rows_per_wg) > (1 << 29))
+        return hipErrorInvalidValue;
     const bool may_split = steps > s.min_steps;
     if (dtype == DLM_F16)
         return c.head_dim == 128 ? launch<true, 128>(a, items, may_split, st) : launch<true, 64>(a, items, may_split, st);

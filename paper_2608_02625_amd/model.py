@@ -253,6 +253,8 @@ class Refiner:
         the window rows that a row sees (default: all of its window's).  Returns (top-1
         int32, confidence float, max logit float), each [rows]."""
         T = tokens.numel()
+        if cache.device.index != (self.device.index if self.device.index is not None else torch.cuda.current_device()):
+            raise ValueError("the cache and the model must be on one GPU")
         for t, name, n in ((tokens, "tokens", T), (positions, "positions", T),
                            (row_start, "row_start", cache.n_seqs + 1), (n_invalid, "n_invalid", 1)):
             if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):

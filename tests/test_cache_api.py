@@ -168,6 +168,10 @@ def test_attend_refusals():
                      (dict(lse=FAKE + 2), "lse"), (dict(scale=-1.0), "scale"), (dict(scale=math.nan), "scale"),
                      (dict(scale=math.inf), "scale"), (dict(ws=None), "workspace"), (dict(ws=FAKE + 16), "256-byte")]:
         _refused(lib, call(**kw), word)
+    _refused(lib, call(total=1 << 24, most=1 << 24, heads=1024, qs=65536, os=65536), "too large")
+    many = ctypes.byref(_cache(L, n_seqs=1024))
+    _refused(lib, lib.dlm_cache_attend(many, 0, FAKE, 1 << 20, 1 << 20, 0, 16, FAKE, 1024, None, 0, 0.0, FAKE, 1024, None,
+                                       FAKE, 1 << 40, None), "2^33")
     _refused(lib, call(size=1024), "too small", -5)
     assert call(total=0, most=0) == 0
 

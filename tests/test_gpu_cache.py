@@ -387,6 +387,36 @@ def test_attend_split_over_keys(dtype, H, KV, hd, page, lens, rows, kind):
     assert (err <= 4 * h * (out[:T].double().abs() + 1)).all()
 
 
+@pytest.mark.parametrize("dtype,H,KV,hd,page,seqs,top,kind", [
+    (BF, 4, 4, 64, 16, 130, 1, "full"), (HF, 4, 1, 128, 32, 1000, 2, "tree"), (BF, 8, 2, 64, 64, 70, 12, "tree"),
+    (BF, 16, 4, 64, 16, 100, 30, "tree"), (HF, 16, 16, 64, 32, 11, 200, "blocks"), (BF, 8, 1, 128, 128, 90, 9, "random")])
+def test_attend_batches(dtype, H, KV, hd, page, seqs, top, kind):
+    """More sequences than lanes, ragged, some idle or empty; few and many rows each."""
+    rng = random.Random(seqs)
+    lens = [rng.choice([0, rng.randint(1, 40), rng.randint(1, 150)]) for _ in range(seqs)]
+    rows = [rng.choice([0, 1, top, rng.randint(1, top)]) for _ in range(seqs)]
+    rows[rng.randrange(seqs)] = top
+    if seqs < 1000:
+        lens[3] = 1500                                # one that is split, if it has rows
+    _attend_case(dtype, H, KV, hd, page, lens, rows, kind, seed=seqs)
+
+
+def test_row_starts_that_overlap_stay_in_bounds():
+    """Falling row starts are not allowed; they reach no memory of others."""
+    c, _ = _cache([300] * 64, 16, 4, 64, BF)
+    c.k.normal_()
+    c.v.normal_()
+    c.len.fill_(100)
+    q = torch.randn(200, 16, 64, device="cuda").to(BF)
+    guard = torch.full((400, 16, 64), 5.0, dtype=BF, device="cuda")
+    starts = _ints([0 if i % 2 == 0 else 200 for i in range(65)])
+    c.attend(0, q, starts, 200, out=guard[100:300])
+    assert (guard[:100] == 5).all() and (guard[300:] == 5).all()
+    c.append(0, q[:, :4], q[:, :4], starts, 200)
+    ok = c.reserve(starts)
+    assert set(ok.tolist()) <= {0, 1}
+
+
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("rows", [1, 40])
 def test_attend_extreme_scores(dtype, rows):
