@@ -6,7 +6,7 @@
 // rows, 32 per wave, and one run of keys.
 //
 // Keys.  Tiles of 32 keys go from their pages to LDS by buffer copies that bypass
-// registers (NS stages, XOR-swizzled 16-byte chunks); a page is a scalar, so a
+// registers (staged, XOR-swizzled 16-byte chunks); a page is a scalar, so a
 // copy's descriptor is the page itself, cut to the tokens it holds: places behind
 // the last token and entries without a page read as zeros, and nothing outside a
 // page is ever touched.  64-bit page addresses put no limit on the pool's size.
@@ -18,7 +18,7 @@
 // 16 lanes hand in 4 rows of 16 values and get a column of 4 each), 4 keys per
 // read in the order that the scores' accumulator has them.  Probabilities are
 // rounded to the cache's type for the product (the matrix instruction takes
-// nothing wider at this rate; relative 2^-9 or 2^-12 of each, of no sign), sums
+// nothing wider at this rate; half a step, 2^-8 or 2^-11 of each, to either side), sums
 // add the unrounded ones.  The running maximum moves only when a tile raises it
 // by more than 2^8 in the exp2 domain.
 //
@@ -151,6 +151,7 @@ struct AttnArgs {
     float* lse;
     int rows_per_wg;                          // packed rows of a workgroup
     int step;                                 // keys of a step
+    int rows_log2, step_log2;                 // both are powers of two
     int min_steps;                            // least steps of a unit
     int units;                                // units aimed at: the workgroups that the chip holds at once
     int max_slots;                            // places for parts; enough for any sound row starts
@@ -210,10 +211,9 @@ __device__ __forceinline__ int from_lane(int v, int l) {
 template <bool ITEMS>
 __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u) {
     const int lane = threadIdx.x & 63;
-    const int per_tile = a.rows_per_wg;
     auto shape = [&](const Seq& s, int& tiles, int& steps) {
-        tiles = (s.n * a.group + per_tile - 1) / per_tile;
-        steps = max((s.keys + a.step - 1) / a.step, 1);
+        tiles = (s.n * a.group + a.rows_per_wg - 1) >> a.rows_log2;
+        steps = max((s.keys + a.step - 1) >> a.step_log2, 1);
     };
     const Seq first = sequence(a, lane);
     // Steps of all items: float32, since row starts that overlap may make more of them
@@ -235,7 +235,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
         int tiles, steps;
         const Seq s = b0 ? sequence(a, b0 + lane) : first;
         shape(s, tiles, steps);
-        const int parts = (steps + most - 1) / most;
+        const int parts = (int)((uint32_t)(steps + most - 1) / (uint32_t)most);
         const int all = tiles * a.c.n_kv * parts, split = parts > 1 ? all : 0;
         const int count = ITEMS ? (parts > 1 ? tiles * a.c.n_kv : 0) : all;
         const int end = before + wave_scan(count), slot_end = slots_before + wave_scan(split);
@@ -250,19 +250,19 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             u.parts = from_lane(parts, l);
             const int n_tiles = from_lane(tiles, l);
             const int all_steps = from_lane(steps, l);
-            int i = index - from_lane(end - count, l);
+            uint32_t i = (uint32_t)(index - from_lane(end - count, l));
             const int slot0 = from_lane(slot_end - split, l);
-            u.row_tile = uniform(i % n_tiles);
-            i /= n_tiles;
+            u.row_tile = uniform((int)(i % (uint32_t)n_tiles));
+            i /= (uint32_t)n_tiles;
             int part = 0;
             if (!ITEMS) {
-                part = uniform(i % u.parts);
-                i /= u.parts;
+                part = uniform((int)(i % (uint32_t)u.parts));
+                i /= (uint32_t)u.parts;
             }
-            u.kvh = uniform(i);
+            u.kvh = uniform((int)i);
             // slots of an item's parts lie next to each other
             u.slot = slot0 + (u.kvh * n_tiles + u.row_tile) * u.parts + part;
-            const int each = (all_steps + u.parts - 1) / u.parts * (a.step / kTile);
+            const int each = (int)((uint32_t)(all_steps + u.parts - 1) / (uint32_t)u.parts) << (a.step_log2 - 5);
             u.t0 = uniform(part * each);
             u.t1 = uniform(min(u.t0 + each, (u.s.keys + kTile - 1) / kTile));
             return u.parts == 1 || u.slot + u.parts - part <= a.max_slots;
@@ -580,8 +580,8 @@ attend_many_kernel(const AttnArgs a) {
     const int rows = min(u.s.n * a.group - u.row_tile * kManyRows, kManyRows);           // of this workgroup
     const bool busy = wave * 32 < rows;                   // this wave has rows
     const int r = min(wave * 32 + j, rows - 1) + u.row_tile * kManyRows;
-    const int head = u.kvh * a.group + r % a.group;
-    const int64_t t = (int64_t)u.s.start + r / a.group;   // packed row
+    const int head = u.kvh * a.group + (int)((uint32_t)r % (uint32_t)a.group);
+    const int64_t t = (int64_t)u.s.start + (uint32_t)r / (uint32_t)a.group;   // packed row
     Keys<HD> keys(a, u);
 
     // Copies: lane L of copy p reads the chunk that belongs at byte 16 L of its 1 KB
@@ -792,8 +792,8 @@ attend_few_kernel(const AttnArgs a) {
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(x * 32 + j, rows - 1);
-        const int64_t t = (int64_t)u.s.start + r / a.group;
-        const uint16_t* qp = a.q + t * a.q_stride + (u.kvh * a.group + r % a.group) * HD + g * 8;
+        const int64_t t = (int64_t)u.s.start + (uint32_t)r / (uint32_t)a.group;
+        const uint16_t* qp = a.q + t * a.q_stride + (u.kvh * a.group + (int)((uint32_t)r % (uint32_t)a.group)) * HD + g * 8;
 #pragma unroll
         for (int ks = 0; ks < D::NKS; ++ks) qf[x][ks] = *reinterpret_cast<const s16x8*>(qp + ks * 16);
         mrow[x] = a.mask ? a.mask + t * a.mask_words : nullptr;
@@ -955,8 +955,8 @@ attend_few_kernel(const AttnArgs a) {
             *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
             if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
         } else {
-            const int64_t t = (int64_t)u.s.start + row / a.group;
-            const int h = u.kvh * a.group + row % a.group;
+            const int64_t t = (int64_t)u.s.start + (uint32_t)row / (uint32_t)a.group;
+            const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
             if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
         }
@@ -1013,8 +1013,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 #pragma unroll
             for (int i = 1; i < kJoinRuns; ++i) add(run_ml[i][local], run_o[i][local][c4]);
             const int pr = row + u.row_tile * a.rows_per_wg;
-            const int64_t t = (int64_t)u.s.start + pr / a.group;
-            const int h = u.kvh * a.group + pr % a.group;
+            const int64_t t = (int64_t)u.s.start + (uint32_t)pr / (uint32_t)a.group;
+            const int h = u.kvh * a.group + (int)((uint32_t)pr % (uint32_t)a.group);
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
             if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
         }
@@ -1025,7 +1025,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 // How a call is laid out: packed rows of a workgroup, keys of a step, units, least
 // steps of a unit.  A second kernel that joins parts costs about 5 us, so short
 // sequences are not split: up to 1024 keys a unit of few rows takes them whole (641
-// keys, head_dim 64: 8.5 us, split 6.3 + 3.8 and a launch), up to 256 one of many rows.
+// keys, head_dim 64: 8.5 us, split 6.3 + 3.8 and a launch), up to 512 one of many (8
+// windows of 64 rows over 320 keys, 16 heads on 4: 16.0 us, split and joined 24.8).
 // Many rows: with no more row tiles than CUs two wave groups each (8 trees of up to 64
 // rows over 512 to 4096 keys: 18.0 + 7.6 us with the join, one group 20.7 + 9.0); with
 // more of them one group, three workgroups per CU (8 x 1024 rows: 87 us, two groups
@@ -1037,7 +1038,7 @@ Shape shape_for(int max_rows, int group, int64_t many_items, int max_keys) {
     const int64_t rows = (int64_t)max_rows * group;
     if (rows <= 32) return {32, 4 * kTile, 512, max_keys <= 1024 ? 8 : 2};
     if (rows <= 64) return {64, 4 * kTile, 256, max_keys <= 1024 ? 8 : 2};
-    if (many_items <= 256) return {kManyRows, 2 * kTile, 256, 4};
+    if (many_items <= 256) return {kManyRows, 2 * kTile, 256, max_keys <= 512 ? 8 : 4};
     return {kManyRows, kTile, 512, 8};
 }
 // Split items have at least two parts of which all but one are full, so they make
@@ -1114,6 +1115,8 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
                               max_keys);
     a.rows_per_wg = s.rows_per_wg;
     a.step = s.step;
+    a.rows_log2 = __builtin_ctz((unsigned)s.rows_per_wg);
+    a.step_log2 = __builtin_ctz((unsigned)s.step);
     a.units = s.units;
     a.min_steps = s.min_steps;
     const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
