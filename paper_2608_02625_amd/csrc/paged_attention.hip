@@ -145,7 +145,7 @@ struct AttnArgs {
     int64_t q_stride;
     const uint32_t* mask;
     int mask_words;
-    float scale_log2;
+    float scale_log2, lim;                    // lim: 2^8 in the exp2 domain, in units of the scores
     uint16_t* o;
     int64_t o_stride;
     float* lse;
@@ -293,6 +293,7 @@ struct Keys {
     const int32_t* table;
     uint32_t page_bytes;
     int keys, n_pages, max_pages, page_log2, page_mask, base, held;
+    int gaps = 0;                                         // some entry so far that has tokens has no page
 
     __device__ __forceinline__ Keys(const AttnArgs& a, const Unit& u) {
         const uint32_t head = (uint32_t)a.c.page_len * Dims<HD>::ROW;
@@ -315,12 +316,23 @@ struct Keys {
 #if defined(__HIP_DEVICE_COMPILE__)
         asm volatile("" : "+v"(held));                    // waited for here, not wherever it is used
 #endif
+        const int e = first + (int)(threadIdx.x & 63);
+        const uint64_t none = __ballot((int64_t)e << page_log2 < keys && !is_page(held));
+        gaps = uniform(gaps | (int)((uint32_t)none | (uint32_t)(none >> 32)));
     }
-    // Entries of the two groups of 16 keys of a tile.
-    __device__ __forceinline__ int2 entries(int kt) {
-        const int e0 = (kt * kTile) >> page_log2, e1 = (kt * kTile + 16) >> page_log2;
+    // Entries of the two groups of 16 keys of a tile, or of one of them.
+    __device__ __forceinline__ void need(int kt) {
+        const int e0 = (kt * kTile) >> page_log2;
         if (__builtin_expect((uint32_t)(e0 - base) > 62u, 0)) fetch(e0);
-        return int2{from_lane(held, e0 - base), from_lane(held, e1 - base)};
+    }
+    __device__ __forceinline__ int entry(int kt, int s) {
+        need(kt);
+        return from_lane(held, ((kt * kTile + s * 16) >> page_log2) - base);
+    }
+    __device__ __forceinline__ int2 entries(int kt) {
+        need(kt);
+        return int2{from_lane(held, ((kt * kTile) >> page_log2) - base),
+                    from_lane(held, ((kt * kTile + 16) >> page_log2) - base)};
     }
     __device__ __forceinline__ bool is_page(int page) const { return (uint32_t)page < (uint32_t)n_pages; }
     // Bit s: group s of the tile has no page.
@@ -366,7 +378,7 @@ template <bool F16, int HD>
 struct RowTile {
     using D = Dims<HD>;
     f32x16 o[D::NB];
-    float m, l;                                           // m in units of the scores
+    float m, l, bias;                                     // m in units of the scores; bias: -m scale_log2
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -374,7 +386,7 @@ struct RowTile {
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
         m = -INFINITY;
-        l = 0.f;
+        l = bias = 0.f;
     }
     __device__ __forceinline__ static void hide(f32x16& st, uint32_t see, int g) {
         see >>= 4 * g;
@@ -383,13 +395,14 @@ struct RowTile {
             if (!((see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
     }
     // Scores to probabilities, the B operand of O^T = V^T P^T.
-    __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, s16x8 (&pf)[2]) {
+    // `lim`: how far, in units of the scores, a maximum may lie above m.
+    __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, float lim, s16x8 (&pf)[2]) {
         float mt = st[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mt = fmaxf(mt, st[e]);
         mt = both_max(mt);
         // Each row by its own scores alone, so that its bits do not depend on others'.
-        const bool move = (mt - m) * scale_log2 > 8.f;
+        const bool move = mt - m > lim;                   // not if both are -inf
         if (__any(move)) {
             const float m_new = move ? mt : m;
             const float alpha = move ? __builtin_amdgcn_exp2f((m - m_new) * scale_log2) : 1.f;
@@ -399,16 +412,16 @@ struct RowTile {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[n][e] *= alpha;
             m = m_new;
+            bias = m == -INFINITY ? 0.f : -m * scale_log2;
         }
-        const float nb = m == -INFINITY ? 0.f : -m * scale_log2;
         float sum = 0.f;
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
             u32x4 w;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i], scale_log2, nb));
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i + 1], scale_log2, nb));
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i], scale_log2, bias));
+                const float p1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i + 1], scale_log2, bias));
                 sum += p0 + p1;
                 w[i] = pack2<F16>(p0, p1);
             }
@@ -554,16 +567,27 @@ __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
 
 // More than 64 packed rows: 4 waves of 32 rows share tiles of K and V in LDS, three
 // stages of them, copied by all.  WK = 1: 168 VGPRs at head_dim 128, so three
-// workgroups (12 waves) share a CU, 48 KB of LDS each.  WK = 2, for calls with too few
+// workgroups (12 waves) share a CU, 50 KB of LDS each.  WK = 2, for calls with too few
 // rows to fill the chip: two such groups of waves take tiles in turn and add up in the
 // end, half the steps and half the parts to join for the same split.
 constexpr int kManyRows = 128, kManyStages = 3;
+
+// A K tile of these kernels: 64 bytes of space behind each 1 KB copy turn its rows by
+// a quarter of the banks against the next copy's, so that only two address bits are
+// left to xor (a row's place within a copy): fragments four chunks apart differ by a
+// constant, which is the read's offset.
+constexpr int kCopyStep = 1024 + 64;
+template <int HD>
+__device__ __forceinline__ int k_turn(int row) {          // of a chunk's number
+    return HD == 128 ? row & 3 : (row >> 1) & 3;
+}
 
 template <bool F16, int HD, bool ONCE, int WK>
 __global__ __launch_bounds__(256 * WK) __attribute__((amdgpu_waves_per_eu(WK == 1 ? 3 : 2))) void
 attend_many_kernel(const AttnArgs a) {
     using D = Dims<HD>;
-    constexpr int NS = kManyStages, STAGE = 2 * D::HALF;
+    constexpr int K_TILE = kTile / D::ROWS_PER_COPY * kCopyStep;
+    constexpr int NS = kManyStages, STAGE = K_TILE + D::HALF;
     constexpr int COPIES = D::HALF / 1024 / 4;            // 1 KB copies per wave of a K or V tile
     // The kernel's only LDS variable: with a second one the compiler tells the two
     // apart, takes a fragment read to depend on every copy in flight into this one,
@@ -590,24 +614,21 @@ attend_many_kernel(const AttnArgs a) {
 #pragma unroll
     for (int p = 0; p < COPIES; ++p) {
         const int row = (wave * COPIES + p) * D::ROWS_PER_COPY + lane / D::CPR, pc = lane % D::CPR;
-        k_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ k_key<D::CPR>(row)) << 4));
+        k_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ k_turn<HD>(row)) << 4));
         v_off[p] = (uint32_t)((row & 15) * D::ROW + ((pc ^ v_key<D::CPR>(row)) << 4));
     }
     const lds_ptr_t lds = (lds_ptr_t)smem;
-    const int ring = wk * NS * STAGE;
     const int sub = wave * COPIES * D::ROWS_PER_COPY / 16;
-    uint32_t missing = 0;                                 // two bits per stage: groups without a page
-    auto issue = [&](int kt, int stage) {
-        const int2 e = keys.entries(kt);
-        missing = (missing & ~(3u << (2 * stage))) | keys.missing(e) << (2 * stage);
-        const int page = sub ? e.y : e.x, bytes = keys.bytes(page, kt, sub);
+    auto issue = [&](int kt, int at_lds) {                // at_lds: the stage
+        const int page = keys.entry(kt, sub), bytes = keys.bytes(page, kt, sub);
         const int64_t at = keys.offset(page, kt, sub);
         const buf_rsrc_t kr = make_rsrc(keys.k + at, bytes), vr = make_rsrc(keys.v + at, bytes);
-        const int d = ring + stage * STAGE + wave * COPIES * 1024;
+        lds_char* kd = (lds_char*)lds + at_lds + wave * COPIES * kCopyStep;
+        lds_char* vd = (lds_char*)lds + at_lds + K_TILE + wave * COPIES * 1024;
 #pragma unroll
-        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(kr, k_off[p], (lds_ptr_t)((lds_char*)lds + d + p * 1024));
+        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(kr, k_off[p], (lds_ptr_t)(kd + p * kCopyStep));
 #pragma unroll
-        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(vr, v_off[p], (lds_ptr_t)((lds_char*)lds + d + D::HALF + p * 1024));
+        for (int p = 0; p < COPIES; ++p) copy16<ONCE>(vr, v_off[p], (lds_ptr_t)(vd + p * 1024));
     };
 
     s16x8 qf[D::NKS];
@@ -618,7 +639,9 @@ attend_many_kernel(const AttnArgs a) {
     }
     RowTile<F16, HD> rt[1];
     rt[0].clear();
-    const int kfrag = j * D::ROW + ((g ^ k_key<D::CPR>(j)) << 4);      // chunk 2 ks + g: xor ks << 5
+    // K fragments: chunk 2 ks + g of row j, by the parity of ks.
+    const int krow = j / D::ROWS_PER_COPY * kCopyStep + j % D::ROWS_PER_COPY * D::ROW;
+    const int kfrag[2] = {krow + ((g ^ k_turn<HD>(j)) << 4), krow + (((2 + g) ^ k_turn<HD>(j)) << 4)};
     const int vfrag = v_base<HD>(lane);
     const uint32_t* mrow = a.mask ? a.mask + t * a.mask_words : nullptr;
     const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
@@ -627,66 +650,66 @@ attend_many_kernel(const AttnArgs a) {
     // copies past the last tile repeat it, and a step on it is one that no row sees.
     const int n = (u.t1 - u.t0 + WK - 1) / WK;
     auto tile_at = [&](int i) { return min(u.t0 + wk + i * WK, u.t1 - 1); };
-    if (n > 0) {
-#pragma unroll
-        for (int s = 0; s < NS - 1; ++s) issue(tile_at(s), s);
-    }
-    // The queries' loads end here and not inside the loop, where their wait would
-    // take the copies in flight with it.
-#if defined(__HIP_DEVICE_COMPILE__)
-#pragma unroll
-    for (int ks = 0; ks < D::NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
-#endif
-    // Words of the row's mask for this tile, read a tile ahead: in front of that tile's
-    // copies, so that waiting for them does not wait for those.
-    uint32_t lo = 0, hi = 0;
-    auto word_of = [&](int kt) { return (kt * kTile - u.s.len) >> 5; };
-    if (a.mask && n > 0) {
-        lo = mask_word(a, mrow, word_of(tile_at(0)));
-        hi = mask_word(a, mrow, word_of(tile_at(0)) + 1);
-    }
-    int stage = 0;
     bool wild = false;
-    for (int i = 0; i < n; ++i) {
-        wait_vmcnt<(NS - 2) * 2 * COPIES>();              // this wave's copies of the tile have landed
-        lds_barrier();                                    // everyone's have; the stage before is free
-        uint32_t lo_next = 0, hi_next = 0;
-        if (a.mask) {
-            lo_next = mask_word(a, mrow, word_of(tile_at(i + 1)));
-            hi_next = mask_word(a, mrow, word_of(tile_at(i + 1)) + 1);
-        }
-        issue(tile_at(i + NS - 1), stage == 0 ? NS - 1 : stage - 1);
-        const int kt = u.t0 + wk + i * WK, sb = ring + stage * STAGE;
-        const uint32_t gone = kt < u.t1 ? (missing >> (2 * stage)) & 3 : 3;
-        stage = stage + 1 == NS ? 0 : stage + 1;
-        const uint32_t w0 = lo, w1 = hi;
-        lo = lo_next;
-        hi = hi_next;
-        if (!busy) continue;
-        const int k0 = kt * kTile;
-        const bool masked = k0 + kTile > clear || gone;
+    if (n > 0) {
+        int use = wk * NS * STAGE, then = use + STAGE, put = then + STAGE;    // the stages, in turn
+        static_assert(NS == 3, "two tiles in flight beside the one at work");
+        // Words of the row's mask for a tile, where it meets the window.
+        uint32_t lo = 0, hi = 0;
+        auto words = [&](int kt) {
+            if (__builtin_expect(kt * kTile + kTile > clear, 0)) {
+                const int w = (kt * kTile - u.s.len) >> 5;
+                lo = mask_word(a, mrow, w);
+                hi = mask_word(a, mrow, w + 1);
+            }
+        };
+        words(tile_at(0));
+        issue(tile_at(0), use);
+        issue(tile_at(1), then);
+        // The queries' and the words' loads end here and not inside the loop, where
+        // their wait would take the copies in flight with it.
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(lo), "+v"(hi));
+#pragma unroll
+        for (int ks = 0; ks < D::NKS; ++ks) asm volatile("" ::"v"(qf[ks]));
+#endif
+        for (int i = 0; i < n; ++i) {
+            wait_vmcnt<(NS - 2) * 2 * COPIES>();          // this wave's copies of the tile have landed
+            lds_barrier();                                // everyone's have; the stage before is free
+            issue(tile_at(i + NS - 1), put);
+            const int sb = use;
+            use = then;
+            then = put;
+            put = sb;
+            if (!busy) continue;
+            const int kt = u.t0 + wk + i * WK, k0 = kt * kTile;
+            int gone = kt < u.t1 ? 0 : 3;                 // groups that no row sees
+            if (__builtin_expect(keys.gaps, 0)) gone |= (int)keys.missing(keys.entries(min(kt, u.t1 - 1)));
+            const int masked = ((clear - k0 - kTile) >> 31) | gone;
 
-        const int ka = sb + kfrag;
-        f32x16 st;
+            f32x16 st;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) st[e] = 0.f;
+            for (int e = 0; e < 16; ++e) st[e] = 0.f;
+            lds_char* ka[2] = {(lds_char*)lds + sb + kfrag[0], (lds_char*)lds + sb + kfrag[1]};
 #pragma unroll
-        for (int k4 = 0; k4 < D::NKS; k4 += 4) {
-            s16x8 kf[4];
+            for (int k4 = 0; k4 < D::NKS; k4 += 4) {
+                s16x8 kf[4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                kf[x] = *(__attribute__((address_space(3))) const s16x8*)((lds_char*)lds + (ka ^ ((k4 + x) << 5)));
+                for (int x = 0; x < 4; ++x)
+                    kf[x] = *(__attribute__((address_space(3))) const s16x8*)(ka[x & 1] + ((k4 + x) >> 1) * 64);
+                sched_fence();
+#pragma unroll
+                for (int x = 0; x < 4; ++x) st = mfma<F16>(kf[x], qf[k4 + x], st);
+            }
+            s16x8 vf[2][2];
+            read_values<HD>(vf, lds, sb + K_TILE + vfrag, 0);
             sched_fence();
-#pragma unroll
-            for (int x = 0; x < 4; ++x) st = mfma<F16>(kf[x], qf[k4 + x], st);
+            if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, lo, hi, k0, (uint32_t)gone), g);
+            if (a.mask) words(tile_at(i + 1));
+            s16x8 pf[1][2];
+            rt[0].softmax(st, a.scale_log2, a.lim, pf[0]);
+            wild |= add_values<F16, HD, 1>(rt, pf, vf, lds, sb + K_TILE, lane, vfrag, masked);
         }
-        s16x8 vf[2][2];
-        read_values<HD>(vf, lds, sb + D::HALF + vfrag, 0);
-        sched_fence();
-        if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, w0, w1, k0, gone), g);
-        s16x8 pf[1][2];
-        rt[0].softmax(st, a.scale_log2, pf[0]);
-        wild |= add_values<F16, HD, 1>(rt, pf, vf, lds, sb + D::HALF, lane, vfrag, masked);
     }
 
     wait_all_memory();                                    // no copy may still land in LDS
@@ -859,8 +882,8 @@ attend_few_kernel(const AttnArgs a) {
             const int w = (kt * kTile - u.s.len) >> 5;
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
-                l[x] = a.mask ? mask_word(a, mrow[x], w) : 0;
-                h[x] = a.mask ? mask_word(a, mrow[x], w + 1) : 0;
+                l[x] = mask_word(a, mrow[x], w);
+                h[x] = mask_word(a, mrow[x], w + 1);
             }
         };
         words(tile_at(0), lo, hi);
@@ -897,7 +920,7 @@ attend_few_kernel(const AttnArgs a) {
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
                 if (__builtin_expect(masked, 0)) rt[x].hide(st[x], seen_keys(a, u.s, lo[x], hi[x], k0, gone), g);
-                rt[x].softmax(st[x], a.scale_log2, pf[x]);
+                rt[x].softmax(st[x], a.scale_log2, a.lim, pf[x]);
             }
             landed();
             s16x8 vf[2][2];
@@ -1028,8 +1051,8 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 // keys, head_dim 64: 8.5 us, split 6.3 + 3.8 and a launch), up to 512 one of many (8
 // windows of 64 rows over 320 keys, 16 heads on 4: 16.0 us, split and joined 24.8).
 // Many rows: with no more row tiles than CUs two wave groups each (8 trees of up to 64
-// rows over 512 to 4096 keys: 18.0 + 7.6 us with the join, one group 20.7 + 9.0); with
-// more of them one group, three workgroups per CU (8 x 1024 rows: 87 us, two groups
+// rows over 512 to 4096 keys: 16.7 + 6.9 us with the join, one group 20.7 + 9.0); with
+// more of them one group, three workgroups per CU (8 x 1024 rows: 80 us, two groups
 // 107).
 struct Shape {
     int rows_per_wg, step, units, min_steps;
@@ -1106,8 +1129,9 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.q = (const uint16_t*)q;
     a.q_stride = q_stride;
     a.mask = mask;
-    a.mask_words = mask_words;
+    a.mask_words = mask ? mask_words : 0;                 // no words without a mask
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.lim = std::min(8.f / a.scale_log2, 3e38f);
     a.o = (uint16_t*)o;
     a.o_stride = o_stride;
     a.lse = lse;
