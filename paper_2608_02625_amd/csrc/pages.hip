@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256) void reserve_copy_kernel(CacheArgs c, const in
 // A sequence's list of kept rows, checked by the whole workgroup.
 struct Kept {
     int n, len, m, first;     // window rows, tokens before, kept rows, index of the first kept one
-    bool ok, moves;           // the list and the pages allow it; some row changes its place
+    bool ok;                  // the list and the pages allow it
 };
 __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start, int total_rows, const int32_t* keep,
                              const int32_t* keep_start, int total_keep) {
@@ -221,60 +221,16 @@ __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start
         }
     }
     k.ok = !__syncthreads_or(wrong);
-    k.moves = moved;
     return k;
 }
 
-// Kept rows to the front of the window: one workgroup per (layer, K or V, key head)
-// and sequence.  A chunk of rows is read whole before it is written; later rows lie
-// behind every place already written (the list rises, so its i-th row is never in
-// front of place i).  The first chunk is read before the list has been checked, since
-// the checks are a chain of loads themselves: from places cut to the window's pages,
-// and not written if the list fails.
-constexpr int kMoveLoads = 4;
-
-__global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
-                                                          int total_rows, const int32_t* __restrict__ keep,
-                                                          const int32_t* __restrict__ keep_start, int total_keep) {
-    const int b = blockIdx.y;
-    const int chunks = c.head_dim / 8, rows_at_once = 256 * kMoveLoads / chunks;
-    const int h = blockIdx.x % c.n_kv, lk = blockIdx.x / c.n_kv;
-    const int64_t head = (int64_t)c.page_len * c.head_dim * 2, page = head * c.n_kv;
-    char* pool = (lk & 1 ? c.v : c.k) + (int64_t)(lk >> 1) * c.n_pages * page + h * head;
-    const int len = max(c.len[b], 0), first = max(keep_start[b], 0);
-    const int listed = min(max(keep_start[b + 1] - first, 0), total_keep - min(first, total_keep));
-    const int n = window_rows(row_start, b, total_rows);
-    if (n == 0) return;
-    // Place of a token (chunk threadIdx % chunks of it), in some page whatever the table holds.
-    auto place = [&](int64_t t) {
-        const int e = (int)min(t >> c.page_log2, (int64_t)c.max_pages - 1);
-        const int p = c.table[(int64_t)b * c.max_pages + e];
-        return pool + (names_page(p, c) ? p : 0) * page + (t & (c.page_len - 1)) * c.head_dim * 2 +
-               (threadIdx.x % chunks) * 16;
-    };
-    u32x4 x[kMoveLoads];
-    int from[kMoveLoads];
-    auto read = [&](int r0) {
-#pragma unroll
-        for (int i = 0; i < kMoveLoads; ++i) {
-            const int r = r0 + (i * 256 + (int)threadIdx.x) / chunks;
-            from[i] = r < listed ? min(max(keep[first + r], 0), n - 1) : r;
-            if (from[i] != r) x[i] = *reinterpret_cast<const u32x4*>(place((int64_t)len + from[i]));
-        }
-    };
-    read(0);
-    const Kept k = check_commit(c, b, row_start, total_rows, keep, keep_start, total_keep);
-    if (!k.ok || !k.moves) return;                    // else k.m is `listed`, and no row was cut
-    for (int r0 = 0; r0 < k.m; r0 += rows_at_once) {
-        if (r0) read(r0);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kMoveLoads; ++i) {
-            const int r = r0 + (i * 256 + (int)threadIdx.x) / chunks;
-            if (from[i] != r) *reinterpret_cast<u32x4*>(place((int64_t)len + r)) = x[i];
-        }
-        __syncthreads();
-    }
+// A sequence that passed its checks counts its new tokens at once, with this added
+// until its pages are freed: more than any table row holds, so the kernels behind see
+// which sequences go through (references change as soon as the first one frees pages,
+// so none is checked after that).
+constexpr int kCounted = 1 << 30;
+__device__ __forceinline__ int counted(int len, const CacheArgs& c) {     // new length, -1 if left out
+    return len >= kCounted && pages_for((int64_t)len - kCounted, c.page_log2) <= c.max_pages ? len - kCounted : -1;
 }
 
 // Entries of a table row from `from` on: their pages lose a reference.
@@ -287,7 +243,8 @@ __device__ __forceinline__ void release_from(const CacheArgs& c, int b, int from
     }
 }
 
-__global__ __launch_bounds__(256) void commit_count_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
+// Checks, and without a list (no row moves, no reference counts) the whole of it.
+__global__ __launch_bounds__(256) void commit_check_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
                                                            int total_rows, const int32_t* __restrict__ keep,
                                                            const int32_t* __restrict__ keep_start, int total_keep,
                                                            int32_t* ok) {
@@ -297,11 +254,63 @@ __global__ __launch_bounds__(256) void commit_count_kernel(CacheArgs c, const in
         return;
     }
     const Kept k = check_commit(c, b, row_start, total_rows, keep, keep_start, total_keep);
-    if (k.ok) {
-        release_from(c, b, pages_for((int64_t)k.len + k.m, c.page_log2));
-        if (threadIdx.x == 0) c.len[b] = k.len + k.m;
+    if (k.ok && !keep) release_from(c, b, pages_for((int64_t)k.len + k.m, c.page_log2));
+    if (threadIdx.x == 0) {
+        if (k.ok) c.len[b] = k.len + k.m + (keep ? kCounted : 0);
+        if (ok) ok[b] = k.ok;
     }
-    if (ok && threadIdx.x == 0) ok[b] = k.ok;
+}
+
+// Kept rows to the front of the window: one workgroup per (layer, K or V, key head)
+// and sequence.  A chunk of rows is read whole before it is written; later rows lie
+// behind every place already written (the list rises, so its i-th row is never in
+// front of place i).
+constexpr int kMoveLoads = 4;
+
+__global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ keep,
+                                                          const int32_t* __restrict__ keep_start, int total_keep) {
+    const int b = blockIdx.y;
+    const int chunks = c.head_dim / 8, rows_at_once = 256 * kMoveLoads / chunks;
+    const int h = blockIdx.x % c.n_kv, lk = blockIdx.x / c.n_kv;
+    const int64_t head = (int64_t)c.page_len * c.head_dim * 2, page = head * c.n_kv;
+    char* pool = (lk & 1 ? c.v : c.k) + (int64_t)(lk >> 1) * c.n_pages * page + h * head;
+    const int first = keep_start[b], m = keep_start[b + 1] - first, len = counted(c.len[b], c) - m;
+    if (len < 0 || first < 0 || m <= 0 || first > total_keep - m) return;
+    // Place of a token (chunk threadIdx % chunks of it), in some page whatever the table holds.
+    auto place = [&](int row) {
+        const int64_t t = (int64_t)len + max(row, 0);
+        const int e = (int)min(t >> c.page_log2, (int64_t)c.max_pages - 1);
+        const int p = c.table[(int64_t)b * c.max_pages + e];
+        return pool + (names_page(p, c) ? p : 0) * page + (t & (c.page_len - 1)) * c.head_dim * 2 +
+               (threadIdx.x % chunks) * 16;
+    };
+    for (int r0 = 0; r0 < m; r0 += rows_at_once) {
+        u32x4 x[kMoveLoads];
+        char* to[kMoveLoads];
+        bool moves[kMoveLoads];
+#pragma unroll
+        for (int i = 0; i < kMoveLoads; ++i) {
+            const int r = r0 + (i * 256 + (int)threadIdx.x) / chunks;
+            const int from = r < m ? keep[first + r] : r;
+            moves[i] = from != r;
+            to[i] = place(r);
+            if (moves[i]) x[i] = *reinterpret_cast<const u32x4*>(place(from));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kMoveLoads; ++i)
+            if (moves[i]) *reinterpret_cast<u32x4*>(to[i]) = x[i];
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void commit_release_kernel(CacheArgs c) {
+    const int b = blockIdx.x;
+    const int len = counted(c.len[b], c);
+    if (len < 0) return;
+    __syncthreads();                                  // every thread has read the length
+    release_from(c, b, pages_for(len, c.page_log2));
+    if (threadIdx.x == 0) c.len[b] = len;
 }
 
 // ------------------------------------------------------------------ fork, truncate, reset
@@ -442,11 +451,13 @@ hipError_t launch_reserve(const CacheArgs& c, const int32_t* row_start, int tota
 
 hipError_t launch_commit(const CacheArgs& c, const int32_t* row_start, int total_rows, const int32_t* keep,
                          const int32_t* keep_start, int total_keep, int32_t* ok, hipStream_t st) {
-    if (keep)
-        hipLaunchKernelGGL(commit_move_kernel, dim3(2 * c.n_layers * c.n_kv, c.n_seqs), dim3(256), 0, st, c, row_start,
-                           total_rows, keep, keep_start, total_keep);
-    hipLaunchKernelGGL(commit_count_kernel, dim3(c.n_seqs), dim3(256), 0, st, c, row_start, total_rows, keep,
+    hipLaunchKernelGGL(commit_check_kernel, dim3(c.n_seqs), dim3(256), 0, st, c, row_start, total_rows, keep,
                        keep_start, total_keep, ok);
+    if (keep) {
+        hipLaunchKernelGGL(commit_move_kernel, dim3(2 * c.n_layers * c.n_kv, c.n_seqs), dim3(256), 0, st, c, keep,
+                           keep_start, total_keep);
+        hipLaunchKernelGGL(commit_release_kernel, dim3(c.n_seqs), dim3(256), 0, st, c);
+    }
     return hipGetLastError();
 }
 

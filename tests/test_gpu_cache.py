@@ -690,6 +690,31 @@ def test_commit_bounds():
     assert c.commit(rs).tolist() == [0, 0] and c.len.tolist() == [60, -5]
 
 
+def test_commit_judges_every_sequence_before_any_page_is_freed():
+    """Windows that name each other's pages (tables written by hand): the first sequence
+    of each pair keeps nothing and gives its page up; the second one's rows would move
+    into that page, so it is left out, length and tokens."""
+    P = _lib()
+    B, page, hd = 512, 16, 64
+    c = P.PagedCache(2, B // 2, page, 1, hd, B, 1)
+    shared = torch.arange(B // 2, dtype=torch.int32).repeat_interleave(2)
+    c.table.copy_(shared.view(B, 1))
+    c.ref.fill_(2)
+    c.k.copy_(torch.randn(c.k.shape, generator=torch.Generator().manual_seed(3)).to(BF))
+    c.v.copy_(-c.k)
+    k0 = c.k.clone()
+    rs = _starts([4] * B)
+    keep, starts = [], [0]
+    for b in range(B):
+        keep += [1, 3] if b % 2 else []
+        starts.append(len(keep))
+    ok = c.commit(rs, keep=_ints(keep), keep_start=_ints(starts))
+    assert ok.tolist() == [1, 0] * (B // 2)
+    assert c.len.tolist() == [0] * B and c.ref.tolist() == [1] * (B // 2)
+    assert c.table[::2].flatten().tolist() == [-1] * (B // 2) and torch.equal(c.table[1::2, 0].cpu(), shared[::2])
+    assert torch.equal(c.k, k0) and torch.equal(c.v, -k0)
+
+
 # ------------------------------------------------------------------ together
 
 @pytest.mark.parametrize("dtype", [BF, HF])
