@@ -486,6 +486,39 @@ def test_missing_pages_are_seen_by_no_row():
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("page,rows,H,kind", [(16, 1, 4, "full"), (16, 12, 8, "tree"), (16, 150, 8, "tree"), (32, 40, 8, "full"),
+                                              (16, 300, 4, "blocks")])
+def test_holes_anywhere_in_long_tables(page, rows, H, kind):
+    """Holes at both ends of what a wave holds of a table row, next to each other, in
+    single groups of 16 keys, in the window and in the last page."""
+    g = torch.Generator().manual_seed(page + rows)
+    rng = random.Random(rows)
+    lens = [16 * 200 + 5, 16 * 70]
+    counts = [rows, rows]
+    c, table = _cache([n + rows for n in lens], page, 2, 64, BF, seed=page)
+    c.k.fill_(math.nan)
+    c.v.fill_(math.nan)
+    ks, vs = _fill(c, table, lens, counts, 2, 64, BF, g)
+    c.len.copy_(_ints(lens))
+    q = torch.randn(2 * rows, H, 64, generator=g).to(BF)
+    sees = [_see(kind, n, rng) for n in counts]
+    mask = None if kind == "full" else ref.pack_mask(sees, (rows + 31) // 32).cuda()
+    holes = [[0, 61, 62, 63, 64, 65, 99, 126], [5, (lens[1] + rows - 1) // page]]
+    for b in range(2):
+        for i, e in enumerate(holes[b]):
+            if e * page < lens[b] + rows:
+                c.table[b, e] = (-1, c.ref.numel(), -(1 << 31), (1 << 31) - 1)[i % 4]
+    out = c.attend(0, q.cuda(), _starts(counts), rows, mask=mask, max_keys=max(lens) + rows)
+    h = ref.half_step(BF)
+    for b in range(2):
+        see = torch.cat([torch.ones(rows, lens[b], dtype=torch.bool), sees[b]], 1)
+        for e in holes[b]:
+            see[:, e * page:(e + 1) * page] = False
+        part = slice(b * rows, (b + 1) * rows)
+        want, mag, _ = ref.attend(q[part], ks[b], vs[b], see, 64 ** -0.5)
+        _within(out[part], want, h * want.abs() + (h + 2e-4) * mag + ref.half_subnormal(BF), f"holes {page} {rows} {b}")
+
+
 def test_attend_cuts_off_what_does_not_fit():
     """Starts, lengths and row counts out of range reach no memory of others; rows in
     range are computed."""
