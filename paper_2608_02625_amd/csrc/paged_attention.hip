@@ -570,10 +570,12 @@ __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
 // workgroups (12 waves) share a CU, 50 KB of LDS each.  WK = 2, for calls with too few
 // rows to fill the chip: two such groups of waves take tiles in turn and add up in the
 // end, half the steps and half the parts to join for the same split.
-// Bound by the vector unit and the chain of a tile (a tile is 16 matrix and about 90
-// other vector instructions, 16 of them exponentials of four times the cost), not by
-// bytes: 16 heads of 128 on 4, windows that see themselves, 8 x 1024 rows 80 us (860
-// TFLOP/s; 8 us of it start and end), 4 x 4096 rows 534 us (1030).
+// A tile is 16 matrix and about 90 other vector instructions per wave; on long windows
+// the matrix cores are busy 59 % of the cycles and the clock falls to 1.7 - 1.9 GHz, so
+// what bounds it is the card's power as much as the cycles (two tiles per step, 15 %
+// fewer instructions: no faster).  16 heads of 128 on 4, windows that see themselves:
+// 8 x 1024 rows 80 us (860 TFLOP/s; 8 us of it start and end), 4 x 4096 rows 534 to 570
+// us by the box (965 to 1030).
 constexpr int kManyRows = 128, kManyStages = 3;
 
 // A K tile of these kernels: 64 bytes of space behind each 1 KB copy turn its rows by
