@@ -145,8 +145,8 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
         // Results must not overlap: heads inside a row, or rows inside a head.
         const int64_t hd = rope->head_dim;
         const int64_t h = heads > 1 ? y_head_stride : 0, r = rows > 1 ? y_row_stride : 0;
-        const bool rows_outer = (rows == 1 || r >= (heads - 1) * h + hd) && (heads == 1 || h >= hd);
-        const bool heads_outer = (heads == 1 || h >= (rows - 1) * r + hd) && (rows == 1 || r >= hd);
+        const bool rows_outer = (rows == 1 || r >= (__int128)(heads - 1) * h + hd) && (heads == 1 || h >= hd);
+        const bool heads_outer = (heads == 1 || h >= (__int128)(rows - 1) * r + hd) && (rows == 1 || r >= hd);
         if (!rows_outer && !heads_outer) return fail(DLM_ERR_INVALID_ARG, "rows or heads of y overlap");
         if (d_x == d_y && ((rows > 1 && x_row_stride != y_row_stride) || (heads > 1 && x_head_stride != y_head_stride)))
             return fail(DLM_ERR_INVALID_ARG, "in place, x and y must have the same strides");
@@ -221,6 +221,8 @@ dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t
             if (d_q == d_q_out && (src_dtype != cache->dtype || q_stride != q_out_stride))
                 return fail(DLM_ERR_INVALID_ARG, "in place, q and q_out must have the same type and stride");
         }
+        if ((int64_t)cache->n_seqs * std::max(d_q ? n_heads : 0, cache->n_kv_heads) * std::min(max_rows, total_rows) > ((int64_t)1 << 33))
+            return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
         return launched(launch_append(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows,
                                       std::min(max_rows, total_rows), src_dtype, d_k, k_stride, d_v, v_stride, rope, d_pos,
                                       d_q ? n_heads : 0, d_q, q_stride, d_q_out, q_out_stride, (hipStream_t)hip_stream),

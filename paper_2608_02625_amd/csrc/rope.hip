@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
                                                    int rows, int heads, Lanes ln, bool back) {
     const int lanes = ln.turn + ln.pass;
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes;
-    const int64_t r = (int64_t)blockIdx.x * ln.rows + slot / ln.slots;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;
     const int h0 = slot % ln.slots;
     if (slot >= ln.slots * ln.rows || r >= rows) return;
     x += r * x_row;
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
     const int b = blockIdx.y;
     const int lanes = ln.turn + ln.pass;
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes;
-    const int i = blockIdx.x * ln.rows + slot / ln.slots;
+    const int i = (int)(blockIdx.z * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;    // max_rows <= 2^24
     const int h0 = slot % ln.slots;
     const int start = row_start[b], end = min(row_start[b + 1], total_rows), len = c.len[b];
     if (slot >= ln.slots * ln.rows || start < 0 || i >= max_rows || start >= end || i >= end - start) return;
@@ -256,11 +256,15 @@ Lanes lay_out(const dlm_rope& r, int V, int64_t rows, int heads) {
     return best;
 }
 
+// A grid has fewer than 2^32 threads along an axis.
+constexpr int64_t kWgsAcross = 1 << 20;
+
 template <typename T, int V, bool STREAM = false>
 hipError_t rope_layout(const dlm_rope& r, int rows, int heads, const void* x, int64_t xr, int64_t xh, void* y,
                        int64_t yr, int64_t yh, const int32_t* pos, bool back, hipStream_t st) {
     const Lanes ln = lay_out(r, V, rows, heads);
-    const dim3 grid((rows + ln.rows - 1) / ln.rows);
+    const int64_t wgs = ((int64_t)rows + ln.rows - 1) / ln.rows;
+    const dim3 grid((unsigned)std::min(wgs, kWgsAcross), (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
     if (r.interleaved)
         hipLaunchKernelGGL((rope_kernel<T, V, true, STREAM>), grid, dim3(256), 0, st, r, (const T*)x, xr, xh, (T*)y, yr, yh, pos,
                            rows, heads, ln, back);
@@ -307,7 +311,8 @@ template <typename S, typename D, int V, bool STREAM = false>
 hipError_t append_layout(const AppendCall& a) {
     const int n_all = 2 * a.c.n_kv + (a.q ? a.n_heads : 0);
     const Lanes ln = lay_out(a.rope, V, a.max_rows, n_all);
-    const dim3 grid((a.max_rows + ln.rows - 1) / ln.rows, a.c.n_seqs);
+    const int64_t wgs = ((int64_t)a.max_rows + ln.rows - 1) / ln.rows;
+    const dim3 grid((unsigned)std::min(wgs, kWgsAcross), a.c.n_seqs, (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
     const int64_t layer_base = (int64_t)a.layer * a.c.n_pages * a.c.n_kv * a.c.page_len * a.c.head_dim;
     if (a.rope.interleaved)
         hipLaunchKernelGGL((append_kernel<S, D, V, true, STREAM>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base,

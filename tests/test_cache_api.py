@@ -148,6 +148,18 @@ def test_append_refusals():
     assert call(total=0, most=0, rope=ctypes.byref(r)) == 0      # nothing to do
 
 
+def test_append_and_rope_limits():
+    """More work than a call may ask for; strides whose products pass 64 bits."""
+    L, lib = _lib()
+    many = ctypes.byref(_cache(L, n_seqs=1024))
+    for heads, rows, q in ((16, 1 << 20, FAKE), (0, 1 << 24, None)):
+        _refused(lib, lib.dlm_cache_append(many, 0, FAKE, rows, rows, 0, FAKE, 256, FAKE, 256, None, None, heads, q,
+                                           heads * 64, q, heads * 64, None), "2^33")
+    r = ctypes.byref(_rope(L, lib))
+    for yr, yh in ((1 << 62, 1 << 62), ((1 << 63) - 1, 1 << 61)):
+        _refused(lib, lib.dlm_rope_apply(r, 0, 1 << 30, 5, FAKE, 0, 0, 2 * FAKE, yr, yh, FAKE, 0, None), "overlap")
+
+
 def test_attend_refusals():
     L, lib = _lib()
     c = ctypes.byref(_cache(L))

@@ -117,6 +117,24 @@ def test_rotation(dtype, hd, rot, heads, interleaved, scaling, layout):
         assert not buf[:, :8].any() and not buf[:, 8 + heads * hd:].any()
 
 
+def test_rotation_of_more_rows_than_a_grid_has_places():
+    """A workgroup a row, more rows than 2^32 threads along one axis hold; offsets past
+    2^32 (the results are 9 GB)."""
+    P = _lib()
+    rows, hd = (1 << 24) + 3, 256
+    x = torch.randn(1, 1, hd, generator=torch.Generator().manual_seed(4)).to(BF).cuda().expand(rows, 1, hd)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    out = torch.empty(rows * (hd + 1), dtype=BF, device="cuda").view(rows, hd + 1)[:, 1:].view(rows, 1, hd)
+    P.Rope(hd, 2, interleaved=True).apply(x, pos, out=out)
+    at = torch.tensor([0, 1, (1 << 20) - 1, 1 << 20, (1 << 23) + 5, rows - 2, rows - 1])
+    w, scale = ref.frequencies(2)
+    host = x[:1].cpu().expand(len(at), 1, hd)
+    want = ref.rotate(host, at.to(torch.int32), w, scale, True)
+    tol = _rotation_tol(host, w, scale, True, want, BF)
+    _within(out[at.cuda()], want, tol, "rope of many rows")
+    assert torch.equal(out[:, 0, 2:].amin(0), x[0, 0, 2:]) and torch.equal(out[:, 0, 2:].amax(0), x[0, 0, 2:])
+
+
 def test_rotation_gradient_is_the_transpose():
     """d/dx of sum(g * rotate(x)), by differences and by the inner product."""
     P = _lib()
