@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import DlmConfig, DlmStats, check
-from .cache import PagedCache
+from .cache import PagedCache, _ints
 
 CONFIG_FIELDS = [f for f, _ in DlmConfig._fields_]
 
@@ -251,18 +251,19 @@ class Refiner:
         reserved places take their keys and values.  row_start int32 [n_seqs + 1];
         positions int32 [rows] (default: the tokens' places); mask int32 [rows, words]:
         the window rows that a row sees (default: all of its window's).  Returns (top-1
-        int32, confidence float, max logit float), each [rows]."""
+        int32, confidence float, max logit float), each [rows].  Calls of one model share
+        workspaces (kept, so that captured graphs stay valid): order them on one stream."""
         T = tokens.numel()
         if cache.device.index != (self.device.index if self.device.index is not None else torch.cuda.current_device()):
             raise ValueError("the cache and the model must be on one GPU")
-        for t, name, n in ((tokens, "tokens", T), (positions, "positions", T),
-                           (row_start, "row_start", cache.n_seqs + 1), (n_invalid, "n_invalid", 1)):
-            if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n):
-                raise ValueError(f"{name} must be a contiguous int32 tensor of {n} values")
+        device = cache.device
+        ints = [_ints(t, name, n, device) for t, name, n in (
+            (tokens, "tokens", T), (row_start, "row_start", cache.n_seqs + 1), (positions, "positions", T),
+            (mask, "mask", None), (n_invalid, "n_invalid", 1))]
         words = 0
         if mask is not None:
-            if mask.dtype != torch.int32 or mask.dim() != 2 or mask.shape[0] != T or not mask.is_contiguous():
-                raise ValueError("mask must be a contiguous int32 tensor [rows, words]")
+            if mask.dim() != 2 or mask.shape[0] != T:
+                raise ValueError("mask must be int32 [rows, words]")
             words = mask.shape[1]
         key = ("cache", T, min(int(max_rows), T), cache.n_seqs)
         ws = self._ws.get(key)
@@ -270,15 +271,22 @@ class Refiner:
             n = self.lib.dlm_cache_step_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(cache.c), T, int(max_rows))
             if n == 0:
                 raise ValueError(f"invalid window shape ({T} rows, {max_rows} at most) or a cache of another model")
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            # Row counts change from step to step: sizes are rounded up to powers of two,
+            # so that all workspaces together stay below four times the largest need.
+            size = ("cache", 1 << (n - 1).bit_length())
+            ws = self._ws.get(size)
+            if ws is None:
+                ws = self._ws[size] = torch.empty(size[1], dtype=torch.uint8, device=device)
             self._ws[key] = ws
-        top1 = torch.empty(T, dtype=torch.int32, device=self.device)
-        conf = torch.empty(T, dtype=torch.float32, device=self.device)
-        mx = torch.empty(T, dtype=torch.float32, device=self.device)
-        check(self.lib.dlm_cache_step(self._handle, ctypes.byref(cache.c), row_start.data_ptr(), T, int(max_rows),
-                                      int(max_keys), tokens.data_ptr(), _ptr(positions), _ptr(mask), words,
-                                      ws.data_ptr(), ws.numel(), self.stream, top1.data_ptr(), conf.data_ptr(),
-                                      mx.data_ptr(), _ptr(n_invalid)), "dlm_cache_step")
+        top1 = torch.empty(T, dtype=torch.int32, device=device)
+        conf = torch.empty(T, dtype=torch.float32, device=device)
+        mx = torch.empty(T, dtype=torch.float32, device=device)
+        toks, starts, pos, bits, bad = ints
+        with torch.cuda.device(device):
+            check(self.lib.dlm_cache_step(self._handle, ctypes.byref(cache.c), starts, T, int(max_rows), int(max_keys),
+                                          toks, pos, bits, words, ws.data_ptr(), ws.numel(),
+                                          torch.cuda.current_stream(device).cuda_stream, top1.data_ptr(),
+                                          conf.data_ptr(), mx.data_ptr(), bad), "dlm_cache_step")
         return top1, conf, mx
 
     def debug_forward(self, tokens: torch.Tensor, prompt_len: int, want_logits: bool = False,

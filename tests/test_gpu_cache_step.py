@@ -220,3 +220,32 @@ def test_tokens_rows_and_replays():
                dict(mask=torch.zeros(2, 1, dtype=torch.int32, device="cuda")), dict(max_rows=0)):
         with pytest.raises(ValueError):
             R.cache_step(**dict(dict(cache=c, tokens=src, row_start=rs, max_rows=20), **kw))
+
+
+def test_steps_of_many_sizes_share_workspaces_and_refuse_other_devices():
+    """Packed rows come in any number: their workspaces are few.  Host tensors are
+    refused before anything runs."""
+    torch = _torch()
+    shape, R, _ = _setup("tiny")
+    c = R.cache(16, 16, 2, 4)
+    toks = _i32(np.arange(100, dtype=np.int32) % shape.vocab)
+    first = {}
+    for rows in list(range(1, 41)) + [64, 100]:
+        rs = _i32([0, (rows + 1) // 2, rows])
+        c.truncate()
+        assert c.reserve(rs).tolist() == [1, 1]
+        out = R.cache_step(c, toks[:rows], rs, 50)
+        first[rows] = [x.clone() for x in out]
+    sizes = {ws.data_ptr(): ws.numel() for ws in R._ws.values()}
+    assert len(sizes) <= 10 and sum(sizes.values()) <= 4 * max(sizes.values())
+    for rows in (40, 1, 100, 7):                      # again, after others have used them
+        rs = _i32([0, (rows + 1) // 2, rows])
+        c.truncate()
+        c.reserve(rs)
+        assert all(torch.equal(a, b) for a, b in zip(R.cache_step(c, toks[:rows], rs, 50), first[rows]))
+    rs = _i32([0, 2, 4])
+    host = torch.zeros(4, dtype=torch.int32)
+    for kw in (dict(tokens=host), dict(row_start=torch.tensor([0, 2, 4], dtype=torch.int32)), dict(positions=host),
+               dict(mask=host.view(4, 1)), dict(n_invalid=host[:1])):
+        with pytest.raises(ValueError):
+            R.cache_step(**dict(dict(cache=c, tokens=toks[:4], row_start=rs, max_rows=2), **kw))
