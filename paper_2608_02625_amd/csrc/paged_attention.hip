@@ -167,7 +167,8 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     if (b < a.c.n_seqs) {
         s.start = a.row_start[b];
         const int end = min(a.row_start[b + 1], a.total_rows);
-        s.n = s.start >= 0 ? min(max(end - s.start, 0), a.max_rows) : 0;
+        // compared first: the difference of two unsound starts may pass 32 bits
+        s.n = s.start >= 0 && end > s.start ? min(end - s.start, a.max_rows) : 0;
         s.len = max(a.c.len[b], 0);
         s.keys = (int)min((int64_t)s.len + s.n, (int64_t)a.max_keys);
     }
