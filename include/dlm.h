@@ -516,7 +516,8 @@ dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t
  * -infinity.  What a row does not see does not change it, whatever it holds.
  * Rows of d_o behind the last window keep their values.  Scores, softmax and
  * sums are float32, probabilities are rounded to the cache's dtype for the
- * product with V.
+ * product with V (DLM_F16: to half a step where they are above 2^-25 of the row's
+ * largest, within 2^-36 of it below).
  */
 dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
                             int32_t max_rows, int32_t max_keys, int32_t n_heads, const void* d_q, int64_t q_stride,

@@ -18,9 +18,9 @@
 // 16 lanes hand in 4 rows of 16 values and get a column of 4 each), 4 keys per
 // read in the order that the scores' accumulator has them.  Probabilities are
 // rounded to the cache's type for the product (the matrix instruction takes
-// nothing wider at this rate; half a step, 2^-8 or 2^-11 of each, to either side), sums
-// add the unrounded ones.  The running maximum moves only when a tile raises it
-// by more than 2^8 in the exp2 domain.
+// nothing wider at this rate; half a step, 2^-8 or 2^-11 of each, to either side: see
+// kShift for float16's range), sums add the unrounded ones.  The running maximum moves
+// only when a tile raises it by more than 2^8 (float16: 2^4) in the exp2 domain.
 //
 // Masks.  Only tiles that meet the window, the last token or a missing page are
 // masked, by a 32-bit word per row.  A product with 0 does not hide an infinity
@@ -47,6 +47,19 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
+
+// Probabilities are held times 2^kShift, relative to the running maximum, which a row's
+// scores may pass by up to kHeadroom in the exp2 domain.  float16 keeps half a step only
+// down to 2^-14 (2^-25 of absolute error below): with its largest values at 2^15 that is 25
+// bits below the maximum, a score 17 lower, and what is lost below that is 2^-36 of the
+// maximum's weight per key (2^-16 for a million keys).  Without the factor keys 17 below one
+// other count 41 % too much, keys 18 below not at all.  A smaller headroom moves the maximum
+// more often: 8 windows of 1024 rows, 16 heads of 128 on 4, f16: 90.7 us, with 7 and 8 (half
+// a step kept to 14 below) 88.3, with 13 and 2 93.3; few rows cost the same with any.
+template <bool F16>
+constexpr int kShift = F16 ? 11 : 0;
+template <bool F16>
+constexpr int kHeadroom = F16 ? 15 - kShift<F16> : 8;
 
 template <bool F16>
 __device__ __forceinline__ f32x16 mfma(const s16x8& a, const s16x8& b, const f32x16& c) {
@@ -145,7 +158,7 @@ struct AttnArgs {
     int64_t q_stride;
     const uint32_t* mask;
     int mask_words;
-    float scale_log2, lim;                    // lim: 2^8 in the exp2 domain, in units of the scores
+    float scale_log2, lim;                    // lim: 2^kHeadroom in the exp2 domain, in units of the scores
     uint16_t* o;
     int64_t o_stride;
     float* lse;
@@ -395,7 +408,7 @@ struct RowTile {
         for (int e = 0; e < 16; ++e)
             if (!((see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
     }
-    // Scores to probabilities, the B operand of O^T = V^T P^T.
+    // Scores to probabilities (times 2^kShift), the B operand of O^T = V^T P^T.
     // `lim`: how far, in units of the scores, a maximum may lie above m.
     __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, float lim, s16x8 (&pf)[2]) {
         float mt = st[0];
@@ -413,7 +426,7 @@ struct RowTile {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[n][e] *= alpha;
             m = m_new;
-            bias = m == -INFINITY ? 0.f : -m * scale_log2;
+            bias = m == -INFINITY ? 0.f : fmaf(-m, scale_log2, (float)kShift<F16>);
         }
         float sum = 0.f;
 #pragma unroll
@@ -560,8 +573,9 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t t, int head
     const u32x2 w = {pack2<F16>(v[0] * inv, v[1] * inv), pack2<F16>(v[2] * inv, v[3] * inv)};
     *reinterpret_cast<u32x2*>(a.o + t * a.o_stride + head * hd + feature) = w;
 }
+template <bool F16>
 __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
-    return l == 0.f ? -INFINITY : (m * a.scale_log2 + __builtin_amdgcn_logf(l)) * 0.69314718f;
+    return l == 0.f ? -INFINITY : (fmaf(m, a.scale_log2, -(float)kShift<F16>) + __builtin_amdgcn_logf(l)) * 0.69314718f;
 }
 
 // ------------------------------------------------------------------ many rows
@@ -783,7 +797,7 @@ attend_many_kernel(const AttnArgs a) {
             *reinterpret_cast<u32x4*>(dst + 8) = u32x4{p[1][0], p[1][1], p[3][0], p[3][1]};
         }
     }
-    if (a.lse && g == 0 && row < rows) a.lse[t * a.n_heads + head] = log_sum(a, m, l);
+    if (a.lse && g == 0 && row < rows) a.lse[t * a.n_heads + head] = log_sum<F16>(a, m, l);
 }
 
 // ------------------------------------------------------------------ few rows
@@ -992,7 +1006,7 @@ attend_few_kernel(const AttnArgs a) {
             const int64_t t = (int64_t)u.s.start + (uint32_t)row / (uint32_t)a.group;
             const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
+            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
         }
     }
 }
@@ -1051,7 +1065,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
             const int64_t t = (int64_t)u.s.start + (uint32_t)pr / (uint32_t)a.group;
             const int h = u.kvh * a.group + (int)((uint32_t)pr % (uint32_t)a.group);
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum(a, m, l);
+            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
         }
         __syncthreads();
     }
@@ -1143,7 +1157,7 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.mask = mask;
     a.mask_words = mask ? mask_words : 0;                 // no words without a mask
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.lim = std::min(8.f / a.scale_log2, 3e38f);
+    a.lim = std::min((dtype == DLM_F16 ? kHeadroom<true> : kHeadroom<false>) / a.scale_log2, 3e38f);
     a.o = (uint16_t*)o;
     a.o_stride = o_stride;
     a.lse = lse;

@@ -5,15 +5,19 @@ largest, heads and rows past 32-bit sums.  Tolerances as in tests/test_gpu_cache
 
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
+from tests import cache_ref as ref
 from tests.gpu_util import need_gpu
-from tests.test_gpu_cache import BF, HF, _cache, _ints
+from tests.test_gpu_cache import BF, HF, _cache, _ints, _within
 
 pytestmark = pytest.mark.gpu
 
 INT_MAX, INT_MIN = (1 << 31) - 1, -(1 << 31)
+SHIFT = 11                                            # of float16 probabilities, in powers of two
 
 
 @pytest.fixture(autouse=True)
@@ -53,3 +57,49 @@ def test_row_starts_whose_difference_passes_32_bits(dtype, H, KV, rows, starts):
             assert torch.equal(c.k, before[0]) and torch.equal(c.v, before[1])
         ok = c.reserve(s)
         assert set(ok.tolist()) <= {0, 1}
+
+
+# ------------------------------------------------------------------ small probabilities
+
+def _sink(dtype, n, gap, noise, at, rows, H, hd, page, max_keys):
+    """One key `gap` above a long tail of (nearly) equal ones, with a value of zero, so
+    that the result is the tail's.  Scores are exact; the tail's probabilities keep
+    half a step each, or what float16 leaves of them: they are held times 2^SHIFT, so
+    2^-(25 + SHIFT) of the largest one's weight (the sum's, at least) where they are
+    subnormal, which is more than 14 + SHIFT powers of two below it."""
+    g = torch.Generator().manual_seed(n + rows)
+    c, table = _cache([n], page, 1, hd, dtype, seed=rows)
+    k = torch.zeros(n, 1, hd)
+    k[:, 0, 0] = (noise * torch.randn(n, generator=g)).clamp(-1, 1)
+    k[at, 0, 0] = gap
+    v = 1 + 0.5 * torch.randn(n, 1, hd, generator=g)
+    v[at] = 0
+    k, v = k.to(dtype), v.to(dtype)
+    pages = table[0, :-(-n // page)].long()
+    full = torch.zeros(len(pages) * page, 1, hd, dtype=dtype)
+    for src, pool in ((k, c.k), (v, c.v)):
+        full[:n] = src
+        pool[0, pages.cuda()] = full.view(len(pages), page, 1, hd).transpose(1, 2).contiguous().cuda()
+    c.len.copy_(_ints([n - rows]))
+    q = torch.zeros(rows, H, hd, dtype=dtype)
+    q[..., 0] = 1
+    lse = torch.empty(rows, H, device="cuda")
+    out = c.attend(0, q.cuda(), _ints([0, rows]), rows, scale=1.0, max_keys=max_keys, lse=lse)
+    want, mag, want_lse = ref.attend(q, k, v, torch.ones(rows, n, dtype=torch.bool), 1.0)
+    h = ref.half_step(dtype)
+    low = dtype == HF and (gap + k[..., 0].abs().clamp(max=1).max().item()) * math.log2(math.e) > 14 + SHIFT
+    tail = n * 2.0 ** -(25 + SHIFT) * v.double().abs().mean() if low else 0.0
+    tol = h * want.abs() + (h + 1e-5) * mag + tail + ref.half_subnormal(dtype)
+    what = f"sink {dtype} {n} keys {gap} below {at}, {rows} rows of {H} heads"
+    _within(out, want, tol, what)
+    _within(lse, want_lse, 1e-5 + 2.0 ** -22 * want_lse.abs(), what + " lse")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("noise", [0.0, 0.25])
+@pytest.mark.parametrize("gap", [9.0, 14.0, 16.0, 17.0, 17.5, 21.0])
+@pytest.mark.parametrize("n,at,rows,H,hd,page,max_keys", [
+    (131072, 0, 1, 1, 64, 64, 0), (131072, 5, 1, 4, 128, 128, 131072), (40000, 39000, 13, 4, 64, 16, 0),
+    (131072, 70000, 40, 4, 128, 64, 131072), (20000, 3, 200, 2, 64, 32, 0), (900, 0, 1, 4, 64, 16, 900)])
+def test_a_long_tail_far_below_one_key(dtype, gap, noise, n, at, rows, H, hd, page, max_keys):
+    _sink(dtype, n, gap, noise, at, rows, H, hd, page, max_keys)
