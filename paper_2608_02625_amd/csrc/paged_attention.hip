@@ -575,7 +575,7 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t t, int head
 }
 template <bool F16>
 __device__ __forceinline__ float log_sum(const AttnArgs& a, float m, float l) {
-    return l == 0.f ? -INFINITY : (fmaf(m, a.scale_log2, -(float)kShift<F16>) + __builtin_amdgcn_logf(l)) * 0.69314718f;
+    return l == 0.f ? -INFINITY : fmaf(m, a.scale_log2, __builtin_amdgcn_logf(l) - (float)kShift<F16>) * 0.69314718f;
 }
 
 // ------------------------------------------------------------------ many rows
