@@ -665,7 +665,7 @@ attend_many_kernel(const AttnArgs a) {
     const int kfrag[2] = {krow + ((g ^ k_turn<HD>(j)) << 4), krow + (((2 + g) ^ k_turn<HD>(j)) << 4)};
     const int vfrag = v_base<HD>(lane);
     const uint32_t* mrow = a.mask ? a.mask + t * a.mask_words : nullptr;
-    const int clear = a.mask ? u.s.len : u.s.keys;        // keys that every row sees
+    const int clear = a.mask ? min(u.s.len, u.s.keys) : u.s.keys;         // keys that every row sees
 
     // Tiles u.t0 + wk + WK i, i < n, the same n for all waves (they meet at every one):
     // copies past the last tile repeat it, and a step on it is one that no row sees.
@@ -868,7 +868,7 @@ attend_few_kernel(const AttnArgs a) {
     for (int x = 0; x < RT; ++x) rt[x].clear();
     const int kfrag = j * D::ROW + ((g ^ k_key<D::CPR>(j)) << 4);
     const int vfrag = v_base<HD>(lane);
-    const int clear = a.mask ? u.s.len : u.s.keys;
+    const int clear = a.mask ? min(u.s.len, u.s.keys) : u.s.keys;
 
     // Tiles u.t0 + wave + WAVES i, i < n.  Copies past the last one repeat it.
     const int n = (u.t1 - u.t0 - wave + WAVES - 1) / WAVES;           // may be <= 0

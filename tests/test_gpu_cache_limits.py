@@ -103,3 +103,39 @@ def _sink(dtype, n, gap, noise, at, rows, H, hd, page, max_keys):
     (131072, 70000, 40, 4, 128, 64, 131072), (20000, 3, 200, 2, 64, 32, 0), (900, 0, 1, 4, 64, 16, 900)])
 def test_a_long_tail_far_below_one_key(dtype, gap, noise, n, at, rows, H, hd, page, max_keys):
     _sink(dtype, n, gap, noise, at, rows, H, hd, page, max_keys)
+
+
+# ------------------------------------------------------------------ bounds on the keys
+
+@pytest.mark.parametrize("dtype,H,KV,hd", [(BF, 4, 2, 64), (HF, 8, 2, 128)])
+@pytest.mark.parametrize("rows", [1, 12, 70])
+@pytest.mark.parametrize("length,max_keys,width", [(200, 161, 40), (200, 199, 40), (96, 40, 40), (3000, 2567, 400),
+                                                   (190, 0, 11), (1 << 29, 0, 11), (176, 0, 11)])
+def test_a_mask_does_not_bring_back_keys_behind_the_last(dtype, H, KV, hd, rows, length, max_keys, width):
+    """Lengths above max_keys, or above what a table row (of an odd number of 16 keys)
+    holds: keys from the bound on are seen by no row, with a mask as without one; rows
+    of the window below it follow the mask."""
+    page = 16
+    room = width * page
+    keys = min(length + rows, max_keys or room, room)
+    g = torch.Generator().manual_seed(rows + max_keys)
+    c, table = _cache([room], page, KV, hd, dtype, width=width, seed=rows)
+    k, v = (torch.randn(room, KV, hd, generator=g).to(dtype) for _ in range(2))
+    for src, pool in ((k, c.k), (v, c.v)):
+        pool[0, table[0].long().cuda()] = src.view(width, page, KV, hd).transpose(1, 2).contiguous().cuda()
+    c.len.copy_(_ints([length]))
+    q = torch.randn(rows, H, hd, generator=g).to(dtype)
+    mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (rows, 3), generator=g, dtype=torch.int32)
+    rs = _ints([0, rows])
+    n = min(length, keys)
+    bits = [[(int(mask[i, j // 32]) >> (j % 32)) & 1 for j in range(keys - n)] for i in range(rows)]
+    see = torch.cat([torch.ones(rows, n, dtype=torch.bool), torch.tensor(bits, dtype=torch.bool).view(rows, keys - n)], 1)
+    h = ref.half_step(dtype)
+    for m, s in ((mask.cuda(), see), (None, torch.ones_like(see))):
+        lse = torch.empty(rows, H, device="cuda")
+        out = c.attend(0, q.cuda(), rs, rows, mask=m, max_keys=max_keys, lse=lse)
+        want, mag, want_lse = ref.attend(q, k[:keys], v[:keys], s, hd ** -0.5)
+        what = f"{rows} rows behind {length} tokens, {keys} keys"
+        _within(out, want, h * want.abs() + (h + 2e-4) * mag + ref.half_subnormal(dtype), what)
+        # float32 scores: hd 2^-24 of the sum of absolute products, below 64 here
+        _within(lse, want_lse, torch.full_like(want_lse, 1e-3), what + " lse")
