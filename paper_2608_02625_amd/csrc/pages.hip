@@ -187,6 +187,7 @@ __global__ __launch_bounds__(256) void reserve_copy_kernel(CacheArgs c, const in
 // A sequence's list of kept rows, checked by the whole workgroup.
 struct Kept {
     int n, len, m, first;     // window rows, tokens before, kept rows, index of the first kept one
+    int entry;                // of the window's first token, in thread 0, if ok
     bool ok;                  // the list and the pages allow it
 };
 __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start, int total_rows, const int32_t* keep,
@@ -196,6 +197,7 @@ __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start
     k.len = c.len[b];
     k.first = 0;
     k.m = k.n;
+    k.entry = -1;
     bool bad = k.len < 0 || pages_for((int64_t)k.len + k.n, c.page_log2) > c.max_pages;
     if (keep_start) {
         k.first = keep_start[b];
@@ -216,6 +218,7 @@ __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start
         const int w = pages_for((int64_t)k.len + k.m, c.page_log2);        // written if rows move
         for (int e = lo + threadIdx.x; e < hi; e += blockDim.x) {
             const int p = c.table[(int64_t)b * c.max_pages + e];
+            if (e == lo) k.entry = p;
             if (!names_page(p, c))
                 wrong = 1;
             else if (moved && e < w)
@@ -226,22 +229,27 @@ __device__ Kept check_commit(const CacheArgs& c, int b, const int32_t* row_start
     return k;
 }
 
-// A sequence that passed its checks counts its new tokens at once, with this added
-// until its pages are freed: more than any table row holds, so the kernels behind see
-// which sequences go through (references change as soon as the first one frees pages,
-// so none is checked after that).
-constexpr int kCounted = 1 << 30;
-__device__ __forceinline__ int counted(int len, const CacheArgs& c) {     // new length, -1 if left out
-    return len >= kCounted && pages_for((int64_t)len - kCounted, c.page_log2) <= c.max_pages ? len - kCounted : -1;
+// References change as soon as the first sequence frees pages, so none is checked after
+// that, and a sequence that passed its checks says so to the kernels behind in its own
+// table: the entry of its window's first token, which names a page p of the pool, holds
+// -2 - p until its pages are freed.  A table that comes with such an entry names no page
+// there, so its sequence is left out, and the check makes the entry -1, which is none too.
+__device__ __forceinline__ bool is_verdict(int entry, const CacheArgs& c) { return entry < -1 && -2 - entry < c.n_pages; }
+__device__ __forceinline__ int page_of(int entry, const CacheArgs& c) { return is_verdict(entry, c) ? -2 - entry : entry; }
+// The verdict's place in the table, null if the window is empty or lies outside of the row.
+__device__ __forceinline__ int32_t* verdict_entry(const CacheArgs& c, int b, int n, int len) {
+    if (n == 0 || len < 0 || pages_for((int64_t)len + n, c.page_log2) > c.max_pages) return nullptr;
+    return c.table + (int64_t)b * c.max_pages + (len >> c.page_log2);
 }
 
-// Entries of a table row from `from` on: their pages lose a reference.
-__device__ __forceinline__ void release_from(const CacheArgs& c, int b, int from) {
+// Entries of a table row from `from` on: their pages lose a reference.  Entry `verdict`
+// (-1: none) stands for `page`.
+__device__ __forceinline__ void release_from(const CacheArgs& c, int b, int from, int verdict = -1, int page = -1) {
     for (int e = from + (int)threadIdx.x; e < c.max_pages; e += blockDim.x) {
         const int64_t at = (int64_t)b * c.max_pages + e;
-        const int p = c.table[at];
+        const int entry = c.table[at], p = e == verdict ? page : entry;
         if (names_page(p, c)) atomicSub(&c.ref[p], 1);
-        if (p != -1) c.table[at] = -1;
+        if (entry != -1) c.table[at] = -1;
     }
 }
 
@@ -258,7 +266,10 @@ __global__ __launch_bounds__(256) void commit_check_kernel(CacheArgs c, const in
     const Kept k = check_commit(c, b, row_start, total_rows, keep, keep_start, total_keep);
     if (k.ok && !keep) release_from(c, b, pages_for((int64_t)k.len + k.m, c.page_log2));
     if (threadIdx.x == 0) {
-        if (k.ok) c.len[b] = k.len + k.m + (keep ? kCounted : 0);
+        if (k.ok && !keep) c.len[b] = k.len + k.m;
+        int32_t* verdict = verdict_entry(c, b, k.n, k.len);
+        if (keep && k.ok) *verdict = -2 - k.entry;
+        else if (keep && verdict && is_verdict(*verdict, c)) *verdict = -1;
         if (ok) ok[b] = k.ok;
     }
 }
@@ -271,20 +282,22 @@ __global__ __launch_bounds__(256) void commit_check_kernel(CacheArgs c, const in
 // and the freeing 17).
 constexpr int kMoveLoads = 4;
 
-__global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ keep,
+__global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
+                                                          int total_rows, const int32_t* __restrict__ keep,
                                                           const int32_t* __restrict__ keep_start, int total_keep) {
     const int b = blockIdx.y;
     const int chunks = c.head_dim / 8, rows_at_once = 256 * kMoveLoads / chunks;
     const int h = blockIdx.x % c.n_kv, lk = blockIdx.x / c.n_kv;
     const int64_t head = (int64_t)c.page_len * c.head_dim * 2, page = head * c.n_kv;
     char* pool = (lk & 1 ? c.v : c.k) + (int64_t)(lk >> 1) * c.n_pages * page + h * head;
-    const int first = keep_start[b], m = keep_start[b + 1] - first, len = counted(c.len[b], c) - m;
-    if (len < 0 || first < 0 || m <= 0 || first > total_keep - m) return;
+    const int first = keep_start[b], m = keep_start[b + 1] - first, len = c.len[b];
+    const int32_t* verdict = verdict_entry(c, b, window_rows(row_start, b, total_rows), len);
+    if (!verdict || !is_verdict(*verdict, c) || first < 0 || m <= 0 || first > total_keep - m) return;
     // Place of a token (chunk threadIdx % chunks of it), in some page whatever the table holds.
     auto place = [&](int row) {
         const int64_t t = (int64_t)len + max(row, 0);
         const int e = (int)min(t >> c.page_log2, (int64_t)c.max_pages - 1);
-        const int p = c.table[(int64_t)b * c.max_pages + e];
+        const int p = page_of(c.table[(int64_t)b * c.max_pages + e], c);
         return pool + (names_page(p, c) ? p : 0) * page + (t & (c.page_len - 1)) * c.head_dim * 2 +
                (threadIdx.x % chunks) * 16;
     };
@@ -308,13 +321,19 @@ __global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int
     }
 }
 
-__global__ __launch_bounds__(256) void commit_release_kernel(CacheArgs c) {
+__global__ __launch_bounds__(256) void commit_release_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
+                                                             int total_rows, const int32_t* __restrict__ keep_start) {
     const int b = blockIdx.x;
-    const int len = counted(c.len[b], c);
-    if (len < 0) return;
-    __syncthreads();                                  // every thread has read the length
-    release_from(c, b, pages_for(len, c.page_log2));
-    if (threadIdx.x == 0) c.len[b] = len;
+    const int before = c.len[b], len = before + keep_start[b + 1] - keep_start[b];
+    int32_t* verdict = verdict_entry(c, b, window_rows(row_start, b, total_rows), before);
+    if (!verdict || !is_verdict(*verdict, c)) return;
+    const int page = page_of(*verdict, c), at = before >> c.page_log2, held = pages_for(len, c.page_log2);
+    __syncthreads();                                  // every thread has read the length and the entry
+    release_from(c, b, held, at, page);
+    if (threadIdx.x == 0) {
+        if (at < held) *verdict = page;
+        c.len[b] = len;
+    }
 }
 
 // ------------------------------------------------------------------ fork, truncate, reset
@@ -459,9 +478,9 @@ hipError_t launch_commit(const CacheArgs& c, const int32_t* row_start, int total
     hipLaunchKernelGGL(commit_check_kernel, dim3(c.n_seqs), dim3(256), 0, st, c, row_start, total_rows, keep,
                        keep_start, total_keep, ok);
     if (keep) {
-        hipLaunchKernelGGL(commit_move_kernel, dim3(2 * c.n_layers * c.n_kv, c.n_seqs), dim3(256), 0, st, c, keep,
-                           keep_start, total_keep);
-        hipLaunchKernelGGL(commit_release_kernel, dim3(c.n_seqs), dim3(256), 0, st, c);
+        hipLaunchKernelGGL(commit_move_kernel, dim3(2 * c.n_layers * c.n_kv, c.n_seqs), dim3(256), 0, st, c,
+                           row_start, total_rows, keep, keep_start, total_keep);
+        hipLaunchKernelGGL(commit_release_kernel, dim3(c.n_seqs), dim3(256), 0, st, c, row_start, total_rows, keep_start);
     }
     return hipGetLastError();
 }

@@ -139,3 +139,77 @@ def test_a_mask_does_not_bring_back_keys_behind_the_last(dtype, H, KV, hd, rows,
         _within(out, want, h * want.abs() + (h + 2e-4) * mag + ref.half_subnormal(dtype), what)
         # float32 scores: hd 2^-24 of the sum of absolute products, below 64 here
         _within(lse, want_lse, torch.full_like(want_lse, 1e-3), what + " lse")
+
+
+# ------------------------------------------------------------------ commit
+
+@pytest.mark.parametrize("length", [1 << 30, (1 << 30) + 5, (1 << 30) + 64, (1 << 31) - 1, -1, -(1 << 31), 65])
+@pytest.mark.parametrize("rows", [0, 4])
+def test_commit_leaves_out_lengths_out_of_range_whole(length, rows):
+    """A kept list with a length that no table row holds, with window rows and without:
+    the sequence keeps its length, pages and tokens, and the ones beside it go through."""
+    c, table = _cache([64, 64, 64], 16, 2, 64, BF, layers=2)
+    c.k.copy_(torch.randn(c.k.shape, generator=torch.Generator().manual_seed(3)).to(BF))
+    c.v.copy_(-c.k)
+    c.len.copy_(_ints([10, length, 20]))
+    before, k0 = c.meta.clone(), c.k.clone()
+    rs = _ints([0, 8, 8 + rows, 12 + rows])
+    keep, keep_start = _ints([0, 3, 5, 1, 3, 2]), _ints([0, 3, 5, 6])
+    want_ok = [1, 1 if rows == 0 else 0, 1]
+    assert c.commit(rs, keep=keep, keep_start=keep_start).tolist() == want_ok
+    assert c.len.tolist() == [13, length, 21]
+    n = c.ref.numel()
+    assert torch.equal(c.table[1].cpu(), table[1]) and (c.ref[table[1].long().cuda()] == 1).all()
+    assert c.table[0].tolist() == [int(table[0, 0]), -1, -1, -1]
+    assert c.table[2].tolist() == [int(x) for x in table[2, :2]] + [-1, -1]
+    want = k0.clone()
+    for b, start, kept in ((0, 10, [0, 3, 5]), (2, 20, [2])):
+        for i, x in enumerate(kept):
+            t, f = start + i, start + x
+            want[:, int(table[b, t // 16]), :, t % 16] = k0[:, int(table[b, f // 16]), :, f % 16]
+    assert torch.equal(c.k, want) and torch.equal(c.v, -want)
+    assert c.meta.numel() == before.numel() and c.ref.sum().item() == int((c.table >= 0).sum()) and n == c.ref.numel()
+
+
+@pytest.mark.parametrize("kept,per", [([1, 3], 2), ([0, 1, 2, 3, 4], 5), ([3, 1], 2), ([], 0), ([0, 1, 2, 3], 4)])
+def test_commit_of_tables_that_hold_any_ids(kept, per):
+    """Ids below 0 or past the pool at a window's first token: left out, nothing moves and
+    nothing is freed, whatever the id and the list."""
+    ids = [-1, -2, -3, -16, -17, -18, -(1 << 31), 1 << 30, (1 << 31) - 1, 15, 16]
+    c, table = _cache([32] * len(ids), 16, 1, 64, BF, spare=0)
+    n = c.ref.numel()
+    c.k.copy_(torch.randn(c.k.shape, generator=torch.Generator().manual_seed(5)).to(BF))
+    c.v.copy_(-c.k)
+    c.len.fill_(20)
+    wild = [x for x in ids if not 0 <= x < n] + [-2 - (n - 1), -1 - n, -2 - n]
+    wild = (wild + [-2] * len(ids))[:len(ids)]
+    c.table[:, 1] = _ints(wild)
+    k0, ref0, first = c.k.clone(), c.ref.clone(), c.table[:, 0].clone()
+    rs = _ints([4 * b for b in range(len(ids) + 1)])
+    keep = _ints(kept * len(ids))
+    ok = c.commit(rs, keep=keep, keep_start=_ints([per * b for b in range(len(ids) + 1)]))
+    assert ok.tolist() == [0] * len(ids) and c.len.tolist() == [20] * len(ids)
+    assert torch.equal(c.ref, ref0) and torch.equal(c.table[:, 0], first) and torch.equal(c.k, k0)
+    now = c.table[:, 1].tolist()
+    assert all(a == b or (b == -1 and a < 0) for a, b in zip(wild, now))     # none stays none
+    c.table[:, 1] = _ints(wild)
+    for starts in ([-1] * (len(ids) + 1), [1 << 30] * (len(ids) + 1), [(-1) ** b * 3 for b in range(len(ids) + 1)]):
+        ok = c.commit(rs, keep=keep, keep_start=_ints(starts))       # lists out of range
+        assert ok.tolist() == [0] * len(ids) and c.len.tolist() == [20] * len(ids)
+        assert torch.equal(c.ref, ref0) and torch.equal(c.table[:, 0], first) and torch.equal(c.k, k0)
+    ok = c.commit(rs)                                  # without a list too
+    assert ok.tolist() == [0] * len(ids) and torch.equal(c.ref, ref0)
+
+
+def test_commit_frees_only_pages_that_entries_name():
+    """Ids below 0 in entries behind an accepted window are none of the pool's pages."""
+    c, table = _cache([64, 64], 16, 1, 64, BF)
+    c.len.copy_(_ints([5, 5]))
+    c.table[0, 1:] = _ints([-2, -5, -1 - c.ref.numel()])
+    c.ref[table[0, 1:].long().cuda()] = 0
+    held = c.ref.clone()
+    ok = c.commit(_ints([0, 4, 8]), keep=_ints([2, 1, 3]), keep_start=_ints([0, 1, 3]))
+    assert ok.tolist() == [1, 1] and c.len.tolist() == [6, 7]
+    held[table[1, 1:].long().cuda()] -= 1
+    assert torch.equal(c.ref, held)
+    assert c.table.tolist() == [[int(table[b, 0]), -1, -1, -1] for b in range(2)]
