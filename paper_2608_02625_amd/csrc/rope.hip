@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
     const int lanes = ln.turn + ln.pass;
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes;
     const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;
-    const int h0 = slot % ln.slots;
+    const uint32_t h0 = slot % ln.slots;                      // unsigned: heads up to 2^31 - 1 and a step more
     if (slot >= ln.slots * ln.rows || r >= rows) return;
     x += r * x_row;
     y += r * y_row;
@@ -152,12 +152,12 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
         float c[V], s[V];
         angles<V>(rope.phase, rope.scale, pos[r], lane * V, back, c, s);
 #pragma unroll 4
-        for (int h = h0; h < heads; h += ln.slots)
+        for (uint32_t h = h0; h < (uint32_t)heads; h += ln.slots)
             turn_pairs<T, T, V, INTER, STREAM>(x + h * x_head, y + h * y_head, lane * V, rope.rot_dim / 2, c, s, true);
     } else {
         const int o = rope.rot_dim + (lane - ln.turn) * V;
 #pragma unroll 2
-        for (int h = h0; h < heads; h += ln.slots) pass_values<T, T, V, STREAM>(x + h * x_head + o, y + h * y_head + o);
+        for (uint32_t h = h0; h < (uint32_t)heads; h += ln.slots) pass_values<T, T, V, STREAM>(x + h * x_head + o, y + h * y_head + o);
     }
 }
 
@@ -246,7 +246,7 @@ Lanes lay_out(const dlm_rope& r, int V, int64_t rows, int heads) {
     double best_use = 0.;
     for (int s = 1; s <= heads && s <= most; ++s) {
         const int rows_at_once = (int)std::min<int64_t>(most / s, rows);
-        const double use = (double)(s * rows_at_once) / most * heads / (s * ((heads + s - 1) / s));
+        const double use = (double)(s * rows_at_once) / most * heads / (s * (((int64_t)heads + s - 1) / s));
         if (use >= best_use) {
             best_use = use;
             best.slots = s;

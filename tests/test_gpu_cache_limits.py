@@ -213,3 +213,21 @@ def test_commit_frees_only_pages_that_entries_name():
     held[table[1, 1:].long().cuda()] -= 1
     assert torch.equal(c.ref, held)
     assert c.table.tolist() == [[int(table[b, 0]), -1, -1, -1] for b in range(2)]
+
+
+# ------------------------------------------------------------------ rotary positions
+
+@pytest.mark.parametrize("heads", [(1 << 31) - 1, (1 << 31) - 200])
+def test_rotation_of_as_many_heads_as_a_call_may_name(heads):
+    """Heads whose index passes 2^31 - 1 by the step to the next one end there (the
+    results are 8.6 GB; one head is read for all)."""
+    from paper_2608_02625_amd import Rope
+    guard = 600
+    x = torch.tensor([[[0.75, -1.5]]], dtype=BF, device="cuda").expand(1, heads, 2)
+    buf = torch.full((heads + 2 * guard, 2), 5.0, dtype=BF, device="cuda")
+    out = buf[guard:guard + heads].view(1, heads, 2)
+    Rope(2).apply(x, _ints([3]), out=out)
+    want = Rope(2).apply(x[:, :1], _ints([3]))[0, 0]
+    assert (buf[:guard] == 5).all() and (buf[guard + heads:] == 5).all()
+    for i in range(2):
+        assert out[0, :, i].amin() == want[i] and out[0, :, i].amax() == want[i]
