@@ -442,7 +442,9 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
  * cannot be checked by the host.  The kernels never touch memory outside the
  * buffers whatever they hold: rows, lengths and entries out of range are cut
  * off, keys in an entry that names no page of the pool are seen by no row, and
- * rows appended there are dropped.  d_ok outputs (int32, may be NULL) say per
+ * rows appended there are dropped, as are rows that would go over a token which
+ * another sequence counts (in a shared page that a reserve with ok 0 left in
+ * place).  d_ok outputs (int32, may be NULL) say per
  * sequence or pair whether an operation took place (1) or was left out whole
  * (0).  All calls that share a cache or a workspace must be ordered on one
  * stream (or by events); they may be captured in a HIP graph.

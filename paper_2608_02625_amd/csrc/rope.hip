@@ -12,8 +12,8 @@
 // Bound by the bytes of the rows: a thread takes one vector of pairs of a row,
 // computes its sines and cosines once and walks heads with them.  32768 rows of 20
 // heads of 128 (336 MB): 63 us, 5.3 TB/s; 32 prompts of up to 1024 rows, float32 to
-// pages of bf16 (378 MB): 65 us, 5.8 TB/s; one row of each of 32 sequences: 5.2 us,
-// three loads that need each other.
+// pages of bf16 (378 MB): 66 us, 5.7 TB/s; one row of each of 32 sequences: 5.4 us,
+// four loads that need each other (the page's references among them, beside the sines).
 #include <algorithm>
 
 #include "common.h"
@@ -161,6 +161,15 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
     }
 }
 
+// Whether a sequence other than b counts token t, in this page (shared pages stand in the
+// same entry of every table row: they come from forks).
+__device__ bool counted_elsewhere(const CacheArgs& c, int b, int64_t t, int page) {
+    const int64_t entry = t >> c.page_log2;
+    for (int s = 0; s < c.n_seqs; ++s)
+        if (s != b && c.len[s] > t && c.table[(int64_t)s * c.max_pages + entry] == page) return true;
+    return false;
+}
+
 // Keys, values and queries of the rows of sequence blockIdx.y.  Head indexes run
 // over the keys, the values, then the queries.  Values take the keys' lanes
 // without a rotation.
@@ -183,7 +192,8 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
     const int64_t entry = t >> c.page_log2;
     int page = -1;
     if (len >= 0 && entry < c.max_pages) page = c.table[(int64_t)b * c.max_pages + entry];
-    const bool held = page >= 0 && page < c.n_pages;          // else the row's keys and values are dropped
+    bool held = page >= 0 && page < c.n_pages;                // else the row's keys and values are dropped
+    const int refs = held ? c.ref[page] : 0;
     const int hd = c.head_dim;
     const int64_t head_stride = (int64_t)c.page_len * hd;     // within a page
     const int64_t base = layer_base + (int64_t)(held ? page : 0) * c.n_kv * head_stride + (t & (c.page_len - 1)) * hd;
@@ -193,6 +203,9 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
     float co[V], si[V];
     const bool rotate = rope.scale != 0.f;                    // 0: no rotation asked for
     if (turns && rotate) angles<V>(rope.phase, rope.scale, pos ? pos[r] : t, o, false, co, si);
+    // Only a window without room of its own gets here with a page of others (or one forked
+    // since it was reserved).
+    if (refs > 1 && counted_elsewhere(c, b, t, page)) held = false;
 #pragma unroll 4
     for (int h = h0; h < n_all; h += ln.slots) {
         const S* src;

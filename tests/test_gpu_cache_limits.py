@@ -231,3 +231,50 @@ def test_rotation_of_as_many_heads_as_a_call_may_name(heads):
     assert (buf[:guard] == 5).all() and (buf[guard + heads:] == 5).all()
     for i in range(2):
         assert out[0, :, i].amin() == want[i] and out[0, :, i].amax() == want[i]
+
+
+# ------------------------------------------------------------------ append
+
+@pytest.mark.parametrize("dtype,src", [(BF, BF), (HF, torch.float32)])
+def test_append_overwrites_no_token_of_another_sequence(dtype, src):
+    """A pool without a free page: a copy that was cut back gets no page of its own, and
+    its rows do not go over the tokens that its original counts; rows behind every
+    sequence's tokens are written as ever, and queries come out whole."""
+    from paper_2608_02625_amd import PagedCache, Rope
+    page, KV, H, hd = 16, 2, 4, 64
+    c = PagedCache(2, 3, page, KV, hd, 3, 4, dtype=dtype)
+    c.k.zero_()
+    c.v.zero_()
+    first = torch.randn(40, KV, hd, device="cuda").to(src)
+    rs = _ints([0, 40, 40, 40])
+    assert c.reserve(rs).tolist() == [1, 1, 1]
+    for layer in range(2):
+        c.append(layer, first, -first, rs, 40)
+    assert c.commit(rs).tolist() == [1, 1, 1]
+    assert c.fork(_ints([0, 0]), _ints([1, 2])).tolist() == [1, 1]
+    c.truncate(_ints([-1, 36, 30]))                   # 40, 36 and 30 tokens; the last page is shared by two of them
+    rows = torch.randn(30, KV, hd, device="cuda").to(src)
+    q = torch.randn(30, H, hd, device="cuda").to(src)
+    rs = _ints([0, 0, 7, 14])                         # tokens 36 - 42 and 30 - 36
+    assert c.reserve(rs).tolist() == [1, 0, 0]
+    k0, v0, meta = c.k.clone(), c.v.clone(), c.meta.clone()
+    rope = Rope(hd)
+    got = [c.append(layer, rows, -rows, rs, 7, q=q, rope=rope) for layer in range(2)]
+    assert torch.equal(c.meta, meta)
+    p1, p2 = int(c.table[0, 1]), int(c.table[0, 2])
+    want = k0.clone(), v0.clone()
+    pos = torch.arange(36, 43, dtype=torch.int32, device="cuda")
+    turned = rope.apply(rows[:7].contiguous(), pos).to(dtype) if src == dtype else None
+    for layer in range(2):
+        assert torch.equal(c.k[layer, p1], k0[layer, p1]) and torch.equal(c.v[layer, p1], v0[layer, p1])
+        assert torch.equal(c.k[layer, p2, :, :8], k0[layer, p2, :, :8])     # tokens 32 - 39 of the first sequence
+        assert torch.equal(c.v[layer, p2, :, :8], v0[layer, p2, :, :8])
+        assert torch.equal(c.v[layer, p2, :, 8:11], -rows[4:7].to(dtype).transpose(0, 1))   # its tokens 40 - 42
+        if turned is not None:
+            assert torch.equal(c.k[layer, p2, :, 8:11], turned[4:7].transpose(0, 1))
+        assert torch.equal(c.k[layer, p2, :, 11:], want[0][layer, p2, :, 11:])
+    both = torch.cat([pos, torch.arange(30, 37, dtype=torch.int32, device="cuda")])
+    w, scale = ref.frequencies(hd)
+    turn = ref.rotate(q[:14].cpu(), both.cpu(), w, scale, False)
+    for x in got:
+        _within(x[:14], turn, ref.half_step(dtype) * turn.abs() + 2.0 ** -19 * 4 + ref.half_subnormal(dtype), "queries")
