@@ -59,6 +59,14 @@ def _rows(t: torch.Tensor, name: str, heads: int | None, head_dim: int, device: 
     return n, h, row if n > 1 else h * head_dim           # a single row has any stride
 
 
+def _mask_words(mask: torch.Tensor, rows: int) -> int:
+    """Words per row of a mask; one of no words would have no address, which stands for
+    no mask."""
+    if mask.dim() != 2 or mask.shape[0] != rows or (rows and mask.shape[1] == 0):
+        raise ValueError(f"mask must be int32 [{rows}, words] with at least one word")
+    return mask.shape[1]
+
+
 class Rope:
     """Frequencies of rotary positions; a plain host structure, no device memory.
 
@@ -276,9 +284,7 @@ class PagedCache:
             raise ValueError("q and out must have the cache's type and the same rows")
         words = 0
         if mask is not None:
-            if mask.dim() != 2 or mask.shape[0] != T:
-                raise ValueError("mask must be int32 [rows, words]")
-            words = mask.shape[1]
+            words = _mask_words(mask, T)
         bits = _ints(mask, "mask", None, device)
         if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, heads) or not lse.is_contiguous()
                                 or lse.device != device):

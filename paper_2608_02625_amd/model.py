@@ -12,7 +12,7 @@ import torch
 
 from . import _lib
 from ._lib import DlmConfig, DlmStats, check
-from .cache import PagedCache, _ints
+from .cache import PagedCache, _ints, _mask_words
 
 CONFIG_FIELDS = [f for f, _ in DlmConfig._fields_]
 
@@ -262,9 +262,7 @@ class Refiner:
             (mask, "mask", None), (n_invalid, "n_invalid", 1))]
         words = 0
         if mask is not None:
-            if mask.dim() != 2 or mask.shape[0] != T:
-                raise ValueError("mask must be int32 [rows, words]")
-            words = mask.shape[1]
+            words = _mask_words(mask, T)
         key = ("cache", T, min(int(max_rows), T), cache.n_seqs)
         ws = self._ws.get(key)
         if ws is None:

@@ -278,3 +278,22 @@ def test_append_overwrites_no_token_of_another_sequence(dtype, src):
     turn = ref.rotate(q[:14].cpu(), both.cpu(), w, scale, False)
     for x in got:
         _within(x[:14], turn, ref.half_step(dtype) * turn.abs() + 2.0 ** -19 * 4 + ref.half_subnormal(dtype), "queries")
+
+
+# ------------------------------------------------------------------ masks
+
+def test_a_mask_of_no_words_is_refused():
+    """It shows a row nothing, and is not the missing mask that shows it everything."""
+    c, _ = _cache([40], 16, 2, 64, BF)
+    q = torch.randn(4, 4, 64, device="cuda").to(BF)
+    for rows in (1, 4):
+        with pytest.raises(ValueError, match="mask"):
+            c.attend(0, q[:rows], _ints([0, rows]), rows, mask=torch.empty(rows, 0, dtype=torch.int32, device="cuda"))
+    from paper_2608_02625_amd import Refiner
+    from workloads import WORKLOADS
+    w = WORKLOADS["tiny"]
+    model = Refiner(w.model.as_dict(), w.weight_seed)
+    pages = model.cache(4, 16, 1, 4)
+    tokens = torch.zeros(3, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="mask"):
+        model.cache_step(pages, tokens, _ints([0, 3]), 3, mask=torch.empty(3, 0, dtype=torch.int32, device="cuda"))
