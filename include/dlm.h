@@ -570,7 +570,10 @@ dlm_status dlm_cache_compact(const dlm_cache* cache, int32_t* d_n_used, void* d_
  * mask_words, max_keys as above; a window with d_mask NULL is a block that sees
  * itself and everything before it, so a prompt, then blocks, is block-AR
  * drafting's visibility.  The cache has the model's layers and key heads, and
- * dtype DLM_BF16.  Rows that no window covers are computed without meaning.
+ * dtype DLM_BF16.  At most 65536 rows, and of a width whose activations stay below
+ * 2 GiB (total_rows * d_model * 2 bytes, and with n_heads * head_dim); no rows are
+ * a pass with nothing to do, without a workspace (whose size is then 0).  Rows that
+ * no window covers are computed without meaning.
  * d_top1 int32, d_conf float, d_max_logit float [total_rows] as
  * dlm_draft_step, each may be NULL.  d_n_invalid int32 (may be NULL): token ids
  * outside [0, vocab); they are read as a valid one.

@@ -77,6 +77,13 @@ dlm_status check_rope(const dlm_rope* r) {
 
 dlm_status dlm_internal_check_cache(const dlm_cache* cache) { return check_cache(cache); }
 
+std::string dlm_internal_check_windows(const dlm_cache& cache, int n_heads, int64_t rows) {
+    if (rows * (n_heads / cache.n_kv_heads) > (1 << 28)) return "max_rows times query heads per key head too large";
+    if (cache.n_seqs * (int64_t)std::max(n_heads, cache.n_kv_heads) * rows > ((int64_t)1 << 33))
+        return "n_seqs * n_heads * max_rows must be at most 2^33";
+    return "";
+}
+
 extern "C" {
 
 dlm_status dlm_rope_init(const dlm_rope_spec* s, dlm_rope* out) {
@@ -255,11 +262,10 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
             return fail(DLM_ERR_INVALID_ARG, "mask must be 4-byte aligned and hold max_rows bits per row");
         if (d_lse && !aligned(d_lse, 4)) return fail(DLM_ERR_INVALID_ARG, "lse must be 4-byte aligned");
         const int group = n_heads / cache->n_kv_heads;
-        if ((int64_t)rows * group > (1 << 28)) return fail(DLM_ERR_INVALID_ARG, "max_rows times query heads per key head too large");
+        const std::string bad = dlm_internal_check_windows(*cache, n_heads, rows);
+        if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
         TRY(check_workspace(d_workspace, workspace_bytes,
                             attend_workspace_bytes(cache->n_seqs, cache->n_kv_heads, cache->head_dim, total_rows, rows, group)));
-        if ((int64_t)cache->n_seqs * n_heads * rows > ((int64_t)1 << 33))
-            return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
         const int keys = (int)std::min<int64_t>(max_keys ? max_keys : capacity(*cache), capacity(*cache));
         return launched(launch_attend(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows, rows, keys, n_heads,
                                       d_q, q_stride, d_mask, d_mask ? mask_words : 0,

@@ -884,14 +884,18 @@ StepPlan plan_step(const dlm_config& c, const dlm_cache& cache, int T, int max_r
     return p;
 }
 
+// T may be 0: a pass with nothing to do.
 std::string check_step(const dlm_config& c, const dlm_cache* cache, int T, int max_rows) {
     if (!cache) return "cache is NULL";
     if (cache->dtype != DLM_BF16) return "the cache's dtype must be DLM_BF16";
     if (cache->n_layers != c.n_layers || cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim)
         return "the cache's layers, key heads and head_dim must be the model's";
-    if (max_rows < 1) return "max_rows must be >= 1";
+    if (max_rows < 0) return "max_rows must be >= 0";
+    if (T == 0) return "";
+    if (max_rows == 0) return "max_rows is 0 but there are rows";
     std::string e = check_shape(1, 0, T);
     if (e.empty()) e = check_offsets(c, T);
+    if (e.empty()) e = dlm_internal_check_windows(*cache, c.n_heads, std::min(max_rows, T));
     return e;
 }
 
@@ -1362,7 +1366,7 @@ dlm_status dlm_cascade(dlm_model* drafter, dlm_model* refiner, int32_t batch, in
 size_t dlm_cache_step_workspace_bytes(const dlm_config* cfg, const dlm_cache* cache, int32_t total_rows,
                                       int32_t max_rows) {
     try {
-        if (!validate(cfg).empty() || !check_step(*cfg, cache, total_rows, max_rows).empty()) return 0;
+        if (!validate(cfg).empty() || total_rows == 0 || !check_step(*cfg, cache, total_rows, max_rows).empty()) return 0;
         if (dlm_cache_workspace_bytes(cache, total_rows, max_rows, cfg->n_heads) == 0) return 0;
         return plan_step(*cfg, *cache, total_rows, std::min(max_rows, total_rows)).total;
     } catch (...) {
@@ -1381,8 +1385,13 @@ dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d
         const std::string bad = check_step(c, cache, total_rows, max_rows);
         if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
         TRY(dlm_internal_check_cache(cache));
-        if (!d_row_start || !d_tokens) return fail(DLM_ERR_INVALID_ARG, "row_start or tokens is NULL");
         if (max_keys < 0) return fail(DLM_ERR_INVALID_ARG, "max_keys must be >= 0");
+        if (total_rows == 0) {
+            if (d_n_invalid) launch_zero_i32(d_n_invalid, 1, (hipStream_t)hip_stream);
+            HIP_TRY(hipGetLastError());
+            return DLM_OK;
+        }
+        if (!d_row_start || !d_tokens) return fail(DLM_ERR_INVALID_ARG, "row_start or tokens is NULL");
         const int rows = std::min(max_rows, total_rows);
         if (d_mask && (int64_t)mask_words * 32 < rows) return fail(DLM_ERR_INVALID_ARG, "mask must hold max_rows bits per row");
         const StepPlan plan = plan_step(c, *cache, total_rows, rows);

@@ -14,3 +14,5 @@ dlm_status dlm_internal_fail(dlm_status s, const std::string& msg);
 dlm_status dlm_internal_caught() noexcept;
 // Shape, buffers and alignment of a caller's cache.
 dlm_status dlm_internal_check_cache(const dlm_cache* cache);
+// Sizes of windows of up to `rows` rows whose heads a call takes; "" if it may.
+std::string dlm_internal_check_windows(const dlm_cache& cache, int n_heads, int64_t rows);

@@ -251,8 +251,9 @@ class Refiner:
         reserved places take their keys and values.  row_start int32 [n_seqs + 1];
         positions int32 [rows] (default: the tokens' places); mask int32 [rows, words]:
         the window rows that a row sees (default: all of its window's).  Returns (top-1
-        int32, confidence float, max logit float), each [rows].  Calls of one model share
-        workspaces (kept, so that captured graphs stay valid): order them on one stream."""
+        int32, confidence float, max logit float), each [rows]; at most 65536 rows, none is
+        a pass with nothing to do.  Calls of one model share workspaces (kept, so that
+        captured graphs stay valid): order them on one stream."""
         T = tokens.numel()
         if cache.device.index != (self.device.index if self.device.index is not None else torch.cuda.current_device()):
             raise ValueError("the cache and the model must be on one GPU")
@@ -265,7 +266,9 @@ class Refiner:
             words = _mask_words(mask, T)
         key = ("cache", T, min(int(max_rows), T), cache.n_seqs)
         ws = self._ws.get(key)
-        if ws is None:
+        if ws is None and T == 0 <= int(max_rows):
+            ws = torch.empty(0, dtype=torch.uint8, device=device)
+        elif ws is None:
             n = self.lib.dlm_cache_step_workspace_bytes(ctypes.byref(self.cfg), ctypes.byref(cache.c), T, int(max_rows))
             if n == 0:
                 raise ValueError(f"invalid window shape ({T} rows, {max_rows} at most) or a cache of another model")

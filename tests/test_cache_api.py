@@ -282,3 +282,17 @@ def test_plain_reference_keeps_its_books():
         assert [names_of.count(p) for p in range(12)] == c.ref
         serial += 1
     assert c.fork([0, 1], [2, 2]) == [0, 0] and c.fork([0, 2], [2, 3]) == [0, 1] and c.fork([1], [1]) == [0]
+
+
+def test_step_limits():
+    """What the cache's own calls refuse by size, a model's step refuses before anything
+    is launched (its workspace has no size)."""
+    L, lib = _lib()
+    from paper_2608_02625_amd.model import make_config
+    from workloads import MODELS
+    wide = ctypes.byref(make_config(MODELS["tiny"].replace(n_heads=192, n_kv_heads=4)))
+    for seqs, rows, most, fits in ((1024, 65535, 65535, False), (1024, 65535, 40000, True), (512, 65535, 65535, True),
+                                   (1024, 65536, 1, True), (1024, 65537, 1, False)):
+        c = _cache(L, n_seqs=seqs)
+        n = lib.dlm_cache_step_workspace_bytes(wide, ctypes.byref(c), rows, most)
+        assert (n > 0) == fits, (seqs, rows, most, n)

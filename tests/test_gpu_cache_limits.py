@@ -297,3 +297,35 @@ def test_a_mask_of_no_words_is_refused():
     tokens = torch.zeros(3, dtype=torch.int32, device="cuda")
     with pytest.raises(ValueError, match="mask"):
         model.cache_step(pages, tokens, _ints([0, 3]), 3, mask=torch.empty(3, 0, dtype=torch.int32, device="cuda"))
+
+
+# ------------------------------------------------------------------ a model's step
+
+def test_a_step_of_no_rows():
+    """Every sequence sits the pass out: nothing is computed, no token is invalid, and
+    the same call may be captured."""
+    from paper_2608_02625_amd import Refiner
+    from workloads import WORKLOADS
+    w = WORKLOADS["tiny"]
+    model = Refiner(w.model.as_dict(), w.weight_seed)
+    c = model.cache(4, 16, 2, 4)
+    before = c.meta.clone()
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    rs, bad = _ints([0, 0, 0]), _ints([7])
+    for kw in (dict(), dict(positions=none), dict(mask=none.view(0, 1)), dict(mask=none.view(0, 0)), dict(max_keys=5)):
+        for max_rows in (0, 1, 9):
+            bad.fill_(7)
+            out = model.cache_step(c, none, rs, max_rows, n_invalid=bad, **kw)
+            assert bad.item() == 0 and [x.numel() for x in out] == [0, 0, 0]
+    assert c.attend(0, torch.empty(0, 4, c.k.shape[-1], dtype=BF, device="cuda"), rs, 0, mask=none.view(0, 0)).numel() == 0
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model.cache_step(c, none, rs, 0, n_invalid=bad)
+    for _ in range(3):
+        bad.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bad.item() == 0
+    assert torch.equal(c.meta, before)
+    with pytest.raises(ValueError):
+        model.cache_step(c, none, rs, -1)
