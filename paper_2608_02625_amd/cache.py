@@ -99,7 +99,15 @@ class Rope:
               transpose: bool = False) -> torch.Tensor:
         """x [rows, heads, head_dim] (any row and head strides) rotated to `positions`
         (int32 [rows]); into `out` (may be x).  transpose: the gradient with respect
-        to x, given the gradient x of a rotation's result."""
+        to x, given the gradient x of a rotation's result; autograd takes it by itself
+        where x requires a gradient (`out` cannot be part of that)."""
+        if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
+            if out is not None:
+                raise ValueError("a result in `out` carries no gradient: detach x and out, or leave out away")
+            return _Rotation.apply(x, positions, self, transpose)
+        return self._apply(x, positions, out, transpose)
+
+    def _apply(self, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None, transpose: bool) -> torch.Tensor:
         shape, kind, device = x.shape, _DTYPES.get(x.dtype), x.device
         if len(shape) != 3 or shape[2] != self._head_dim or kind is None or device.type != "cuda":
             raise ValueError(f"x must be a bfloat16, float16 or float32 device tensor [rows, heads, {self._head_dim}]")
@@ -116,6 +124,22 @@ class Rope:
         return out
 
 
+class _Rotation(torch.autograd.Function):
+    """A rotation is linear in x: its gradient is the rotation back, times the scale."""
+
+    @staticmethod
+    def forward(ctx, x, positions, rope, transpose):
+        ctx.save_for_backward(positions)
+        ctx.rope, ctx.transpose = rope, transpose
+        return rope._apply(x, positions, None, transpose)
+
+    @staticmethod
+    def backward(ctx, grad):
+        if grad.stride(-1) != 1:                      # a head's values lie next to each other
+            grad = grad.clone(memory_format=torch.contiguous_format)
+        return ctx.rope.apply(grad, ctx.saved_tensors[0], transpose=not ctx.transpose), None, None, None
+
+
 class PagedCache:
     """A paged key/value cache: n_pages pages of page_len tokens in n_layers layers,
     shared by n_seqs sequences of up to max_pages pages.
@@ -124,7 +148,8 @@ class PagedCache:
     unless given.  meta (int32) holds ref [n_pages], len [n_seqs] and table
     [n_seqs, max_pages], which are views of it.  Windows of rows are packed:
     row_start int32 [n_seqs + 1] on the device.  Calls on one cache share its
-    workspaces: order them on one stream.
+    workspaces: order them on one stream.  It serves: no gradient passes through
+    append and attend.
     """
 
     def __init__(self, n_layers: int, n_pages: int, page_len: int, n_kv_heads: int, head_dim: int, n_seqs: int,

@@ -329,3 +329,98 @@ def test_a_step_of_no_rows():
     assert torch.equal(c.meta, before)
     with pytest.raises(ValueError):
         model.cache_step(c, none, rs, -1)
+
+
+# ------------------------------------------------------------------ gradients of a rotation
+
+@pytest.mark.parametrize("dtype", [BF, HF, torch.float32])
+@pytest.mark.parametrize("interleaved,transpose", [(False, False), (True, False), (False, True)])
+def test_rotation_under_autograd(dtype, interleaved, transpose):
+    """The gradient is the formula's (the inner product with a fixed result), for a leaf, a
+    broadcast row, a slice and a gradient of any layout; a second derivative is zero, and
+    the gradient's own gradient is the rotation."""
+    from paper_2608_02625_amd import Rope
+    rows, heads, hd, rot = 7, 3, 64, 48
+    g = torch.Generator().manual_seed(rot)
+    rope = Rope(hd, rot, 10000.0, interleaved, "yarn", 4.0, 1024)
+    pos = torch.tensor([0, 1, 5, 100, 4096, 131071, 7], dtype=torch.int32)
+    w, scale = ref.frequencies(rot, 10000.0, "yarn", 4.0, 1024)
+    up = torch.randn(rows, heads, hd, generator=g).to(dtype)
+    h = ref.half_step(dtype)
+    want = ref.rotate(up, pos, w, scale, interleaved, not transpose)
+    # 2^-21 of the pair's magnitudes (below 16), times the scale, as in test_gpu_cache.py
+    tol = h * want.abs() + ref.half_subnormal(dtype) + 2.0 ** -17 * scale
+    leaf = torch.randn(rows, heads, hd, generator=g).to(dtype).cuda().requires_grad_()
+    y = rope.apply(leaf, pos.cuda(), transpose=transpose)
+    assert y.requires_grad and torch.equal(y.detach(), rope.apply(leaf.detach(), pos.cuda(), transpose=transpose))
+    grads = {"plain": up.cuda(), "turned": up.cuda().permute(2, 0, 1).contiguous().permute(1, 2, 0)}
+    for what, grad in grads.items():
+        (got,) = torch.autograd.grad(y, leaf, grad, retain_graph=True)
+        _within(got, want, tol, f"gradient {dtype} {what}")
+    flat = torch.ones((), dtype=dtype, device="cuda").expand(rows, heads, hd)          # as from a sum
+    (got,) = torch.autograd.grad(y, leaf, flat)
+    ones = ref.rotate(torch.ones(rows, heads, hd), pos, w, scale, interleaved, not transpose)
+    _within(got, ones, h * ones.abs() + ref.half_subnormal(dtype) + 2.0 ** -17 * scale, "gradient of a sum")
+    one = torch.randn(1, heads, hd, generator=g).to(dtype).cuda().requires_grad_()      # one row for all positions
+    (got,) = torch.autograd.grad(rope.apply(one.expand(rows, heads, hd), pos.cuda(), transpose=transpose), one, up.cuda())
+    # torch adds the rows: seven roundings of sums below 32
+    _within(got, want.sum(0, keepdim=True), tol.sum(0, keepdim=True) + 7 * 32 * h, "gradient of a shared row")
+    wide = torch.randn(rows, heads * hd + 16, generator=g).to(dtype).cuda().requires_grad_()
+    part = wide[:, 8:8 + heads * hd].view(rows, heads, hd)
+    (got,) = torch.autograd.grad(rope.apply(part, pos.cuda(), transpose=transpose), wide, up.cuda())
+    _within(got[:, 8:8 + heads * hd].view(rows, heads, hd), want, tol, "gradient of a slice")
+    assert not got[:, :8].any() and not got[:, 8 + heads * hd:].any()
+    again = up.cuda().requires_grad_()
+    (first,) = torch.autograd.grad(rope.apply(leaf, pos.cuda(), transpose=transpose), leaf, again, create_graph=True)
+    (got,) = torch.autograd.grad(first, again, leaf.detach())
+    assert torch.equal(got, rope.apply(leaf.detach(), pos.cuda(), transpose=transpose))
+
+
+def test_rotation_gradients_where_they_cannot_be():
+    """`out` takes no part in autograd; without a graph nothing changes."""
+    from paper_2608_02625_amd import Rope
+    rope, pos = Rope(64), _ints([3, 4])
+    leaf = torch.randn(2, 2, 64, device="cuda", requires_grad=True)
+    plain = leaf.detach().clone()
+    for x, out in ((leaf, torch.empty_like(plain)), (plain, (plain * 1).requires_grad_()), (leaf * 1, plain)):
+        with pytest.raises(ValueError, match="out"):
+            rope.apply(x, pos, out=out)
+    with torch.no_grad():
+        y = rope.apply(leaf, pos)
+        assert not y.requires_grad and torch.equal(rope.apply(leaf, pos, out=torch.empty_like(plain)), y)
+    assert not rope.apply(plain, pos).requires_grad
+    for bad in (leaf[0], leaf.double()):
+        with pytest.raises(ValueError):
+            rope.apply(bad, pos)
+    empty = torch.empty(0, 2, 64, device="cuda", requires_grad=True)
+    rope.apply(empty, _ints([])).sum().backward()
+    assert empty.grad.shape == (0, 2, 64)
+
+
+def test_rotation_gradients_on_a_stream_and_in_a_graph():
+    """The backward pass runs on the stream of the forward; captured, it replays to the
+    eager gradient, with eager work in between."""
+    from paper_2608_02625_amd import Rope
+    rope, pos = Rope(128), torch.arange(33, dtype=torch.int32, device="cuda")
+    x = torch.randn(33, 4, 128, device="cuda").to(BF)
+    up = torch.randn(33, 4, 128, device="cuda").to(BF)
+    want = rope.apply(up, pos, transpose=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        leaf = x.clone().requires_grad_()
+        (got,) = torch.autograd.grad(rope.apply(leaf, pos), leaf, up)
+    side.synchronize()
+    assert torch.equal(got, want)
+    del leaf, got
+    leaf = x.clone().requires_grad_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        (got,) = torch.autograd.grad(rope.apply(leaf, pos), leaf, up)
+    for _ in range(3):
+        got.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert torch.equal(rope.apply(up, pos, transpose=True), want)
+        torch.cuda.synchronize()
