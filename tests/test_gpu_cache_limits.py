@@ -12,7 +12,7 @@ import torch
 
 from tests import cache_ref as ref
 from tests.gpu_util import need_gpu
-from tests.test_gpu_cache import BF, HF, _cache, _ints, _within
+from tests.test_gpu_cache import BF, HF, _cache, _fill, _ints, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -424,3 +424,45 @@ def test_rotation_gradients_on_a_stream_and_in_a_graph():
         assert torch.equal(got, want)
         assert torch.equal(rope.apply(up, pos, transpose=True), want)
         torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ large scores
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens,rows,H,KV,hd", [([300, 50], [1, 1], 4, 2, 64), ([300, 50], [40, 40], 4, 2, 64),
+                                               ([9000], [1], 4, 4, 64), ([7000, 40], [13, 5], 8, 2, 128),
+                                               ([5000], [90], 4, 2, 64)])
+def test_scores_of_thousands(dtype, lens, rows, H, KV, hd):
+    """Both signs, whole and split over keys, held to the error of the scores at hand: a
+    float32 product of hd values is summed by matrix instructions of 16 in a tree and one
+    chain of hd / 16, so a value takes part in at most 4 + hd / 16 additions and the score
+    is within (4 + hd / 16) 2^-24 of the sum of absolute products; the exponent's two
+    roundings add 2^-23 of the row's maximum.  Probabilities and their sum are off by that
+    much, relative, each; the log of the sum is, absolute."""
+    g = torch.Generator().manual_seed(hd + rows[0])
+    page = 16
+    c, table = _cache([n + r for n, r in zip(lens, rows)], page, KV, hd, dtype, seed=2)
+    ks, vs = _fill(c, table, lens, rows, KV, hd, dtype, g)
+    c.len.copy_(_ints(lens))
+    T = sum(rows)
+    q = (300 * torch.randn(T, H, hd, generator=g)).to(dtype)
+    sees = [torch.ones(n, n, dtype=torch.bool).tril() for n in rows]
+    mask = ref.pack_mask(sees, (max(rows) + 31) // 32).cuda()
+    lse = torch.empty(T, H, device="cuda")
+    starts = [sum(rows[:b]) for b in range(len(rows) + 1)]
+    out = c.attend(0, q.cuda(), _ints(starts), max(rows), mask=mask, scale=1.0, lse=lse, max_keys=max(lens) + max(rows))
+    h = ref.half_step(dtype)
+    for b, n in enumerate(rows):
+        part = slice(starts[b], starts[b] + n)
+        see = torch.cat([torch.ones(n, lens[b], dtype=torch.bool), sees[b]], 1)
+        want, mag, want_lse = ref.attend(q[part], ks[b], vs[b], see, 1.0)
+        keys = ks[b].double().repeat_interleave(H // KV, 1)
+        total = torch.einsum("nhd,mhd->nhm", q[part].double().abs(), keys.abs()).masked_fill(~see[:, None], 0).amax(-1)
+        e = (4 + hd / 16) * 2.0 ** -24 * total + 2.0 ** -23 * want_lse.abs() + 1e-5
+        # At most 12 2^-24 of 128 * 300 * 0.64 * 1.6 = 39000 (the largest of thousands of sums
+        # lies 1.6 times over their mean) and 2^-23 of 6000: a wrong factor between tiles or
+        # parts, 2 at least, does not fit in.
+        assert e.max() < 0.04
+        what = f"scores of thousands {dtype} {rows[b]} rows behind {lens[b]}"
+        _within(out[part], want, h * want.abs() + (h + 2 * e[..., None]) * mag + ref.half_subnormal(dtype), what)
+        _within(lse[part], want_lse, e, what + " lse")

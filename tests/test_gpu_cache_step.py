@@ -249,3 +249,30 @@ def test_steps_of_many_sizes_share_workspaces_and_refuse_other_devices():
                dict(mask=host.view(4, 1)), dict(n_invalid=host[:1])):
         with pytest.raises(ValueError):
             R.cache_step(**dict(dict(cache=c, tokens=toks[:4], row_start=rs, max_rows=2), **kw))
+
+
+def test_top1_of_the_cache_step_and_the_drafting_step(model):
+    """The same block both ways: equal top-1, and the oracle's, where its logit margin
+    exceeds the exemption."""
+    from oracle.draft import block_key_limit
+    torch = _torch()
+    shape, R, W = model
+    rng = np.random.default_rng(9)
+    P, blk = 48, 16
+    for seed in range(3):
+        toks = rng.integers(0, shape.vocab - 1, size=(1, P + blk)).astype(np.int32)
+        toks[0, P + 1 + seed::2] = shape.mask_id
+        c = R.cache(8, 16, 1, 8)
+        for a, n in ((0, P), (P, blk)):
+            rs = _i32([0, n])
+            assert c.reserve(rs).tolist() == [1]
+            top1, conf, mx = R.cache_step(c, _i32(toks[0, a:a + n]), rs, n)
+            assert c.commit(rs).tolist() == [1]
+        t1 = torch.empty(1, blk, dtype=torch.int32, device="cuda")
+        R.draft_step(_i32(toks), P, blk, 0, 4, 2.0, top1=t1)
+        want = _oracle_rows(W, toks[0], None, block_key_limit(P, P + blk, blk), np.arange(P, P + blk))
+        _check(f"block {seed}", (top1, conf, mx), want, shape.lm_head_scale)
+        sure = (want["gap"] > MARGIN) & (want["margin"] > MARGIN * shape.lm_head_scale)
+        log(f"[draft step {seed}] {sure.sum()} of {blk} top-1 compared")
+        assert sure.any()
+        assert np.array_equal(t1[0].cpu().numpy()[sure], top1.cpu().numpy()[sure])
