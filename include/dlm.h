@@ -519,7 +519,8 @@ dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t
  * Rows of d_o behind the last window keep their values.  Scores, softmax and
  * sums are float32, probabilities are rounded to the cache's dtype for the
  * product with V (DLM_F16: to half a step where they are above 2^-25 of the row's
- * largest, within 2^-36 of it below).
+ * largest, within 2^-36 of it below); with up to 32 query heads of a window's rows
+ * per key head the product takes twice as many of their bits.
  */
 dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
                             int32_t max_rows, int32_t max_keys, int32_t n_heads, const void* d_q, int64_t q_stride,

@@ -19,8 +19,13 @@
 // read in the order that the scores' accumulator has them.  Probabilities are
 // rounded to the cache's type for the product (the matrix instruction takes
 // nothing wider at this rate; half a step, 2^-8 or 2^-11 of each, to either side: see
-// kShift for float16's range), sums add the unrounded ones.  The running maximum moves
-// only when a tile raises it by more than 2^8 (float16: 2^4) in the exp2 domain.
+// kShift for float16's range), sums add the unrounded ones.  Up to 32 packed rows a
+// second product adds what the rounding left over: the kernel waits for bytes there
+// (64 sequences 81.2 -> 81.7 us, 641 keys of one 7.7 -> 8.2), and the error in bf16 goes
+// from 0.0022 to 0.0017 of the result's size, the result's own rounding.  Above that it
+// would cost 7 % (13 rows of 4 heads per key head, 97.8 -> 105.0), 6 % (trees, 24.0 ->
+// 25.5) and 25 % (prompts, 86.8 -> 108.7).  The running maximum moves only when a tile
+// raises it by more than 2^8 (float16: 2^4) in the exp2 domain.
 //
 // Masks.  Only tiles that meet the window, the last token or a missing page are
 // masked, by a 32-bit word per row.  A product with 0 does not hide an infinity
@@ -408,9 +413,11 @@ struct RowTile {
         for (int e = 0; e < 16; ++e)
             if (!((see >> (8 * (e >> 2) + (e & 3))) & 1)) st[e] = -INFINITY;
     }
-    // Scores to probabilities (times 2^kShift), the B operand of O^T = V^T P^T.
+    // Scores to probabilities (times 2^kShift), the B operand of O^T = V^T P^T: rounded,
+    // and, of two TERMS, what the rounding left over.
     // `lim`: how far, in units of the scores, a maximum may lie above m.
-    __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, float lim, s16x8 (&pf)[2]) {
+    template <int TERMS>
+    __device__ __forceinline__ void softmax(const f32x16& st, float scale_log2, float lim, s16x8 (&pf)[TERMS][2]) {
         float mt = st[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mt = fmaxf(mt, st[e]);
@@ -431,15 +438,18 @@ struct RowTile {
         float sum = 0.f;
 #pragma unroll
         for (int s2 = 0; s2 < 2; ++s2) {
-            u32x4 w;
+            u32x4 w, rest;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p0 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i], scale_log2, bias));
                 const float p1 = __builtin_amdgcn_exp2f(fmaf(st[8 * s2 + 2 * i + 1], scale_log2, bias));
                 sum += p0 + p1;
                 w[i] = pack2<F16>(p0, p1);
+                if constexpr (TERMS == 2)
+                    rest[i] = pack2<F16>(p0 - widen<F16>(w[i] & 0xffffu), p1 - widen<F16>(w[i] >> 16));
             }
-            pf[s2] = __builtin_bit_cast(s16x8, w);
+            pf[0][s2] = __builtin_bit_cast(s16x8, w);
+            if constexpr (TERMS == 2) pf[1][s2] = __builtin_bit_cast(s16x8, rest);
         }
         l += sum;
     }
@@ -477,8 +487,8 @@ __device__ __forceinline__ void read_values(s16x8 (&vf)[2][2], lds_ptr_t lds, in
 // row does not see all of it, so that infinities and NaN are looked for and, if there
 // are any (the result), left out.  One path with scalar branches: two copies of the
 // products would hold the accumulators twice.
-template <bool F16, int HD, int RT>
-__device__ __forceinline__ bool add_values(RowTile<F16, HD> (&rt)[RT], const s16x8 (&pf)[RT][2], s16x8 (&vf)[2][2],
+template <bool F16, int HD, int RT, int TERMS>
+__device__ __forceinline__ bool add_values(RowTile<F16, HD> (&rt)[RT], const s16x8 (&pf)[RT][TERMS][2], s16x8 (&vf)[2][2],
                                            lds_ptr_t lds, int v, int lane, int base, bool masked) {
     using D = Dims<HD>;
     const int g = lane >> 5, j = lane & 31;
@@ -516,11 +526,12 @@ __device__ __forceinline__ bool add_values(RowTile<F16, HD> (&rt)[RT], const s16
                 }
         }
 #pragma unroll
-        for (int s2 = 0; s2 < 2; ++s2)
+        for (int x = 0; x < 2 * TERMS; ++x)               // 16 keys, then the terms
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) rt[r].o[n2 + n] = mfma<F16>(vf[n][s2], pf[r][s2], rt[r].o[n2 + n]);
+                for (int r = 0; r < RT; ++r)
+                    rt[r].o[n2 + n] = mfma<F16>(vf[n][x / TERMS], pf[r][x % TERMS][x / TERMS], rt[r].o[n2 + n]);
     }
     return wild != 0;
 }
@@ -727,9 +738,9 @@ attend_many_kernel(const AttnArgs a) {
             sched_fence();
             if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, lo, hi, k0, (uint32_t)gone), g);
             if (a.mask) words(tile_at(i + 1));
-            s16x8 pf[1][2];
+            s16x8 pf[1][1][2];
             rt[0].softmax(st, a.scale_log2, a.lim, pf[0]);
-            wild |= add_values<F16, HD, 1>(rt, pf, vf, lds, sb + K_TILE, lane, vfrag, masked);
+            wild |= add_values<F16, HD, 1, 1>(rt, pf, vf, lds, sb + K_TILE, lane, vfrag, masked);
         }
     }
 
@@ -810,15 +821,15 @@ attend_many_kernel(const AttnArgs a) {
 // KB (66 with the join's sums) leave room for a second one, which works while the first
 // starts or ends; 64 rows hold twice the accumulators (420 VGPRs, one wave per SIMD):
 // two stages.  All of the 128 KB per CU are in flight but for the tiles at work.
-// 64 sequences of 256 to 16384 tokens, a row each, 16 heads of 128 on 4 (472 MB): 81 us,
+// 64 sequences of 256 to 16384 tokens, a row each, 16 heads of 128 on 4 (472 MB): 82 us,
 // 5.8 TB/s; 13 rows of 32 heads on 8 behind 131072 tokens (537 MB): 92 us, 5.8 TB/s; 641
-// keys of 64: 7.5 us, of which 5.3 are there for a single key (a launch, four loads that
+// keys of 64: 8.2 us, of which 5.3 are there for a single key (a launch, four loads that
 // need each other, the end).
 template <bool F16, int HD, int RT, int S>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 && RT == 1 ? 4 : RT == 1 ? 2 : 1))) void
 attend_few_kernel(const AttnArgs a) {
     using D = Dims<HD>;
-    constexpr int WAVES = 4;
+    constexpr int WAVES = 4, TERMS = RT == 1 ? 2 : 1;
     constexpr int COPIES = D::HALF / 1024;                // 1 KB copies of a V tile
     constexpr int C4 = HD / 4;
     constexpr int RING = 2 * S * D::HALF;                 // a wave's stages: S tiles of K, then of V
@@ -941,7 +952,7 @@ attend_few_kernel(const AttnArgs a) {
             issue(keys.k, k_off, tile_at(i + S), ks_at, next);
             const uint32_t gone = keys.missing(now);
             const bool masked = k0 + kTile > clear || gone;
-            s16x8 pf[RT][2];
+            s16x8 pf[RT][TERMS][2];
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
                 if (__builtin_expect(masked, 0)) rt[x].hide(st[x], seen_keys(a, u.s, lo[x], hi[x], k0, gone), g);
@@ -951,7 +962,7 @@ attend_few_kernel(const AttnArgs a) {
             s16x8 vf[2][2];
             read_values<HD>(vf, lds, vs_at + vfrag, 0);
             sched_fence();
-            wild |= add_values<F16, HD, RT>(rt, pf, vf, lds, vs_at, lane, vfrag, masked);
+            wild |= add_values<F16, HD, RT, TERMS>(rt, pf, vf, lds, vs_at, lane, vfrag, masked);
             reads_done();
             issue(keys.v, v_off, tile_at(i + S), vs_at, next);
             now = S == 1 ? next : keys.entries(tile_at(i + 1));

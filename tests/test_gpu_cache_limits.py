@@ -466,3 +466,32 @@ def test_scores_of_thousands(dtype, lens, rows, H, KV, hd):
         what = f"scores of thousands {dtype} {rows[b]} rows behind {lens[b]}"
         _within(out[part], want, h * want.abs() + (h + 2 * e[..., None]) * mag + ref.half_subnormal(dtype), what)
         _within(lse[part], want_lse, e, what + " lse")
+
+
+# ------------------------------------------------------------------ few rows
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("H,KV,hd,page,lens,rows", [
+    (16, 4, 128, 64, [3000, 17, 700], [1, 1, 1]), (16, 4, 64, 16, [900], [8]), (4, 4, 64, 32, [5000, 5], [32, 3]),
+    (32, 1, 128, 128, [2000], [1]), (8, 8, 128, 16, [1, 40000], [1, 2])])
+def test_probabilities_of_few_rows_lose_no_bits(dtype, H, KV, hd, page, lens, rows):
+    """Up to 32 packed rows: the result is the formula's, rounded once.  A probability is
+    taken in two terms, the second rounded to half a step h of at most h of it, so h^2 of
+    the sum of p |v| is left, float16's 2^-36 of |v| per key, the float32 scores' error
+    (hd 2^-24 of the sum of absolute products, below 2 hd 2^-24 sqrt(hd) for normal values)
+    and the float32 sums' (1e-5)."""
+    g = torch.Generator().manual_seed(hd + sum(rows))
+    c, table = _cache([n + r for n, r in zip(lens, rows)], page, KV, hd, dtype, seed=3)
+    ks, vs = _fill(c, table, lens, rows, KV, hd, dtype, g)
+    c.len.copy_(_ints(lens))
+    q = torch.randn(sum(rows), H, hd, generator=g).to(dtype)
+    starts = [sum(rows[:b]) for b in range(len(rows) + 1)]
+    out = c.attend(0, q.cuda(), _ints(starts), max(rows))
+    h = ref.half_step(dtype)
+    for b, n in enumerate(rows):
+        part = slice(starts[b], starts[b] + n)
+        want, mag, _ = ref.attend(q[part], ks[b], vs[b], torch.ones(n, lens[b] + n, dtype=torch.bool), hd ** -0.5)
+        left = h * h + 2 * hd ** 1.5 * 2.0 ** -24 + 1e-5
+        low = (lens[b] + n) * 2.0 ** -36 if dtype == HF else 0.0
+        tol = h * want.abs() + left * mag + low + ref.half_subnormal(dtype)
+        _within(out[part], want, tol, f"few rows {dtype} {H}/{KV}x{hd} behind {lens[b]}")
