@@ -1084,9 +1084,14 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 
 // How a call is laid out: packed rows of a workgroup, keys of a step, units, least
 // steps of a unit.  A second kernel that joins parts costs about 5 us, so short
-// sequences are not split: up to 1024 keys a unit of few rows takes them whole (641
-// keys, head_dim 64: 8.5 us, split 6.3 + 3.8 and a launch), up to 512 one of many (8
-// windows of 64 rows over 320 keys, 16 heads on 4: 16.0 us, split and joined 24.8).
+// sequences are not split.  Whole against split, us per call of a replayed graph, 16
+// heads on 4.  Few rows, up to 1024 keys whole: one row of 128, one sequence, 640 keys
+// 8.5 / 8.9, 1024 11.0 / 9.1, 1280 12.7 / 9.5; of 32 sequences 768 12.0 / 15.1, 1024
+// 14.8 / 18.3, 2048 25.7 / 28.0 (a single sequence would change over at 768, 32 of them
+// not below 3000).  33 to 64 rows, the same line: 8 windows of 16 rows of 64, 512 keys
+// 10.9 / 11.8, 768 13.4 / 12.0, 1280 18.5 / 12.5.  Many rows, up to 512 whole: 8 windows
+// of 64 rows of 128, 320 keys 11.4 / 21.4, 1024 21.1 / 27.9, 1536 28.3 / 26.9; one of 64
+// rows of 64, 512 10.6 / 11.4, 640 12.1 / 11.5, 1024 16.6 / 11.7.
 // Many rows: with no more row tiles than CUs two wave groups each (8 trees of up to 64
 // rows over 512 to 4096 keys: 16.7 + 6.9 us with the join, one group 20.7 + 9.0); with
 // more of them one group, three workgroups per CU (8 x 1024 rows: 80 us, two groups

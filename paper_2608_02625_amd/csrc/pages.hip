@@ -278,8 +278,8 @@ __global__ __launch_bounds__(256) void commit_check_kernel(CacheArgs c, const in
 // and sequence.  A chunk of rows is read whole before it is written; later rows lie
 // behind every place already written (the list rises, so its i-th row is never in
 // front of place i).  Latency: five loads that need each other (8 sequences that keep
-// one of four blocks of 64, 20 layers of 4 heads of 128, 37 MB: 9 us, with the checks
-// and the freeing 17).
+// one of four blocks of 64, 20 layers of 4 heads of 128, 37 MB: 10 us, with the checks
+// and the freeing 18).
 constexpr int kMoveLoads = 4;
 
 __global__ __launch_bounds__(256) void commit_move_kernel(CacheArgs c, const int32_t* __restrict__ row_start,
