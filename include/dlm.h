@@ -416,6 +416,54 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
                           int64_t y_head_stride, const int32_t* d_pos, int32_t transpose, void* hip_stream);
 
 /*
+ * Norms of queries and keys for each head, with the rotation in the same pass.
+ *
+ * A head's values x at position p become y = R(p) (g x r), r = 1 / sqrt(mean(x^2) +
+ * eps) over all head_dim values, R the rotation of dlm_rope_apply (its scale with it),
+ * g the set's gain d_gain [head_dim] (NULL: ones) of gain_dtype, which is `dtype` or
+ * DLM_F32.  Two sets of heads of the same rows, each with its own gain, go through one
+ * launch: queries and keys, which may lie in one row of a product's result (strides in
+ * elements, as dlm_rope_apply's; d_y may be d_x with the same strides; the sets' results
+ * must not overlap).  k NULL or n_heads 0: no such set; at most 2^24 heads each.
+ * Computed in float32 (squares up to its range), rounded once.
+ *
+ * dlm_rope_norm_grad: gradients of a loss with respect to x (d_dx, of `dtype`) and the
+ * gain (d_dgain, of gain_dtype, may be NULL; the sum over rows and heads, in the same
+ * order on every call), given that with respect to y (d_dy, of `dtype`).  d_y of the
+ * sets is not read.  d_dx may be d_dy with the same strides.
+ * d_workspace: dlm_rope_norm_grad_workspace_bytes(rope), 256-byte aligned; it keeps
+ * nothing between calls, and calls that share it must be ordered.
+ */
+typedef struct dlm_norm_heads {
+    int32_t n_heads;
+    int32_t gain_dtype;
+    const void* d_gain;
+    const void* d_x;
+    int64_t x_row_stride;
+    int64_t x_head_stride;
+    void* d_y;
+    int64_t y_row_stride;
+    int64_t y_head_stride;
+} dlm_norm_heads;
+
+typedef struct dlm_norm_grads {
+    const void* d_dy;
+    int64_t dy_row_stride;
+    int64_t dy_head_stride;
+    void* d_dx;
+    int64_t dx_row_stride;
+    int64_t dx_head_stride;
+    void* d_dgain;
+} dlm_norm_grads;
+
+dlm_status dlm_rope_norm(const dlm_rope* rope, int32_t dtype, int32_t rows, const dlm_norm_heads* q,
+                         const dlm_norm_heads* k, float eps, const int32_t* d_pos, void* hip_stream);
+size_t dlm_rope_norm_grad_workspace_bytes(const dlm_rope* rope);
+dlm_status dlm_rope_norm_grad(const dlm_rope* rope, int32_t dtype, int32_t rows, const dlm_norm_heads* q,
+                              const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
+                              const int32_t* d_pos, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * A paged key/value cache, shared by sequences and by alternative drafts.
  *
  * The caller owns every buffer; dlm_cache is a host structure that names them.
@@ -502,6 +550,18 @@ dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t
                             int32_t max_rows, int32_t src_dtype, const void* d_k, int64_t k_stride, const void* d_v,
                             int64_t v_stride, const dlm_rope* rope, const int32_t* d_pos, int32_t n_heads,
                             const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, void* hip_stream);
+
+/*
+ * dlm_cache_append with the keys and queries normalised before they are rotated, as
+ * dlm_rope_norm does: d_k_gain, d_q_gain [head_dim] of gain_dtype (src_dtype or
+ * DLM_F32; NULL: ones), eps > 0.  Values are not normalised.  rope NULL: norms alone.
+ */
+dlm_status dlm_cache_append_norm(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                                 int32_t max_rows, int32_t src_dtype, const void* d_k, int64_t k_stride, const void* d_v,
+                                 int64_t v_stride, const dlm_rope* rope, const int32_t* d_pos, int32_t n_heads,
+                                 const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride,
+                                 int32_t gain_dtype, const void* d_q_gain, const void* d_k_gain, float eps,
+                                 void* hip_stream);
 
 /*
  * Attention of the windows' rows in one layer: a row sees its sequence's d_len

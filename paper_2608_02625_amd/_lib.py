@@ -69,6 +69,18 @@ class DlmRope(ctypes.Structure):
                 ("scale", ctypes.c_float), ("phase", ctypes.c_uint64 * 128)]
 
 
+class DlmNormHeads(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("gain_dtype", ctypes.c_int32), ("d_gain", ctypes.c_void_p),
+                ("d_x", ctypes.c_void_p), ("x_row_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64),
+                ("d_y", ctypes.c_void_p), ("y_row_stride", ctypes.c_int64), ("y_head_stride", ctypes.c_int64)]
+
+
+class DlmNormGrads(ctypes.Structure):
+    _fields_ = [("d_dy", ctypes.c_void_p), ("dy_row_stride", ctypes.c_int64), ("dy_head_stride", ctypes.c_int64),
+                ("d_dx", ctypes.c_void_p), ("dx_row_stride", ctypes.c_int64), ("dx_head_stride", ctypes.c_int64),
+                ("d_dgain", ctypes.c_void_p)]
+
+
 class DlmCache(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("page_len", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -85,6 +97,8 @@ _L = ctypes.c_int64
 _CFG = ctypes.POINTER(DlmConfig)
 _CACHE = ctypes.POINTER(DlmCache)
 _ROPE = ctypes.POINTER(DlmRope)
+_NORM = ctypes.POINTER(DlmNormHeads)
+_NGRAD = ctypes.POINTER(DlmNormGrads)
 SIGNATURES = [
     ("dlm_weights_bytes", _SZ, [_CFG]),
     ("dlm_workspace_bytes", _SZ, [_CFG, _I, _I, _I]),
@@ -108,10 +122,15 @@ SIGNATURES = [
                          ctypes.POINTER(DlmCascadeStats)]),
     ("dlm_rope_init", _I, [ctypes.POINTER(DlmRopeSpec), _ROPE]),
     ("dlm_rope_apply", _I, [_ROPE, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _I, _P]),
+    ("dlm_rope_norm", _I, [_ROPE, _I, _I, _NORM, _NORM, _F, _P, _P]),
+    ("dlm_rope_norm_grad_workspace_bytes", _SZ, [_ROPE]),
+    ("dlm_rope_norm_grad", _I, [_ROPE, _I, _I, _NORM, _NORM, _NGRAD, _NGRAD, _F, _P, _P, _SZ, _P]),
     ("dlm_cache_workspace_bytes", _SZ, [_CACHE, _I, _I, _I]),
     ("dlm_cache_reset", _I, [_CACHE, _P]),
     ("dlm_cache_reserve", _I, [_CACHE, _P, _I, _P, _P, _SZ, _P]),
     ("dlm_cache_append", _I, [_CACHE, _I, _P, _I, _I, _I, _P, _L, _P, _L, _ROPE, _P, _I, _P, _L, _P, _L, _P]),
+    ("dlm_cache_append_norm", _I, [_CACHE, _I, _P, _I, _I, _I, _P, _L, _P, _L, _ROPE, _P, _I, _P, _L, _P, _L, _I, _P, _P,
+                                   _F, _P]),
     ("dlm_cache_attend", _I, [_CACHE, _I, _P, _I, _I, _I, _I, _P, _L, _P, _I, _F, _P, _L, _P, _P, _SZ, _P]),
     ("dlm_cache_commit", _I, [_CACHE, _P, _I, _P, _P, _I, _P, _P]),
     ("dlm_cache_fork", _I, [_CACHE, _I, _P, _P, _P, _P]),

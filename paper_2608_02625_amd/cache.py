@@ -11,7 +11,7 @@ import ctypes
 import torch
 
 from . import _lib
-from ._lib import DlmCache, DlmRope, DlmRopeSpec, check
+from ._lib import DlmCache, DlmNormGrads, DlmNormHeads, DlmRope, DlmRopeSpec, check
 
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _SCALINGS = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
@@ -65,6 +65,15 @@ def _mask_words(mask: torch.Tensor, rows: int) -> int:
     if mask.dim() != 2 or mask.shape[0] != rows or (rows and mask.shape[1] == 0):
         raise ValueError(f"mask must be int32 [{rows}, words] with at least one word")
     return mask.shape[1]
+
+
+def _gain(t: torch.Tensor | None, name: str, head_dim: int, dtype: torch.dtype, device: torch.device):
+    """(address, type) of a gain [head_dim] of the rows' type or float32."""
+    if t is None:
+        return None, _DTYPES[dtype]
+    if t.shape != (head_dim,) or t.dtype not in (dtype, torch.float32) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor [{head_dim}] of type {dtype} or float32 on {device}")
+    return t.data_ptr(), _DTYPES[t.dtype]
 
 
 class Rope:
@@ -122,6 +131,108 @@ class Rope:
         _launch(self.lib.dlm_rope_apply, "dlm_rope_apply", device.index, self._ref, kind, shape[0], shape[1],
                 x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0], ys[1], pos, 1 if transpose else 0)
         return out
+
+
+    # -------------------------------------------------------------- norms of heads
+    def norm_apply(self, q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor,
+                   q_gain: torch.Tensor | None = None, k_gain: torch.Tensor | None = None, eps: float = 1e-6,
+                   out: torch.Tensor | None = None, k_out: torch.Tensor | None = None):
+        """Queries and keys [rows, heads, head_dim] (any row and head strides, each its own
+        number of heads), each head over the root of its mean square, times its gain
+        [head_dim] (their type or float32; None: ones), rotated to `positions`, in one
+        launch: (queries, keys).  k None: queries alone.  out, k_out: results of queries and
+        keys (may be q and k).  Gradients of q, k and the gains come by autograd (`out` and
+        `k_out` cannot be part of that, nor a gradient of the gradient)."""
+        given = [t for t in (out, k_out) if t is not None]
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_gain, k_gain, *given)):
+            if given:
+                raise ValueError("a result in `out` carries no gradient: detach the inputs and out, or leave out away")
+            return _NormRotation.apply(q, k, positions, q_gain, k_gain, self, eps)
+        return self._norm_apply(q, k, positions, q_gain, k_gain, eps, out, k_out)
+
+    def _norm_set(self, x: torch.Tensor | None, gain: torch.Tensor | None, like: torch.Tensor, name: str) -> DlmNormHeads:
+        """Rows, gain and type of a set of heads, its results still open."""
+        if x is None:
+            if gain is not None:
+                raise ValueError(f"{name}_gain without {name}")
+            return DlmNormHeads()
+        shape = x.shape
+        if len(shape) != 3 or shape[2] != self._head_dim or x.dtype not in _DTYPES or x.device.type != "cuda":
+            raise ValueError(f"{name} must be a bfloat16, float16 or float32 device tensor [rows, heads, {self._head_dim}]")
+        if x.dtype is not like.dtype or x.device != like.device or shape[0] != like.shape[0]:
+            raise ValueError("q and k must have the same rows, type and device")
+        row, head, one = x.stride()
+        if one != 1:
+            raise ValueError("the values of a head must lie next to each other")
+        g, kind = _gain(gain, f"{name}_gain", self._head_dim, x.dtype, x.device)
+        return DlmNormHeads(shape[1], kind, g, x.data_ptr(), row, head)
+
+    def _norm_apply(self, q, k, positions, q_gain, k_gain, eps, out, k_out):
+        sets = [self._norm_set(q, q_gain, q, "q"), self._norm_set(k, k_gain, q, "k")]
+        if k is None and k_out is not None:
+            raise ValueError("k_out without k")
+        results = []
+        for c, x, y, name in ((sets[0], q, out, "out"), (sets[1], k, k_out, "k_out")):
+            if x is not None:
+                if y is None:
+                    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                elif y.shape != x.shape or y.dtype is not x.dtype or y.device != x.device or y.stride(2) != 1:
+                    raise ValueError(f"{name} must have its input's shape, type and device, a head's values next to each other")
+                c.d_y = y.data_ptr()
+                c.y_row_stride, c.y_head_stride = y.stride(0), y.stride(1)
+            results.append(y)
+        pos = _ints(positions, "positions", q.shape[0], q.device)
+        _launch(self.lib.dlm_rope_norm, "dlm_rope_norm", q.device.index, self._ref, _DTYPES[q.dtype], q.shape[0],
+                ctypes.byref(sets[0]), ctypes.byref(sets[1]), eps, pos)
+        return tuple(results)
+
+    def _norm_grad(self, q, k, positions, q_gain, k_gain, eps, dq, dk, needs):
+        """Gradients of (q, k, q_gain, k_gain), given those of the results (None: none);
+        needs: which are asked for."""
+        device, kind = q.device, q.dtype
+        rows, sets, grads, got = q.shape[0], [], [], []
+        for x, gain, dy, name, need in ((q, q_gain, dq, "q", needs[2]), (k, k_gain, dk, "k", needs[3])):
+            if x is None or dy is None:
+                sets.append(DlmNormHeads())
+                grads.append(DlmNormGrads())
+                got.append((None, None))
+                continue
+            if dy.stride(2) != 1:                     # a head's values lie next to each other
+                dy = dy.clone(memory_format=torch.contiguous_format)
+            sets.append(self._norm_set(x, gain, q, name))
+            dx = torch.empty(x.shape, dtype=kind, device=device)
+            dg = torch.empty_like(gain) if gain is not None and need else None
+            grads.append(DlmNormGrads(dy.data_ptr(), dy.stride(0), dy.stride(1), dx.data_ptr(), dx.stride(0), dx.stride(1),
+                                      None if dg is None else dg.data_ptr()))
+            got.append((dx, dg, dy))
+        n = self.lib.dlm_rope_norm_grad_workspace_bytes(self._ref)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        _launch(self.lib.dlm_rope_norm_grad, "dlm_rope_norm_grad", device.index, self._ref, _DTYPES[kind], rows,
+                ctypes.byref(sets[0]), ctypes.byref(sets[1]), ctypes.byref(grads[0]), ctypes.byref(grads[1]), eps,
+                positions.data_ptr(), ws.data_ptr(), n)
+        return got[0][0], got[1][0], got[0][1], got[1][1]
+
+
+class _NormRotation(torch.autograd.Function):
+    """Norms of heads, then a rotation."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, q_gain, k_gain, rope, eps):
+        ctx.save_for_backward(q, k, positions, q_gain, k_gain)
+        ctx.rope, ctx.eps = rope, eps
+        ctx.set_materialize_grads(False)
+        return rope._norm_apply(q, k, positions, q_gain, k_gain, eps, None, None)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk):
+        q, k, positions, q_gain, k_gain = ctx.saved_tensors
+        if dq is None and dk is None:
+            return (None,) * 7
+        need = ctx.needs_input_grad
+        gq, gk, gqg, gkg = ctx.rope._norm_grad(q, k, positions, q_gain, k_gain, ctx.eps, dq, dk,
+                                               (need[0], need[1], need[3], need[4]))
+        return gq, gk, None, gqg, gkg, None, None
 
 
 class _Rotation(torch.autograd.Function):
@@ -265,10 +376,13 @@ class PagedCache:
     # -------------------------------------------------------------- windows
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, max_rows: int,
                q: torch.Tensor | None = None, rope: Rope | None = None, positions: torch.Tensor | None = None,
-               q_out: torch.Tensor | None = None) -> torch.Tensor | None:
+               q_out: torch.Tensor | None = None, q_gain: torch.Tensor | None = None,
+               k_gain: torch.Tensor | None = None, norm_eps: float | None = None) -> torch.Tensor | None:
         """Keys and values [rows, n_kv_heads, head_dim] of the windows into their reserved
         places; keys and queries rotated by `rope` to `positions` (default: the tokens'
-        places).  Returns the rotated queries (in q_out if given)."""
+        places).  Returns the rotated queries (in q_out if given).  norm_eps: keys and
+        queries are normalised first, each head over the root of its mean square and times
+        its gain [head_dim] (both of k's type or both float32; None: ones)."""
         device, kind = self.device, k.dtype
         starts = self._starts(row_start)
         T, _, ks = _rows(k, "k", self._kv, self._hd, device)
@@ -288,9 +402,20 @@ class PagedCache:
             if To != T or q_out.dtype is not self.dtype:
                 raise ValueError("q_out must have q's rows and the cache's type")
             qp, qop = q.data_ptr(), q_out.data_ptr()
+        call = (layer, starts, T, max_rows, _DTYPES[kind], k.data_ptr(), ks, v.data_ptr(), vs,
+                None if rope is None else rope._ref, pos, heads, qp, qs, qop, qos)
+        if norm_eps is None:
+            if q_gain is not None or k_gain is not None:
+                raise ValueError("gains without norm_eps")
+            if T:
+                self._call("dlm_cache_append", *call)
+            return q_out
+        qg, q_type = _gain(q_gain, "q_gain", self._hd, kind, device)
+        kg, k_type = _gain(k_gain, "k_gain", self._hd, kind, device)
+        if q_gain is not None and k_gain is not None and q_type != k_type:
+            raise ValueError("q_gain and k_gain must have the same type")
         if T:
-            self._call("dlm_cache_append", layer, starts, T, max_rows, _DTYPES[kind], k.data_ptr(), ks, v.data_ptr(), vs,
-                       None if rope is None else rope._ref, pos, heads, qp, qs, qop, qos)
+            self._call("dlm_cache_append_norm", *call, q_type if q_gain is not None else k_type, qg, kg, norm_eps)
         return q_out
 
     def attend(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int,

@@ -35,6 +35,19 @@ hipError_t launch_append(const CacheArgs& c, int dtype, int layer, const int32_t
                          const dlm_rope* rope, const int32_t* pos, int n_heads, const void* q, int64_t q_stride,
                          void* q_out, int64_t q_out_stride, hipStream_t st);
 
+// ------------------------------------------------------------- head_norm.hip
+hipError_t launch_rope_norm(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q, const dlm_norm_heads* k,
+                            float eps, const int32_t* pos, hipStream_t st);
+size_t norm_grad_workspace_bytes(int head_dim);
+hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q,
+                                 const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
+                                 const int32_t* pos, void* ws, hipStream_t st);
+hipError_t launch_append_norm(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
+                              int max_rows, int src_dtype, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const dlm_rope* rope, const int32_t* pos, int n_heads, const void* q,
+                              int64_t q_stride, void* q_out, int64_t q_out_stride, int gain_dtype, const void* q_gain,
+                              const void* k_gain, float eps, hipStream_t st);
+
 // ----------------------------------------------------------------- pages.hip
 // Workspace of reserve and compact.
 size_t pages_workspace_bytes(int n_seqs, int n_pages);

@@ -73,6 +73,102 @@ dlm_status check_rope(const dlm_rope* r) {
         if (_s != DLM_OK) return _s;     \
     } while (0)
 
+// Results must not overlap: heads inside a row, or rows inside a head.
+bool overlaps(int64_t rows, int64_t heads, int64_t row_stride, int64_t head_stride, int64_t hd) {
+    const int64_t h = heads > 1 ? head_stride : 0, r = rows > 1 ? row_stride : 0;
+    const bool rows_outer = (rows == 1 || r >= (__int128)(heads - 1) * h + hd) && (heads == 1 || h >= hd);
+    const bool heads_outer = (heads == 1 || h >= (__int128)(rows - 1) * r + hd) && (rows == 1 || r >= hd);
+    return !rows_outer && !heads_outer;
+}
+bool same_layout(int64_t rows, int64_t heads, int64_t a_row, int64_t a_head, int64_t b_row, int64_t b_head) {
+    return (rows <= 1 || a_row == b_row) && (heads <= 1 || a_head == b_head);
+}
+
+dlm_status check_eps(float eps) {
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(DLM_ERR_INVALID_ARG, "eps must be finite and > 0");
+    return DLM_OK;
+}
+dlm_status check_gain(int dtype, int gain_dtype, const void* gain, const void* dgain) {
+    if (gain_dtype != dtype && gain_dtype != DLM_F32)
+        return fail(DLM_ERR_INVALID_ARG, "gain_dtype must be the rows' dtype or DLM_F32");
+    const size_t size = gain_dtype == DLM_F32 ? 4 : 2;
+    if (!aligned(gain, size) || !aligned(dgain, size)) return fail(DLM_ERR_INVALID_ARG, "gains must be aligned to their elements");
+    return DLM_OK;
+}
+// A set of heads of dlm_rope_norm or, with `grad`, of its gradient.
+dlm_status check_norm_set(const dlm_norm_heads* s, const dlm_norm_grads* g, bool grad, int dtype, int64_t rows, int64_t hd) {
+    if (!s || s->n_heads == 0) return DLM_OK;
+    if (s->n_heads < 0 || s->n_heads > (1 << 24)) return fail(DLM_ERR_INVALID_ARG, "n_heads must be in [0, 2^24]");
+    if (grad && !g) return fail(DLM_ERR_INVALID_ARG, "a set of heads without its gradients");
+    TRY(check_gain(dtype, s->gain_dtype, s->d_gain, grad ? g->d_dgain : nullptr));
+    if (rows == 0) return DLM_OK;
+    const size_t size = dtype == DLM_F32 ? 4 : 2;
+    const int64_t n = s->n_heads;
+    const void* out = grad ? g->d_dx : s->d_y;
+    const int64_t out_row = grad ? g->dx_row_stride : s->y_row_stride, out_head = grad ? g->dx_head_stride : s->y_head_stride;
+    if (!s->d_x || !out || (grad && !g->d_dy)) return fail(DLM_ERR_INVALID_ARG, grad ? "x, dy or dx is NULL" : "x or y is NULL");
+    if (!aligned(s->d_x, size) || !aligned(out, size) || (grad && !aligned(g->d_dy, size)))
+        return fail(DLM_ERR_INVALID_ARG, "rows must be aligned to their elements");
+    if (s->x_row_stride < 0 || s->x_head_stride < 0 || out_row < 0 || out_head < 0 ||
+        (grad && (g->dy_row_stride < 0 || g->dy_head_stride < 0)))
+        return fail(DLM_ERR_INVALID_ARG, "strides must be >= 0");
+    if (overlaps(rows, n, out_row, out_head, hd)) return fail(DLM_ERR_INVALID_ARG, "rows or heads of the result overlap");
+    if ((s->d_x == out && !same_layout(rows, n, s->x_row_stride, s->x_head_stride, out_row, out_head)) ||
+        (grad && g->d_dy == out && !same_layout(rows, n, g->dy_row_stride, g->dy_head_stride, out_row, out_head)))
+        return fail(DLM_ERR_INVALID_ARG, "in place, rows and results must have the same strides");
+    return DLM_OK;
+}
+dlm_status check_norm(const dlm_rope* rope, int dtype, int rows, float eps, const dlm_norm_heads* q, const dlm_norm_heads* k,
+                      const int32_t* pos) {
+    if (!rope) return fail(DLM_ERR_INVALID_ARG, "rope is NULL");
+    TRY(check_rope(rope));
+    if (dtype != DLM_BF16 && dtype != DLM_F16 && dtype != DLM_F32) return fail(DLM_ERR_INVALID_ARG, "unknown dtype");
+    if (rows < 0) return fail(DLM_ERR_INVALID_ARG, "rows must be >= 0");
+    TRY(check_eps(eps));
+    if (!q) return fail(DLM_ERR_INVALID_ARG, "q is NULL");
+    const bool any = q->n_heads != 0 || (k && k->n_heads != 0);
+    if (rows > 0 && any && (!pos || !aligned(pos, 4))) return fail(DLM_ERR_INVALID_ARG, "pos must not be NULL and be 4-byte aligned");
+    return DLM_OK;
+}
+bool norm_idle(int rows, const dlm_norm_heads* q, const dlm_norm_heads* k) {
+    return rows == 0 || (q->n_heads == 0 && (!k || k->n_heads == 0));
+}
+
+// What the two forms of append ask for; *nothing: no rows.
+dlm_status check_append(const dlm_cache* cache, int layer, const int32_t* d_row_start, int total_rows, int max_rows,
+                        int src_dtype, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                        const dlm_rope* rope, int n_heads, const void* d_q, int64_t q_stride, const void* d_q_out,
+                        int64_t q_out_stride, bool* nothing) {
+    TRY(check_cache(cache));
+    if (layer < 0 || layer >= cache->n_layers) return fail(DLM_ERR_INVALID_ARG, "layer out of range");
+    TRY(check_rows(d_row_start, total_rows, max_rows));
+    if (src_dtype != cache->dtype && src_dtype != DLM_F32)
+        return fail(DLM_ERR_INVALID_ARG, "src_dtype must be the cache's dtype or DLM_F32");
+    if (rope) {
+        TRY(check_rope(rope));
+        if (rope->head_dim != cache->head_dim) return fail(DLM_ERR_INVALID_ARG, "rope and cache differ in head_dim");
+    }
+    *nothing = total_rows == 0;
+    if (*nothing) return DLM_OK;
+    if (!d_k || !d_v) return fail(DLM_ERR_INVALID_ARG, "k or v is NULL");
+    const int64_t kv_width = (int64_t)cache->n_kv_heads * cache->head_dim;
+    if (k_stride < kv_width || v_stride < kv_width) return fail(DLM_ERR_INVALID_ARG, "k_stride or v_stride below a row");
+    const size_t size = src_dtype == DLM_F32 ? 4 : 2;
+    if (!aligned(d_k, size) || !aligned(d_v, size)) return fail(DLM_ERR_INVALID_ARG, "k and v must be aligned to their elements");
+    if (d_q) {
+        if (n_heads < 1 || n_heads > (1 << 16)) return fail(DLM_ERR_INVALID_ARG, "n_heads must be in [1, 65536]");
+        if (!d_q_out) return fail(DLM_ERR_INVALID_ARG, "q_out is NULL");
+        const int64_t width = (int64_t)n_heads * cache->head_dim;
+        if (q_stride < width || q_out_stride < width) return fail(DLM_ERR_INVALID_ARG, "q_stride or q_out_stride below a row");
+        if (!aligned(d_q, size) || !aligned(d_q_out, 2)) return fail(DLM_ERR_INVALID_ARG, "q and q_out must be aligned to their elements");
+        if (d_q == d_q_out && (src_dtype != cache->dtype || q_stride != q_out_stride))
+            return fail(DLM_ERR_INVALID_ARG, "in place, q and q_out must have the same type and stride");
+    }
+    if ((int64_t)cache->n_seqs * std::max(d_q ? n_heads : 0, cache->n_kv_heads) * std::min(max_rows, total_rows) > ((int64_t)1 << 33))
+        return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
+    return DLM_OK;
+}
+
 }  // namespace
 
 dlm_status dlm_internal_check_cache(const dlm_cache* cache) { return check_cache(cache); }
@@ -149,16 +245,50 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
             return fail(DLM_ERR_INVALID_ARG, "x, y and pos must be aligned to their elements");
         if (x_row_stride < 0 || x_head_stride < 0 || y_row_stride < 0 || y_head_stride < 0)
             return fail(DLM_ERR_INVALID_ARG, "strides must be >= 0");
-        // Results must not overlap: heads inside a row, or rows inside a head.
-        const int64_t hd = rope->head_dim;
-        const int64_t h = heads > 1 ? y_head_stride : 0, r = rows > 1 ? y_row_stride : 0;
-        const bool rows_outer = (rows == 1 || r >= (__int128)(heads - 1) * h + hd) && (heads == 1 || h >= hd);
-        const bool heads_outer = (heads == 1 || h >= (__int128)(rows - 1) * r + hd) && (rows == 1 || r >= hd);
-        if (!rows_outer && !heads_outer) return fail(DLM_ERR_INVALID_ARG, "rows or heads of y overlap");
-        if (d_x == d_y && ((rows > 1 && x_row_stride != y_row_stride) || (heads > 1 && x_head_stride != y_head_stride)))
+        if (overlaps(rows, heads, y_row_stride, y_head_stride, rope->head_dim))
+            return fail(DLM_ERR_INVALID_ARG, "rows or heads of y overlap");
+        if (d_x == d_y && !same_layout(rows, heads, x_row_stride, x_head_stride, y_row_stride, y_head_stride))
             return fail(DLM_ERR_INVALID_ARG, "in place, x and y must have the same strides");
         return launched(launch_rope(*rope, dtype, rows, heads, d_x, x_row_stride, x_head_stride, d_y, y_row_stride,
                                     y_head_stride, d_pos, transpose != 0, (hipStream_t)hip_stream), "rope");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+dlm_status dlm_rope_norm(const dlm_rope* rope, int32_t dtype, int32_t rows, const dlm_norm_heads* q,
+                         const dlm_norm_heads* k, float eps, const int32_t* d_pos, void* hip_stream) {
+    try {
+        TRY(check_norm(rope, dtype, rows, eps, q, k, d_pos));
+        TRY(check_norm_set(q, nullptr, false, dtype, rows, rope->head_dim));
+        TRY(check_norm_set(k, nullptr, false, dtype, rows, rope->head_dim));
+        if (norm_idle(rows, q, k)) return DLM_OK;
+        return launched(launch_rope_norm(*rope, dtype, rows, q, k, eps, d_pos, (hipStream_t)hip_stream), "rope_norm");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+size_t dlm_rope_norm_grad_workspace_bytes(const dlm_rope* rope) {
+    try {
+        if (!rope || check_rope(rope) != DLM_OK) return 0;
+        return norm_grad_workspace_bytes(rope->head_dim);
+    } catch (...) {
+        dlm_internal_caught();
+        return 0;
+    }
+}
+
+dlm_status dlm_rope_norm_grad(const dlm_rope* rope, int32_t dtype, int32_t rows, const dlm_norm_heads* q,
+                              const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
+                              const int32_t* d_pos, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    try {
+        TRY(check_norm(rope, dtype, rows, eps, q, k, d_pos));
+        TRY(check_norm_set(q, dq, true, dtype, rows, rope->head_dim));
+        TRY(check_norm_set(k, dk, true, dtype, rows, rope->head_dim));
+        TRY(check_workspace(d_workspace, workspace_bytes, norm_grad_workspace_bytes(rope->head_dim)));
+        return launched(launch_rope_norm_grad(*rope, dtype, rows, q, k, dq, dk, eps, d_pos, d_workspace,
+                                              (hipStream_t)hip_stream), "rope_norm_grad");
     } catch (...) {
         return dlm_internal_caught();
     }
@@ -204,36 +334,36 @@ dlm_status dlm_cache_append(const dlm_cache* cache, int32_t layer, const int32_t
                             int64_t v_stride, const dlm_rope* rope, const int32_t* d_pos, int32_t n_heads,
                             const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, void* hip_stream) {
     try {
-        TRY(check_cache(cache));
-        if (layer < 0 || layer >= cache->n_layers) return fail(DLM_ERR_INVALID_ARG, "layer out of range");
-        TRY(check_rows(d_row_start, total_rows, max_rows));
-        if (src_dtype != cache->dtype && src_dtype != DLM_F32)
-            return fail(DLM_ERR_INVALID_ARG, "src_dtype must be the cache's dtype or DLM_F32");
-        if (rope) {
-            TRY(check_rope(rope));
-            if (rope->head_dim != cache->head_dim) return fail(DLM_ERR_INVALID_ARG, "rope and cache differ in head_dim");
-        }
-        if (total_rows == 0) return DLM_OK;
-        if (!d_k || !d_v) return fail(DLM_ERR_INVALID_ARG, "k or v is NULL");
-        const int64_t kv_width = (int64_t)cache->n_kv_heads * cache->head_dim;
-        if (k_stride < kv_width || v_stride < kv_width) return fail(DLM_ERR_INVALID_ARG, "k_stride or v_stride below a row");
-        const size_t size = src_dtype == DLM_F32 ? 4 : 2;
-        if (!aligned(d_k, size) || !aligned(d_v, size)) return fail(DLM_ERR_INVALID_ARG, "k and v must be aligned to their elements");
-        if (d_q) {
-            if (n_heads < 1 || n_heads > (1 << 16)) return fail(DLM_ERR_INVALID_ARG, "n_heads must be in [1, 65536]");
-            if (!d_q_out) return fail(DLM_ERR_INVALID_ARG, "q_out is NULL");
-            const int64_t width = (int64_t)n_heads * cache->head_dim;
-            if (q_stride < width || q_out_stride < width) return fail(DLM_ERR_INVALID_ARG, "q_stride or q_out_stride below a row");
-            if (!aligned(d_q, size) || !aligned(d_q_out, 2)) return fail(DLM_ERR_INVALID_ARG, "q and q_out must be aligned to their elements");
-            if (d_q == d_q_out && (src_dtype != cache->dtype || q_stride != q_out_stride))
-                return fail(DLM_ERR_INVALID_ARG, "in place, q and q_out must have the same type and stride");
-        }
-        if ((int64_t)cache->n_seqs * std::max(d_q ? n_heads : 0, cache->n_kv_heads) * std::min(max_rows, total_rows) > ((int64_t)1 << 33))
-            return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
+        bool nothing;
+        TRY(check_append(cache, layer, d_row_start, total_rows, max_rows, src_dtype, d_k, k_stride, d_v, v_stride, rope,
+                         n_heads, d_q, q_stride, d_q_out, q_out_stride, &nothing));
+        if (nothing) return DLM_OK;
         return launched(launch_append(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows,
                                       std::min(max_rows, total_rows), src_dtype, d_k, k_stride, d_v, v_stride, rope, d_pos,
                                       d_q ? n_heads : 0, d_q, q_stride, d_q_out, q_out_stride, (hipStream_t)hip_stream),
                         "cache_append");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+dlm_status dlm_cache_append_norm(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                                 int32_t max_rows, int32_t src_dtype, const void* d_k, int64_t k_stride, const void* d_v,
+                                 int64_t v_stride, const dlm_rope* rope, const int32_t* d_pos, int32_t n_heads,
+                                 const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride,
+                                 int32_t gain_dtype, const void* d_q_gain, const void* d_k_gain, float eps,
+                                 void* hip_stream) {
+    try {
+        TRY(check_eps(eps));
+        bool nothing;
+        TRY(check_append(cache, layer, d_row_start, total_rows, max_rows, src_dtype, d_k, k_stride, d_v, v_stride, rope,
+                         n_heads, d_q, q_stride, d_q_out, q_out_stride, &nothing));
+        TRY(check_gain(src_dtype, gain_dtype, d_q_gain, d_k_gain));
+        if (nothing) return DLM_OK;
+        return launched(launch_append_norm(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows,
+                                           std::min(max_rows, total_rows), src_dtype, d_k, k_stride, d_v, v_stride, rope,
+                                           d_pos, d_q ? n_heads : 0, d_q, q_stride, d_q_out, q_out_stride, gain_dtype,
+                                           d_q_gain, d_k_gain, eps, (hipStream_t)hip_stream), "cache_append_norm");
     } catch (...) {
         return dlm_internal_caught();
     }

@@ -1,0 +1,620 @@
+// Norms of queries and keys for each head with the rotation in the same pass
+// (dlm_rope_norm), their gradient (dlm_rope_norm_grad), and the form that puts keys
+// and values into their pages (dlm_cache_append_norm).
+//
+// A head's row x of n values becomes y = R (g x r), r = 1 / sqrt(mean(x^2) + eps), R
+// the rotation at the row's position.  Given dy, with u = R^T dy and h = g u: dg = the
+// sum of u x r over rows and heads, dx = r (h - x r mean(h x r)).
+//
+// A head belongs to a run of lanes of one wave, a power of two of them, each with one
+// vector of pairs (or of values behind the rotated ones): the sums over a head are a few
+// lane moves and a head is read once, kept in registers and written once.  Sines and
+// cosines are worked out once per row, and the lanes walk heads with them, several heads'
+// loads in flight.
+#include <algorithm>
+
+#include "rotary.h"
+
+namespace {
+
+// How a workgroup's threads are laid over a head, the heads and the rows: runs of
+// `run` lanes (a power of two), of which `turn` chunks hold V pairs each and `pass`
+// chunks the V values behind the rotated ones; `slots` heads at a time of `rows` rows.
+struct NormLanes {
+    int turn, pass, run, slots, rows;
+};
+
+// Chunks of a lane: more than one only where a head of up to 256 values is taken in
+// pieces so small that a wave has too few lanes for it.
+template <int V>
+constexpr int kChunks = V >= 4 ? 1 : V == 2 ? 2 : 4;
+
+// Sum over the run of lanes that this one belongs to.
+__device__ __forceinline__ float run_sum(float v, int run) {
+    if (run >= 2) v += dpp_f<0xB1>(v);                        // quad_perm [1,0,3,2]
+    if (run >= 4) v += dpp_f<0x4E>(v);                        // quad_perm [2,3,0,1]
+    if (run >= 8) v += dpp_f<0x141>(v);                       // row_half_mirror
+    if (run >= 16) v += dpp_f<0x140>(v);                      // row_mirror
+    if (run >= 32) v += __shfl_xor(v, 16, 64);
+    if (run >= 64) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
+// A chunk of a head in registers: V pairs (a[i], a[V + i]), or V values and zeros.
+template <typename S, int V, bool INTER, bool STREAM>
+__device__ __forceinline__ void load_chunk(const S* src, int c, const NormLanes& ln, int rot_dim, float (&a)[2 * V]) {
+    if (c < ln.turn) {
+        if constexpr (INTER) {
+            const auto x = load<STREAM, Vec<S, 2 * V>>(src + 2 * V * c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                a[i] = to_f32(x.v[2 * i]);
+                a[V + i] = to_f32(x.v[2 * i + 1]);
+            }
+        } else {
+            const auto x = load<STREAM, Vec<S, V>>(src + V * c), y = load<STREAM, Vec<S, V>>(src + V * c + rot_dim / 2);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                a[i] = to_f32(x.v[i]);
+                a[V + i] = to_f32(y.v[i]);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) a[i] = 0.f;
+    if (c < ln.turn + ln.pass) {
+        const auto x = load<STREAM, Vec<S, V>>(src + rot_dim + (c - ln.turn) * V);
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = to_f32(x.v[i]);
+    }
+}
+template <typename D, int V, bool INTER, bool STREAM>
+__device__ __forceinline__ void store_chunk(D* dst, int c, const NormLanes& ln, int rot_dim, const float (&a)[2 * V]) {
+    if (c < ln.turn) {
+        if constexpr (INTER) {
+            Vec<D, 2 * V> x;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x.v[2 * i] = (D)a[i];
+                x.v[2 * i + 1] = (D)a[V + i];
+            }
+            store<STREAM>(dst + 2 * V * c, x);
+        } else {
+            Vec<D, V> x, y;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                x.v[i] = (D)a[i];
+                y.v[i] = (D)a[V + i];
+            }
+            store<STREAM>(dst + V * c, x);
+            store<STREAM>(dst + V * c + rot_dim / 2, y);
+        }
+    } else if (c < ln.turn + ln.pass) {
+        Vec<D, V> x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x.v[i] = (D)a[i];
+        store<STREAM>(dst + rot_dim + (c - ln.turn) * V, x);
+    }
+}
+// Offset in the head of value i of a chunk, as load_chunk lays it out; -1: none.
+template <int V, bool INTER>
+__device__ __forceinline__ int value_at(int c, int i, const NormLanes& ln, int rot_dim) {
+    if (c < ln.turn) {
+        if constexpr (INTER) return 2 * (V * c + (i < V ? i : i - V)) + (i < V ? 0 : 1);
+        else return i < V ? V * c + i : V * c + i - V + rot_dim / 2;
+    }
+    return i < V && c < ln.turn + ln.pass ? rot_dim + (c - ln.turn) * V + i : -1;
+}
+
+// A row's cosines and sines; 1 and 0 for the values behind the rotated ones, so that
+// every lane turns what it holds.
+template <int V>
+__device__ __forceinline__ void chunk_angles(const dlm_rope& rope, int64_t pos, int c, const NormLanes& ln, bool back,
+                                             float (&co)[V], float (&si)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        co[i] = 1.f;
+        si[i] = 0.f;
+    }
+    if (c < ln.turn) angles<V>(rope.phase, rope.scale, pos, c * V, back, co, si);
+}
+template <int V>
+__device__ __forceinline__ void turn(float (&a)[2 * V], const float (&co)[V], const float (&si)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float t = a[i] * co[i] - a[V + i] * si[i];
+        a[V + i] = a[V + i] * co[i] + a[i] * si[i];
+        a[i] = t;
+    }
+}
+
+__device__ __forceinline__ float gain_value(const void* gain, int dtype, int i) {
+    if (!gain) return 1.f;
+    if (dtype == DLM_F32) return reinterpret_cast<const float*>(gain)[i];
+    if (dtype == DLM_BF16) return (float)reinterpret_cast<const __bf16*>(gain)[i];
+    return (float)reinterpret_cast<const _Float16*>(gain)[i];
+}
+// The two gains in LDS in the order of the chunks: chunk c's at [c][2 V].
+template <int V, bool INTER>
+__device__ __forceinline__ void stage_gains(float* lds, int width, const void* gq, int tq, const void* gk, int tk,
+                                            const NormLanes& ln, int rot_dim) {
+    for (int x = threadIdx.x; x < 2 * width; x += blockDim.x) {
+        const int set = x >= width, y = set ? x - width : x;
+        const int at = value_at<V, INTER>(y / (2 * V), y % (2 * V), ln, rot_dim);
+        lds[x] = at < 0 ? 0.f : gain_value(set ? gk : gq, set ? tk : tq, at);
+    }
+    __syncthreads();
+}
+// Chunks of a head, a lane's unused ones included, times their values: at most 256
+// lanes' chunks of V = 1 hold 512 values, of V = 8 no more.
+constexpr int kGainWords = 512;
+
+template <int V>
+__device__ __forceinline__ float sum_squares(const float (&a)[2 * V]) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) s = fmaf(a[i], a[i], s);
+    return s;
+}
+
+struct NormSet {
+    int heads, gain_dtype;
+    const void* gain;
+    const void* x;
+    int64_t x_row, x_head;
+    void* y;
+    int64_t y_row, y_head;
+};
+
+// Heads that a lane has in flight.
+template <int V>
+constexpr int kFlight = V >= 4 ? 4 : 1;
+
+template <typename T, int V, bool INTER, bool STREAM>
+__global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const NormSet q, const NormSet k, float eps,
+                                                   const int32_t* __restrict__ pos, int rows, NormLanes ln) {
+    constexpr int CH = kChunks<V>, U = kFlight<V>;
+    __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
+    const int width = CH * ln.run * 2 * V;
+    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
+    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;
+    if (slot >= ln.slots * ln.rows || r >= rows) return;      // whole runs
+    float co[CH][V], si[CH][V];
+    const int64_t p = pos[r];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, false, co[j], si[j]);
+    const T *xq = (const T*)q.x + r * q.x_row, *xk = (const T*)k.x + r * k.x_row;
+    T *yq = (T*)q.y + r * q.y_row, *yk = (T*)k.y + r * k.y_row;
+    const float inv_n = 1.f / (float)rope.head_dim;
+    const uint32_t n_all = (uint32_t)q.heads + (uint32_t)k.heads;
+    for (uint32_t h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
+        float a[U][CH][2 * V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t h = h0 + u * ln.slots;
+            if (h >= n_all) continue;
+            const T* src = h < (uint32_t)q.heads ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                load_chunk<T, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t h = h0 + u * ln.slots;
+            if (h >= n_all) continue;
+            const bool is_q = h < (uint32_t)q.heads;
+            T* dst = is_q ? yq + h * q.y_head : yk + (h - q.heads) * k.y_head;
+            float ss = 0.f;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) ss += sum_squares<V>(a[u][j]);
+            const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
+            const float* g = gains + (is_q ? 0 : width);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const float* gc = g + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+                for (int i = 0; i < 2 * V; ++i) a[u][j][i] *= rs * gc[i];
+                turn<V>(a[u][j], co[j], si[j]);
+                store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+
+struct NormGrad {
+    const void* dy;
+    int64_t dy_row, dy_head;
+    void* dx;
+    int64_t dx_row, dx_head;
+};
+// Workgroups of the gradient, each with a part of both gains' gradients: what the chip
+// holds at once (4 per CU), so that the parts are few.
+constexpr int kGradWgs = 1024;
+
+// A workgroup takes every gridDim.x-th group of rows.  The gains' sums stay in registers
+// over all of them, are added over the workgroup's runs in order, and leave one part per
+// workgroup; the second kernel adds the parts in order.
+template <typename T, int V, bool INTER, bool STREAM>
+__global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, const NormSet q, const NormSet k,
+                                                        const NormGrad gq, const NormGrad gk, float eps,
+                                                        const int32_t* __restrict__ pos, int rows, NormLanes ln,
+                                                        float* __restrict__ parts) {
+    constexpr int CH = kChunks<V>, U = V >= 4 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
+    __shared__ float sums[256];
+    const int width = CH * ln.run * 2 * V;
+    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
+    const bool busy = slot < ln.slots * ln.rows;
+    const float inv_n = 1.f / (float)rope.head_dim;
+    const uint32_t n_all = (uint32_t)q.heads + (uint32_t)k.heads;
+    float acc[2][CH][2 * V];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) acc[s][j][i] = 0.f;
+    for (int64_t r = (int64_t)blockIdx.x * ln.rows + slot / ln.slots; busy && r < rows; r += (int64_t)gridDim.x * ln.rows) {
+        float co[CH][V], si[CH][V];
+        const int64_t p = pos[r];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, true, co[j], si[j]);
+        const T *xq = (const T*)q.x + r * q.x_row, *xk = (const T*)k.x + r * k.x_row;
+        const T *yq = (const T*)gq.dy + r * gq.dy_row, *yk = (const T*)gk.dy + r * gk.dy_row;
+        T *oq = (T*)gq.dx + r * gq.dx_row, *ok = (T*)gk.dx + r * gk.dx_row;
+        for (uint32_t h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
+            float a[U][CH][2 * V], b[U][CH][2 * V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t h = h0 + u * ln.slots;
+                if (h >= n_all) continue;
+                const bool is_q = h < (uint32_t)q.heads;
+                const T* x = is_q ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
+                const T* y = is_q ? yq + h * gq.dy_head : yk + (h - q.heads) * gk.dy_head;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    load_chunk<T, V, INTER, STREAM>(x, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                    load_chunk<T, V, INTER, STREAM>(y, lane + j * ln.run, ln, rope.rot_dim, b[u][j]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t h = h0 + u * ln.slots;
+                if (h >= n_all) continue;
+                const bool is_q = h < (uint32_t)q.heads;
+                T* dst = is_q ? oq + h * gq.dx_head : ok + (h - q.heads) * gk.dx_head;
+                const float* g = gains + (is_q ? 0 : width);
+                float ss = 0.f;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    turn<V>(b[u][j], co[j], si[j]);           // u = R^T dy
+                    ss += sum_squares<V>(a[u][j]);
+                }
+                const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
+                float dot = 0.f;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const float* gc = g + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+                    for (int i = 0; i < 2 * V; ++i) {
+                        a[u][j][i] *= rs;                     // x r
+                        const float t = b[u][j][i] * a[u][j][i];
+                        if (is_q) acc[0][j][i] += t;
+                        else acc[1][j][i] += t;
+                        dot = fmaf(t, gc[i], dot);
+                    }
+                }
+                dot = run_sum(dot, ln.run) * inv_n;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const float* gc = g + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+                    for (int i = 0; i < 2 * V; ++i) a[u][j][i] = rs * (b[u][j][i] * gc[i] - a[u][j][i] * dot);
+                    store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                }
+            }
+        }
+    }
+    // Over the runs of the workgroup, value by value.
+    const int runs = ln.slots * ln.rows;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) {
+                __syncthreads();
+                sums[threadIdx.x] = acc[s][j][i];
+                __syncthreads();
+                if ((int)threadIdx.x < ln.run) {
+                    float t = 0.f;
+                    for (int x = 0; x < runs; ++x) t += sums[x * ln.run + threadIdx.x];
+                    const int at = value_at<V, INTER>(threadIdx.x + j * ln.run, i, ln, rope.rot_dim);
+                    if (at >= 0) parts[((int64_t)blockIdx.x * 2 + s) * rope.head_dim + at] = t;
+                }
+            }
+}
+
+// The parts added in order: blockIdx.x takes 16 values of one gain, 16 runs of parts each.
+__global__ __launch_bounds__(256) void gain_sum_kernel(const float* __restrict__ parts, int n_parts, int head_dim,
+                                                       void* out_q, int type_q, void* out_k, int type_k) {
+    __shared__ float run[16][17];
+    const int v = threadIdx.x & 15, at = threadIdx.x >> 4;
+    const int per = (head_dim + 15) / 16, set = blockIdx.x / per, i = blockIdx.x % per * 16 + v;
+    const int each = (n_parts + 15) / 16;
+    float t = 0.f;
+    if (i < head_dim)
+        for (int p = at * each; p < min(n_parts, (at + 1) * each); ++p) t += parts[((int64_t)p * 2 + set) * head_dim + i];
+    run[at][v] = t;
+    __syncthreads();
+    void* out = set ? out_k : out_q;
+    if (at || i >= head_dim || !out) return;
+    for (int x = 1; x < 16; ++x) t += run[x][v];
+    const int type = set ? type_k : type_q;
+    if (type == DLM_F32) reinterpret_cast<float*>(out)[i] = t;
+    else if (type == DLM_BF16) reinterpret_cast<__bf16*>(out)[i] = (__bf16)t;
+    else reinterpret_cast<_Float16*>(out)[i] = (_Float16)t;
+}
+
+// ------------------------------------------------------------------ into pages
+
+// As append_kernel of rope.hip, keys and queries normalised.  Head indexes run over the
+// keys, the values, then the queries.
+template <typename S, typename D, int V, bool INTER, bool STREAM>
+__global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, CacheArgs c, int64_t layer_base,
+                                                          const int32_t* __restrict__ row_start, int total_rows,
+                                                          int max_rows, const NormSet q, const NormSet k, const S* v,
+                                                          int64_t v_stride, float eps, const int32_t* __restrict__ pos,
+                                                          NormLanes ln) {
+    constexpr int CH = kChunks<V>, U = kFlight<V>;
+    __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
+    const int width = CH * ln.run * 2 * V;
+    const int b = blockIdx.y;
+    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
+    const int i = (int)(blockIdx.z * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;    // max_rows <= 2^24
+    const int start = row_start[b], end = min(row_start[b + 1], total_rows), len = c.len[b];
+    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    if (slot >= ln.slots * ln.rows || start < 0 || i >= max_rows || start >= end || i >= end - start) return;
+    const int64_t r = (int64_t)start + i;
+    const int64_t t = (int64_t)len + i;                       // the row's token
+    const int64_t entry = t >> c.page_log2;
+    int page = -1;
+    if (len >= 0 && entry < c.max_pages) page = c.table[(int64_t)b * c.max_pages + entry];
+    bool held = page >= 0 && page < c.n_pages;                // else the row's keys and values are dropped
+    const int refs = held ? c.ref[page] : 0;
+    const int hd = c.head_dim;
+    const int64_t head_stride = (int64_t)c.page_len * hd;     // within a page
+    const int64_t base = layer_base + (int64_t)(held ? page : 0) * c.n_kv * head_stride + (t & (c.page_len - 1)) * hd;
+    const int n_all = 2 * c.n_kv + q.heads;
+    float co[CH][V], si[CH][V];
+    const bool rotate = rope.scale != 0.f;                    // 0: no rotation asked for
+    const int64_t p = pos ? pos[r] : t;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int chunk = rotate ? lane + j * ln.run : ln.turn;           // chunk ln.turn: cosine 1
+        chunk_angles<V>(rope, p, chunk, ln, false, co[j], si[j]);
+    }
+    if (refs > 1 && counted_elsewhere(c, b, t, page)) held = false;
+    const float inv_n = 1.f / (float)hd;
+    for (int h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
+        float a[U][CH][2 * V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * ln.slots;
+            if (h >= n_all || (h < 2 * c.n_kv && !held)) continue;
+            const S* src = h < c.n_kv       ? (const S*)k.x + r * k.x_row + h * hd
+                           : h < 2 * c.n_kv ? v + r * v_stride + (h - c.n_kv) * hd
+                                            : (const S*)q.x + r * q.x_row + (h - 2 * c.n_kv) * hd;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                load_chunk<S, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * ln.slots;
+            if (h >= n_all || (h < 2 * c.n_kv && !held)) continue;
+            const bool is_k = h < c.n_kv, is_v = !is_k && h < 2 * c.n_kv;
+            D* dst = is_k   ? reinterpret_cast<D*>(c.k) + base + h * head_stride
+                     : is_v ? reinterpret_cast<D*>(c.v) + base + (h - c.n_kv) * head_stride
+                            : (D*)q.y + r * q.y_row + (h - 2 * c.n_kv) * hd;
+            if (!is_v) {
+                float ss = 0.f;
+#pragma unroll
+                for (int j = 0; j < CH; ++j) ss += sum_squares<V>(a[u][j]);
+                const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
+                const float* g = gains + (is_k ? width : 0);
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const float* gc = g + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+                    for (int x = 0; x < 2 * V; ++x) a[u][j][x] *= rs * gc[x];
+                    turn<V>(a[u][j], co[j], si[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                store_chunk<D, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+// Runs of a power of two of lanes; how many heads a workgroup takes at a time: the number
+// that leaves the fewest lanes and turns idle, the largest of those.
+NormLanes lay_out(const dlm_rope& r, int V, int64_t rows, int64_t heads) {
+    NormLanes ln{r.rot_dim / 2 / V, (r.head_dim - r.rot_dim) / V, 1, 1, 1};
+    while (ln.run < ln.turn + ln.pass && ln.run < 64) ln.run *= 2;
+    const int most = 256 / ln.run;
+    double best_use = 0.;
+    for (int s = 1; s <= heads && s <= most; ++s) {
+        const int at_once = (int)std::min<int64_t>(most / s, rows);
+        const double use = (double)(s * at_once) / most * heads / (s * ((heads + s - 1) / s));
+        if (use >= best_use) {
+            best_use = use;
+            ln.slots = s;
+            ln.rows = at_once;
+        }
+    }
+    return ln;
+}
+
+struct NormCall {
+    const dlm_rope& rope;
+    int rows;
+    NormSet q, k;
+    float eps;
+    const int32_t* pos;
+    hipStream_t st;
+    const NormGrad *gq = nullptr, *gk = nullptr;
+    float* parts = nullptr;
+    int* n_parts = nullptr;
+};
+template <typename T, int V, bool STREAM = false>
+hipError_t norm_layout(const NormCall& a) {
+    const NormLanes ln = lay_out(a.rope, V, a.rows, (int64_t)a.q.heads + a.k.heads);
+    const int64_t wgs = ((int64_t)a.rows + ln.rows - 1) / ln.rows;
+    if (a.gq) {
+        const int n = (int)std::min<int64_t>(wgs, kGradWgs);
+        *a.n_parts = n;
+        auto kernel = a.rope.interleaved ? norm_grad_kernel<T, V, true, STREAM> : norm_grad_kernel<T, V, false, STREAM>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, a.st, a.rope, a.q, a.k, *a.gq, *a.gk, a.eps, a.pos,
+                           a.rows, ln, a.parts);
+    } else {
+        const dim3 grid((unsigned)std::min(wgs, kWgsAcross), (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
+        auto kernel = a.rope.interleaved ? norm_kernel<T, V, true, STREAM> : norm_kernel<T, V, false, STREAM>;
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.st, a.rope, a.q, a.k, a.eps, a.pos, a.rows, ln);
+    }
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t norm_type(const NormCall& a) {
+    auto set_fits = [&](const NormSet& s, const NormGrad* g, int n) {
+        if (s.heads == 0) return true;
+        constexpr int e = sizeof(T);
+        auto one = [&](const void* p, int64_t row, int64_t head) { return fits(p, e, n, row) && fits(p, e, n, head); };
+        if (!one(s.x, s.x_row, s.x_head)) return false;
+        return g ? one(g->dy, g->dy_row, g->dy_head) && one(g->dx, g->dx_row, g->dx_head) : one(s.y, s.y_row, s.y_head);
+    };
+    const int V = pairs_per_access(a.rope, sizeof(T), [&](int n) { return set_fits(a.q, a.gq, n) && set_fits(a.k, a.gk, n); });
+    constexpr int W = 16 / sizeof(T);
+    const bool stream = streams((a.gq ? 3 : 2) * (int64_t)a.rows * ((int64_t)a.q.heads + a.k.heads) * a.rope.head_dim * sizeof(T));
+    if (V == W && stream) return norm_layout<T, W, true>(a);
+    if (a.rope.interleaved && V == W / 2 && stream) return norm_layout<T, W / 2, true>(a);
+    if constexpr (sizeof(T) == 2)
+        if (V == 8) return norm_layout<T, 8>(a);
+    if (V == 4) return norm_layout<T, 4>(a);
+    if (V == 2) return norm_layout<T, 2>(a);
+    return norm_layout<T, 1>(a);
+}
+hipError_t norm_any(const NormCall& a, int dtype) {
+    if (dtype == DLM_BF16) return norm_type<__bf16>(a);
+    if (dtype == DLM_F16) return norm_type<_Float16>(a);
+    return norm_type<float>(a);
+}
+NormSet norm_set(const dlm_norm_heads* h) {
+    if (!h || h->n_heads == 0) return NormSet{};
+    NormSet s{h->n_heads, h->gain_dtype, h->d_gain, h->d_x, h->x_row_stride, h->x_head_stride,
+              h->d_y, h->y_row_stride, h->y_head_stride};
+    if (s.heads == 1) s.x_head = s.y_head = 0;
+    return s;
+}
+NormGrad norm_grad(const dlm_norm_heads* h, const dlm_norm_grads* g) {
+    if (!h || h->n_heads == 0) return NormGrad{};
+    NormGrad s{g->d_dy, g->dy_row_stride, g->dy_head_stride, g->d_dx, g->dx_row_stride, g->dx_head_stride};
+    if (h->n_heads == 1) s.dy_head = s.dx_head = 0;
+    return s;
+}
+
+struct AppendNormCall {
+    const CacheArgs& c;
+    int layer;
+    const int32_t* row_start;
+    int total_rows, max_rows;
+    NormSet q, k;
+    const void* v;
+    int64_t v_stride;
+    const dlm_rope& rope;
+    const int32_t* pos;
+    float eps;
+    hipStream_t st;
+};
+template <typename S, typename D, int V, bool STREAM = false>
+hipError_t append_layout(const AppendNormCall& a) {
+    const NormLanes ln = lay_out(a.rope, V, a.max_rows, 2 * a.c.n_kv + a.q.heads);
+    const int64_t wgs = ((int64_t)a.max_rows + ln.rows - 1) / ln.rows;
+    const dim3 grid((unsigned)std::min(wgs, kWgsAcross), a.c.n_seqs, (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
+    const int64_t layer_base = (int64_t)a.layer * a.c.n_pages * a.c.n_kv * a.c.page_len * a.c.head_dim;
+    auto kernel = a.rope.interleaved ? append_norm_kernel<S, D, V, true, STREAM> : append_norm_kernel<S, D, V, false, STREAM>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.st, a.rope, a.c, layer_base, a.row_start, a.total_rows, a.max_rows,
+                       a.q, a.k, (const S*)a.v, a.v_stride, a.eps, a.pos, ln);
+    return hipGetLastError();
+}
+template <typename S, typename D>
+hipError_t append_type(const AppendNormCall& a) {
+    const int V = pairs_per_access(a.rope, sizeof(S), [&](int n) {
+        return fits(a.k.x, sizeof(S), n, a.k.x_row) && fits(a.v, sizeof(S), n, a.v_stride) &&
+               (!a.q.heads || (fits(a.q.x, sizeof(S), n, a.q.x_row) && fits(a.q.y, sizeof(D), n, a.q.y_row)));
+    });
+    constexpr int W = 16 / sizeof(S);
+    const int64_t width = (int64_t)(2 * a.c.n_kv + a.q.heads) * a.c.head_dim;
+    const bool stream = streams(a.total_rows * width * (int64_t)(sizeof(S) + sizeof(D)));
+    if (V == W && stream) return append_layout<S, D, W, true>(a);
+    if (a.rope.interleaved && V == W / 2 && stream) return append_layout<S, D, W / 2, true>(a);
+    if constexpr (sizeof(S) == 2)
+        if (V == 8) return append_layout<S, D, 8>(a);
+    if (V == 4) return append_layout<S, D, 4>(a);
+    if (V == 2) return append_layout<S, D, 2>(a);
+    return append_layout<S, D, 1>(a);
+}
+
+}  // namespace
+
+hipError_t launch_rope_norm(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q, const dlm_norm_heads* k,
+                            float eps, const int32_t* pos, hipStream_t st) {
+    return norm_any(NormCall{rope, rows, norm_set(q), norm_set(k), eps, pos, st}, dtype);
+}
+
+size_t norm_grad_workspace_bytes(int head_dim) { return (size_t)kGradWgs * 2 * head_dim * sizeof(float); }
+
+hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q,
+                                 const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
+                                 const int32_t* pos, void* ws, hipStream_t st) {
+    NormCall a{rope, rows, norm_set(q), norm_set(k), eps, pos, st};
+    const NormGrad gq = norm_grad(q, dq), gk = norm_grad(k, dk);
+    int n_parts = 0;
+    a.gq = &gq;
+    a.gk = &gk;
+    a.parts = (float*)ws;
+    a.n_parts = &n_parts;
+    if (rows > 0 && a.q.heads + (int64_t)a.k.heads > 0) {
+        const hipError_t e = norm_any(a, dtype);
+        if (e != hipSuccess) return e;
+    }
+    void* out_q = q && dq && q->n_heads ? dq->d_dgain : nullptr;
+    void* out_k = k && dk && k->n_heads ? dk->d_dgain : nullptr;
+    if (!out_q && !out_k) return hipSuccess;
+    hipLaunchKernelGGL(gain_sum_kernel, dim3(2 * ((rope.head_dim + 15) / 16)), dim3(256), 0, st, (const float*)ws, n_parts,
+                       rope.head_dim, out_q, q ? q->gain_dtype : 0, out_k, k ? k->gain_dtype : 0);
+    return hipGetLastError();
+}
+
+hipError_t launch_append_norm(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
+                              int max_rows, int src_dtype, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, const dlm_rope* rope, const int32_t* pos, int n_heads, const void* q,
+                              int64_t q_stride, void* q_out, int64_t q_out_stride, int gain_dtype, const void* q_gain,
+                              const void* k_gain, float eps, hipStream_t st) {
+    dlm_rope none{};
+    none.head_dim = none.rot_dim = c.head_dim;                // scale 0: values are not rotated
+    const NormSet qs{q ? n_heads : 0, gain_dtype, q_gain, q, q_stride, 0, q_out, q_out_stride, 0};
+    const NormSet ks{c.n_kv, gain_dtype, k_gain, k, k_stride, 0, nullptr, 0, 0};
+    const AppendNormCall a{c, layer, row_start, total_rows, max_rows, qs, ks, v, v_stride, rope ? *rope : none, pos, eps, st};
+    if (dtype == DLM_BF16)
+        return src_dtype == DLM_F32 ? append_type<float, __bf16>(a) : append_type<__bf16, __bf16>(a);
+    return src_dtype == DLM_F32 ? append_type<float, _Float16>(a) : append_type<_Float16, _Float16>(a);
+}

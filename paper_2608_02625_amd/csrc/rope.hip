@@ -16,50 +16,9 @@
 // four loads that need each other (the page's references among them, beside the sines).
 #include <algorithm>
 
-#include "common.h"
-#include "cache.h"
+#include "rotary.h"
 
 namespace {
-
-__device__ __forceinline__ void turn_sincos(uint64_t phase, float& s, float& c) {
-    const uint64_t t = phase + (1ull << 61);
-    const int quad = (int)(t >> 62);
-    // signed distance from the quadrant's centre: 2^31 is an eighth of a turn
-    const int32_t r = (int32_t)(((int64_t)(t & ((1ull << 62) - 1)) - (1ll << 61)) >> 30);
-    float s0, c0;
-    sincospif((float)r * 0x1p-33f, &s0, &c0);
-    s = quad & 1 ? c0 : s0;
-    c = quad & 1 ? s0 : c0;
-    if (quad == 1 || quad == 2) c = -c;
-    if (quad >= 2) s = -s;
-}
-
-template <typename T>
-__device__ __forceinline__ float to_f32(T v);
-template <>
-__device__ __forceinline__ float to_f32<__bf16>(__bf16 v) { return (float)v; }
-template <>
-__device__ __forceinline__ float to_f32<_Float16>(_Float16 v) { return (float)v; }
-template <>
-__device__ __forceinline__ float to_f32<float>(float v) { return v; }
-
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-    T v[N];
-};
-// One access; STREAM: past the caches' replacement.
-template <bool STREAM, typename V>
-__device__ __forceinline__ V load(const void* p) {
-    if constexpr (STREAM && sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_nontemporal_load((const u32x4*)p));
-    else if constexpr (STREAM && sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_nontemporal_load((const u32x2*)p));
-    else return *(const V*)p;
-}
-template <bool STREAM, typename V>
-__device__ __forceinline__ void store(void* p, const V& v) {
-    if constexpr (STREAM && sizeof(V) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-    else if constexpr (STREAM && sizeof(V) == 8) __builtin_nontemporal_store(__builtin_bit_cast(u32x2, v), (u32x2*)p);
-    else *(V*)p = v;
-}
 
 // V pairs of a head: from src to dst (rotated by (c, s) where `rotate`), the
 // pairs being values at offsets o .. o + V - 1 and o + half .. (INTER: at 2 o ..
@@ -126,17 +85,6 @@ struct Lanes {
     int turn, pass, slots, rows;
 };
 
-template <int V>
-__device__ __forceinline__ void angles(const uint64_t* phase, float scale, int64_t pos, int o, bool back, float (&c)[V],
-                                       float (&s)[V]) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        turn_sincos(phase[o + i] * (uint64_t)pos, s[i], c[i]);
-        s[i] *= back ? -scale : scale;
-        c[i] *= scale;
-    }
-}
-
 template <typename T, int V, bool INTER, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T* x, int64_t x_row, int64_t x_head, T* y,
                                                    int64_t y_row, int64_t y_head, const int32_t* __restrict__ pos,
@@ -159,15 +107,6 @@ __global__ __launch_bounds__(256) void rope_kernel(const dlm_rope rope, const T*
 #pragma unroll 2
         for (uint32_t h = h0; h < (uint32_t)heads; h += ln.slots) pass_values<T, T, V, STREAM>(x + h * x_head + o, y + h * y_head + o);
     }
-}
-
-// Whether a sequence other than b counts token t, in this page (shared pages stand in the
-// same entry of every table row: they come from forks).
-__device__ bool counted_elsewhere(const CacheArgs& c, int b, int64_t t, int page) {
-    const int64_t entry = t >> c.page_log2;
-    for (int s = 0; s < c.n_seqs; ++s)
-        if (s != b && c.len[s] > t && c.table[(int64_t)s * c.max_pages + entry] == page) return true;
-    return false;
 }
 
 // Keys, values and queries of the rows of sequence blockIdx.y.  Head indexes run
@@ -228,25 +167,6 @@ __global__ __launch_bounds__(256) void append_kernel(const dlm_rope rope, CacheA
     }
 }
 
-// Whether accesses of n values of `elem` bytes stay aligned at p and on a stride
-// (in elements).
-bool fits(const void* p, int elem, int n, int64_t stride) {
-    return (uintptr_t)p % ((size_t)n * elem) == 0 && stride % n == 0;
-}
-// Whether a call's bytes are too many for the 256 MB memory-side cache to keep any for
-// the next kernel: then they go past it.  A copy of 2 x 160 MB runs at 5.6 TB/s, past
-// the caches at 6.2; one of 2 x 32 MB (which stays cached) at 6.8 and 5.7.
-bool streams(int64_t bytes) { return bytes >= (int64_t)128 << 20; }
-// Most pairs per access: V values (half layout) or 2 V (interleaved) make at most
-// 16 bytes of the wider type; `aligned(n)` tells whether accesses of n values are.
-template <typename F>
-int pairs_per_access(const dlm_rope& r, int elem, F aligned) {
-    for (int V = 16 / elem / (r.interleaved ? 2 : 1); V > 1; V /= 2) {
-        const int n = r.interleaved ? 2 * V : V;
-        if ((r.rot_dim / 2) % V == 0 && (r.head_dim - r.rot_dim) % V == 0 && r.head_dim % n == 0 && aligned(n)) return V;
-    }
-    return 1;
-}
 // A thread walks heads with its sines and cosines.  How many heads a workgroup takes at
 // a time: the number that leaves the fewest threads and turns idle, the largest of
 // those (4099 rows of 16 heads of 20 lanes: 9.0 us, where 8 heads of one row leave a
@@ -268,9 +188,6 @@ Lanes lay_out(const dlm_rope& r, int V, int64_t rows, int heads) {
     }
     return best;
 }
-
-// A grid has fewer than 2^32 threads along an axis.
-constexpr int64_t kWgsAcross = 1 << 20;
 
 template <typename T, int V, bool STREAM = false>
 hipError_t rope_layout(const dlm_rope& r, int rows, int heads, const void* x, int64_t xr, int64_t xh, void* y,
