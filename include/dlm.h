@@ -647,6 +647,56 @@ dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d
                           void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid);
 
 /*
+ * dlm_cache_step with every row's logits, float [total_rows][vocab] in d_logits (not
+ * NULL), for what the vocabulary reduction does not answer: verification, sampling.
+ */
+dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                                 int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                                 const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                                 void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit,
+                                 int32_t* d_n_invalid, float* d_logits);
+
+/*
+ * Verification of drafted tokens against the target's logits, with given random numbers:
+ * what is kept and drawn is distributed as if the target alone had drawn it.
+ *
+ * Windows are packed as a cache's: row i of sequence s is row d_row_start[s] + i.  Row 0
+ * is a token that is decided (the one drawn last), the others are drafted below it: the
+ * parent of row i is row d_parent[d_row_start[s] + i] of the window, an earlier one, or,
+ * with d_parent NULL, row i - 1.  A row whose parent is no earlier row is never reached.
+ * d_target: logits after each row's token, `vocab` per row of `dtype`, rows
+ * target_stride elements apart; p_r(v) is the softmax of row r's logits / temperature.
+ * d_draft, the same for the distribution q_r that the child of row r was drawn from, or
+ * NULL: drafted tokens are certain, q is 1 for each child's token.  With d_draft, windows
+ * are chains (d_parent NULL).
+ *
+ * From row 0 on, the children of the row r at hand are tried in order of their rows.  Child
+ * i with token x = d_tokens[..i] is kept if d_u[..i] q_r(x) < p_r(x), and then is the row at
+ * hand; if not, p_r becomes max(p_r - q_r, 0) over its sum (certain drafts: p_r without x,
+ * over its sum; p_r as it is where nothing is left).  When no child is left, d_next[s] is
+ * drawn from p_r: the first v at which the running sum passes d_u_next[s] times the whole.
+ * d_u float [total_rows] and d_u_next float [n_seqs] hold numbers in [0, 1) (others are read
+ * as if cut off to it); entries of rows 0 are not read.  temperature 0: p_r is 1 for the
+ * largest logit (the lowest such v), and d_draft is not read.  A token outside [0, vocab) is
+ * never kept.  Logits: -infinity and NaN are chances of 0, +infinity counts as the largest
+ * float32.  Where a row has no chance above 0, d_next is -1, as for a sequence without rows.
+ *
+ * d_keep int32 [total_rows]: the kept rows of each window, row 0 among them, sequence after
+ * sequence, -1 behind them; d_keep_start int32 [n_seqs + 1]: where each begins.  Both are
+ * what dlm_cache_commit takes.  Sums are float64.
+ * Limits: n_seqs <= 65535; total_rows <= 2^20; max_rows <= 1024 (later rows of a window are
+ * not read); vocab <= 2^24; total_rows * (vocab / 8192 + 2) < 2^31.  d_workspace:
+ * dlm_verify_workspace_bytes, 256-byte aligned; it keeps nothing between calls, and calls
+ * that share it must be ordered.
+ */
+size_t dlm_verify_workspace_bytes(int32_t n_seqs, int32_t total_rows, int32_t vocab, int32_t with_draft);
+dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
+                      const int32_t* d_tokens, const int32_t* d_parent, int32_t dtype, int32_t vocab, const void* d_target,
+                      int64_t target_stride, const void* d_draft, int64_t draft_stride, float temperature,
+                      const float* d_u, const float* d_u_next, int32_t* d_next, int32_t* d_keep, int32_t* d_keep_start,
+                      void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Test hooks (same kernels as dlm_refine_step, intermediate results exposed).
  *
  * dlm_debug_forward: forward over d_tokens without the reduction; writes the

@@ -10,7 +10,7 @@ and attention of windows (tokens, trees and blocks of drafted tokens) over it.  
 
 from ._lib import DlmConfig, DlmError, DlmStats, LIB_PATH, load  # noqa: F401
 
-__all__ = ["DlmConfig", "DlmError", "DlmStats", "LIB_PATH", "load", "PagedCache", "Refiner", "Rope", "cascade"]
+__all__ = ["DlmConfig", "DlmError", "DlmStats", "LIB_PATH", "load", "PagedCache", "Refiner", "Rope", "cascade", "verify"]
 
 
 def __getattr__(name):
@@ -23,4 +23,7 @@ def __getattr__(name):
     if name in ("PagedCache", "Rope"):
         from . import cache
         return getattr(cache, name)
+    if name == "verify":
+        from .verification import verify
+        return verify
     raise AttributeError(name)

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdlm.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["init.hip", "gemm.hip", "attention.hip", "elementwise.hip", "moe.hip", "rope.hip", "head_norm.hip",
-           "pages.hip", "paged_attention.hip", "cache.hip", "engine.hip"]
+           "pages.hip", "paged_attention.hip", "verify.hip", "cache.hip", "engine.hip"]
 HOST_SOURCES = ["cache.hip", "engine.hip"]     # the C ABI's host code: what build_host_sanitized() instruments
 ARCH = os.environ.get("DLM_OFFLOAD_ARCH", "gfx950")
 

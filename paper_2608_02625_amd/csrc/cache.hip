@@ -1,5 +1,5 @@
-// C entry points of the rotary positions and of the paged cache (see
-// include/dlm.h): argument checks, sizes, launches.
+// C entry points of the rotary positions, the paged cache and the verification of
+// drafted tokens (see include/dlm.h): argument checks, sizes, launches.
 #include <math.h>
 
 #include <algorithm>
@@ -7,6 +7,7 @@
 
 #include "cache.h"
 #include "status.h"
+#include "verify.h"
 
 namespace {
 
@@ -167,6 +168,14 @@ dlm_status check_append(const dlm_cache* cache, int layer, const int32_t* d_row_
     if ((int64_t)cache->n_seqs * std::max(d_q ? n_heads : 0, cache->n_kv_heads) * std::min(max_rows, total_rows) > ((int64_t)1 << 33))
         return fail(DLM_ERR_INVALID_ARG, "n_seqs * n_heads * max_rows must be at most 2^33");
     return DLM_OK;
+}
+
+std::string check_verify_sizes(int n_seqs, int total_rows, int vocab) {
+    if (n_seqs < 1 || n_seqs > 65535) return "n_seqs must be in [1, 65535]";
+    if (total_rows < 0 || total_rows > (1 << 20)) return "total_rows must be in [0, 2^20]";
+    if (vocab < 1 || vocab > (1 << 24)) return "vocab must be in [1, 2^24]";
+    if (verify_workgroups(total_rows, vocab) > 0x7fffffff) return "total_rows * (vocab / 8192 + 2) must be below 2^31";
+    return "";
 }
 
 }  // namespace
@@ -448,6 +457,67 @@ dlm_status dlm_cache_compact(const dlm_cache* cache, int32_t* d_n_used, void* d_
         TRY(check_cache(cache));
         TRY(check_workspace(d_workspace, workspace_bytes, pages_workspace_bytes(cache->n_seqs, cache->n_pages)));
         return launched(launch_compact(cache_args(*cache), d_n_used, d_workspace, (hipStream_t)hip_stream), "cache_compact");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+size_t dlm_verify_workspace_bytes(int32_t n_seqs, int32_t total_rows, int32_t vocab, int32_t with_draft) {
+    try {
+        if (!check_verify_sizes(n_seqs, total_rows, vocab).empty()) return 0;
+        return verify_workspace_bytes(n_seqs, total_rows, vocab, with_draft != 0);
+    } catch (...) {
+        dlm_internal_caught();
+        return 0;
+    }
+}
+
+dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
+                      const int32_t* d_tokens, const int32_t* d_parent, int32_t dtype, int32_t vocab, const void* d_target,
+                      int64_t target_stride, const void* d_draft, int64_t draft_stride, float temperature,
+                      const float* d_u, const float* d_u_next, int32_t* d_next, int32_t* d_keep, int32_t* d_keep_start,
+                      void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    try {
+        const std::string bad = check_verify_sizes(n_seqs, total_rows, vocab);
+        if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
+        TRY(check_rows(d_row_start, total_rows, max_rows));
+        const int rows = std::min(max_rows, total_rows);
+        if (rows > kVerifyMaxRows) return fail(DLM_ERR_INVALID_ARG, "max_rows must be at most 1024");
+        if (dtype != DLM_BF16 && dtype != DLM_F16 && dtype != DLM_F32) return fail(DLM_ERR_INVALID_ARG, "unknown dtype");
+        if (!(temperature >= 0.f) || !std::isfinite(temperature))
+            return fail(DLM_ERR_INVALID_ARG, "temperature must be finite and >= 0");
+        if (d_draft && d_parent) return fail(DLM_ERR_INVALID_ARG, "with the draft's logits windows are chains: parent must be NULL");
+        if (!d_next || !d_keep_start || !d_u_next) return fail(DLM_ERR_INVALID_ARG, "next, keep_start or u_next is NULL");
+        if (total_rows > 0 && (!d_tokens || !d_target || !d_u || !d_keep))
+            return fail(DLM_ERR_INVALID_ARG, "tokens, target, u or keep is NULL");
+        const size_t size = dtype == DLM_F32 ? 4 : 2;
+        if (!aligned(d_target, size) || !aligned(d_draft, size) || !aligned(d_row_start, 4) || !aligned(d_tokens, 4) ||
+            !aligned(d_parent, 4) || !aligned(d_u, 4) || !aligned(d_u_next, 4) || !aligned(d_next, 4) || !aligned(d_keep, 4) ||
+            !aligned(d_keep_start, 4))
+            return fail(DLM_ERR_INVALID_ARG, "buffers must be aligned to their elements");
+        if (total_rows > 0 && ((total_rows > 1 && target_stride < vocab) || (d_draft && total_rows > 1 && draft_stride < vocab)))
+            return fail(DLM_ERR_INVALID_ARG, "target_stride or draft_stride below a row");
+        const bool drafts = d_draft && temperature > 0.f;
+        TRY(check_workspace(d_workspace, workspace_bytes, verify_workspace_bytes(n_seqs, total_rows, vocab, drafts)));
+        VerifyArgs a{};
+        a.n_seqs = n_seqs;
+        a.total_rows = total_rows;
+        a.max_rows = rows;
+        a.vocab = vocab;
+        a.row_start = d_row_start;
+        a.tokens = d_tokens;
+        a.parent = d_parent;
+        a.target = d_target;
+        a.draft = drafts ? d_draft : nullptr;
+        a.target_stride = target_stride;
+        a.draft_stride = draft_stride;
+        a.c = temperature > 0.f ? 1.4426950408889634 / (double)temperature : 0.0;
+        a.u = d_u;
+        a.u_next = d_u_next;
+        a.next = d_next;
+        a.keep = d_keep;
+        a.keep_start = d_keep_start;
+        return launched(launch_verify(a, dtype, d_workspace, (hipStream_t)hip_stream), "verify");
     } catch (...) {
         return dlm_internal_caught();
     }

@@ -654,7 +654,7 @@ dlm_status run_head(Ctx& x, int32_t* top1, float* conf, float* maxlogit, float* 
         GemmArgs b = gemm_args(x.wt(x.m->plan.lm), c.d_model, hfin, c.d_model, c.vocab, x.R, c.d_model);
         b.out = logits_out;
         b.ldo = c.vocab;
-        TRY(gemm(x, "gemm_logits_debug", b, EPI_F32_T, false, 256, 256, 0));
+        TRY(gemm(x, "gemm_logits", b, EPI_F32_T, false, 256, 256, 0));
     }
     return DLM_OK;
 }
@@ -1375,10 +1375,11 @@ size_t dlm_cache_step_workspace_bytes(const dlm_config* cfg, const dlm_cache* ca
     }
 }
 
-dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
-                          int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
-                          const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
-                          void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid) {
+static dlm_status cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                             int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                             const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                             void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid,
+                             float* d_logits) {
     try {
         if (!m) return fail(DLM_ERR_INVALID_ARG, "model handle is NULL");
         const dlm_config& c = m->cfg;
@@ -1428,7 +1429,7 @@ dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d
         int32_t* top1 = d_top1 ? d_top1 : x.at<int32_t>(plan.w.top1);
         float* conf = d_conf ? d_conf : x.at<float>(plan.w.conf);
         float* mx = d_max_logit ? d_max_logit : x.at<float>(plan.w.maxlogit);
-        TRY(run_head(x, top1, conf, mx, nullptr));
+        TRY(run_head(x, top1, conf, mx, d_logits));
         if (d_n_invalid)
             HIP_TRY(hipMemcpyAsync(d_n_invalid, counters + CNT_INVALID, 4, hipMemcpyDeviceToDevice, x.st));
         HIP_TRY(hipGetLastError());
@@ -1436,6 +1437,30 @@ dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d
     } catch (...) {
         return caught_exception();
     }
+}
+
+dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                          int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                          const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                          void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit, int32_t* d_n_invalid) {
+    return cache_step(m, cache, d_row_start, total_rows, max_rows, max_keys, d_tokens, d_pos, d_mask, mask_words, d_workspace,
+                      workspace_bytes, hip_stream, d_top1, d_conf, d_max_logit, d_n_invalid, nullptr);
+}
+
+dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
+                                 int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
+                                 const uint32_t* d_mask, int32_t mask_words, void* d_workspace, size_t workspace_bytes,
+                                 void* hip_stream, int32_t* d_top1, float* d_conf, float* d_max_logit,
+                                 int32_t* d_n_invalid, float* d_logits) {
+    if (total_rows > 0 && (!d_logits || (uintptr_t)d_logits % 4)) {
+        try {
+            return fail(DLM_ERR_INVALID_ARG, "logits must not be NULL and be 4-byte aligned");
+        } catch (...) {
+            return caught_exception();
+        }
+    }
+    return cache_step(m, cache, d_row_start, total_rows, max_rows, max_keys, d_tokens, d_pos, d_mask, mask_words, d_workspace,
+                      workspace_bytes, hip_stream, d_top1, d_conf, d_max_logit, d_n_invalid, d_logits);
 }
 
 dlm_status dlm_debug_forward(dlm_model* m, int32_t batch, int32_t prompt_len, int32_t draft_len,

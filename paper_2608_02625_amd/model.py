@@ -246,13 +246,14 @@ class Refiner:
 
     def cache_step(self, cache: "PagedCache", tokens: torch.Tensor, row_start: torch.Tensor, max_rows: int,
                    positions: torch.Tensor | None = None, mask: torch.Tensor | None = None, max_keys: int = 0,
-                   n_invalid: torch.Tensor | None = None):
+                   n_invalid: torch.Tensor | None = None, logits: torch.Tensor | None = None):
         """Forward of the packed window rows tokens (int32 [rows]) behind the cache, whose
         reserved places take their keys and values.  row_start int32 [n_seqs + 1];
         positions int32 [rows] (default: the tokens' places); mask int32 [rows, words]:
         the window rows that a row sees (default: all of its window's).  Returns (top-1
         int32, confidence float, max logit float), each [rows]; at most 65536 rows, none is
-        a pass with nothing to do.  Calls of one model share workspaces (kept, so that
+        a pass with nothing to do.  logits: float32 [rows, vocab], takes every row's logits
+        (what verify asks for).  Calls of one model share workspaces (kept, so that
         captured graphs stay valid): order them on one stream."""
         T = tokens.numel()
         if cache.device.index != (self.device.index if self.device.index is not None else torch.cuda.current_device()):
@@ -264,6 +265,9 @@ class Refiner:
         words = 0
         if mask is not None:
             words = _mask_words(mask, T)
+        if logits is not None and (logits.shape != (T, self.cfg.vocab) or logits.dtype is not torch.float32
+                                   or logits.device != device or not logits.is_contiguous()):
+            raise ValueError(f"logits must be a contiguous float32 tensor [{T}, {self.cfg.vocab}] on {device}")
         key = ("cache", T, min(int(max_rows), T), cache.n_seqs)
         ws = self._ws.get(key)
         if ws is None and T == 0 <= int(max_rows):
@@ -283,11 +287,14 @@ class Refiner:
         conf = torch.empty(T, dtype=torch.float32, device=device)
         mx = torch.empty(T, dtype=torch.float32, device=device)
         toks, starts, pos, bits, bad = ints
+        call = [self._handle, ctypes.byref(cache.c), starts, T, int(max_rows), int(max_keys), toks, pos, bits, words,
+                ws.data_ptr(), ws.numel(), torch.cuda.current_stream(device).cuda_stream, top1.data_ptr(), conf.data_ptr(),
+                mx.data_ptr(), bad]
         with torch.cuda.device(device):
-            check(self.lib.dlm_cache_step(self._handle, ctypes.byref(cache.c), starts, T, int(max_rows), int(max_keys),
-                                          toks, pos, bits, words, ws.data_ptr(), ws.numel(),
-                                          torch.cuda.current_stream(device).cuda_stream, top1.data_ptr(),
-                                          conf.data_ptr(), mx.data_ptr(), bad), "dlm_cache_step")
+            if logits is None:
+                check(self.lib.dlm_cache_step(*call), "dlm_cache_step")
+            else:
+                check(self.lib.dlm_cache_step_logits(*call, logits.data_ptr()), "dlm_cache_step_logits")
         return top1, conf, mx
 
     def debug_forward(self, tokens: torch.Tensor, prompt_len: int, want_logits: bool = False,

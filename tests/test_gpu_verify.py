@@ -1,0 +1,366 @@
+"""Verification of drafted tokens on the GPU against the rule in float64 on the CPU.
+
+Outputs are whole numbers and have to be equal.  Both sides compute in float64, so a
+decision can only differ where u q(x) and p(x), or a running sum and its border, are
+within a few thousand 2^-53 of each other: the reference raises if an input comes within
+1e-11 (float32 random numbers against sums of rounded powers do not, but by chance)."""
+
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.gpu_util import need_gpu
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F32 = torch.bfloat16, torch.float16, torch.float32
+NEAR = 1e-11
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    need_gpu()
+
+
+def _verify(*a, **kw):
+    from paper_2608_02625_amd import verify
+    return verify(*a, **kw)
+
+
+def _i32(x):
+    return torch.tensor(np.ascontiguousarray(x, dtype=np.int32), device="cuda")
+
+
+def _chances(z, temperature):
+    z = np.minimum(np.where(np.isnan(z), -np.inf, z.astype(np.float64)), 3.4028234663852886e38)
+    top = z.max()
+    if top == -np.inf:
+        return np.zeros_like(z)
+    if temperature == 0.0:
+        return (np.arange(len(z)) == int(z.argmax())).astype(np.float64)
+    w = np.exp((z - top) / temperature)
+    return w / w.sum()
+
+
+def _unit(u):
+    return min(max(float(np.nan_to_num(u, nan=0.0)), 0.0), 1.0 - 2.0 ** -24)
+
+
+def _less(a, b):
+    if a != b and abs(a - b) <= NEAR * max(abs(a), abs(b)):
+        raise AssertionError("the inputs put a decision on a border")
+    return a < b
+
+
+def reference(starts, tokens, target, u, u_next, parent=None, draft=None, temperature=1.0, max_rows=1024):
+    """(next, keep, keep_start) as the rule reads; target and draft numpy [rows, vocab]."""
+    total, V = target.shape
+    nxt, keep, keep_start = [], [], [0]
+    if temperature == 0.0:
+        draft = None
+    for s in range(len(starts) - 1):
+        a, b = starts[s], min(starts[s + 1], total)
+        n = min(b - a, max_rows) if a >= 0 and b > a else 0
+        token = -1
+        if n:
+            at, path = 0, [0]
+            p = _chances(target[a], temperature)
+            for i in range(1, n):
+                up = i - 1 if parent is None else parent[a + i]
+                if up != at or up >= i:
+                    continue
+                x = tokens[a + i]
+                known = 0 <= x < V
+                if draft is not None:
+                    q = _chances(draft[a + at], temperature)
+                    if known and _less(_unit(u[a + i]) * q[x], p[x]):
+                        at, p = i, _chances(target[a + i], temperature)
+                        path.append(i)
+                        continue
+                    rest = np.maximum(p - q, 0.0)
+                    rest[rest < 1e-16] = 0.0          # p = q but for rounding
+                    if rest.sum() > 0:
+                        p = rest
+                    break
+                if known and _less(_unit(u[a + i]) * p.sum(), p[x]):
+                    at, p = i, _chances(target[a + i], temperature)
+                    path.append(i)
+                elif known:
+                    p[x] = 0.0
+            c = np.cumsum(p)
+            if c[-1] > 0:
+                border = _unit(u_next[s]) * c[-1]
+                token = int(np.searchsorted(c, border, side="right"))
+                near = [abs(c[v] - border) for v in (token - 1, token) if 0 <= v < V]
+                if min(near) <= NEAR * c[-1] and border > 0:
+                    raise AssertionError("the inputs put a draw on a border")
+                token = min(token, V - 1)
+            keep += path
+        nxt.append(token)
+        keep_start.append(len(keep))
+    return nxt, keep + [-1] * (total - len(keep)), keep_start
+
+
+def _layout(t, how):
+    """The same rows with another stride or address."""
+    if how == "dense":
+        return t.cuda()
+    pad = 5 if how == "padded" else 0
+    flat = torch.full((t.shape[0] * (t.shape[1] + pad) + 3,), 99.0, dtype=t.dtype)
+    view = flat[3:].view(t.shape[0], -1)[:, :t.shape[1]]
+    view.copy_(t)
+    flat = flat.cuda()
+    return flat[3:].view(t.shape[0], -1)[:, :t.shape[1]]
+
+
+def _case(seed, rows, V, dtype, shape, temperature=1.0, noise=0.8):
+    g = torch.Generator().manual_seed(seed)
+    starts = [0]
+    for n in rows:
+        starts.append(starts[-1] + n)
+    T = starts[-1]
+    target = (2.0 * torch.randn(T, V, generator=g)).to(dtype)
+    draft = (target.float() + noise * torch.randn(T, V, generator=g)).to(dtype) if shape == "chain" else None
+    rng = np.random.default_rng(seed)
+    parent = []
+    for n in rows:
+        parent += [i - 1 if shape != "tree" else (-1 if i == 0 else int(rng.integers(max(0, i - 4), i))) for i in range(n)]
+    src = (draft if draft is not None else target).double().numpy()
+    tokens = np.zeros(T, dtype=np.int32)
+    for s, n in enumerate(rows):
+        for i in range(1, n):
+            p = _chances(src[starts[s] + parent[starts[s] + i]], temperature or 1.0)
+            tokens[starts[s] + i] = rng.choice(V, p=p / p.sum())
+    u = torch.rand(T, generator=g)
+    u_next = torch.rand(len(rows), generator=g)
+    return dict(starts=starts, tokens=tokens, target=target, u=u, u_next=u_next,
+                parent=np.array(parent, dtype=np.int32) if shape == "tree" else None, draft=draft, temperature=temperature)
+
+
+def _run(c, how="dense", **kw):
+    return _verify(_i32(c["starts"]), _i32(c["tokens"]), _layout(c["target"], how), c["u"].cuda(), c["u_next"].cuda(),
+                   parent=None if c["parent"] is None else _i32(c["parent"]),
+                   draft=None if c["draft"] is None else _layout(c["draft"], how), temperature=c["temperature"], **kw)
+
+
+def _want(c, **kw):
+    return reference(c["starts"], c["tokens"], c["target"].double().numpy(), c["u"].numpy(), c["u_next"].numpy(), c["parent"],
+                     None if c["draft"] is None else c["draft"].double().numpy(), c["temperature"], **kw)
+
+
+def _same(got, want):
+    assert got.next.tolist() == want[0]
+    assert got.keep_start.tolist() == want[2]
+    assert got.keep.tolist() == want[1]
+
+
+VOCABS = [1, 2, 3, 100, 2047, 8184, 8185, 8191, 8192, 8193, 16385, 20001]
+
+
+@pytest.mark.parametrize("shape", ["chain", "certain", "tree"])
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
+@pytest.mark.parametrize("V", VOCABS)
+def test_equal_to_the_rule(V, dtype, shape):
+    rows = [6, 1, 0, 13, 2, 9] if V < 8000 else [5, 1, 0, 9]
+    for k, how in enumerate(("dense", "odd", "padded")):
+        for temperature in (1.0, 0.6):
+            c = _case(V * 7 + k, rows, V, dtype, shape, temperature)
+            _same(_run(c, how), _want(c))
+
+
+@pytest.mark.parametrize("shape,dtype,V,rows", [
+    ("chain", BF, 157184, [8, 5, 1]), ("tree", F32, 157184, [17, 9]), ("tree", HF, 50, [1024, 700, 3]),
+    ("certain", F32, 11, [1024]), ("chain", F32, 40, [3] * 300)])
+def test_large_sizes(shape, dtype, V, rows):
+    c = _case(3, rows, V, dtype, shape)
+    _same(_run(c), _want(c))
+
+
+@pytest.mark.parametrize("shape", ["certain", "tree"])
+def test_greedy(shape):
+    for dtype in (BF, F32):
+        c = _case(11, [7, 30, 1, 0, 12], 3000, dtype, shape, 0.0)
+        c["target"][3, 100] = c["target"][3, 2500] = c["target"][3].max()         # the lowest of equals
+        best = c["target"].float().argmax(1).numpy()
+        for s in range(5):                                                        # drafts that are often right
+            for i in range(c["starts"][s] + 1, c["starts"][s + 1]):
+                up = i - 1 if c["parent"] is None else c["starts"][s] + c["parent"][i]
+                if i % 3:
+                    c["tokens"][i] = best[up]
+        _same(_run(c, "odd"), _want(c))
+        c["draft"] = None if shape == "tree" else torch.randn_like(c["target"].float()).to(dtype)
+        _same(_run(c), _want(c))                                                  # the draft is not read
+
+
+def test_rows_without_chances_and_wild_logits():
+    inf, nan = math.inf, math.nan
+    for shape in ("chain", "certain"):
+        c = _case(5, [4, 4, 4, 4, 2], 700, F32, shape)
+        t = c["target"]
+        t[0] = -inf                                   # nothing may follow the first row
+        t[4] = nan
+        t[8, 5:] = -inf                               # masked to five tokens
+        c["tokens"][9] = 3
+        t[12, 10], t[12, 20] = inf, inf               # both count as the largest float
+        c["tokens"][13] = 20
+        t[16, 7] = nan
+        c["tokens"][17] = 7                           # a token without a chance
+        if shape == "chain":
+            c["draft"][5] = -inf
+            c["draft"][8, 100:] = nan
+            c["draft"][12, 20] = inf
+        want = _want(c)
+        assert want[0][0] == -1 and want[0][1] == -1 and want[2][1] == 1
+        _same(_run(c), want)
+    zero = torch.full((1, 9), -inf)
+    v = _verify(_i32([0, 1]), _i32([0]), zero.cuda(), torch.zeros(1).cuda(), torch.zeros(1).cuda(), temperature=0.0)
+    assert v.next.tolist() == [-1] and v.keep.tolist() == [0] and v.keep_start.tolist() == [0, 1]
+
+
+def test_random_numbers_and_tokens_out_of_range():
+    for shape in ("chain", "certain", "tree"):
+        c = _case(21, [6, 6, 6, 6], 300, HF, shape)
+        c["u"][:6] = torch.tensor([9.0, 1.0, 2.0, -1.0, math.nan, math.inf])
+        c["u_next"] = torch.tensor([1.0, -3.0, math.nan, math.inf])
+        c["tokens"][[7, 14, 20]] = [-1, 300, 1 << 30]
+        _same(_run(c), _want(c))
+    # the largest number in [0, 1) draws the last token that has a chance
+    t = torch.full((1, 9000), -math.inf)
+    t[0, [4, 8500]] = torch.tensor([0.0, -40.0])
+    v = _verify(_i32([0, 1]), _i32([0]), t.cuda(), torch.zeros(1).cuda(), torch.tensor([1.0 - 2.0 ** -24]).cuda())
+    assert v.next.tolist() == [4]                     # e^-40 of the weight lies behind it
+    t[0, 8500] = -10.0
+    v = _verify(_i32([0, 1]), _i32([0]), t.cuda(), torch.zeros(1).cuda(), torch.tensor([1.0 - 2.0 ** -24]).cuda())
+    assert v.next.tolist() == [8500]
+
+
+def test_a_draft_equal_to_the_target_is_kept():
+    c = _case(31, [9, 9, 5], 5000, BF, "chain", noise=0.0)
+    c["u"] = torch.full_like(c["u"], 1.0 - 2.0 ** -24)
+    v = _run(c)
+    assert v.keep_start.tolist() == [0, 9, 18, 23]
+    # a token that neither has: refused, and the next one drawn from the target itself
+    c["target"][:, 17], c["draft"][:, 17] = -math.inf, -math.inf
+    c["tokens"][1] = 17
+    _same(_run(c), _want(c))
+
+
+def test_equal_siblings_and_unsound_parents():
+    c = _case(41, [8, 8, 8], 30, F32, "tree")
+    c["parent"][:8] = [5, 0, 0, 0, 0, 0, 0, 0]
+    c["tokens"][:8] = [3, 4, 4, 4, 9, 4, 9, 2]
+    c["parent"][8:16] = [0, 0, 2, 3, -5, 7, 99, 6]    # of themselves, of none, of later rows
+    c["u"][1:8] = 0.999
+    _same(_run(c), _want(c))
+    # everything that has a chance is refused, but for rounding: what is left is drawn
+    t = torch.full((3, 50), -math.inf)
+    t[0, [3, 40]] = torch.tensor([0.0, -30.0])
+    for u, kept in ((0.5, [0, 1]), (1.0 - 2.0 ** -24, [0, 1])):
+        v = _verify(_i32([0, 3]), _i32([0, 3, 3]), t.cuda(), torch.full((3,), u).cuda(), torch.zeros(1).cuda(),
+                    parent=_i32([-1, 0, 0]))
+        assert v.keep.tolist()[:2] == kept
+
+
+def test_windows_cut_off():
+    c = _case(51, [9, 6, 7], 60, F32, "tree")
+    for max_rows in (1, 4, 9):
+        _same(_run(c, max_rows=max_rows), _want(c, max_rows=max_rows))
+    for starts in ([0, 9, 15, 900], [-4, 9, 15, 22], [0, 9, 5, 22], [22, 22, 22, 22], [3, 9, 15, 20], [9, 0, 0, 0]):
+        c["starts"] = starts
+        want = _want(c)
+        got = _run(c)
+        assert got.next.tolist() == want[0] and got.keep_start.tolist() == want[2]
+        assert got.keep.tolist() == want[1]
+    none = torch.zeros(0, 7, device="cuda")
+    v = _verify(_i32([0, 0, 0]), _i32([]), none, torch.zeros(0).cuda(), torch.zeros(2).cuda())
+    assert v.next.tolist() == [-1, -1] and v.keep.tolist() == [] and v.keep_start.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("shape", ["chain", "certain", "tree"])
+def test_what_comes_out_is_distributed_as_the_target(shape):
+    """The token behind row 0, kept or drawn, over 32768 sequences: each of its counts is
+    binomial, so within 6 of its deviations (a chance of 2e-9 each)."""
+    B, V = 32768, 6
+    g = torch.Generator().manual_seed(7)
+    n = 2 if shape != "tree" else 4
+    z = torch.tensor([0.3, -1.0, 1.2, 0.0, -2.0, 0.9])
+    zq = torch.tensor([1.0, 0.5, -0.4, 0.0, -1.0, 0.2])
+    target = z.repeat(B * n, 1)
+    draft = zq.repeat(B * n, 1) if shape == "chain" else None
+    tokens = torch.multinomial(torch.softmax(zq, 0), B * n, True, generator=g).to(torch.int32)
+    starts = torch.arange(0, B * n + 1, n, dtype=torch.int32)
+    parent = torch.tensor([-1, 0, 0, 0], dtype=torch.int32).repeat(B).cuda() if shape == "tree" else None
+    v = _verify(starts.cuda(), tokens.cuda(), target.cuda(), torch.rand(B * n, generator=g).cuda(),
+                torch.rand(B, generator=g).cuda(), parent=parent, draft=None if draft is None else draft.cuda())
+    count = v.keep_start.cpu().long().diff()
+    keep, first = v.keep.cpu().long(), v.keep_start.cpu().long()[:-1]
+    row = torch.arange(B) * n + torch.where(count > 1, keep[(first + 1).clamp(max=B * n - 1)], 0)
+    out = torch.where(count > 1, tokens[row].long(), v.next.cpu().long())
+    assert 0.05 * B < int((count > 1).sum()) < 0.95 * B
+    p = torch.softmax(z.double(), 0)
+    seen = torch.bincount(out, minlength=V).double()
+    assert ((seen - B * p).abs() <= 6 * (B * p * (1 - p)).sqrt()).all(), (seen / B, p)
+
+
+def test_kept_rows_go_into_commit():
+    from paper_2608_02625_amd import PagedCache
+    c = PagedCache(1, 32, 16, 1, 64, 3, 8)
+    case = _case(61, [6, 0, 9], 40, F32, "tree")
+    starts = _i32(case["starts"])
+    assert bool(c.reserve(starts).all())
+    rows = torch.arange(15, dtype=torch.float32, device="cuda").view(15, 1, 1).expand(15, 1, 64).contiguous().to(BF)
+    c.append(0, rows, rows, starts, 9)
+    v = _run(case)
+    assert c.commit(starts, v.keep, v.keep_start).tolist() == [1, 1, 1]
+    want = _want(case)
+    for s in (0, 2):
+        path = want[1][want[2][s]:want[2][s + 1]]
+        assert c.len[s].item() == len(path)
+        page = c.table[s, 0].item()
+        assert c.k[0, page, 0, :len(path), 0].tolist() == [case["starts"][s] + i for i in path]
+
+
+def test_another_stream_and_a_graph():
+    c = _case(71, [8, 3, 0, 5], 9001, BF, "chain")
+    args = (_i32(c["starts"]), _i32(c["tokens"]), c["target"].cuda(), c["u"].cuda(), c["u_next"].cuda())
+    draft = c["draft"].cuda()
+    want = _want(c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _verify(*args, draft=draft)
+    side.synchronize()
+    _same(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = _verify(*args, draft=draft)
+    for k in range(3):
+        c["u"], c["u_next"] = c["u"].roll(1), (c["u_next"] + 0.3) % 1.0
+        args[3].copy_(c["u"])
+        args[4].copy_(c["u_next"])
+        graph.replay()
+        torch.cuda.synchronize()
+        _same(held, _want(c))
+        _same(_verify(*args, draft=draft), _want(c))
+
+
+def test_refusals_of_the_binding():
+    c = _case(81, [3, 2], 20, F32, "certain")
+    a = [_i32(c["starts"]), _i32(c["tokens"]), c["target"].cuda(), c["u"].cuda(), c["u_next"].cuda()]
+    from paper_2608_02625_amd import DlmError
+    for i, bad in ((0, a[0].long()), (1, a[1].cpu()), (2, a[2].double()), (2, a[2][:4]), (2, a[2].t().contiguous().t()),
+                   (3, a[3][:3]), (3, a[3].half()), (4, a[3])):
+        args = list(a)
+        args[i] = bad
+        with pytest.raises(ValueError):
+            _verify(*args)
+    with pytest.raises(ValueError):
+        _verify(*a, draft=a[2].half())
+    for kw in (dict(temperature=-1.0), dict(temperature=math.nan), dict(max_rows=-1), dict(max_rows=0),
+               dict(parent=a[1], draft=a[2])):
+        with pytest.raises(DlmError):
+            _verify(*a, **kw)
