@@ -588,6 +588,33 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
                             float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Attention of sequences that begin with the same pages (copies of dlm_cache_fork), which
+ * reads what they share once for all of them.
+ *
+ * dlm_cache_share: d_group int32 [n_seqs] says which sequences belong together (numbers in
+ * [0, n_seqs); others: a sequence by itself).  What the members with rows have in common
+ * is found in their tables: the pages at the front that all of them name and count whole,
+ * in multiples of 32 tokens.  max_group_rows: an upper bound of the rows of a group that the
+ * caller vouches for; a group of more rows shares nothing, nor does one with a single member.
+ * d_share (dlm_cache_share_bytes(cache, total_rows) bytes, 256-byte aligned) takes what was
+ * found.  It holds for these row starts as long as lengths and tables stay as they are, that
+ * is for all layers of a pass: make it after reserve.
+ * dlm_cache_attend_shared: dlm_cache_attend with d_share, in the same total_rows, max_rows and
+ * max_group_rows; the results are the same but for the order of sums.
+ */
+size_t dlm_cache_share_bytes(const dlm_cache* cache, int32_t total_rows);
+dlm_status dlm_cache_share(const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
+                           const int32_t* d_group, int32_t max_group_rows, void* d_share, size_t share_bytes,
+                           void* hip_stream);
+size_t dlm_cache_shared_workspace_bytes(const dlm_cache* cache, int32_t total_rows, int32_t max_rows,
+                                        int32_t max_group_rows, int32_t n_heads);
+dlm_status dlm_cache_attend_shared(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                                   int32_t max_rows, int32_t max_group_rows, int32_t max_keys, const void* d_share,
+                                   size_t share_bytes, int32_t n_heads, const void* d_q, int64_t q_stride,
+                                   const uint32_t* d_mask, int32_t mask_words, float scale, void* d_o, int64_t o_stride,
+                                   float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * End of a pass: of a sequence's window the rows d_keep[d_keep_start[s]] ..
  * (rising, d_keep_start int32 [n_seqs + 1] within 0 .. total_keep) become its
  * next tokens, in every layer, and the pages behind them are freed.  d_keep and

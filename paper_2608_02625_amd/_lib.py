@@ -132,6 +132,11 @@ SIGNATURES = [
     ("dlm_cache_append_norm", _I, [_CACHE, _I, _P, _I, _I, _I, _P, _L, _P, _L, _ROPE, _P, _I, _P, _L, _P, _L, _I, _P, _P,
                                    _F, _P]),
     ("dlm_cache_attend", _I, [_CACHE, _I, _P, _I, _I, _I, _I, _P, _L, _P, _I, _F, _P, _L, _P, _P, _SZ, _P]),
+    ("dlm_cache_share_bytes", _SZ, [_CACHE, _I]),
+    ("dlm_cache_share", _I, [_CACHE, _P, _I, _I, _P, _I, _P, _SZ, _P]),
+    ("dlm_cache_shared_workspace_bytes", _SZ, [_CACHE, _I, _I, _I, _I]),
+    ("dlm_cache_attend_shared", _I, [_CACHE, _I, _P, _I, _I, _I, _I, _P, _SZ, _I, _P, _L, _P, _I, _F, _P, _L, _P, _P, _SZ,
+                                     _P]),
     ("dlm_cache_commit", _I, [_CACHE, _P, _I, _P, _P, _I, _P, _P]),
     ("dlm_cache_fork", _I, [_CACHE, _I, _P, _P, _P, _P]),
     ("dlm_cache_truncate", _I, [_CACHE, _P, _P]),

@@ -251,6 +251,17 @@ class _Rotation(torch.autograd.Function):
         return ctx.rope.apply(grad, ctx.saved_tensors[0], transpose=not ctx.transpose), None, None, None
 
 
+class Share:
+    """What groups of sequences have in common (PagedCache.share), for the attention of one
+    pass."""
+
+    __slots__ = ("cache", "epoch", "rows", "max_rows", "max_group_rows", "data")
+
+    def __init__(self, cache: "PagedCache", rows: int, max_rows: int, max_group_rows: int, data: torch.Tensor):
+        self.cache, self.epoch, self.data = cache, cache._epoch, data
+        self.rows, self.max_rows, self.max_group_rows = rows, max_rows, max_group_rows
+
+
 class PagedCache:
     """A paged key/value cache: n_pages pages of page_len tokens in n_layers layers,
     shared by n_seqs sequences of up to max_pages pages.
@@ -297,6 +308,7 @@ class PagedCache:
         self._ref = ctypes.byref(c)
         self._n_seqs, self._kv, self._hd, self._kind = int(n_seqs), int(n_kv_heads), int(head_dim), _DTYPES[dtype]
         self._ws, self._by_size = {}, {}
+        self._epoch = 0                                   # of lengths and tables
         self.reset()
 
     # -------------------------------------------------------------- plumbing
@@ -306,12 +318,14 @@ class PagedCache:
 
     def workspace(self, total_rows: int = 0, max_rows: int = 0, n_heads: int = 0) -> torch.Tensor:
         """Workspace of calls with these sizes; kept, so that captured graphs stay valid."""
-        key = (total_rows, max_rows, n_heads)
+        return self._workspace((total_rows, max_rows, n_heads), self.lib.dlm_cache_workspace_bytes)
+
+    def _workspace(self, key: tuple, size) -> torch.Tensor:
         ws = self._ws.get(key)
         if ws is None:
-            n = self.lib.dlm_cache_workspace_bytes(self._ref, total_rows, max_rows, n_heads)
+            n = size(self._ref, *key)
             if n == 0:
-                raise ValueError(f"invalid sizes: {total_rows} rows, {max_rows} at most, {n_heads} heads")
+                raise ValueError(f"invalid sizes: {key[0]} rows, {key[1]} at most, {key[-1]} heads")
             ws = self._by_size.get(n)
             if ws is None:
                 ws = self._by_size[n] = torch.empty(n, dtype=torch.uint8, device=self.device)
@@ -321,13 +335,18 @@ class PagedCache:
     def _call(self, name: str, *args):
         _launch(getattr(self.lib, name), name, self.device.index, self._ref, *args)
 
+    def _change(self, name: str, *args):
+        """A call that changes lengths or tables."""
+        self._epoch += 1
+        self._call(name, *args)
+
     def _starts(self, row_start: torch.Tensor) -> int:
         return _ints(row_start, "row_start", self._n_seqs + 1, self.device)
 
     # -------------------------------------------------------------- pages
     def reset(self):
         """Empty every sequence, free every page."""
-        self._call("dlm_cache_reset")
+        self._change("dlm_cache_reset")
 
     def reserve(self, row_start: torch.Tensor, total_rows: int | None = None) -> torch.Tensor:
         """Room for the windows' rows; ok int32 [n_seqs].  total_rows: rows that count
@@ -335,7 +354,7 @@ class PagedCache:
         starts = self._starts(row_start)
         ok = torch.empty(self._n_seqs, dtype=torch.int32, device=self.device)
         ws = self.workspace()
-        self._call("dlm_cache_reserve", starts, 1 << 24 if total_rows is None else int(total_rows), ok.data_ptr(),
+        self._change("dlm_cache_reserve", starts, 1 << 24 if total_rows is None else int(total_rows), ok.data_ptr(),
                    ws.data_ptr(), ws.numel())
         return ok
 
@@ -350,7 +369,7 @@ class PagedCache:
         n_keep = 0 if keep is None else keep.numel()
         if keep is not None and n_keep == 0:
             kept = starts                                 # an empty list has no address; nothing of it is read
-        self._call("dlm_cache_commit", starts, 1 << 24 if total_rows is None else int(total_rows), kept, kept_start,
+        self._change("dlm_cache_commit", starts, 1 << 24 if total_rows is None else int(total_rows), kept, kept_start,
                    n_keep, ok.data_ptr())
         return ok
 
@@ -359,18 +378,18 @@ class PagedCache:
         n = src.numel()
         a, b = _ints(src, "src", None, self.device), _ints(dst, "dst", n, self.device)
         ok = torch.empty(n, dtype=torch.int32, device=self.device)
-        self._call("dlm_cache_fork", n, a, b, ok.data_ptr())
+        self._change("dlm_cache_fork", n, a, b, ok.data_ptr())
         return ok
 
     def truncate(self, new_len: torch.Tensor | None = None):
         """Keep at most new_len[s] tokens of sequence s (negative: leave it; None: 0 for all)."""
-        self._call("dlm_cache_truncate", _ints(new_len, "new_len", self._n_seqs, self.device))
+        self._change("dlm_cache_truncate", _ints(new_len, "new_len", self._n_seqs, self.device))
 
     def compact(self) -> torch.Tensor:
         """Move the pages in use to the lowest ids; int32 [1], how many there are."""
         used = torch.empty(1, dtype=torch.int32, device=self.device)
         ws = self.workspace()
-        self._call("dlm_cache_compact", used.data_ptr(), ws.data_ptr(), ws.numel())
+        self._change("dlm_cache_compact", used.data_ptr(), ws.data_ptr(), ws.numel())
         return used
 
     # -------------------------------------------------------------- windows
@@ -418,12 +437,32 @@ class PagedCache:
             self._call("dlm_cache_append_norm", *call, q_type if q_gain is not None else k_type, qg, kg, norm_eps)
         return q_out
 
+    def share(self, row_start: torch.Tensor, groups: torch.Tensor, rows: int, max_rows: int,
+              max_group_rows: int | None = None) -> Share:
+        """What groups of sequences (int32 [n_seqs], a number per sequence in [0, n_seqs);
+        others: by itself) have in common at the front of their tables, for attend in every
+        layer of a pass: rows in all, at most max_rows of a sequence and max_group_rows of a
+        group (default: all).  It stands until lengths or tables change (a group with more
+        rows than it says shares nothing)."""
+        starts = self._starts(row_start)
+        group = _ints(groups, "groups", self._n_seqs, self.device)
+        rows, max_rows = int(rows), int(max_rows)
+        most = rows if max_group_rows is None else int(max_group_rows)
+        n = self.lib.dlm_cache_share_bytes(self._ref, rows)
+        if n == 0:
+            raise ValueError(f"invalid number of rows: {rows}")
+        data = torch.empty(n, dtype=torch.uint8, device=self.device)
+        self._call("dlm_cache_share", starts, rows, max_rows, group, most, data.data_ptr(), n)
+        return Share(self, rows, max_rows, most, data)
+
     def attend(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int,
                mask: torch.Tensor | None = None, max_keys: int = 0, scale: float = 0.0,
-               out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
+               out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+               share: Share | None = None) -> torch.Tensor:
         """Attention of the windows' rows q [rows, heads, head_dim] over their sequences'
         tokens and the window rows whose bits are set in mask (int32 [rows, words];
-        None: all of them)."""
+        None: all of them).  share: what groups of sequences have in common is read once for
+        each group (made for these windows, lengths and tables)."""
         device = self.device
         starts = self._starts(row_start)
         T, heads, qs = _rows(q, "q", None, self._hd, device)
@@ -439,6 +478,18 @@ class PagedCache:
         if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, heads) or not lse.is_contiguous()
                                 or lse.device != device):
             raise ValueError("lse must be a contiguous float32 tensor [rows, heads]")
+        if share is not None:
+            if share.cache is not self or share.rows != T or share.max_rows != max_rows:
+                raise ValueError("share was made for another cache or for other windows")
+            if share.epoch != self._epoch:
+                raise ValueError("lengths or tables have changed since share was made")
+            if T:
+                most = share.max_group_rows
+                ws = self._workspace((T, max_rows, most, heads), self.lib.dlm_cache_shared_workspace_bytes)
+                self._call("dlm_cache_attend_shared", layer, starts, T, max_rows, most, max_keys, share.data.data_ptr(),
+                           share.data.numel(), heads, q.data_ptr(), qs, bits, words, scale, out.data_ptr(), os,
+                           None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel())
+            return out
         if T:
             ws = self.workspace(T, max_rows, heads)
             self._call("dlm_cache_attend", layer, starts, T, max_rows, max_keys, heads, q.data_ptr(), qs, bits, words, scale,

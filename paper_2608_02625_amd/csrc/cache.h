@@ -67,3 +67,14 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
                          int max_rows, int max_keys, int n_heads, const void* q, int64_t q_stride,
                          const uint32_t* mask, int mask_words, float scale, void* o, int64_t o_stride, float* lse,
                          void* ws, hipStream_t st);
+// What the sequences of a group share (its words are paged_attention.hip's own), and
+// attention that reads it once per group.
+size_t share_bytes(int n_seqs, int total_rows);
+hipError_t launch_share(const CacheArgs& c, const int32_t* row_start, int total_rows, int max_rows, const int32_t* group,
+                        int max_group_rows, int32_t* share, hipStream_t st);
+size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int max_group_rows,
+                                     int group);
+hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
+                                int max_rows, int max_group_rows, int max_keys, const int32_t* share, int n_heads,
+                                const void* q, int64_t q_stride, const uint32_t* mask, int mask_words, float scale, void* o,
+                                int64_t o_stride, float* lse, void* ws, hipStream_t st);

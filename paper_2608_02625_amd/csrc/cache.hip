@@ -170,6 +170,42 @@ dlm_status check_append(const dlm_cache* cache, int layer, const int32_t* d_row_
     return DLM_OK;
 }
 
+// What the two forms of attend ask for; *nothing: no rows.
+dlm_status check_attend(const dlm_cache* cache, int layer, const int32_t* d_row_start, int total_rows, int max_rows,
+                        int max_keys, int n_heads, const void* d_q, int64_t q_stride, const uint32_t* d_mask, int mask_words,
+                        float scale, const void* d_o, int64_t o_stride, const float* d_lse, bool* nothing) {
+    TRY(check_cache(cache));
+    if (layer < 0 || layer >= cache->n_layers) return fail(DLM_ERR_INVALID_ARG, "layer out of range");
+    TRY(check_rows(d_row_start, total_rows, max_rows));
+    if (n_heads < 1 || n_heads % cache->n_kv_heads) return fail(DLM_ERR_INVALID_ARG, "n_heads must be a positive multiple of n_kv_heads");
+    if (max_keys < 0) return fail(DLM_ERR_INVALID_ARG, "max_keys must be >= 0");
+    if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(DLM_ERR_INVALID_ARG, "scale must be finite and >= 0");
+    *nothing = total_rows == 0;
+    if (*nothing) return DLM_OK;
+    if (!d_q || !d_o) return fail(DLM_ERR_INVALID_ARG, "q or o is NULL");
+    const int rows = std::min(max_rows, total_rows);
+    const int64_t width = (int64_t)n_heads * cache->head_dim;
+    if (q_stride < width || o_stride < width) return fail(DLM_ERR_INVALID_ARG, "q_stride or o_stride below a row");
+    if (!aligned(d_q, 16) || !aligned(d_o, 16) || q_stride % 8 || o_stride % 8)
+        return fail(DLM_ERR_INVALID_ARG, "q and o must be 16-byte aligned, with strides that are multiples of 8");
+    if (d_q == d_o && q_stride != o_stride) return fail(DLM_ERR_INVALID_ARG, "in place, q and o must have the same stride");
+    if (d_mask && (!aligned(d_mask, 4) || (int64_t)mask_words * 32 < rows))
+        return fail(DLM_ERR_INVALID_ARG, "mask must be 4-byte aligned and hold max_rows bits per row");
+    if (d_lse && !aligned(d_lse, 4)) return fail(DLM_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+    const std::string bad = dlm_internal_check_windows(*cache, n_heads, rows);
+    if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
+    return DLM_OK;
+}
+
+dlm_status check_share(const dlm_cache& c, int total_rows, int max_group_rows, const void* share, size_t bytes) {
+    if (max_group_rows < 0) return fail(DLM_ERR_INVALID_ARG, "max_group_rows must be >= 0");
+    if (!share || !aligned(share, 256)) return fail(DLM_ERR_INVALID_ARG, "share must not be NULL and be 256-byte aligned");
+    const size_t need = share_bytes(c.n_seqs, total_rows);
+    if (bytes < need)
+        return fail(DLM_ERR_WORKSPACE, "share too small: need " + std::to_string(need) + " bytes, got " + std::to_string(bytes));
+    return DLM_OK;
+}
+
 std::string check_verify_sizes(int n_seqs, int total_rows, int vocab) {
     if (n_seqs < 1 || n_seqs > 65535) return "n_seqs must be in [1, 65535]";
     if (total_rows < 0 || total_rows > (1 << 20)) return "total_rows must be in [0, 2^20]";
@@ -383,26 +419,11 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
                             const uint32_t* d_mask, int32_t mask_words, float scale, void* d_o, int64_t o_stride,
                             float* d_lse, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     try {
-        TRY(check_cache(cache));
-        if (layer < 0 || layer >= cache->n_layers) return fail(DLM_ERR_INVALID_ARG, "layer out of range");
-        TRY(check_rows(d_row_start, total_rows, max_rows));
-        if (n_heads < 1 || n_heads % cache->n_kv_heads) return fail(DLM_ERR_INVALID_ARG, "n_heads must be a positive multiple of n_kv_heads");
-        if (max_keys < 0) return fail(DLM_ERR_INVALID_ARG, "max_keys must be >= 0");
-        if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(DLM_ERR_INVALID_ARG, "scale must be finite and >= 0");
-        if (total_rows == 0) return DLM_OK;
-        if (!d_q || !d_o) return fail(DLM_ERR_INVALID_ARG, "q or o is NULL");
-        const int rows = std::min(max_rows, total_rows);
-        const int64_t width = (int64_t)n_heads * cache->head_dim;
-        if (q_stride < width || o_stride < width) return fail(DLM_ERR_INVALID_ARG, "q_stride or o_stride below a row");
-        if (!aligned(d_q, 16) || !aligned(d_o, 16) || q_stride % 8 || o_stride % 8)
-            return fail(DLM_ERR_INVALID_ARG, "q and o must be 16-byte aligned, with strides that are multiples of 8");
-        if (d_q == d_o && q_stride != o_stride) return fail(DLM_ERR_INVALID_ARG, "in place, q and o must have the same stride");
-        if (d_mask && (!aligned(d_mask, 4) || (int64_t)mask_words * 32 < rows))
-            return fail(DLM_ERR_INVALID_ARG, "mask must be 4-byte aligned and hold max_rows bits per row");
-        if (d_lse && !aligned(d_lse, 4)) return fail(DLM_ERR_INVALID_ARG, "lse must be 4-byte aligned");
-        const int group = n_heads / cache->n_kv_heads;
-        const std::string bad = dlm_internal_check_windows(*cache, n_heads, rows);
-        if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
+        bool nothing;
+        TRY(check_attend(cache, layer, d_row_start, total_rows, max_rows, max_keys, n_heads, d_q, q_stride, d_mask, mask_words,
+                         scale, d_o, o_stride, d_lse, &nothing));
+        if (nothing) return DLM_OK;
+        const int rows = std::min(max_rows, total_rows), group = n_heads / cache->n_kv_heads;
         TRY(check_workspace(d_workspace, workspace_bytes,
                             attend_workspace_bytes(cache->n_seqs, cache->n_kv_heads, cache->head_dim, total_rows, rows, group)));
         const int keys = (int)std::min<int64_t>(max_keys ? max_keys : capacity(*cache), capacity(*cache));
@@ -410,6 +431,74 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
                                       d_q, q_stride, d_mask, d_mask ? mask_words : 0,
                                       scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim), d_o, o_stride, d_lse,
                                       d_workspace, (hipStream_t)hip_stream), "cache_attend");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+size_t dlm_cache_share_bytes(const dlm_cache* cache, int32_t total_rows) {
+    try {
+        if (!check_shape(cache).empty() || total_rows < 0 || total_rows > (1 << 24)) return 0;
+        return share_bytes(cache->n_seqs, total_rows);
+    } catch (...) {
+        dlm_internal_caught();
+        return 0;
+    }
+}
+
+dlm_status dlm_cache_share(const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
+                           const int32_t* d_group, int32_t max_group_rows, void* d_share, size_t bytes, void* hip_stream) {
+    try {
+        TRY(check_cache(cache));
+        TRY(check_rows(d_row_start, total_rows, max_rows));
+        TRY(check_share(*cache, total_rows, max_group_rows, d_share, bytes));
+        if (!d_group || !aligned(d_group, 4)) return fail(DLM_ERR_INVALID_ARG, "group must not be NULL and be 4-byte aligned");
+        return launched(launch_share(cache_args(*cache), d_row_start, total_rows, std::min(max_rows, total_rows), d_group,
+                                     std::min(max_group_rows, total_rows), (int32_t*)d_share, (hipStream_t)hip_stream),
+                        "cache_share");
+    } catch (...) {
+        return dlm_internal_caught();
+    }
+}
+
+size_t dlm_cache_shared_workspace_bytes(const dlm_cache* c, int32_t total_rows, int32_t max_rows, int32_t max_group_rows,
+                                        int32_t n_heads) {
+    try {
+        if (max_group_rows < 0 || dlm_cache_workspace_bytes(c, total_rows, max_rows, n_heads) == 0) return 0;
+        const size_t pages = pages_workspace_bytes(c->n_seqs, c->n_pages);
+        if (total_rows == 0 || max_rows == 0 || n_heads == 0) return pages;
+        return std::max(pages, attend_shared_workspace_bytes(c->n_seqs, c->n_kv_heads, c->head_dim, total_rows,
+                                                             std::min(max_rows, total_rows),
+                                                             std::min(max_group_rows, total_rows), n_heads / c->n_kv_heads));
+    } catch (...) {
+        dlm_internal_caught();
+        return 0;
+    }
+}
+
+dlm_status dlm_cache_attend_shared(const dlm_cache* cache, int32_t layer, const int32_t* d_row_start, int32_t total_rows,
+                                   int32_t max_rows, int32_t max_group_rows, int32_t max_keys, const void* d_share,
+                                   size_t bytes, int32_t n_heads, const void* d_q, int64_t q_stride, const uint32_t* d_mask,
+                                   int32_t mask_words, float scale, void* d_o, int64_t o_stride, float* d_lse,
+                                   void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    try {
+        bool nothing;
+        TRY(check_attend(cache, layer, d_row_start, total_rows, max_rows, max_keys, n_heads, d_q, q_stride, d_mask, mask_words,
+                         scale, d_o, o_stride, d_lse, &nothing));
+        if (nothing) return DLM_OK;
+        const int rows = std::min(max_rows, total_rows), group = n_heads / cache->n_kv_heads;
+        TRY(check_share(*cache, total_rows, max_group_rows, d_share, bytes));
+        const int group_rows = std::min(max_group_rows, total_rows);
+        const std::string bad = dlm_internal_check_windows(*cache, n_heads, group_rows);
+        if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
+        TRY(check_workspace(d_workspace, workspace_bytes,
+                            attend_shared_workspace_bytes(cache->n_seqs, cache->n_kv_heads, cache->head_dim, total_rows, rows,
+                                                          group_rows, group)));
+        const int keys = (int)std::min<int64_t>(max_keys ? max_keys : capacity(*cache), capacity(*cache));
+        return launched(launch_attend_shared(cache_args(*cache), cache->dtype, layer, d_row_start, total_rows, rows, group_rows,
+                                             keys, (const int32_t*)d_share, n_heads, d_q, q_stride, d_mask,
+                                             d_mask ? mask_words : 0, scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim),
+                                             d_o, o_stride, d_lse, d_workspace, (hipStream_t)hip_stream), "cache_attend_shared");
     } catch (...) {
         return dlm_internal_caught();
     }

@@ -175,13 +175,38 @@ struct AttnArgs {
     int max_slots;                            // places for parts; enough for any sound row starts
     float* part_o;                            // [max_slots][rows_per_wg][head_dim]
     float2* part_ml;                          // [max_slots][rows_per_wg]
+    // Shared prefixes (kPrefix, kSuffix): what cache_share wrote, and what the prefixes
+    // leave of each row, [total_rows][n_heads].
+    const int4* groups;                       // [n_seqs]: leader, prefix, first entry of rows, rows
+    const int32_t* skip;                      // [n_seqs]: the prefix that the group's pass reads
+    const int32_t* rows;                      // [total_rows]: the groups' rows
+    float* pre_o;
+    float2* pre_ml;
 };
+
+// What a launch attends to: a sequence's keys; the prefix that the sequences of a group
+// share, for the rows of all of them; a sequence's keys behind its group's prefix, joined
+// with what the prefix left.
+enum Mode { kPlain, kPrefix, kSuffix };
 
 struct Seq {
     int n, start, len, keys;                  // rows, first packed row, tokens before, keys in all
+    int first;                                // first key, a multiple of a tile
+    int table;                                // its table row
 };
+template <int MODE>
 __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
-    Seq s{0, 0, 0, 0};
+    Seq s{0, 0, 0, 0, 0, b};
+    if constexpr (MODE == kPrefix) {
+        if (b < a.c.n_seqs) {
+            const int4 g = a.groups[b];
+            s.table = min(max(g.x, 0), a.c.n_seqs - 1);
+            s.start = max(g.z, 0);
+            s.n = min(max(g.w, 0), a.max_rows);
+            s.len = s.keys = min(max(g.y, 0), a.max_keys) & ~(kTile - 1);     // as kSuffix's first
+        }
+        return s;
+    }
     if (b < a.c.n_seqs) {
         s.start = a.row_start[b];
         const int end = min(a.row_start[b + 1], a.total_rows);
@@ -189,8 +214,18 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
         s.n = s.start >= 0 && end > s.start ? min(end - s.start, a.max_rows) : 0;
         s.len = max(a.c.len[b], 0);
         s.keys = (int)min((int64_t)s.len + s.n, (int64_t)a.max_keys);
+        if constexpr (MODE == kSuffix) s.first = min(max(a.skip[b], 0), s.keys) & ~(kTile - 1);
     }
     return s;
+}
+// Packed row of row i of a sequence or a group.
+template <int MODE>
+__device__ __forceinline__ int64_t packed_row(const AttnArgs& a, const Seq& s, uint32_t i) {
+    if constexpr (MODE == kPrefix) {
+        const int64_t at = min((int64_t)s.start + i, (int64_t)a.total_rows - 1);
+        return min(max(a.rows[at], 0), a.total_rows - 1);
+    }
+    return (int64_t)s.start + i;
 }
 
 // What a wave works out about one unit, or one split item, of the list.
@@ -227,21 +262,21 @@ __device__ __forceinline__ int from_lane(int v, int l) {
 // The index-th unit (or, with `items`, the index-th item of several parts) in the
 // order sequence, key head, part, row tile; false if there are fewer.  A lane
 // looks after a sequence, 64 at a time.
-template <bool ITEMS>
+template <bool ITEMS, int MODE>
 __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u) {
     const int lane = threadIdx.x & 63;
     auto shape = [&](const Seq& s, int& tiles, int& steps) {
         tiles = (s.n * a.group + a.rows_per_wg - 1) >> a.rows_log2;
-        steps = max((s.keys + a.step - 1) >> a.step_log2, 1);
+        steps = max((s.keys - s.first + a.step - 1) >> a.step_log2, 1);
     };
-    const Seq first = sequence(a, lane);
+    const Seq first = sequence<MODE>(a, lane);
     // Steps of all items: float32, since row starts that overlap may make more of them
     // than an int holds, and what follows needs no more than its bound (max_slots).
     float sum = 0.f;
     int items = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
-        shape(b0 ? sequence(a, b0 + lane) : first, tiles, steps);
+        shape(b0 ? sequence<MODE>(a, b0 + lane) : first, tiles, steps);
         sum += wave_sum_dpp((float)tiles * (float)steps * (float)a.c.n_kv);
         items += from_lane(wave_scan(tiles * a.c.n_kv), 63);
     }
@@ -252,7 +287,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
     int before = 0, slots_before = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
-        const Seq s = b0 ? sequence(a, b0 + lane) : first;
+        const Seq s = b0 ? sequence<MODE>(a, b0 + lane) : first;
         shape(s, tiles, steps);
         const int parts = (int)((uint32_t)(steps + most - 1) / (uint32_t)most);
         const int all = tiles * a.c.n_kv * parts, split = parts > 1 ? all : 0;
@@ -266,6 +301,8 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             u.s.start = from_lane(s.start, l);
             u.s.len = from_lane(s.len, l);
             u.s.keys = from_lane(s.keys, l);
+            u.s.first = MODE == kSuffix ? from_lane(s.first, l) : 0;
+            u.s.table = MODE == kPrefix ? from_lane(s.table, l) : u.b;
             u.parts = from_lane(parts, l);
             const int n_tiles = from_lane(tiles, l);
             const int all_steps = from_lane(steps, l);
@@ -282,7 +319,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             // slots of an item's parts lie next to each other
             u.slot = slot0 + (u.kvh * n_tiles + u.row_tile) * u.parts + part;
             const int each = (int)((uint32_t)(all_steps + u.parts - 1) / (uint32_t)u.parts) << (a.step_log2 - 5);
-            u.t0 = uniform(part * each);
+            u.t0 = uniform((MODE == kSuffix ? u.s.first / kTile : 0) + part * each);
             u.t1 = uniform(min(u.t0 + each, (u.s.keys + kTile - 1) / kTile));
             return u.parts == 1 || u.slot + u.parts - part <= a.max_slots;
         }
@@ -319,7 +356,7 @@ struct Keys {
         k = a.c.k + a.layer_base + (int64_t)u.kvh * head;
         v = a.c.v + a.layer_base + (int64_t)u.kvh * head;
         page_bytes = head * a.c.n_kv;                     // at most 4 MB
-        table = a.c.table + (int64_t)u.b * a.c.max_pages;
+        table = a.c.table + (int64_t)u.s.table * a.c.max_pages;
         keys = u.s.keys;
         n_pages = a.c.n_pages;
         max_pages = a.c.max_pages;
@@ -614,7 +651,7 @@ __device__ __forceinline__ int k_turn(int row) {          // of a chunk's number
     return HD == 128 ? row & 3 : (row >> 1) & 3;
 }
 
-template <bool F16, int HD, bool ONCE, int WK>
+template <bool F16, int HD, bool ONCE, int WK, int MODE>
 __global__ __launch_bounds__(256 * WK) __attribute__((amdgpu_waves_per_eu(WK == 1 ? 3 : 2))) void
 attend_many_kernel(const AttnArgs a) {
     using D = Dims<HD>;
@@ -632,12 +669,12 @@ attend_many_kernel(const AttnArgs a) {
     // Neighbouring units share their keys (row tiles): workgroups go to the 8 XCDs
     // in turn, so each XCD takes runs of 8 units.
     const int wg = blockIdx.x;
-    if (!find_unit<false>(a, (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7), u)) return;
+    if (!find_unit<false, MODE>(a, (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7), u)) return;
     const int rows = min(u.s.n * a.group - u.row_tile * kManyRows, kManyRows);           // of this workgroup
     const bool busy = wave * 32 < rows;                   // this wave has rows
     const int r = min(wave * 32 + j, rows - 1) + u.row_tile * kManyRows;
     const int head = u.kvh * a.group + (int)((uint32_t)r % (uint32_t)a.group);
-    const int64_t t = (int64_t)u.s.start + (uint32_t)r / (uint32_t)a.group;   // packed row
+    const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)r / (uint32_t)a.group);
     Keys<HD> keys(a, u);
 
     // Copies: lane L of copy p reads the chunk that belongs at byte 16 L of its 1 KB
@@ -777,16 +814,36 @@ attend_many_kernel(const AttnArgs a) {
         m = mn;
     }
     if (!busy) return;
-    if (u.parts > 1) {                                    // what is left of a row until its parts are joined
+    if constexpr (MODE == kSuffix)
+        if (u.s.first > 0 && u.t0 == u.s.first / kTile) { // the part that takes the prefix in
+            const float2 pre = a.pre_ml[t * a.n_heads + head];
+            const float mn = fmaxf(m, pre.x);
+            const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
+            const float f1 = pre.x == mn ? 1.f : __builtin_amdgcn_exp2f((pre.x - mn) * a.scale_log2);
+            const float* p = a.pre_o + (t * a.n_heads + head) * HD + 4 * g;
+#pragma unroll
+            for (int nb = 0; nb < D::NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(p + nb * 32 + 8 * e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nb][4 * e + i] = o[nb][4 * e + i] * f0 + v[i] * f1;
+                }
+            l = l * f0 + pre.y * f1;
+            m = mn;
+        }
+    const bool split = u.parts > 1;
+    if (split || MODE == kPrefix) {                       // what is left of a row until its parts are joined
         if (row < rows) {
-            float* p = a.part_o + ((int64_t)u.slot * kManyRows + row) * HD + 4 * g;
+            const int64_t at = split ? (int64_t)u.slot * kManyRows + row : t * a.n_heads + head;
+            float* p = (split ? a.part_o : a.pre_o) + at * HD + 4 * g;
 #pragma unroll
             for (int nb = 0; nb < D::NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     *reinterpret_cast<f32x4*>(p + nb * 32 + 8 * e) =
                         f32x4{o[nb][4 * e], o[nb][4 * e + 1], o[nb][4 * e + 2], o[nb][4 * e + 3]};
-            if (g == 0) a.part_ml[(int64_t)u.slot * kManyRows + row] = float2{m, l};
+            if (g == 0) (split ? a.part_ml : a.pre_ml)[at] = float2{m, l};
         }
         return;
     }
@@ -825,7 +882,7 @@ attend_many_kernel(const AttnArgs a) {
 // 5.8 TB/s; 13 rows of 32 heads on 8 behind 131072 tokens (537 MB): 92 us, 5.8 TB/s; 641
 // keys of 64: 8.2 us, of which 5.3 are there for a single key (a launch, four loads that
 // need each other, the end).
-template <bool F16, int HD, int RT, int S>
+template <bool F16, int HD, int RT, int S, int MODE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 && RT == 1 ? 4 : RT == 1 ? 2 : 1))) void
 attend_few_kernel(const AttnArgs a) {
     using D = Dims<HD>;
@@ -840,7 +897,7 @@ attend_few_kernel(const AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int g = lane >> 5, j = lane & 31;
     Unit u;
-    if (!find_unit<false>(a, blockIdx.x, u)) return;
+    if (!find_unit<false, MODE>(a, blockIdx.x, u)) return;
     const int rows = u.s.n * a.group;                     // one row tile: all rows of (sequence, key head)
     Keys<HD> keys(a, u);
     const lds_ptr_t lds = (lds_ptr_t)smem;
@@ -851,7 +908,7 @@ attend_few_kernel(const AttnArgs a) {
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
         const int r = min(x * 32 + j, rows - 1);
-        const int64_t t = (int64_t)u.s.start + (uint32_t)r / (uint32_t)a.group;
+        const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)r / (uint32_t)a.group);
         const uint16_t* qp = a.q + t * a.q_stride + (u.kvh * a.group + (int)((uint32_t)r % (uint32_t)a.group)) * HD + g * 8;
 #pragma unroll
         for (int ks = 0; ks < D::NKS; ++ks) qf[x][ks] = *reinterpret_cast<const s16x8*>(qp + ks * 16);
@@ -1010,12 +1067,25 @@ attend_few_kernel(const AttnArgs a) {
             l += part.y * f;
             o += v * f;
         }
+        const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)row / (uint32_t)a.group);
+        const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
+        if constexpr (MODE == kSuffix)
+            if (u.s.first > 0 && u.t0 == u.s.first / kTile) {     // the part that takes the prefix in
+                const float2 pre = a.pre_ml[t * a.n_heads + h];
+                const float mn = fmaxf(m, pre.x);
+                const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
+                const float f1 = pre.x == mn ? 1.f : __builtin_amdgcn_exp2f((pre.x - mn) * a.scale_log2);
+                o = o * f0 + *reinterpret_cast<const f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) * f1;
+                l = l * f0 + pre.y * f1;
+                m = mn;
+            }
         if (u.parts > 1) {
             *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
             if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
+        } else if constexpr (MODE == kPrefix) {
+            *reinterpret_cast<f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
+            if (c4 == 0) a.pre_ml[t * a.n_heads + h] = float2{m, l};
         } else {
-            const int64_t t = (int64_t)u.s.start + (uint32_t)row / (uint32_t)a.group;
-            const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
             if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
         }
@@ -1028,13 +1098,13 @@ attend_few_kernel(const AttnArgs a) {
 // latency: 5 us with nothing to join, 6.9 for 256 parts of 64 KB.
 constexpr int kJoinRuns = 4;
 
-template <bool F16, int HD>
+template <bool F16, int HD, int MODE>
 __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
     constexpr int C4 = HD / 4, ROWS = 256 / (C4 * kJoinRuns);
     __shared__ f32x4 run_o[kJoinRuns][ROWS][C4];
     __shared__ float2 run_ml[kJoinRuns][ROWS];
     Unit u;
-    if (!find_unit<true>(a, blockIdx.x, u)) return;
+    if (!find_unit<true, MODE>(a, blockIdx.x, u)) return;
     const int rows = min(u.s.n * a.group - u.row_tile * a.rows_per_wg, a.rows_per_wg);
     const int c4 = threadIdx.x % C4, local = threadIdx.x / C4 % ROWS, run = threadIdx.x / (C4 * ROWS);
     const int each = (u.parts + kJoinRuns - 1) / kJoinRuns;
@@ -1073,10 +1143,15 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 #pragma unroll
             for (int i = 1; i < kJoinRuns; ++i) add(run_ml[i][local], run_o[i][local][c4]);
             const int pr = row + u.row_tile * a.rows_per_wg;
-            const int64_t t = (int64_t)u.s.start + (uint32_t)pr / (uint32_t)a.group;
+            const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)pr / (uint32_t)a.group);
             const int h = u.kvh * a.group + (int)((uint32_t)pr % (uint32_t)a.group);
-            store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
+            if constexpr (MODE == kPrefix) {
+                *reinterpret_cast<f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
+                if (c4 == 0) a.pre_ml[t * a.n_heads + h] = float2{m, l};
+            } else {
+                store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
+                if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
+            }
         }
         __syncthreads();
     }
@@ -1115,26 +1190,26 @@ int64_t item_bound(int n_seqs, int n_kv, int total_rows, int max_rows, int group
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-template <bool F16, int HD>
+template <bool F16, int HD, int MODE>
 hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t st) {
     const int64_t wgs = (items + (may_split ? a.units : 0) + 63) / 64 * 64;
     if (wgs > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)wgs), block(256);
     if (a.rows_per_wg == 32)
-        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 1, 1>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 1, 1, MODE>), grid, block, 0, st, a);
     else if (a.rows_per_wg == 64)
-        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 2, 2>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((attend_few_kernel<F16, HD, 2, 2, MODE>), grid, block, 0, st, a);
     else {
         const bool once = (int64_t)a.max_rows * a.group <= kManyRows;     // one row tile: each key is read once
         const bool two = a.step == 2 * kTile;
         if (two && once)
-            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 2>), grid, dim3(512), 0, st, a);
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 2, MODE>), grid, dim3(512), 0, st, a);
         else if (two)
-            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 2>), grid, dim3(512), 0, st, a);
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 2, MODE>), grid, dim3(512), 0, st, a);
         else if (once)
-            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 1>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, true, 1, MODE>), grid, block, 0, st, a);
         else
-            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 1>), grid, block, 0, st, a);
+            hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 1, MODE>), grid, block, 0, st, a);
     }
     if (may_split) {
         // Where there are many items few of them are split: a workgroup then walks rows.
@@ -1142,23 +1217,41 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
         const int per = 256 / (HD / 4 * kJoinRuns);
         const int64_t x = std::min<int64_t>(items, a.units);
         const int64_t y = std::min<int64_t>((rows + per - 1) / per, std::max<int64_t>(1, 2048 / x));
-        hipLaunchKernelGGL((join_kernel<F16, HD>), dim3((unsigned)x, (unsigned)y), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((join_kernel<F16, HD, MODE>), dim3((unsigned)x, (unsigned)y), dim3(256), 0, st, a);
     }
     return hipGetLastError();
 }
 
-}  // namespace
-
-size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
-    const Shape s = shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), 0);
+// Call of one launch: the shape's fields, and the parts at ws.
+template <int MODE>
+hipError_t attend(AttnArgs& a, int dtype, void* ws, hipStream_t st) {
+    const CacheArgs& c = a.c;
+    const Shape s = shape_for(a.max_rows, a.group, item_bound(c.n_seqs, c.n_kv, a.total_rows, a.max_rows, a.group, kManyRows),
+                              a.max_keys);
+    a.rows_per_wg = s.rows_per_wg;
+    a.step = s.step;
+    a.rows_log2 = __builtin_ctz((unsigned)s.rows_per_wg);
+    a.step_log2 = __builtin_ctz((unsigned)s.step);
+    a.units = s.units;
+    a.min_steps = s.min_steps;
     const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
-    return round256(rows * head_dim * 4) + round256(rows * 8);
+    a.max_slots = slots_for(s);
+    a.part_o = (float*)ws;
+    a.part_ml = (float2*)((char*)ws + round256(rows * c.head_dim * 4));
+    const int64_t items = item_bound(c.n_seqs, c.n_kv, a.total_rows, a.max_rows, a.group, s.rows_per_wg);
+    const int64_t steps = ((int64_t)a.max_keys + s.step - 1) / s.step;
+    // The list's counts are 32-bit, whatever the row starts.
+    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)a.max_rows * a.group + s.rows_per_wg - 1) / s.rows_per_wg) > (1 << 29))
+        return hipErrorInvalidValue;
+    const bool may_split = steps > s.min_steps;
+    if (dtype == DLM_F16)
+        return c.head_dim == 128 ? launch<true, 128, MODE>(a, items, may_split, st) : launch<true, 64, MODE>(a, items, may_split, st);
+    return c.head_dim == 128 ? launch<false, 128, MODE>(a, items, may_split, st) : launch<false, 64, MODE>(a, items, may_split, st);
 }
 
-hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
-                         int max_rows, int max_keys, int n_heads, const void* q, int64_t q_stride,
-                         const uint32_t* mask, int mask_words, float scale, void* o, int64_t o_stride, float* lse,
-                         void* ws, hipStream_t st) {
+AttnArgs attend_args(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows, int max_rows,
+                     int max_keys, int n_heads, const void* q, int64_t q_stride, const uint32_t* mask, int mask_words,
+                     float scale, void* o, int64_t o_stride, float* lse) {
     AttnArgs a{};
     a.c = c;
     a.layer_base = (int64_t)layer * c.n_pages * c.n_kv * c.page_len * c.head_dim * 2;
@@ -1177,25 +1270,177 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
     a.o = (uint16_t*)o;
     a.o_stride = o_stride;
     a.lse = lse;
-    const Shape s = shape_for(max_rows, a.group, item_bound(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, kManyRows),
-                              max_keys);
-    a.rows_per_wg = s.rows_per_wg;
-    a.step = s.step;
-    a.rows_log2 = __builtin_ctz((unsigned)s.rows_per_wg);
-    a.step_log2 = __builtin_ctz((unsigned)s.step);
-    a.units = s.units;
-    a.min_steps = s.min_steps;
+    return a;
+}
+
+// ------------------------------------------------------------------ shared prefixes
+
+// Layout of what cache_share leaves, in int32 words.
+struct ShareWords {
+    int64_t groups, skip, rows, all;
+};
+__host__ __device__ inline ShareWords share_words(int n_seqs, int total_rows) {
+    const int64_t groups = 0, skip = 4 * (int64_t)n_seqs, rows = skip + n_seqs;
+    return {groups, skip, rows, rows + total_rows};
+}
+
+__device__ __forceinline__ int block_add(int v, int* lds) {       // over 1024 threads
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    int t = 0;
+    for (int i = 0; i < 16; ++i) t += lds[i];
+    return t;
+}
+__device__ __forceinline__ int block_min(int v, int* lds) {
+    for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    int t = lds[0];
+    for (int i = 1; i < 16; ++i) t = min(t, lds[i]);
+    return t;
+}
+
+// Group blockIdx.x, a thread per sequence: its members with rows, the tokens whose pages
+// all their tables begin with, and their rows one after the other.  A group is left alone
+// (skip 0) if it has a single member, nothing in common, or more rows than the caller said.
+__global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t* __restrict__ row_start, int total_rows,
+                                                     int max_rows, const int32_t* __restrict__ group, int max_group_rows,
+                                                     int32_t* __restrict__ out) {
+    __shared__ int lds[16], members[kCacheMaxSeqs], wave_rows[16], wave_members[16];
+    const ShareWords w = share_words(c.n_seqs, total_rows);
+    const int g = blockIdx.x, s = threadIdx.x, lane = s & 63, wave = s >> 6;
+    int id = -1, n = 0, start = 0, len = 0;
+    if (s < c.n_seqs) {
+        id = group[s];
+        start = row_start[s];
+        const int end = min(row_start[s + 1], total_rows);
+        n = start >= 0 && end > start ? min(end - start, max_rows) : 0;
+        len = max(c.len[s], 0);
+        if ((unsigned)id >= (unsigned)c.n_seqs || n == 0) {
+            if (s == g) out[w.skip + s] = 0;
+            id = -1;
+        }
+    }
+    const bool in = id == g;
+    const uint64_t any = __ballot(in);
+    // All rows in 32 bits: total_rows <= 2^24 and at most 1024 sequences, so 2^34 by unsound
+    // row starts; counted in units that cannot pass, and compared as such.
+    const int all = block_add((n + 15) >> 4, lds);                // at most 2^30
+    const int exact = all > (1 << 26) ? total_rows + 1 : block_add(n, lds);
+    const int mine = block_add(in ? 1 : 0, lds);
+    if (mine == 0) {                                              // nobody's group
+        if (s == 0) *reinterpret_cast<int4*>(out + w.groups + 4 * g) = int4{0, 0, 0, 0};
+        return;
+    }
+    const int leader = block_min(in ? s : 0x7fffffff, lds);
+    // Rows and members before this thread's.
+    const int rows_in = in ? n : 0;
+    int scan = rows_in;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(scan, o, 64);
+        if (lane >= o) scan += y;
+    }
+    if (lane == 63) {
+        wave_rows[wave] = scan;
+        wave_members[wave] = __popcll(any);
+    }
+    __syncthreads();
+    int off = scan - rows_in, place = __popcll(any & ((1ull << lane) - 1)), rows = 0;
+    for (int i = 0; i < 16; ++i) {
+        if (i < wave) {
+            off += wave_rows[i];
+            place += wave_members[i];
+        }
+        rows += wave_rows[i];
+    }
+    if (in) members[place] = s;
+    const int list = exact > total_rows ? 0 : block_add(id >= 0 && id < g ? n : 0, lds);
+    // Tokens that every member counts, in whole pages.
+    int pages = block_min(in ? min(len >> c.page_log2, c.max_pages) : 0x7fffffff, lds);
+    if (mine < 2 || rows > max_group_rows || exact > total_rows) pages = 0;
+    int same = pages;
+    const int32_t* front = c.table + (int64_t)leader * c.max_pages;
+    for (int m = wave; m < mine && pages; m += 16) {
+        const int32_t* row = c.table + (int64_t)members[m] * c.max_pages;
+#pragma unroll 4
+        for (int e = lane; e < pages; e += 64) {
+            const int page = row[e];
+            if (page != front[e] || (uint32_t)page >= (uint32_t)c.n_pages) same = min(same, e);
+        }
+    }
+    same = block_min(same, lds);
+    const int prefix = (same << c.page_log2) & ~(kTile - 1);
+    if (in) out[w.skip + s] = prefix;
+    if (s == 0)
+        *reinterpret_cast<int4*>(out + w.groups + 4 * g) = prefix ? int4{leader, prefix, list, rows} : int4{0, 0, 0, 0};
+    if (prefix)
+        for (int i = 0; in && i < n; ++i) out[w.rows + list + off + i] = start + i;
+}
+
+bool shares(int max_rows, int max_group_rows, int group, int max_keys) {
+    return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows && max_keys > kTile;
+}
+size_t pre_bytes(int total_rows, int n_heads, int head_dim) {
+    const size_t n = (size_t)total_rows * n_heads;
+    return round256(n * head_dim * 4) + round256(n * 8);
+}
+
+}  // namespace
+
+size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
+    const Shape s = shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), 0);
     const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
-    a.max_slots = slots_for(s);
-    a.part_o = (float*)ws;
-    a.part_ml = (float2*)((char*)ws + round256(rows * c.head_dim * 4));
-    const int64_t items = item_bound(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, s.rows_per_wg);
-    const int64_t steps = ((int64_t)max_keys + s.step - 1) / s.step;
-    // The list's counts are 32-bit, whatever the row starts.
-    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)max_rows * a.group + s.rows_per_wg - 1) / s.rows_per_wg) > (1 << 29))
-        return hipErrorInvalidValue;
-    const bool may_split = steps > s.min_steps;
-    if (dtype == DLM_F16)
-        return c.head_dim == 128 ? launch<true, 128>(a, items, may_split, st) : launch<true, 64>(a, items, may_split, st);
-    return c.head_dim == 128 ? launch<false, 128>(a, items, may_split, st) : launch<false, 64>(a, items, may_split, st);
+    return round256(rows * head_dim * 4) + round256(rows * 8);
+}
+
+hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
+                         int max_rows, int max_keys, int n_heads, const void* q, int64_t q_stride,
+                         const uint32_t* mask, int mask_words, float scale, void* o, int64_t o_stride, float* lse,
+                         void* ws, hipStream_t st) {
+    AttnArgs a = attend_args(c, dtype, layer, row_start, total_rows, max_rows, max_keys, n_heads, q, q_stride, mask, mask_words,
+                             scale, o, o_stride, lse);
+    return attend<kPlain>(a, dtype, ws, st);
+}
+
+size_t share_bytes(int n_seqs, int total_rows) { return (size_t)share_words(n_seqs, total_rows).all * 4; }
+
+hipError_t launch_share(const CacheArgs& c, const int32_t* row_start, int total_rows, int max_rows, const int32_t* group,
+                        int max_group_rows, int32_t* share, hipStream_t st) {
+    hipLaunchKernelGGL(share_kernel, dim3(c.n_seqs), dim3(1024), 0, st, c, row_start, total_rows, max_rows, group,
+                       max_group_rows, share);
+    return hipGetLastError();
+}
+
+size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int max_group_rows,
+                                     int group) {
+    const size_t own = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_rows, group);
+    if (!shares(max_rows, max_group_rows, group, 0x7fffffff)) return own;
+    const size_t pre = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_group_rows, group);
+    return pre_bytes(total_rows, n_kv * group, head_dim) + std::max(own, pre);
+}
+
+hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
+                                int max_rows, int max_group_rows, int max_keys, const int32_t* share, int n_heads,
+                                const void* q, int64_t q_stride, const uint32_t* mask, int mask_words, float scale, void* o,
+                                int64_t o_stride, float* lse, void* ws, hipStream_t st) {
+    AttnArgs a = attend_args(c, dtype, layer, row_start, total_rows, max_rows, max_keys, n_heads, q, q_stride, mask, mask_words,
+                             scale, o, o_stride, lse);
+    if (!shares(max_rows, max_group_rows, a.group, max_keys)) return attend<kPlain>(a, dtype, ws, st);
+    const ShareWords w = share_words(c.n_seqs, total_rows);
+    a.groups = (const int4*)(share + w.groups);
+    a.skip = share + w.skip;
+    a.rows = share + w.rows;
+    a.pre_o = (float*)ws;
+    a.pre_ml = (float2*)((char*)ws + round256((size_t)total_rows * n_heads * c.head_dim * 4));
+    char* parts = (char*)ws + pre_bytes(total_rows, n_heads, c.head_dim);
+    AttnArgs p = a;
+    p.max_rows = max_group_rows;
+    p.mask = nullptr;
+    p.mask_words = 0;
+    const hipError_t e = attend<kPrefix>(p, dtype, parts, st);
+    if (e != hipSuccess) return e;
+    return attend<kSuffix>(a, dtype, parts, st);
 }
