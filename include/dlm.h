@@ -700,7 +700,7 @@ dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int
  * From row 0 on, the children of the row r at hand are tried in order of their rows.  Child
  * i with token x = d_tokens[..i] is kept if d_u[..i] q_r(x) < p_r(x), and then is the row at
  * hand; if not, p_r becomes max(p_r - q_r, 0) over its sum (certain drafts: p_r without x,
- * over its sum; p_r as it is where nothing is left).  When no child is left, d_next[s] is
+ * over its sum; p_r as it is where less than 2^-43 is left, which is rounding).  When no child is left, d_next[s] is
  * drawn from p_r: the first v at which the running sum passes d_u_next[s] times the whole.
  * d_u float [total_rows] and d_u_next float [n_seqs] hold numbers in [0, 1) (others are read
  * as if cut off to it); entries of rows 0 are not read.  temperature 0: p_r is 1 for the
@@ -719,7 +719,7 @@ dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int
 size_t dlm_verify_workspace_bytes(int32_t n_seqs, int32_t total_rows, int32_t vocab, int32_t with_draft);
 dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
                       const int32_t* d_tokens, const int32_t* d_parent, int32_t dtype, int32_t vocab, const void* d_target,
-                      int64_t target_stride, const void* d_draft, int64_t draft_stride, float temperature,
+                      int64_t target_stride, const void* d_draft, int64_t draft_stride, double temperature,
                       const float* d_u, const float* d_u_next, int32_t* d_next, int32_t* d_keep, int32_t* d_keep_start,
                       void* d_workspace, size_t workspace_bytes, void* hip_stream);
 

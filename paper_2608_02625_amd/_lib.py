@@ -145,7 +145,7 @@ SIGNATURES = [
     ("dlm_cache_step", _I, [_P, _CACHE, _P, _I, _I, _I, _P, _P, _P, _I, _P, _SZ, _P, _P, _P, _P, _P]),
     ("dlm_cache_step_logits", _I, [_P, _CACHE, _P, _I, _I, _I, _P, _P, _P, _I, _P, _SZ, _P, _P, _P, _P, _P, _P]),
     ("dlm_verify_workspace_bytes", _SZ, [_I, _I, _I, _I]),
-    ("dlm_verify", _I, [_I, _P, _I, _I, _P, _P, _I, _I, _P, _L, _P, _L, _F, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    ("dlm_verify", _I, [_I, _P, _I, _I, _P, _P, _I, _I, _P, _L, _P, _L, ctypes.c_double, _P, _P, _P, _P, _P, _P, _SZ, _P]),
     ("dlm_debug_forward", _I, [_P, _I, _I, _I, _P, _P, _SZ, _P, _P, _P, _P, _P, _P, _P, _P]),
     ("dlm_debug_layer", _I, [_P, _I, _I, _I, _P, _P, _P, _SZ, _P, _P, _P]),
     ("dlm_debug_head", _I, [_P, _I, _I, _I, _P, _P, _SZ, _P, _P, _P, _P]),

@@ -563,7 +563,7 @@ size_t dlm_verify_workspace_bytes(int32_t n_seqs, int32_t total_rows, int32_t vo
 
 dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,
                       const int32_t* d_tokens, const int32_t* d_parent, int32_t dtype, int32_t vocab, const void* d_target,
-                      int64_t target_stride, const void* d_draft, int64_t draft_stride, float temperature,
+                      int64_t target_stride, const void* d_draft, int64_t draft_stride, double temperature,
                       const float* d_u, const float* d_u_next, int32_t* d_next, int32_t* d_keep, int32_t* d_keep_start,
                       void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     try {
@@ -573,7 +573,7 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
         const int rows = std::min(max_rows, total_rows);
         if (rows > kVerifyMaxRows) return fail(DLM_ERR_INVALID_ARG, "max_rows must be at most 1024");
         if (dtype != DLM_BF16 && dtype != DLM_F16 && dtype != DLM_F32) return fail(DLM_ERR_INVALID_ARG, "unknown dtype");
-        if (!(temperature >= 0.f) || !std::isfinite(temperature))
+        if (!(temperature >= 0.) || !std::isfinite(temperature))
             return fail(DLM_ERR_INVALID_ARG, "temperature must be finite and >= 0");
         if (d_draft && d_parent) return fail(DLM_ERR_INVALID_ARG, "with the draft's logits windows are chains: parent must be NULL");
         if (!d_next || !d_keep_start || !d_u_next) return fail(DLM_ERR_INVALID_ARG, "next, keep_start or u_next is NULL");
@@ -586,7 +586,7 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
             return fail(DLM_ERR_INVALID_ARG, "buffers must be aligned to their elements");
         if (total_rows > 0 && ((total_rows > 1 && target_stride < vocab) || (d_draft && total_rows > 1 && draft_stride < vocab)))
             return fail(DLM_ERR_INVALID_ARG, "target_stride or draft_stride below a row");
-        const bool drafts = d_draft && temperature > 0.f;
+        const bool drafts = d_draft && temperature > 0.;
         TRY(check_workspace(d_workspace, workspace_bytes, verify_workspace_bytes(n_seqs, total_rows, vocab, drafts)));
         VerifyArgs a{};
         a.n_seqs = n_seqs;
@@ -600,7 +600,7 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
         a.draft = drafts ? d_draft : nullptr;
         a.target_stride = target_stride;
         a.draft_stride = draft_stride;
-        a.c = temperature > 0.f ? 1.4426950408889634 / (double)temperature : 0.0;
+        a.c = temperature > 0. ? std::min(1.4426950408889634 / temperature, 1e250) : 0.;
         a.u = d_u;
         a.u_next = d_u_next;
         a.next = d_next;

@@ -175,13 +175,16 @@ struct AttnArgs {
     int max_slots;                            // places for parts; enough for any sound row starts
     float* part_o;                            // [max_slots][rows_per_wg][head_dim]
     float2* part_ml;                          // [max_slots][rows_per_wg]
-    // Shared prefixes (kPrefix, kSuffix): what cache_share wrote, and what the prefixes
-    // leave of each row, [total_rows][n_heads].
+    // Shared prefixes (kPrefix, kSuffix): what share_kernel wrote, and what is left of rows
+    // that are not split, [total_rows][n_heads].
     const int4* groups;                       // [n_seqs]: leader, prefix, first entry of rows, rows
-    const int32_t* skip;                      // [n_seqs]: the prefix that the group's pass reads
+    const int4* members;                      // [n_seqs]: the group's prefix, group, place of its first row in the group
     const int32_t* rows;                      // [total_rows]: the groups' rows
-    float* pre_o;
-    float2* pre_ml;
+    float* row_o;                             // this launch's (kPrefix; kSuffix behind a prefix)
+    float2* row_ml;
+    const float* pre_o;                       // kSuffix: the prefix's, taken in here; NULL: by join_rows_kernel
+    const float2* pre_ml;
+    int4* info;                               // [n_seqs]: first slot, parts, row tiles of an item
 };
 
 // What a launch attends to: a sequence's keys; the prefix that the sequences of a group
@@ -214,7 +217,7 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
         s.n = s.start >= 0 && end > s.start ? min(end - s.start, a.max_rows) : 0;
         s.len = max(a.c.len[b], 0);
         s.keys = (int)min((int64_t)s.len + s.n, (int64_t)a.max_keys);
-        if constexpr (MODE == kSuffix) s.first = min(max(a.skip[b], 0), s.keys) & ~(kTile - 1);
+        if constexpr (MODE == kSuffix) s.first = min(max(a.members[b].x, 0), s.keys) & ~(kTile - 1);
     }
     return s;
 }
@@ -234,6 +237,7 @@ struct Unit {
     int b, row_tile, kvh;
     int t0, t1;                               // tiles of 32 keys
     int slot, parts;                          // workspace slot of this part; parts of its item
+    int tiles;                                // row tiles of its sequence or group
 };
 
 // Inclusive prefix sum over the wave by lane moves (a shuffle through LDS each would
@@ -308,6 +312,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
             const int all_steps = from_lane(steps, l);
             uint32_t i = (uint32_t)(index - from_lane(end - count, l));
             const int slot0 = from_lane(slot_end - split, l);
+            u.tiles = n_tiles;
             u.row_tile = uniform((int)(i % (uint32_t)n_tiles));
             i /= (uint32_t)n_tiles;
             int part = 0;
@@ -327,6 +332,22 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
         slots_before = from_lane(slot_end, 63);
     }
     return false;
+}
+
+// Where join_rows_kernel finds the parts of a sequence or a group, from its first unit.
+template <int MODE>
+__device__ __forceinline__ void note_item(const AttnArgs& a, const Unit& u) {
+    if constexpr (MODE != kPlain)
+        if (threadIdx.x == 0 && u.row_tile == 0 && u.kvh == 0 && u.t0 == u.s.first / kTile) a.info[u.b] = int4{u.slot, u.parts, u.tiles, 0};
+}
+// A row's maximum, sum and output taken together with another part's.
+struct Two {
+    float m, f0, f1;
+};
+__device__ __forceinline__ Two together(const AttnArgs& a, float m0, float m1) {
+    const float m = fmaxf(m0, m1);
+    return {m, m0 == m ? 1.f : __builtin_amdgcn_exp2f((m0 - m) * a.scale_log2),
+            m1 == m ? 1.f : __builtin_amdgcn_exp2f((m1 - m) * a.scale_log2)};
 }
 
 // ------------------------------------------------------------------ tiles
@@ -670,6 +691,7 @@ attend_many_kernel(const AttnArgs a) {
     // in turn, so each XCD takes runs of 8 units.
     const int wg = blockIdx.x;
     if (!find_unit<false, MODE>(a, (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7), u)) return;
+    note_item<MODE>(a, u);
     const int rows = min(u.s.n * a.group - u.row_tile * kManyRows, kManyRows);           // of this workgroup
     const bool busy = wave * 32 < rows;                   // this wave has rows
     const int r = min(wave * 32 + j, rows - 1) + u.row_tile * kManyRows;
@@ -815,11 +837,9 @@ attend_many_kernel(const AttnArgs a) {
     }
     if (!busy) return;
     if constexpr (MODE == kSuffix)
-        if (u.s.first > 0 && u.t0 == u.s.first / kTile) { // the part that takes the prefix in
+        if (a.pre_o && u.s.first > 0) {                   // not split: the prefix is taken in here
             const float2 pre = a.pre_ml[t * a.n_heads + head];
-            const float mn = fmaxf(m, pre.x);
-            const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
-            const float f1 = pre.x == mn ? 1.f : __builtin_amdgcn_exp2f((pre.x - mn) * a.scale_log2);
+            const Two w = together(a, m, pre.x);
             const float* p = a.pre_o + (t * a.n_heads + head) * HD + 4 * g;
 #pragma unroll
             for (int nb = 0; nb < D::NB; ++nb)
@@ -827,23 +847,23 @@ attend_many_kernel(const AttnArgs a) {
                 for (int e = 0; e < 4; ++e) {
                     const f32x4 v = *reinterpret_cast<const f32x4*>(p + nb * 32 + 8 * e);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nb][4 * e + i] = o[nb][4 * e + i] * f0 + v[i] * f1;
+                    for (int i = 0; i < 4; ++i) o[nb][4 * e + i] = o[nb][4 * e + i] * w.f0 + v[i] * w.f1;
                 }
-            l = l * f0 + pre.y * f1;
-            m = mn;
+            l = l * w.f0 + pre.y * w.f1;
+            m = w.m;
         }
     const bool split = u.parts > 1;
-    if (split || MODE == kPrefix) {                       // what is left of a row until its parts are joined
+    if (split || MODE == kPrefix || (MODE == kSuffix && !a.pre_o && u.s.first > 0)) {                       // what is left of a row until its parts are joined
         if (row < rows) {
             const int64_t at = split ? (int64_t)u.slot * kManyRows + row : t * a.n_heads + head;
-            float* p = (split ? a.part_o : a.pre_o) + at * HD + 4 * g;
+            float* p = (split ? a.part_o : a.row_o) + at * HD + 4 * g;
 #pragma unroll
             for (int nb = 0; nb < D::NB; ++nb)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     *reinterpret_cast<f32x4*>(p + nb * 32 + 8 * e) =
                         f32x4{o[nb][4 * e], o[nb][4 * e + 1], o[nb][4 * e + 2], o[nb][4 * e + 3]};
-            if (g == 0) (split ? a.part_ml : a.pre_ml)[at] = float2{m, l};
+            if (g == 0) (split ? a.part_ml : a.row_ml)[at] = float2{m, l};
         }
         return;
     }
@@ -898,6 +918,7 @@ attend_few_kernel(const AttnArgs a) {
     const int g = lane >> 5, j = lane & 31;
     Unit u;
     if (!find_unit<false, MODE>(a, blockIdx.x, u)) return;
+    note_item<MODE>(a, u);
     const int rows = u.s.n * a.group;                     // one row tile: all rows of (sequence, key head)
     Keys<HD> keys(a, u);
     const lds_ptr_t lds = (lds_ptr_t)smem;
@@ -1070,21 +1091,19 @@ attend_few_kernel(const AttnArgs a) {
         const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)row / (uint32_t)a.group);
         const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
         if constexpr (MODE == kSuffix)
-            if (u.s.first > 0 && u.t0 == u.s.first / kTile) {     // the part that takes the prefix in
+            if (a.pre_o && u.s.first > 0) {               // not split: the prefix is taken in here
                 const float2 pre = a.pre_ml[t * a.n_heads + h];
-                const float mn = fmaxf(m, pre.x);
-                const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale_log2);
-                const float f1 = pre.x == mn ? 1.f : __builtin_amdgcn_exp2f((pre.x - mn) * a.scale_log2);
-                o = o * f0 + *reinterpret_cast<const f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) * f1;
-                l = l * f0 + pre.y * f1;
-                m = mn;
+                const Two w = together(a, m, pre.x);
+                o = o * w.f0 + *reinterpret_cast<const f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) * w.f1;
+                l = l * w.f0 + pre.y * w.f1;
+                m = w.m;
             }
         if (u.parts > 1) {
             *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
             if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
-        } else if constexpr (MODE == kPrefix) {
-            *reinterpret_cast<f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
-            if (c4 == 0) a.pre_ml[t * a.n_heads + h] = float2{m, l};
+        } else if (MODE == kPrefix || (MODE == kSuffix && !a.pre_o && u.s.first > 0)) {
+            *reinterpret_cast<f32x4*>(a.row_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
+            if (c4 == 0) a.row_ml[t * a.n_heads + h] = float2{m, l};
         } else {
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
             if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
@@ -1098,13 +1117,13 @@ attend_few_kernel(const AttnArgs a) {
 // latency: 5 us with nothing to join, 6.9 for 256 parts of 64 KB.
 constexpr int kJoinRuns = 4;
 
-template <bool F16, int HD, int MODE>
+template <bool F16, int HD>
 __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
     constexpr int C4 = HD / 4, ROWS = 256 / (C4 * kJoinRuns);
     __shared__ f32x4 run_o[kJoinRuns][ROWS][C4];
     __shared__ float2 run_ml[kJoinRuns][ROWS];
     Unit u;
-    if (!find_unit<true, MODE>(a, blockIdx.x, u)) return;
+    if (!find_unit<true, kPlain>(a, blockIdx.x, u)) return;
     const int rows = min(u.s.n * a.group - u.row_tile * a.rows_per_wg, a.rows_per_wg);
     const int c4 = threadIdx.x % C4, local = threadIdx.x / C4 % ROWS, run = threadIdx.x / (C4 * ROWS);
     const int each = (u.parts + kJoinRuns - 1) / kJoinRuns;
@@ -1143,18 +1162,90 @@ __global__ __launch_bounds__(256) void join_kernel(const AttnArgs a) {
 #pragma unroll
             for (int i = 1; i < kJoinRuns; ++i) add(run_ml[i][local], run_o[i][local][c4]);
             const int pr = row + u.row_tile * a.rows_per_wg;
-            const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)pr / (uint32_t)a.group);
+            const int64_t t = (int64_t)u.s.start + (uint32_t)pr / (uint32_t)a.group;
             const int h = u.kvh * a.group + (int)((uint32_t)pr % (uint32_t)a.group);
-            if constexpr (MODE == kPrefix) {
-                *reinterpret_cast<f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
-                if (c4 == 0) a.pre_ml[t * a.n_heads + h] = float2{m, l};
-            } else {
-                store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
-                if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
-            }
+            store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
+            if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
         }
         __syncthreads();
     }
+}
+
+// Rows behind a shared prefix, and rows of sequences that are split: what the prefix left
+// (its parts, or one) and what the sequence's own keys left, joined in that order.
+// blockIdx.x: the row; blockIdx.y: some of its heads.
+template <bool F16, int HD>
+__global__ __launch_bounds__(256) void join_rows_kernel(const AttnArgs a, const AttnArgs pre) {
+    constexpr int C4 = HD / 4, ROWS = 256 / (C4 * kJoinRuns);
+    __shared__ f32x4 run_o[kJoinRuns][ROWS][C4];
+    __shared__ float2 run_ml[kJoinRuns][ROWS];
+    const int lane = threadIdx.x & 63, t = blockIdx.x;
+    int b = -1, start = 0;
+    for (int b0 = 0; b0 < a.c.n_seqs && b < 0; b0 += 64) {
+        const Seq s = sequence<kSuffix>(a, b0 + lane);
+        const uint64_t hit = __ballot(s.n > 0 && t >= s.start && t - s.start < s.n);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            b = uniform(b0 + l);
+            start = from_lane(s.start, l);
+        }
+    }
+    if (b < 0) return;                                    // a row that no window covers
+    const int4 own = a.info[b], member = a.members[b];
+    const bool shared = member.x > 0;
+    if (!shared && own.y <= 1) return;                    // written already
+    const int4 front = shared ? pre.info[min(max(member.y, 0), a.c.n_seqs - 1)] : int4{0, 0, 0, 0};
+    const int c4 = threadIdx.x % C4, local = threadIdx.x / C4 % ROWS, run = threadIdx.x / (C4 * ROWS);
+    const int h = min((int)blockIdx.y * ROWS + local, a.n_heads - 1), kvh = h / a.group, j = h % a.group;
+    // Where the parts lie: slot, row in it, or the row's own place.
+    auto parts_of = [&](const AttnArgs& x, const int4& item, int row, int& n, int64_t& at) {
+        const int pr = row * a.group + j, tile = pr >> x.rows_log2;
+        n = min(max(item.y, 0), x.max_slots);
+        const int64_t slot = item.x + ((int64_t)kvh * item.z + tile) * n;
+        if (n > 1 && (slot < 0 || slot + n > x.max_slots)) n = 0;         // unsound row starts
+        at = n > 1 ? slot * x.rows_per_wg + (pr & (x.rows_per_wg - 1)) : (int64_t)t * a.n_heads + h;
+    };
+    int n0 = 0, n1;
+    int64_t at0 = 0, at1;
+    if (shared) parts_of(pre, front, member.z + t - start, n0, at0);
+    parts_of(a, own, t - start, n1, at1);
+    const float* o0 = (n0 > 1 ? pre.part_o : pre.row_o) + at0 * HD + c4 * 4;
+    const float* o1 = (n1 > 1 ? a.part_o : a.row_o) + at1 * HD + c4 * 4;
+    const float2* ml0 = (n0 > 1 ? pre.part_ml : pre.row_ml) + at0;
+    const float2* ml1 = (n1 > 1 ? a.part_ml : a.row_ml) + at1;
+    const int n = n0 + n1, each = (n + kJoinRuns - 1) / kJoinRuns;
+    const int p0 = min(run * each, n), p1 = min(p0 + each, n);
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float2& part, const f32x4& v) {
+        const Two w = together(a, m, part.x);
+        l = l * w.f0 + part.y * w.f1;
+        o = o * w.f0 + v * w.f1;
+        m = w.m;
+    };
+    constexpr int U = 8;
+    for (int p = p0; p < p1; p += U) {
+        float2 part[U];
+        f32x4 v[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int x = min(p + i, p1 - 1);
+            const int64_t k = x < n0 ? (int64_t)x * pre.rows_per_wg : (int64_t)(x - n0) * a.rows_per_wg;
+            part[i] = (x < n0 ? ml0 : ml1)[k];
+            v[i] = *reinterpret_cast<const f32x4*>((x < n0 ? o0 : o1) + k * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (p + i < p1) add(part[i], v[i]);
+    }
+    run_o[run][local][c4] = o;
+    if (c4 == 0) run_ml[run][local] = float2{m, l};
+    __syncthreads();
+    if (run || (int)blockIdx.y * ROWS + local >= a.n_heads) return;
+#pragma unroll
+    for (int i = 1; i < kJoinRuns; ++i) add(run_ml[i][local], run_o[i][local][c4]);
+    store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
+    if (a.lse && c4 == 0) a.lse[(int64_t)t * a.n_heads + h] = log_sum<F16>(a, m, l);
 }
 
 // How a call is laid out: packed rows of a workgroup, keys of a step, units, least
@@ -1211,42 +1302,54 @@ hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t 
         else
             hipLaunchKernelGGL((attend_many_kernel<F16, HD, false, 1, MODE>), grid, block, 0, st, a);
     }
-    if (may_split) {
+    if (MODE == kPlain && may_split) {
         // Where there are many items few of them are split: a workgroup then walks rows.
         const int rows = (int)std::min<int64_t>(a.rows_per_wg, (int64_t)a.max_rows * a.group);
         const int per = 256 / (HD / 4 * kJoinRuns);
         const int64_t x = std::min<int64_t>(items, a.units);
         const int64_t y = std::min<int64_t>((rows + per - 1) / per, std::max<int64_t>(1, 2048 / x));
-        hipLaunchKernelGGL((join_kernel<F16, HD, MODE>), dim3((unsigned)x, (unsigned)y), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((join_kernel<F16, HD>), dim3((unsigned)x, (unsigned)y), dim3(256), 0, st, a);
     }
     return hipGetLastError();
 }
 
-// Call of one launch: the shape's fields, and the parts at ws.
-template <int MODE>
-hipError_t attend(AttnArgs& a, int dtype, void* ws, hipStream_t st) {
-    const CacheArgs& c = a.c;
-    const Shape s = shape_for(a.max_rows, a.group, item_bound(c.n_seqs, c.n_kv, a.total_rows, a.max_rows, a.group, kManyRows),
-                              a.max_keys);
+// Whether some item of a call may have several parts.
+bool may_split(const Shape& s, int max_keys) { return ((int64_t)max_keys + s.step - 1) / s.step > s.min_steps; }
+size_t parts_bytes(const Shape& s, int head_dim) {
+    const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
+    return round256(rows * head_dim * 4) + round256(rows * 8);
+}
+// A launch's shape, and its parts at ws.
+void take_shape(AttnArgs& a, const Shape& s, void* ws) {
     a.rows_per_wg = s.rows_per_wg;
     a.step = s.step;
     a.rows_log2 = __builtin_ctz((unsigned)s.rows_per_wg);
     a.step_log2 = __builtin_ctz((unsigned)s.step);
     a.units = s.units;
     a.min_steps = s.min_steps;
-    const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
     a.max_slots = slots_for(s);
     a.part_o = (float*)ws;
-    a.part_ml = (float2*)((char*)ws + round256(rows * c.head_dim * 4));
-    const int64_t items = item_bound(c.n_seqs, c.n_kv, a.total_rows, a.max_rows, a.group, s.rows_per_wg);
-    const int64_t steps = ((int64_t)a.max_keys + s.step - 1) / s.step;
+    a.part_ml = (float2*)((char*)ws + round256((size_t)a.max_slots * s.rows_per_wg * a.c.head_dim * 4));
+}
+// n_items: sequences or groups at most.
+template <int MODE>
+hipError_t attend(const AttnArgs& a, int dtype, int n_items, bool split, hipStream_t st) {
+    const CacheArgs& c = a.c;
+    const int64_t items = item_bound(n_items, c.n_kv, a.total_rows, a.max_rows, a.group, a.rows_per_wg);
     // The list's counts are 32-bit, whatever the row starts.
-    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)a.max_rows * a.group + s.rows_per_wg - 1) / s.rows_per_wg) > (1 << 29))
+    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)a.max_rows * a.group + a.rows_per_wg - 1) / a.rows_per_wg) > (1 << 29))
         return hipErrorInvalidValue;
-    const bool may_split = steps > s.min_steps;
     if (dtype == DLM_F16)
-        return c.head_dim == 128 ? launch<true, 128, MODE>(a, items, may_split, st) : launch<true, 64, MODE>(a, items, may_split, st);
-    return c.head_dim == 128 ? launch<false, 128, MODE>(a, items, may_split, st) : launch<false, 64, MODE>(a, items, may_split, st);
+        return c.head_dim == 128 ? launch<true, 128, MODE>(a, items, split, st) : launch<true, 64, MODE>(a, items, split, st);
+    return c.head_dim == 128 ? launch<false, 128, MODE>(a, items, split, st) : launch<false, 64, MODE>(a, items, split, st);
+}
+// One launch for all sequences, and the join of their parts.
+hipError_t attend_plain(AttnArgs& a, int dtype, void* ws, hipStream_t st) {
+    const CacheArgs& c = a.c;
+    const Shape s = shape_for(a.max_rows, a.group, item_bound(c.n_seqs, c.n_kv, a.total_rows, a.max_rows, a.group, kManyRows),
+                              a.max_keys);
+    take_shape(a, s, ws);
+    return attend<kPlain>(a, dtype, c.n_seqs, may_split(s, a.max_keys), st);
 }
 
 AttnArgs attend_args(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows, int max_rows,
@@ -1277,11 +1380,11 @@ AttnArgs attend_args(const CacheArgs& c, int dtype, int layer, const int32_t* ro
 
 // Layout of what cache_share leaves, in int32 words.
 struct ShareWords {
-    int64_t groups, skip, rows, all;
+    int64_t groups, members, rows, all;
 };
 __host__ __device__ inline ShareWords share_words(int n_seqs, int total_rows) {
-    const int64_t groups = 0, skip = 4 * (int64_t)n_seqs, rows = skip + n_seqs;
-    return {groups, skip, rows, rows + total_rows};
+    const int64_t groups = 0, members = 4 * (int64_t)n_seqs, rows = 2 * members;
+    return {groups, members, rows, rows + total_rows};
 }
 
 __device__ __forceinline__ int block_add(int v, int* lds) {       // over 1024 threads
@@ -1305,7 +1408,7 @@ __device__ __forceinline__ int block_min(int v, int* lds) {
 
 // Group blockIdx.x, a thread per sequence: its members with rows, the tokens whose pages
 // all their tables begin with, and their rows one after the other.  A group is left alone
-// (skip 0) if it has a single member, nothing in common, or more rows than the caller said.
+// (prefix 0) if it has a single member, nothing in common, or more rows than the caller said.
 __global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t* __restrict__ row_start, int total_rows,
                                                      int max_rows, const int32_t* __restrict__ group, int max_group_rows,
                                                      int32_t* __restrict__ out) {
@@ -1320,7 +1423,7 @@ __global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t*
         n = start >= 0 && end > start ? min(end - start, max_rows) : 0;
         len = max(c.len[s], 0);
         if ((unsigned)id >= (unsigned)c.n_seqs || n == 0) {
-            if (s == g) out[w.skip + s] = 0;
+            if (s == g) *reinterpret_cast<int4*>(out + w.members + 4 * s) = int4{0, 0, 0, 0};
             id = -1;
         }
     }
@@ -1373,17 +1476,26 @@ __global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t*
     }
     same = block_min(same, lds);
     const int prefix = (same << c.page_log2) & ~(kTile - 1);
-    if (in) out[w.skip + s] = prefix;
+    if (in) *reinterpret_cast<int4*>(out + w.members + 4 * s) = int4{prefix, g, off, 0};
     if (s == 0)
         *reinterpret_cast<int4*>(out + w.groups + 4 * g) = prefix ? int4{leader, prefix, list, rows} : int4{0, 0, 0, 0};
     if (prefix)
         for (int i = 0; in && i < n; ++i) out[w.rows + list + off + i] = start + i;
 }
 
+// A group has at least two sequences.
+int most_groups(int n_seqs) { return std::max(n_seqs / 2, 1); }
+Shape prefix_shape(int n_seqs, int n_kv, int total_rows, int max_group_rows, int group, int max_keys) {
+    return shape_for(max_group_rows, group, item_bound(most_groups(n_seqs), n_kv, total_rows, max_group_rows, group, kManyRows),
+                     max_keys);
+}
+Shape own_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int max_keys) {
+    return shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), max_keys);
+}
 bool shares(int max_rows, int max_group_rows, int group, int max_keys) {
     return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows && max_keys > kTile;
 }
-size_t pre_bytes(int total_rows, int n_heads, int head_dim) {
+size_t row_bytes(int total_rows, int n_heads, int head_dim) {
     const size_t n = (size_t)total_rows * n_heads;
     return round256(n * head_dim * 4) + round256(n * 8);
 }
@@ -1391,9 +1503,7 @@ size_t pre_bytes(int total_rows, int n_heads, int head_dim) {
 }  // namespace
 
 size_t attend_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int group) {
-    const Shape s = shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), 0);
-    const size_t rows = (size_t)slots_for(s) * s.rows_per_wg;
-    return round256(rows * head_dim * 4) + round256(rows * 8);
+    return parts_bytes(own_shape(n_seqs, n_kv, total_rows, max_rows, group, 0), head_dim);
 }
 
 hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
@@ -1402,7 +1512,7 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
                          void* ws, hipStream_t st) {
     AttnArgs a = attend_args(c, dtype, layer, row_start, total_rows, max_rows, max_keys, n_heads, q, q_stride, mask, mask_words,
                              scale, o, o_stride, lse);
-    return attend<kPlain>(a, dtype, ws, st);
+    return attend_plain(a, dtype, ws, st);
 }
 
 size_t share_bytes(int n_seqs, int total_rows) { return (size_t)share_words(n_seqs, total_rows).all * 4; }
@@ -1418,8 +1528,8 @@ size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int tot
                                      int group) {
     const size_t own = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_rows, group);
     if (!shares(max_rows, max_group_rows, group, 0x7fffffff)) return own;
-    const size_t pre = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_group_rows, group);
-    return pre_bytes(total_rows, n_kv * group, head_dim) + std::max(own, pre);
+    return own + parts_bytes(prefix_shape(n_seqs, n_kv, total_rows, max_group_rows, group, 0), head_dim) +
+           2 * (row_bytes(total_rows, n_kv * group, head_dim) + round256((size_t)n_seqs * sizeof(int4)));
 }
 
 hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,
@@ -1428,19 +1538,41 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
                                 int64_t o_stride, float* lse, void* ws, hipStream_t st) {
     AttnArgs a = attend_args(c, dtype, layer, row_start, total_rows, max_rows, max_keys, n_heads, q, q_stride, mask, mask_words,
                              scale, o, o_stride, lse);
-    if (!shares(max_rows, max_group_rows, a.group, max_keys)) return attend<kPlain>(a, dtype, ws, st);
+    if (!shares(max_rows, max_group_rows, a.group, max_keys)) return attend_plain(a, dtype, ws, st);
     const ShareWords w = share_words(c.n_seqs, total_rows);
     a.groups = (const int4*)(share + w.groups);
-    a.skip = share + w.skip;
+    a.members = (const int4*)(share + w.members);
     a.rows = share + w.rows;
-    a.pre_o = (float*)ws;
-    a.pre_ml = (float2*)((char*)ws + round256((size_t)total_rows * n_heads * c.head_dim * 4));
-    char* parts = (char*)ws + pre_bytes(total_rows, n_heads, c.head_dim);
     AttnArgs p = a;
     p.max_rows = max_group_rows;
     p.mask = nullptr;
     p.mask_words = 0;
-    const hipError_t e = attend<kPrefix>(p, dtype, parts, st);
-    if (e != hipSuccess) return e;
-    return attend<kSuffix>(a, dtype, parts, st);
+    const Shape sp = prefix_shape(c.n_seqs, c.n_kv, total_rows, max_group_rows, a.group, max_keys);
+    const Shape sa = own_shape(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, max_keys);
+    char* at = (char*)ws;
+    auto carve = [&](AttnArgs& x, const Shape& s) {
+        x.info = (int4*)at;
+        at += round256((size_t)c.n_seqs * sizeof(int4));
+        x.row_o = (float*)at;
+        x.row_ml = (float2*)(at + round256((size_t)total_rows * n_heads * c.head_dim * 4));
+        at += row_bytes(total_rows, n_heads, c.head_dim);
+        take_shape(x, s, at);
+        at += parts_bytes(s, c.head_dim);
+    };
+    carve(p, sp);
+    carve(a, sa);
+    const bool split = may_split(sp, max_keys) || may_split(sa, max_keys);
+    if (!split) {                                         // nothing to join: the second launch takes the prefix in
+        a.pre_o = p.row_o;
+        a.pre_ml = p.row_ml;
+    }
+    hipError_t e = attend<kPrefix>(p, dtype, most_groups(c.n_seqs), may_split(sp, max_keys), st);
+    if (e == hipSuccess) e = attend<kSuffix>(a, dtype, c.n_seqs, may_split(sa, max_keys), st);
+    if (e != hipSuccess || !split) return e;
+    const int per = 256 / (c.head_dim / 4 * kJoinRuns);
+    const dim3 grid((unsigned)total_rows, (unsigned)((n_heads + per - 1) / per));
+    auto kernel = dtype == DLM_F16 ? (c.head_dim == 128 ? join_rows_kernel<true, 128> : join_rows_kernel<true, 64>)
+                                   : (c.head_dim == 128 ? join_rows_kernel<false, 128> : join_rows_kernel<false, 64>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, p);
+    return hipGetLastError();
 }

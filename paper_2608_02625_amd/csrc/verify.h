@@ -15,13 +15,14 @@ struct VerifyArgs {
     const void *target, *draft;
     int64_t target_stride, draft_stride;
     double c;                            // log2(e) / temperature; 0: the largest logit decides
+    float cf;
     const float *u, *u_next;
     int32_t *next, *keep, *keep_start;
     // workspace
     void* parts;
-    int32_t* path;
+    int32_t *path, *removed;
     void* verdicts;
-    double* rest;
+    double *sums, *rest, *inverse;
 };
 int64_t verify_workgroups(int total_rows, int vocab);
 size_t verify_workspace_bytes(int n_seqs, int total_rows, int vocab, bool draft);

@@ -5,18 +5,22 @@
 // not, what is left of p is max(p - q, 0) (a certain draft: p without x), and the next
 // token is the first whose running sum of that passes u' times the whole.
 //
-// Sums and their comparisons are float64: a token is drawn where a running sum over the
-// vocabulary passes a border, and float32 sums over 157184 tokens move the borders by more
-// than many tokens weigh.  The powers are float64 too: reduced to a half around the nearest
-// integer, a polynomial (the series of 2^f to the 11th power, off by 6e-15 of the value).
-//
-//   stats    every row of target and draft in chunks of kChunk tokens: maximum and sum
+//   stats    every row of target and draft in chunks of kChunk tokens, a wave each:
+//            maximum and float32 sum
 //   walk     a workgroup per sequence: rows' totals, drafted tokens' p and q, the path
-//   rest     with a draft: sums of max(p - q, 0) by chunk, for sequences that rejected
+//   sums     float64 sums by chunk of the rows that the next token is drawn from
+//   rest     with a draft: float64 sums of max(p - q, 0) by chunk, where one was rejected
 //   pick     a workgroup per sequence: the next token from chunk sums and one chunk; the
 //            kept rows packed
 //
-// Bound by the bytes of the logits, each read once by `stats`.
+// A token is drawn where a running sum over the vocabulary passes a border, and float32
+// sums over 157184 tokens move the borders by more than many tokens weigh: so the sums of
+// the one row (or pair) that a sequence draws from are float64, of float64 powers (2^t
+// reduced to half around the nearest integer, its series to the 11th power, off by 6e-15).
+// Whether a drafted token is kept is a single comparison, which float32 sums decide but
+// for one in 10^5: when both sides are that near the walk works the row's sum out in
+// float64 itself.  Float64 for every row would be bound by its arithmetic (32 chains of up
+// to 7 tokens of 157184, bf16: 51 us where the bytes take 18).
 #include <float.h>
 
 #include <algorithm>
@@ -26,22 +30,23 @@
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kChunk = 8192;                      // tokens of a chunk: 32 per thread
-constexpr int kPer = kChunk / kThreads;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kChunk = 2048;                      // tokens of a chunk: 32 per lane of a wave, 8 per thread of a workgroup
+constexpr int kPer = kChunk / 64;
 
-// Maximum and sum of 2^(c (z - max)) of a chunk of a row, and the first place of the
+// Maximum and sum of 2^(c (z - max)) of a chunk of a row; greedy: the first place of the
 // maximum (-1: nothing in it).
 struct Part {
-    double s;
-    float m;
-    int32_t at;
+    float m, s;
+    int32_t at, unused;
 };
 // What `walk` found for a sequence.
 struct Verdict {
-    double sp, sq;                                // sums of the node's rows
-    float mp, mq;
-    int32_t count, node, rejected, best;          // kept rows; node; its rejected child (-1: none); greedy's token
+    float mp, mq;                                 // maxima of the node's rows; mp -inf: nothing to draw from
+    int32_t count, node, best;                    // kept rows; node; greedy's token
+    int32_t rest;                                 // its child was rejected, with a draft
+    int32_t removed;                              // rejected certain tokens, from VerifyArgs::removed[start] on
+    int32_t unused;
 };
 
 template <typename T>
@@ -84,80 +89,75 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
+// ------------------------------------------------------------------ chunks
+
+// Chunk ch of a row starts ch * kChunk tokens behind the 16-byte border at or before the
+// row's first token, `off` tokens ahead of it, whatever the stride, so that its vectors are
+// aligned; the vectors that reach past the row's ends are read token by token.
+template <typename T>
+__device__ __forceinline__ int row_offset(const T* row) { return (int)(((uintptr_t)row & 15) / sizeof(T)); }
+
+template <typename T, bool ONCE>
+__device__ __forceinline__ void load_vector(const T* row, int v, int vocab, float* z) {
+    constexpr int E = Elems<T>::N;
+    if (v >= 0 && v + E <= vocab) {
+        typedef T VT __attribute__((ext_vector_type(E)));
+        const VT x = ONCE ? __builtin_nontemporal_load((const VT*)(row + v)) : *(const VT*)(row + v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = (float)x[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = v + e >= 0 && v + e < vocab ? (float)row[v + e] : -INFINITY;
+    }
+}
+// A wave's chunk from token v0 on: lane's tokens v0 + (k * 64 + lane) * E + e.
+template <typename T, bool ONCE>
+__device__ __forceinline__ void load_chunk(const T* row, int v0, int vocab, float (&z)[kPer]) {
+    constexpr int E = Elems<T>::N;
+#pragma unroll
+    for (int k = 0; k < kPer / E; ++k) load_vector<T, ONCE>(row, v0 + (k * 64 + (int)(threadIdx.x & 63)) * E, vocab, z + k * E);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) z[i] = clean(z[i]);
+}
+template <typename T>
+__device__ __forceinline__ int chunk_token(int v0, int i) {
+    constexpr int E = Elems<T>::N;
+    return v0 + (i / E * 64 + (int)(threadIdx.x & 63)) * E + i % E;
+}
+
 // ------------------------------------------------------------------ stats
 
-// Chunk blockIdx.x % chunks of row blockIdx.x / chunks; blockIdx.y: target or draft.
-// A row's vectors start at the 16-byte border at or before its first token, `off` tokens
-// ahead of it, whatever the stride; the vectors that reach past the row's ends are read
-// token by token.
+// Four chunks of row blockIdx.x / groups, a wave each; blockIdx.y: target or draft.
 template <typename T, bool GREEDY>
-__global__ __launch_bounds__(kThreads) void stats_kernel(const VerifyArgs a, int chunks) {
-    constexpr int E = Elems<T>::N, NV = kPer / E;
-    __shared__ float wave_m[4];
-    __shared__ int wave_at[4];
-    __shared__ double wave_s[4];
+__global__ __launch_bounds__(kThreads) void stats_kernel(const VerifyArgs a, int chunks, int groups) {
     const bool draft = blockIdx.y;
-    const int64_t r = blockIdx.x / (unsigned)chunks;
-    const int ch = blockIdx.x % (unsigned)chunks;
+    const int64_t r = blockIdx.x / (unsigned)groups;
+    const int ch = uniform((int)(blockIdx.x % (unsigned)groups) * kWaves + (int)(threadIdx.x >> 6));
+    if (ch >= chunks) return;
     const T* row = (const T*)(draft ? a.draft : a.target) + r * (draft ? a.draft_stride : a.target_stride);
-    const int off = (int)(((uintptr_t)row & 15) / sizeof(T));
-    const int v0 = ch * kChunk - off;
-    float z[NV][E];
-    float m = -INFINITY;
+    const int v0 = ch * kChunk - row_offset(row);
+    float z[kPer];
+    load_chunk<T, true>(row, v0, a.vocab, z);
+    float m = z[0];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int v = v0 + (k * kThreads + (int)threadIdx.x) * E;
-        if (v >= 0 && v + E <= a.vocab) {
-            typedef T VT __attribute__((ext_vector_type(E)));
-            const VT x = __builtin_nontemporal_load((const VT*)(row + v));
+    for (int i = 1; i < kPer; ++i) m = fmaxf(m, z[i]);
+    m = wave_max_dpp(m);
+    float s = 0.f;
+    int at = 0x7fffffff;
+    if (m > -INFINITY) {
+        if constexpr (GREEDY) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) z[k][e] = (float)x[e];
+            for (int i = 0; i < kPer; ++i)
+                if (z[i] == m) at = min(at, chunk_token<T>(v0, i));
+            for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) z[k][e] = v + e >= 0 && v + e < a.vocab ? (float)row[v + e] : -INFINITY;
+            for (int i = 0; i < kPer; ++i) s += __builtin_amdgcn_exp2f((z[i] - m) * a.cf);
+            s = wave_sum_dpp(s);
         }
     }
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            z[k][e] = clean(z[k][e]);
-            m = fmaxf(m, z[k][e]);
-        }
-    const int wave = threadIdx.x >> 6;
-    m = wave_max(m);
-    if ((threadIdx.x & 63) == 0) wave_m[wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
-    if constexpr (GREEDY) {
-        int at = 0x7fffffff;
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (z[k][e] == m && m > -INFINITY) at = min(at, v0 + (k * kThreads + (int)threadIdx.x) * E + e);
-        for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
-        if ((threadIdx.x & 63) == 0) wave_at[wave] = at;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            at = min(min(wave_at[0], wave_at[1]), min(wave_at[2], wave_at[3]));
-            ((Part*)a.parts)[r * chunks + ch] = Part{0.0, m, m > -INFINITY ? at : -1};
-        }
-        return;
-    }
-    double s = 0.0;
-    if (m > -INFINITY) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e) s += weight(z[k][e], m, a.c);
-    }
-    s = wave_sum64(s);
-    if ((threadIdx.x & 63) == 0) wave_s[wave] = s;
-    __syncthreads();
-    if (threadIdx.x == 0)
-        ((Part*)a.parts)[((int64_t)draft * a.total_rows + r) * chunks + ch] =
-            Part{(wave_s[0] + wave_s[1]) + (wave_s[2] + wave_s[3]), m, -1};
+    if ((threadIdx.x & 63) == 0)
+        ((Part*)a.parts)[((int64_t)draft * a.total_rows + r) * chunks + ch] = Part{m, s, at == 0x7fffffff ? -1 : at, 0};
 }
 
 // ------------------------------------------------------------------ walk
@@ -173,134 +173,277 @@ __device__ __forceinline__ Window window(const VerifyArgs& a, int b) {
     return w;
 }
 
+// How near, relative to what is compared, float32 sums may leave a comparison: a power is
+// off by 2^-24 of its exponent, at most 20 or so where it counts, and by its own rounding.
+constexpr double kNear = 1e-5;
+
+// Rows' totals take a wave each, so many waves; the path itself is one wave's work.
+constexpr int kWalkThreads = 1024, kWalkWaves = kWalkThreads / 64;
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void walk_kernel(const VerifyArgs a, int chunks) {
+__global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, int chunks) {
     __shared__ double sum[2][kVerifyMaxRows], p[kVerifyMaxRows], q[kVerifyMaxRows];
-    __shared__ float top[2][kVerifyMaxRows];
+    __shared__ float top[2][kVerifyMaxRows], zp[kVerifyMaxRows], zq[kVerifyMaxRows];
     __shared__ int best[kVerifyMaxRows], parent[kVerifyMaxRows], token[kVerifyMaxRows];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    __shared__ double lds[kWalkWaves];
+    __shared__ int doubt;                         // the row at which the walk waits for exact sums (-1: it is done)
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const Window w = window(a, b);
     const bool greedy = a.c == 0.0;
     Verdict* out = (Verdict*)a.verdicts + b;
     if (w.n == 0) {
-        if (tid == 0) *out = Verdict{0.0, 0.0, 0.f, 0.f, 0, 0, -1, -1};
+        if (tid == 0) *out = Verdict{-INFINITY, 0.f, 0, 0, -1, 0, 0, 0};
         return;
     }
-    // Totals of the rows: a wave each.
+    const T *target = (const T*)a.target + (int64_t)w.start * a.target_stride;
+    const T *draft = (const T*)a.draft + (int64_t)w.start * a.draft_stride;
+    // Drafted tokens and their logits: loads that need no total.
+    if (tid < w.n) {
+        int up = tid - 1;
+        if (tid > 0 && a.parent) up = a.parent[w.start + tid];
+        if (up >= tid || up < 0) up = -1;
+        const int x = a.tokens[w.start + tid];
+        const bool known = up >= 0 && (unsigned)x < (unsigned)a.vocab;
+        parent[tid] = up;
+        token[tid] = x;
+        zp[tid] = known ? logit(target + (int64_t)up * a.target_stride, x) : -INFINITY;
+        zq[tid] = known && a.draft ? logit(draft + (int64_t)up * a.draft_stride, x) : -INFINITY;
+    }
     const int sets = a.draft ? 2 : 1;
-    for (int x = tid >> 6; x < sets * w.n; x += kThreads / 64) {
+    for (int x = wave; x < sets * w.n; x += kWalkWaves) {
         const int d = x >= w.n, i = d ? x - w.n : x;
         const Part* part = (const Part*)a.parts + ((int64_t)d * a.total_rows + w.start + i) * chunks;
-        float m = -INFINITY;
-        for (int ch = lane; ch < chunks; ch += 64) m = fmaxf(m, part[ch].m);
-        m = wave_max(m);
+        const Part none{-INFINITY, 0.f, -1, 0};
+        const Part y0 = lane < chunks ? part[lane] : none, y1 = lane + 64 < chunks ? part[lane + 64] : none;
+        float m = fmaxf(y0.m, y1.m);
+        for (int ch = lane + 128; ch < chunks; ch += 64) m = fmaxf(m, part[ch].m);
+        m = wave_max_dpp(m);
         double s = 0.0;
         int at = 0x7fffffff;
-        for (int ch = lane; ch < chunks; ch += 64) {
-            const Part y = part[ch];
-            if (y.m > -INFINITY) s += y.s * weight(y.m, m, a.c);
+        auto add = [&](const Part& y) {
+            if (y.m > -INFINITY) s += (double)y.s * weight(y.m, m, a.c);
             if (y.at >= 0 && y.m == m) at = min(at, y.at);
-        }
+        };
+        add(y0);
+        add(y1);
+        for (int ch = lane + 128; ch < chunks; ch += 64) add(part[ch]);
         s = wave_sum64(s);
-        for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
+        if (greedy)
+            for (int o = 32; o; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
         if (lane == 0) {
             sum[d][i] = s;
             top[d][i] = m;
             if (!d) best[i] = at == 0x7fffffff ? -1 : at;
         }
     }
-    for (int i = tid; i < w.n; i += kThreads) {
-        const int up = a.parent ? a.parent[w.start + i] : i - 1;
-        parent[i] = i > 0 && up >= 0 && up < i ? up : -1;
-        token[i] = a.tokens[w.start + i];
-    }
     __syncthreads();
-    for (int i = tid; i < w.n; i += kThreads) {
-        const int up = parent[i], x = token[i];
-        double pi = 0.0, qi = a.draft ? 0.0 : 1.0;
-        if (up >= 0 && (unsigned)x < (unsigned)a.vocab) {
-            const int64_t r = (int64_t)w.start + up;
-            if (greedy) {
-                pi = x == best[up] ? 1.0 : 0.0;
-            } else {
-                if (sum[0][up] > 0.0) pi = weight(logit((const T*)a.target + r * a.target_stride, x), top[0][up], a.c) / sum[0][up];
-                if (a.draft) qi = sum[1][up] > 0.0 ? weight(logit((const T*)a.draft + r * a.draft_stride, x), top[1][up], a.c) / sum[1][up] : 0.0;
+    // p and q of the drafted tokens below row `only` (-1: of all).
+    auto chances = [&](int only) {
+        const int i = tid, up = i < w.n ? parent[i] : -1;
+        if (i < w.n && (only < 0 || up == only)) {
+            const int x = token[i];
+            double pi = 0.0, qi = a.draft ? 0.0 : 1.0;
+            if (up >= 0 && greedy) pi = x == best[up] && x >= 0 ? 1.0 : 0.0;
+            if (up >= 0 && !greedy) {
+                if (sum[0][up] > 0.0) pi = weight(zp[i], top[0][up], a.c) / sum[0][up];
+                if (a.draft && sum[1][up] > 0.0) qi = weight(zq[i], top[1][up], a.c) / sum[1][up];
                 // A sibling before it with the same token: nothing is left of it.
                 if (a.parent)
                     for (int j = up + 1; j < i; ++j)
                         if (parent[j] == up && token[j] == x) pi = 0.0;
             }
+            p[i] = pi;
+            q[i] = qi;
         }
-        p[i] = pi;
-        q[i] = qi;
-    }
-    __syncthreads();
-    if (tid) return;
+        __syncthreads();
+    };
+    chances(-1);
+    // The first wave walks, a lane per row, 64 rows at a time: of the rows below the node at
+    // hand the next one is tried, until there is none.
     int* path = a.path + w.start;
-    int at = 0, count = 1, rejected = -1;
+    int* removed = a.removed + w.start;
+    int at = 0, count = 1, rejected = 0, n_removed = 0, exact = -1, from = 1;           // exact: the node of float64 sums
     double mass = 1.0;                            // what is left of the node's p
-    path[0] = 0;
-    for (int i = 1; i < w.n; ++i) {
-        if (parent[i] != at) continue;
-        if (unit(a.u[w.start + i]) * mass * q[i] < p[i]) {
-            at = i;
-            path[count++] = i;
-            rejected = -1;
+    bool done = false;
+    if (tid == 0) path[0] = 0;
+    for (;;) {
+        if (wave == 0) {
+            int stop = -1;
+            for (int i0 = from & ~63; i0 < w.n && !done && stop < 0; i0 += 64) {
+                const int i = i0 + lane;
+                const bool here = i < w.n;
+                const int up = here ? parent[i] : -2;
+                const double x = here ? unit(a.u[w.start + i]) * q[i] : 0.0, r = here ? p[i] : 0.0;
+                for (;;) {
+                    const uint64_t kids = __ballot(up == at && i >= from);
+                    if (!kids) break;
+                    const int l = __builtin_ctzll(kids);
+                    const double lhs = x * mass;
+                    const bool near = !greedy && exact != at && r > 0.0 && fabs(lhs - r) <= kNear * (x + r);
+                    if ((__ballot(near) >> l) & 1) {
+                        stop = i0 + l;
+                        break;
+                    }
+                    from = i0 + l + 1;
+                    if ((__ballot(lhs < r) >> l) & 1) {
+                        at = i0 + l;
+                        if (lane == 0) path[count] = at;
+                        ++count;
+                        rejected = n_removed = 0;
+                        mass = 1.0;
+                        continue;
+                    }
+                    rejected = 1;
+                    if (a.draft) {                // a chain: no other child
+                        done = true;
+                        break;
+                    }
+                    mass = fmax(mass - __shfl(r, l, 64), 0.0);
+                    const int x_l = token[i0 + l];
+                    if ((unsigned)x_l < (unsigned)a.vocab) {
+                        if (lane == 0) removed[n_removed] = x_l;
+                        ++n_removed;
+                    }
+                }
+                from = max(from, i0 + 64 < w.n && stop < 0 && !done ? i0 + 64 : from);
+            }
+            if (lane == 0) doubt = stop;
+            if (stop >= 0) from = stop;
+        }
+        __syncthreads();
+        const int row = doubt;
+        if (row < 0) break;
+        const int node = parent[row];
+        for (int d = 0; d < sets; ++d) {
+            const T* z = d ? draft + (int64_t)node * a.draft_stride : target + (int64_t)node * a.target_stride;
+            double s = 0.0;
+            for (int v = tid; v < a.vocab; v += kWalkThreads) s += weight(logit(z, v), top[d][node], a.c);
+            s = wave_sum64(s);
+            __syncthreads();
+            if (lane == 0) lds[wave] = s;
+            __syncthreads();
+            if (tid == 0) {
+                s = lds[0];
+                for (int i = 1; i < kWalkWaves; ++i) s += lds[i];
+                sum[d][node] = s;
+            }
+        }
+        __syncthreads();
+        chances(node);
+        exact = node;                             // the first wave's `at`
+        if (wave == 0) {                          // the children rejected before it
             mass = 1.0;
-        } else {
-            rejected = i;
-            if (a.draft) break;                   // a chain: no other child
-            mass = fmax(mass - p[i], 0.0);
+            for (int i = node + 1; i < row; ++i)
+                if (parent[i] == node) mass = fmax(mass - p[i], 0.0);
         }
     }
-    *out = Verdict{sum[0][at], a.draft ? sum[1][at] : 0.0, top[0][at], a.draft ? top[1][at] : 0.f, count, at, rejected, best[at]};
+    if (tid) return;
+    const bool any = sum[0][at] > 0.0;
+    *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, n_removed, 0};
 }
 
-// ------------------------------------------------------------------ rest
+// ------------------------------------------------------------------ sums, rest
 
-// A token's weight in what the next one is drawn from: p, or max(p - q, 0).
+// The node's row of a sequence in target or draft.
 template <typename T>
-struct Rest {
-    const T *prow, *qrow;                         // qrow NULL: p alone
-    float mp, mq;
-    double sp, sq, c;
-    __device__ __forceinline__ double operator()(int64_t v) const {
-        const double x = weight(logit(prow, v), mp, c);
-        if (!qrow) return x;
-        return fmax(x / sp - (sq > 0.0 ? weight(logit(qrow, v), mq, c) / sq : 0.0), 0.0);
-    }
-};
-template <typename T>
-__device__ __forceinline__ Rest<T> rest_of(const VerifyArgs& a, const Verdict& d, int start, bool with_draft) {
+__device__ __forceinline__ const T* node_row(const VerifyArgs& a, const Verdict& d, int start, bool draft) {
     const int64_t r = (int64_t)start + d.node;
-    return Rest<T>{(const T*)a.target + r * a.target_stride,
-                   with_draft ? (const T*)a.draft + r * a.draft_stride : nullptr, d.mp, d.mq, d.sp, d.sq, a.c};
+    return (const T*)(draft ? a.draft : a.target) + r * (draft ? a.draft_stride : a.target_stride);
 }
-
-// Sum over the workgroup, the same in every thread.
-__device__ __forceinline__ double block_sum(double v, double* lds) {
+// A workgroup's thread of a chunk: kDraw tokens from v on, those that are gone at -infinity.
+constexpr int kDraw = kChunk / kThreads;
+template <typename T>
+__device__ __forceinline__ void load_target(const VerifyArgs& a, const Verdict& d, int start, const T* row, int v,
+                                            float (&z)[kDraw]) {
+    constexpr int E = Elems<T>::N;
+#pragma unroll
+    for (int k = 0; k < kDraw / E; ++k) load_vector<T, false>(row, v + k * E, a.vocab, z + k * E);
+#pragma unroll
+    for (int i = 0; i < kDraw; ++i) z[i] = clean(z[i]);
+    for (int j = 0; j < d.removed; ++j) {
+        const int x = a.removed[start + j];
+#pragma unroll
+        for (int i = 0; i < kDraw; ++i)
+            if (v + i == x) z[i] = -INFINITY;
+    }
+}
+// The same tokens of the draft's row, whose vectors may lie otherwise.
+template <typename T>
+__device__ __forceinline__ void load_draft(const VerifyArgs& a, const T* row, int v, float (&z)[kDraw]) {
+    constexpr int E = Elems<T>::N;
+    if ((uintptr_t)(row + v) % 16 == 0) {
+#pragma unroll
+        for (int k = 0; k < kDraw / E; ++k) load_vector<T, false>(row, v + k * E, a.vocab, z + k * E);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kDraw; ++i) z[i] = v + i >= 0 && v + i < a.vocab ? (float)row[v + i] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < kDraw; ++i) z[i] = clean(z[i]);
+}
+// Sum over the workgroup, in its first thread.
+__device__ __forceinline__ double first_sum(double v, double* lds) {
     v = wave_sum64(v);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// A workgroup per chunk.  Sums [2][n_seqs][chunks]: blockIdx.z: target or draft.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void rest_kernel(const VerifyArgs a, int chunks) {
-    __shared__ double lds[4];
-    const int b = blockIdx.y, ch = blockIdx.x;
+__global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs a, int chunks) {
+    __shared__ double lds[kWaves];
+    const int ch = blockIdx.x, b = blockIdx.y, set = blockIdx.z;
     const Window w = window(a, b);
     const Verdict d = ((const Verdict*)a.verdicts)[b];
-    if (w.n == 0 || d.rejected < 0 || !(d.sp > 0.0)) return;
-    const Rest<T> rest = rest_of<T>(a, d, w.start, true);
+    if (d.count == 0 || !(d.mp > -INFINITY) || (set && !d.rest)) return;
+    const T* row = node_row<T>(a, d, w.start, set);
+    const int v = ch * kChunk - row_offset(row) + (int)threadIdx.x * kDraw;
+    const float m = set ? d.mq : d.mp;
     double s = 0.0;
-#pragma unroll 4
-    for (int k = 0; k < kPer; ++k) {
-        const int v = ch * kChunk + k * kThreads + (int)threadIdx.x;
-        if (v < a.vocab) s += rest(v);
+    if (m > -INFINITY) {
+        float z[kDraw];
+        load_target(a, d, w.start, row, v, z);            // with a draft nothing is gone
+#pragma unroll
+        for (int i = 0; i < kDraw; ++i) s += weight(z[i], m, a.c);
     }
-    s = block_sum(s, lds);
+    s = first_sum(s, lds);
+    if (threadIdx.x == 0) a.sums[((int64_t)set * a.n_seqs + b) * chunks + ch] = s;
+}
+// 1 over the sum of a row's chunks; 0 if there is none.
+__device__ __forceinline__ double wave_inverse(const double* sums, int chunks) {
+    const int lane = threadIdx.x & 63;
+    double s = 0.0;
+    for (int ch = lane; ch < chunks; ch += 64) s += sums[ch];
+    s = wave_sum64(s);
+    return s > 0.0 ? 1.0 / s : 0.0;
+}
+// Chunks of the target's row: max(p - q, 0).
+template <typename T>
+__global__ __launch_bounds__(kThreads) void rest_kernel(const VerifyArgs a, int chunks) {
+    __shared__ double lds[kWaves];
+    const int ch = blockIdx.x, b = blockIdx.y;
+    const Window w = window(a, b);
+    const Verdict d = ((const Verdict*)a.verdicts)[b];
+    if (!d.rest || !(d.mp > -INFINITY)) return;
+    const T* prow = node_row<T>(a, d, w.start, false);
+    const int v = ch * kChunk - row_offset(prow) + (int)threadIdx.x * kDraw;
+    float z[kDraw], y[kDraw];
+    load_target(a, d, w.start, prow, v, z);
+    load_draft(a, node_row<T>(a, d, w.start, true), v, y);
+    const double ip = wave_inverse(a.sums + (int64_t)b * chunks, chunks);
+    const double iq = wave_inverse(a.sums + ((int64_t)a.n_seqs + b) * chunks, chunks);
+    if (ch == 0 && threadIdx.x == 0) {
+        a.inverse[2 * b] = ip;
+        a.inverse[2 * b + 1] = iq;
+    }
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < kDraw; ++i) {
+        const double x = weight(z[i], d.mp, a.c) * ip;
+        s += iq > 0.0 ? fmax(x - weight(y[i], d.mq, a.c) * iq, 0.0) : x;
+    }
+    s = first_sum(s, lds);
     if (threadIdx.x == 0) a.rest[(int64_t)b * chunks + ch] = s;
 }
 
@@ -315,73 +458,66 @@ __device__ __forceinline__ double block_scan(double v, double* lds, double* tota
         const double y = __shfl_up(x, o, 64);
         if (lane >= o) x += y;
     }
-    __syncthreads();
     if (lane == 63) lds[wave] = x;
     __syncthreads();
-    double before = 0.0;
-    for (int i = 0; i < wave; ++i) before += lds[i];
-    *total = ((lds[0] + lds[1]) + lds[2]) + lds[3];
+    double before = 0.0, t = 0.0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < wave) before += lds[i];
+        t += lds[i];
+    }
+    *total = t;
     return before + (x - v);
 }
-
-// A workgroup finds the first of n items whose running sum of weights passes `target`;
-// thread t has items t * per .. and their weights come from `f`.  Rounding may leave none:
-// then the last of positive weight.  -1: no positive weight.  *base: the sum before it.
-template <typename F>
-__device__ __forceinline__ int first_past(int n, double target, double start, F f, double* lds, int* found, double* base) {
-    const int per = (n + kThreads - 1) / kThreads;
-    const int i0 = min((int)threadIdx.x * per, n), i1 = min(i0 + per, n);
-    double own = 0.0;
-    int last = -1;
-    for (int i = i0; i < i1; ++i) {
-        const double x = f(i);
-        own += x;
-        if (x > 0.0) last = i;
-    }
-    double total;
-    const double before = start + block_scan(own, lds, &total);
+// The first thread of a workgroup with `hit` (-1: none).
+__device__ __forceinline__ int first_thread(bool hit, int* lds) {
+    const uint64_t votes = __ballot(hit);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = votes ? __builtin_ctzll(votes) : -1;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        found[0] = 0x7fffffff;
-        found[1] = -1;
-    }
+    int at = -1;
+#pragma unroll
+    for (int i = kWaves - 1; i >= 0; --i) at = lds[i] >= 0 ? i * 64 + lds[i] : at;
+    return at;
+}
+__device__ __forceinline__ int last_thread(bool hit, int* lds) {
+    const uint64_t votes = __ballot(hit);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = votes ? 63 - __builtin_clzll(votes) : -1;
     __syncthreads();
-    double run = before;
-    int hit = 0x7fffffff;
-    if (before + own > target)                    // monotone: the first such thread holds it
-        for (int i = i0; i < i1; ++i) {
-            const double x = f(i);
-            if (run + x > target && x > 0.0) {
-                hit = i;
-                break;
-            }
-            run += x;
-        }
-    if (hit != 0x7fffffff) atomicMin(&found[0], hit);
-    if (last >= 0) atomicMax(&found[1], last);
-    __syncthreads();
-    const int first = found[0], back = found[1];
-    const int at = first != 0x7fffffff ? first : back;
-    __syncthreads();
-    if (at >= i0 && at < i1) {
-        run = before;
-        for (int i = i0; i < at; ++i) run += f(i);
-        lds[0] = run;
-    }
-    __syncthreads();
-    *base = lds[0];
+    int at = -1;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) at = lds[i] >= 0 ? i * 64 + lds[i] : at;
     return at;
 }
 
+// Of max(p - q, 0) in all: what equal rows may leave by the rounding of their sums and
+// products (a few 2^-53 of p each), with room to spare.
+constexpr double kNothing = 0x1p-43;
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int chunks, int rest_chunks) {
-    __shared__ double lds[4];
-    __shared__ int found[2], counts[2];
-    __shared__ uint32_t gone[kChunk / 32];        // tokens of the chunk that were rejected
-    const int b = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int chunks) {
+    __shared__ double scan[2][kWaves], part_total[kWaves], chosen_before;
+    __shared__ int first[4][kWaves], counts[2][kWaves], chosen;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Verdict* verdicts = (const Verdict*)a.verdicts;
     const Verdict d = verdicts[b];
     const Window w = window(a, b);
+    const bool draws = d.count > 0 && a.c != 0.0 && d.mp > -INFINITY;
+    // A thread's run of chunks: what they weigh, of p and of max(p - q, 0).
+    const double* sums = a.sums + (int64_t)b * chunks;
+    const int per = (chunks + kThreads - 1) / kThreads;
+    const int c0 = min(tid * per, chunks), c1 = min(c0 + per, chunks);
+    double own = 0.0, own_rest = 0.0, ip = 1.0, iq = 0.0;
+    if (draws) {
+        for (int ch = c0; ch < c1; ++ch) {
+            own += sums[ch];
+            if (d.rest) own_rest += a.rest[(int64_t)b * chunks + ch];
+        }
+        if (d.rest) {
+            ip = a.inverse[2 * b];
+            iq = a.inverse[2 * b + 1];
+        }
+    }
+    const double u = draws ? unit(a.u_next[b]) : 0.0;
 
     // The kept rows behind those of the sequences before.
     int mine = 0, all = 0;
@@ -390,84 +526,100 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int 
         all += n;
         if (s < b) mine += n;
     }
-    if (tid < 2) counts[tid] = 0;
+    for (int o = 32; o; o >>= 1) {
+        mine += __shfl_xor(mine, o, 64);
+        all += __shfl_xor(all, o, 64);
+    }
+    const double rest_all = wave_sum64(own_rest);
+    if (lane == 0) {
+        counts[0][wave] = mine;
+        counts[1][wave] = all;
+        part_total[wave] = rest_all;
+    }
     __syncthreads();
-    atomicAdd(&counts[0], mine);
-    atomicAdd(&counts[1], all);
-    __syncthreads();
-    const int base = counts[0], total_keep = min(counts[1], a.total_rows);
+    int base = 0, total_keep = 0;
+    double rest_total = 0.0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        base += counts[0][i];
+        total_keep += counts[1][i];
+        rest_total += part_total[i];
+    }
+    total_keep = min(total_keep, a.total_rows);
     for (int i = tid; i < d.count; i += kThreads)
         if (base + i < a.total_rows) a.keep[base + i] = a.path[w.start + i];
     for (int64_t i = total_keep + (int64_t)b * kThreads + tid; i < a.total_rows; i += (int64_t)a.n_seqs * kThreads) a.keep[i] = -1;
     if (tid == 0) {
         a.keep_start[b] = min(base, a.total_rows);
         if (b == a.n_seqs - 1) a.keep_start[a.n_seqs] = total_keep;
+        if (!draws) a.next[b] = d.count && a.c == 0.0 ? d.best : -1;
     }
+    if (!draws) return;
 
-    if (d.count == 0 || a.c == 0.0 || !(d.sp > 0.0)) {        // nothing to draw from, or nothing to draw
-        if (tid == 0) a.next[b] = d.count && a.c == 0.0 ? d.best : -1;
-        return;
+    const T *prow = node_row<T>(a, d, w.start, false), *qrow = nullptr;
+    if (d.rest && rest_total > kNothing) {        // else p = q but for rounding: then from p
+        sums = a.rest + (int64_t)b * chunks;
+        own = own_rest;
+        if (iq > 0.0) qrow = node_row<T>(a, d, w.start, true);
+    } else {
+        ip = 1.0;
     }
-    const double u = unit(a.u_next[b]);
-    const int64_t row = (int64_t)w.start + d.node;
-    const bool is_tree = !a.draft;
-    bool with_draft = a.draft && d.rejected >= 0;
-    // Rejected children of a certain draft.
-    auto removed = [&](int i) {
-        return is_tree && d.rejected >= 0 && i > d.node && i <= d.rejected &&
-               (a.parent ? a.parent[w.start + i] == d.node : i == d.node + 1);
-    };
-    const Part* part = (const Part*)a.parts + row * chunks;
-    const double* sums = a.rest + (int64_t)b * rest_chunks;
-    if (with_draft) {                             // p = q but for rounding: then from p
-        double s = 0.0;
-        for (int ch = tid; ch < rest_chunks; ch += kThreads) s += sums[ch];
-        if (!(block_sum(s, lds) > 0.0)) with_draft = false;
-    }
-    const Rest<T> rest = rest_of<T>(a, d, w.start, with_draft);
-    const int off = with_draft ? 0 : (int)(((uintptr_t)rest.prow & 15) / sizeof(T));
-    const int n_chunks = with_draft ? rest_chunks : chunks;
-    auto chunk_weight = [&](int ch) {
-        if (with_draft) return sums[ch];
-        const Part y = part[ch];
-        double s = y.m > -INFINITY ? y.s * weight(y.m, d.mp, a.c) : 0.0;
-        if (is_tree && d.rejected >= 0) {
-            for (int i = d.node + 1; i <= d.rejected; ++i) {
-                if (!removed(i)) continue;
-                const int x = a.tokens[w.start + i];
-                if ((unsigned)x >= (unsigned)a.vocab || (x + off) / kChunk != ch) continue;
-                bool again = false;
-                for (int j = d.node + 1; j < i; ++j) again |= removed(j) && a.tokens[w.start + j] == x;
-                if (!again) s -= rest(x);
+    // The first chunk at which the running sum passes the border; rounding may leave none:
+    // then the last of positive weight, and its last such token.
+    double total;
+    double run = block_scan(own, scan[0], &total);
+    const double border = u * total;
+    const int t = first_thread(run + own > border && own > 0.0, first[0]);
+    const int back = t >= 0 ? t : last_thread(own > 0.0, first[1]);
+    if (tid == (back >= 0 ? back : 0)) {
+        int ch = -1;
+        double before = 0.0;
+        for (int i = c0; i < c1; ++i) {
+            const double x = sums[i];
+            if (x > 0.0) {
+                ch = i;
+                before = run;
+                if (t >= 0 && run + x > border) break;
             }
+            run += x;
         }
-        return fmax(s, 0.0);
-    };
-    double sum = 0.0, before;
-    for (int ch = tid; ch < n_chunks; ch += kThreads) sum += chunk_weight(ch);
-    const double target = u * block_sum(sum, lds);
-    int ch = first_past(n_chunks, target, 0.0, chunk_weight, lds, found, &before);
-    int token = -1;
-    // Rounding may leave a chunk of positive weight without such a token: the next ones.
-    for (int tries = 0; ch >= 0 && ch < n_chunks && token < 0; ++tries, ch = ch + 1 == n_chunks ? 0 : ch + 1) {
-        if (tries == n_chunks) break;
-        const int v0 = ch * kChunk - off;
-        for (int i = tid; i < kChunk / 32; i += kThreads) gone[i] = 0;
-        __syncthreads();
-        if (is_tree && d.rejected >= 0)
-            for (int i = d.node + 1 + tid; i <= d.rejected; i += kThreads) {
-                const int x = a.tokens[w.start + i];
-                if (removed(i) && x >= v0 && x < v0 + kChunk && (unsigned)x < (unsigned)a.vocab)
-                    atomicOr(&gone[(x - v0) >> 5], 1u << ((x - v0) & 31));
+        chosen = ch;
+        chosen_before = before;
+    }
+    __syncthreads();
+    int ch = chosen, token = -1;
+    const double before = chosen_before;
+    for (int tries = 0; ch >= 0 && token < 0 && tries < chunks; ++tries, ch = ch + 1 == chunks ? 0 : ch + 1) {
+        const int v = ch * kChunk - row_offset(prow) + tid * kDraw;
+        float z[kDraw], y[kDraw];
+        load_target(a, d, w.start, prow, v, z);
+        if (qrow) load_draft(a, qrow, v, y);
+        double x[kDraw];
+        own = 0.0;
+#pragma unroll
+        for (int i = 0; i < kDraw; ++i) {
+            x[i] = weight(z[i], d.mp, a.c) * ip;
+            if (qrow) x[i] = fmax(x[i] - weight(y[i], d.mq, a.c) * iq, 0.0);
+            own += x[i];
+        }
+        // The first token that passes the border; by rounding none: the last that weighs
+        // anything.  No such token (sums that were rounding alone): the first of the next chunks.
+        run = block_scan(own, scan[1], &total) + before;
+        const double past = tries ? -1.0 : border;
+        const int t1 = first_thread(own > 0.0 && (tries || run + own > past), first[2]);
+        const int t2 = t1 >= 0 ? t1 : last_thread(own > 0.0, first[3]);
+        if (tid == (t2 >= 0 ? t2 : 0)) {
+            int hit = -1;
+#pragma unroll
+            for (int i = 0; i < kDraw; ++i) {
+                const bool passed = hit >= 0 && t1 >= 0 && run > past;
+                if (x[i] > 0.0 && !passed) hit = v + i;
+                run += x[i];
             }
+            chosen = t2 >= 0 ? hit : -1;
+        }
         __syncthreads();
-        double none;
-        const int i = first_past(kChunk, tries ? 0.0 : target, tries ? 0.0 : before, [&](int y) {
-            const int v = v0 + y;
-            if (v < 0 || v >= a.vocab || ((gone[y >> 5] >> (y & 31)) & 1)) return 0.0;
-            return rest(v);
-        }, lds, found, &none);
-        if (i >= 0) token = v0 + i;
+        token = chosen;
         __syncthreads();
     }
     if (tid == 0) a.next[b] = token;
@@ -475,42 +627,57 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int 
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 // A row may start in the middle of a 16-byte vector of up to 8 tokens.
-int64_t stat_chunks(int vocab) { return ((int64_t)vocab + 7 + kChunk - 1) / kChunk; }
-int64_t rest_chunks(int vocab) { return ((int64_t)vocab + kChunk - 1) / kChunk; }
+int64_t row_chunks(int vocab) { return ((int64_t)vocab + 7 + kChunk - 1) / kChunk; }
+int64_t row_groups(int vocab) { return (row_chunks(vocab) + kWaves - 1) / kWaves; }
 
 template <typename T>
 hipError_t verify_type(const VerifyArgs& a, hipStream_t st) {
-    const int chunks = (int)stat_chunks(a.vocab), rest = (int)rest_chunks(a.vocab);
-    const dim3 grid((unsigned)((int64_t)a.total_rows * chunks), a.draft ? 2 : 1);
+    const int chunks = (int)row_chunks(a.vocab), groups = (int)row_groups(a.vocab), sets = a.draft ? 2 : 1;
+    const bool greedy = a.c == 0.0;
     if (a.total_rows > 0) {
-        if (a.c == 0.0) hipLaunchKernelGGL((stats_kernel<T, true>), grid, dim3(kThreads), 0, st, a, chunks);
-        else hipLaunchKernelGGL((stats_kernel<T, false>), grid, dim3(kThreads), 0, st, a, chunks);
+        const dim3 grid((unsigned)((int64_t)a.total_rows * groups), sets);
+        if (greedy) hipLaunchKernelGGL((stats_kernel<T, true>), grid, dim3(kThreads), 0, st, a, chunks, groups);
+        else hipLaunchKernelGGL((stats_kernel<T, false>), grid, dim3(kThreads), 0, st, a, chunks, groups);
     }
-    hipLaunchKernelGGL((walk_kernel<T>), dim3(a.n_seqs), dim3(kThreads), 0, st, a, chunks);
-    if (a.draft) hipLaunchKernelGGL((rest_kernel<T>), dim3(rest, a.n_seqs), dim3(kThreads), 0, st, a, rest);
-    hipLaunchKernelGGL((pick_kernel<T>), dim3(a.n_seqs), dim3(kThreads), 0, st, a, chunks, rest);
+    hipLaunchKernelGGL((walk_kernel<T>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a, chunks);
+    if (!greedy) hipLaunchKernelGGL((sums_kernel<T>), dim3(chunks, a.n_seqs, sets), dim3(kThreads), 0, st, a, chunks);
+    if (a.draft) hipLaunchKernelGGL((rest_kernel<T>), dim3(chunks, a.n_seqs), dim3(kThreads), 0, st, a, chunks);
+    hipLaunchKernelGGL((pick_kernel<T>), dim3(a.n_seqs), dim3(kThreads), 0, st, a, chunks);
     return hipGetLastError();
 }
+// Workspace in order: parts, path, removed, verdicts, sums, rest and inverses.
+struct Sizes {
+    size_t parts, rows, verdicts, sums, rest;
+    Sizes(int n_seqs, int total_rows, int vocab, bool draft) {
+        const size_t chunks = row_chunks(vocab), sets = draft ? 2 : 1;
+        parts = round256(sets * total_rows * chunks * sizeof(Part));
+        rows = round256((size_t)total_rows * 4);
+        verdicts = round256((size_t)n_seqs * sizeof(Verdict));
+        sums = round256(sets * n_seqs * chunks * 8);
+        rest = draft ? round256((size_t)n_seqs * chunks * 8) + round256((size_t)n_seqs * 16) : 0;
+    }
+};
 
 }  // namespace
 
-int64_t verify_workgroups(int total_rows, int vocab) { return total_rows * stat_chunks(vocab); }
+int64_t verify_workgroups(int total_rows, int vocab) { return total_rows * row_groups(vocab); }
 
 size_t verify_workspace_bytes(int n_seqs, int total_rows, int vocab, bool draft) {
-    return round256((size_t)(draft ? 2 : 1) * total_rows * stat_chunks(vocab) * sizeof(Part)) +
-           round256((size_t)total_rows * 4) + round256((size_t)n_seqs * sizeof(Verdict)) +
-           round256(draft ? (size_t)n_seqs * rest_chunks(vocab) * 8 : 0);
+    const Sizes z(n_seqs, total_rows, vocab, draft);
+    return z.parts + 2 * z.rows + z.verdicts + z.sums + z.rest;
 }
 
 hipError_t launch_verify(VerifyArgs a, int dtype, void* ws, hipStream_t st) {
+    const Sizes z(a.n_seqs, a.total_rows, a.vocab, a.draft != nullptr);
     char* at = (char*)ws;
     a.parts = at;
-    at += round256((size_t)(a.draft ? 2 : 1) * a.total_rows * stat_chunks(a.vocab) * sizeof(Part));
-    a.path = (int32_t*)at;
-    at += round256((size_t)a.total_rows * 4);
-    a.verdicts = at;
-    at += round256((size_t)a.n_seqs * sizeof(Verdict));
-    a.rest = (double*)at;
+    a.path = (int32_t*)(at += z.parts);
+    a.removed = (int32_t*)(at += z.rows);
+    a.verdicts = at += z.rows;
+    a.sums = (double*)(at += z.verdicts);
+    a.rest = (double*)(at += z.sums);
+    a.inverse = (double*)(at + round256((size_t)a.n_seqs * row_chunks(a.vocab) * 8));
+    a.cf = (float)std::min(a.c, 3e38);
     if (dtype == DLM_BF16) return verify_type<__bf16>(a, st);
     if (dtype == DLM_F16) return verify_type<_Float16>(a, st);
     return verify_type<float>(a, st);

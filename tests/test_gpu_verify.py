@@ -82,8 +82,7 @@ def reference(starts, tokens, target, u, u_next, parent=None, draft=None, temper
                         path.append(i)
                         continue
                     rest = np.maximum(p - q, 0.0)
-                    rest[rest < 1e-16] = 0.0          # p = q but for rounding
-                    if rest.sum() > 0:
+                    if rest.sum() > 2.0 ** -43:       # else p = q but for rounding
                         p = rest
                     break
                 if known and _less(_unit(u[a + i]) * p.sum(), p[x]):
@@ -158,7 +157,7 @@ def _same(got, want):
     assert got.keep.tolist() == want[1]
 
 
-VOCABS = [1, 2, 3, 100, 2047, 8184, 8185, 8191, 8192, 8193, 16385, 20001]
+VOCABS = [1, 2, 3, 100, 2040, 2041, 2047, 2048, 2049, 4097, 8185, 20001]
 
 
 @pytest.mark.parametrize("shape", ["chain", "certain", "tree"])
@@ -364,3 +363,33 @@ def test_refusals_of_the_binding():
                dict(parent=a[1], draft=a[2])):
         with pytest.raises(DlmError):
             _verify(*a, **kw)
+
+
+@pytest.mark.parametrize("shape", ["chain", "certain", "tree"])
+@pytest.mark.parametrize("V,dtype", [(700, F32), (20001, BF)])
+def test_decisions_on_the_edge(V, dtype, shape):
+    """Random numbers next to p / q, below and above it: decided as float64 does."""
+    rows = [9, 7, 12]
+    c = _case(91 + V, rows, V, dtype, shape, 0.9)
+    target = c["target"].double().numpy()
+    draft = None if c["draft"] is None else c["draft"].double().numpy()
+    for side in range(3):
+        for s, n in enumerate(rows):
+            a = c["starts"][s]
+            left = {}
+            for i in range(1, n):
+                up = i - 1 if c["parent"] is None else int(c["parent"][a + i])
+                p = left.setdefault(up, _chances(target[a + up], 0.9))
+                x = c["tokens"][a + i]
+                q = 1.0 if draft is None else _chances(draft[a + up], 0.9)[x]
+                u = np.float32(min(p[x] / (q * p.sum()), 1.0 - 2.0 ** -24))
+                # the last ones of a window above p / q (rejected), the others below (kept) or either
+                up_side = side == 2 or (side == 1 and i >= n - 3)
+                for _ in range(2):
+                    u = np.nextafter(u, np.float32(2.0 if up_side else -1.0))
+                c["u"][a + i] = float(np.clip(u, 0.0, 1.0 - 2.0 ** -24))
+                if draft is None and up_side:
+                    p[x] = 0.0
+        want = _want(c)
+        _same(_run(c), want)
+    assert want[2][-1] < sum(rows)
