@@ -224,8 +224,13 @@ class _NormRotation(torch.autograd.Function):
         return rope._norm_apply(q, k, positions, q_gain, k_gain, eps, None, None)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dq, dk):
+        if torch.is_grad_enabled():                   # create_graph: a gradient of it is refused
+            return _NormRotation._final(ctx, dq, dk)
+        return _NormRotation._gradients(ctx, dq, dk)
+
+    @staticmethod
+    def _gradients(ctx, dq, dk):
         q, k, positions, q_gain, k_gain = ctx.saved_tensors
         if dq is None and dk is None:
             return (None,) * 7
@@ -233,6 +238,8 @@ class _NormRotation(torch.autograd.Function):
         gq, gk, gqg, gkg = ctx.rope._norm_grad(q, k, positions, q_gain, k_gain, ctx.eps, dq, dk,
                                                (need[0], need[1], need[3], need[4]))
         return gq, gk, None, gqg, gkg, None, None
+
+    _final = staticmethod(torch.autograd.function.once_differentiable(lambda *a: _NormRotation._gradients(*a)))
 
 
 class _Rotation(torch.autograd.Function):

@@ -12,6 +12,7 @@
 // cosines are worked out once per row, and the lanes walk heads with them, several heads'
 // loads in flight.
 #include <algorithm>
+#include <type_traits>
 
 #include "rotary.h"
 
@@ -19,15 +20,13 @@ namespace {
 
 // How a workgroup's threads are laid over a head, the heads and the rows: runs of
 // `run` lanes (a power of two), of which `turn` chunks hold V pairs each and `pass`
-// chunks the V values behind the rotated ones; `slots` heads at a time of `rows` rows.
+// chunks the values behind the rotated ones; `slots` heads at a time of `rows` rows.
 struct NormLanes {
     int turn, pass, run, slots, rows;
 };
-
-// Chunks of a lane: more than one only where a head of up to 256 values is taken in
-// pieces so small that a wave has too few lanes for it.
-template <int V>
-constexpr int kChunks = V >= 4 ? 1 : V == 2 ? 2 : 4;
+// Values of a chunk behind the rotated ones: as many bytes as the accesses of a pair's.
+template <int V, bool INTER>
+constexpr int kPass = INTER && V > 1 ? 2 * V : V;
 
 // Sum over the run of lanes that this one belongs to.
 __device__ __forceinline__ float run_sum(float v, int run) {
@@ -40,37 +39,65 @@ __device__ __forceinline__ float run_sum(float v, int run) {
     return v;
 }
 
-// A chunk of a head in registers: V pairs (a[i], a[V + i]), or V values and zeros.
+// A chunk of a head as it is loaded (whole registers: an array of values would be put
+// into memory), and in float32: V pairs (a[i], a[V + i]), or kPass values and zeros.
+template <int BYTES>
+struct Bits;
+template <>
+struct Bits<16> { typedef u32x4 type; };
+template <>
+struct Bits<8> { typedef u32x2 type; };
+template <>
+struct Bits<4> { typedef uint32_t type; };
+template <>
+struct Bits<2> { typedef uint16_t type; };
+
+template <typename S, int V, bool INTER>
+struct Raw {
+    typedef typename Bits<(INTER ? 2 : 1) * V * sizeof(S)>::type X;
+    typedef typename Bits<V * sizeof(S)>::type Y;
+    X x;                                                      // pairs, their first values, or values
+    Y y;                                                      // half layout: the pairs' second values
+};
 template <typename S, int V, bool INTER, bool STREAM>
-__device__ __forceinline__ void load_chunk(const S* src, int c, const NormLanes& ln, int rot_dim, float (&a)[2 * V]) {
+__device__ __forceinline__ Raw<S, V, INTER> load_chunk(const S* src, int c, const NormLanes& ln, int rot_dim) {
+    constexpr int P = kPass<V, INTER>;
+    Raw<S, V, INTER> r{};
     if (c < ln.turn) {
         if constexpr (INTER) {
-            const auto x = load<STREAM, Vec<S, 2 * V>>(src + 2 * V * c);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                a[i] = to_f32(x.v[2 * i]);
-                a[V + i] = to_f32(x.v[2 * i + 1]);
-            }
+            r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + 2 * V * c);
         } else {
-            const auto x = load<STREAM, Vec<S, V>>(src + V * c), y = load<STREAM, Vec<S, V>>(src + V * c + rot_dim / 2);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                a[i] = to_f32(x.v[i]);
-                a[V + i] = to_f32(y.v[i]);
-            }
+            r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + V * c);
+            r.y = load<STREAM, typename Raw<S, V, INTER>::Y>(src + V * c + rot_dim / 2);
         }
-        return;
+    } else if (c < ln.turn + ln.pass) {
+        if constexpr (INTER && V == 1) r.y = load<false, typename Raw<S, V, INTER>::Y>(src + rot_dim + (c - ln.turn) * P);
+        else r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + rot_dim + (c - ln.turn) * P);
     }
+    return r;
+}
+template <typename S, int V, bool INTER>
+__device__ __forceinline__ void widen_chunk(const Raw<S, V, INTER>& r, int c, const NormLanes& ln, float (&a)[2 * V]) {
+    const bool turns = c < ln.turn;
+    const auto x = __builtin_bit_cast(Vec<S, (INTER ? 2 : 1) * V>, r.x);
+    const auto y = __builtin_bit_cast(Vec<S, V>, r.y);
 #pragma unroll
-    for (int i = 0; i < 2 * V; ++i) a[i] = 0.f;
-    if (c < ln.turn + ln.pass) {
-        const auto x = load<STREAM, Vec<S, V>>(src + rot_dim + (c - ln.turn) * V);
-#pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = to_f32(x.v[i]);
+    for (int i = 0; i < V; ++i) {
+        if constexpr (!INTER) {
+            a[i] = to_f32(x.v[i]);
+            a[V + i] = to_f32(y.v[i]);
+        } else if constexpr (V == 1) {                        // a single value behind the rotated ones
+            a[0] = turns ? to_f32(x.v[0]) : to_f32(y.v[0]);
+            a[1] = to_f32(x.v[1]);
+        } else {                                              // pairs side by side, values in their order
+            a[i] = turns ? to_f32(x.v[2 * i]) : to_f32(x.v[i]);
+            a[V + i] = turns ? to_f32(x.v[2 * i + 1]) : to_f32(x.v[V + i]);
+        }
     }
 }
 template <typename D, int V, bool INTER, bool STREAM>
 __device__ __forceinline__ void store_chunk(D* dst, int c, const NormLanes& ln, int rot_dim, const float (&a)[2 * V]) {
+    constexpr int P = kPass<V, INTER>;
     if (c < ln.turn) {
         if constexpr (INTER) {
             Vec<D, 2 * V> x;
@@ -91,20 +118,21 @@ __device__ __forceinline__ void store_chunk(D* dst, int c, const NormLanes& ln, 
             store<STREAM>(dst + V * c + rot_dim / 2, y);
         }
     } else if (c < ln.turn + ln.pass) {
-        Vec<D, V> x;
+        Vec<D, P> x;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x.v[i] = (D)a[i];
-        store<STREAM>(dst + rot_dim + (c - ln.turn) * V, x);
+        for (int i = 0; i < P; ++i) x.v[i] = (D)a[i];
+        store<STREAM>(dst + rot_dim + (c - ln.turn) * P, x);
     }
 }
-// Offset in the head of value i of a chunk, as load_chunk lays it out; -1: none.
+// Offset in the head of value i of a chunk in float32; -1: none.
 template <int V, bool INTER>
 __device__ __forceinline__ int value_at(int c, int i, const NormLanes& ln, int rot_dim) {
+    constexpr int P = kPass<V, INTER>;
     if (c < ln.turn) {
         if constexpr (INTER) return 2 * (V * c + (i < V ? i : i - V)) + (i < V ? 0 : 1);
         else return i < V ? V * c + i : V * c + i - V + rot_dim / 2;
     }
-    return i < V && c < ln.turn + ln.pass ? rot_dim + (c - ln.turn) * V + i : -1;
+    return i < P && c < ln.turn + ln.pass ? rot_dim + (c - ln.turn) * P + i : -1;
 }
 
 // A row's cosines and sines; 1 and 0 for the values behind the rotated ones, so that
@@ -135,19 +163,16 @@ __device__ __forceinline__ float gain_value(const void* gain, int dtype, int i) 
     if (dtype == DLM_BF16) return (float)reinterpret_cast<const __bf16*>(gain)[i];
     return (float)reinterpret_cast<const _Float16*>(gain)[i];
 }
-// The two gains in LDS in the order of the chunks: chunk c's at [c][2 V].
+// A gain in LDS in the order of the chunks: chunk c's at [c][2 V].
 template <int V, bool INTER>
-__device__ __forceinline__ void stage_gains(float* lds, int width, const void* gq, int tq, const void* gk, int tk,
-                                            const NormLanes& ln, int rot_dim) {
-    for (int x = threadIdx.x; x < 2 * width; x += blockDim.x) {
-        const int set = x >= width, y = set ? x - width : x;
-        const int at = value_at<V, INTER>(y / (2 * V), y % (2 * V), ln, rot_dim);
-        lds[x] = at < 0 ? 0.f : gain_value(set ? gk : gq, set ? tk : tq, at);
+__device__ __forceinline__ void stage_gain(float* lds, int width, const void* gain, int type, const NormLanes& ln, int rot_dim) {
+    for (int x = threadIdx.x; x < width; x += blockDim.x) {
+        const int at = value_at<V, INTER>(x / (2 * V), x % (2 * V), ln, rot_dim);
+        lds[x] = at < 0 ? 0.f : gain_value(gain, type, at);
     }
-    __syncthreads();
 }
-// Chunks of a head, a lane's unused ones included, times their values: at most 256
-// lanes' chunks of V = 1 hold 512 values, of V = 8 no more.
+// Chunks of a head, a lane's unused ones included, times their values: 256 chunks of V = 1
+// hold 512 values, 64 of V = 4 or 32 of V = 8 as many.
 constexpr int kGainWords = 512;
 
 template <int V>
@@ -168,16 +193,18 @@ struct NormSet {
 };
 
 // Heads that a lane has in flight.
-template <int V>
-constexpr int kFlight = V >= 4 ? 4 : 1;
+template <int CH>
+constexpr int kFlight = CH == 1 ? 4 : 1;
 
-template <typename T, int V, bool INTER, bool STREAM>
+template <typename T, int V, bool INTER, bool STREAM, int CH>
 __global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const NormSet q, const NormSet k, float eps,
                                                    const int32_t* __restrict__ pos, int rows, NormLanes ln) {
-    constexpr int CH = kChunks<V>, U = kFlight<V>;
+    constexpr int U = kFlight<CH>;
     __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
     const int width = CH * ln.run * 2 * V;
-    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    stage_gain<V, INTER>(gains, width, q.gain, q.gain_dtype, ln, rope.rot_dim);
+    stage_gain<V, INTER>(gains + width, width, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    __syncthreads();
     const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
     const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;
     if (slot >= ln.slots * ln.rows || r >= rows) return;      // whole runs
@@ -190,7 +217,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const No
     const float inv_n = 1.f / (float)rope.head_dim;
     const uint32_t n_all = (uint32_t)q.heads + (uint32_t)k.heads;
     for (uint32_t h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
-        float a[U][CH][2 * V];
+        Raw<T, V, INTER> raw[U][CH];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint32_t h = h0 + u * ln.slots;
@@ -198,7 +225,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const No
             const T* src = h < (uint32_t)q.heads ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
 #pragma unroll
             for (int j = 0; j < CH; ++j)
-                load_chunk<T, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                raw[u][j] = load_chunk<T, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -206,18 +233,21 @@ __global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const No
             if (h >= n_all) continue;
             const bool is_q = h < (uint32_t)q.heads;
             T* dst = is_q ? yq + h * q.y_head : yk + (h - q.heads) * k.y_head;
-            float ss = 0.f;
+            float a[CH][2 * V], ss = 0.f;
 #pragma unroll
-            for (int j = 0; j < CH; ++j) ss += sum_squares<V>(a[u][j]);
+            for (int j = 0; j < CH; ++j) {
+                widen_chunk<T, V, INTER>(raw[u][j], lane + j * ln.run, ln, a[j]);
+                ss += sum_squares<V>(a[j]);
+            }
             const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
             const float* g = gains + (is_q ? 0 : width);
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const float* gc = g + (lane + j * ln.run) * 2 * V;
 #pragma unroll
-                for (int i = 0; i < 2 * V; ++i) a[u][j][i] *= rs * gc[i];
-                turn<V>(a[u][j], co[j], si[j]);
-                store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                for (int i = 0; i < 2 * V; ++i) a[j][i] *= rs * gc[i];
+                turn<V>(a[j], co[j], si[j]);
+                store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
             }
         }
     }
@@ -231,130 +261,143 @@ struct NormGrad {
     void* dx;
     int64_t dx_row, dx_head;
 };
-// Workgroups of the gradient, each with a part of both gains' gradients: what the chip
-// holds at once (4 per CU), so that the parts are few.
+// Workgroups of the gradient, each with a part of one gain's gradient: at most what the chip
+// holds at once (3 per CU where a lane holds 16 values, 146 VGPRs, else 4), so that the parts
+// are few and no second turn of workgroups runs half empty (16384 rows of 20 heads of 128,
+// bf16: 1024 workgroups 83 us).
 constexpr int kGradWgs = 1024;
+template <int V>
+constexpr int kGradWgsOf = V == 8 ? 768 : kGradWgs;
 
-// A workgroup takes every gridDim.x-th group of rows.  The gains' sums stay in registers
-// over all of them, are added over the workgroup's runs in order, and leave one part per
-// workgroup; the second kernel adds the parts in order.
-template <typename T, int V, bool INTER, bool STREAM>
+// The first q_wgs workgroups take the queries, the others the keys, each every q_wgs-th (or
+// other) group of rows.  A lane asks for its next head before it works on the one at hand.
+// The gain's sums stay in registers over all of them, are added over the workgroup's runs in
+// order, and leave one part per workgroup; the second kernel adds the parts in order.
+template <typename T, int V, bool INTER, bool STREAM, int CH>
 __global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, const NormSet q, const NormSet k,
                                                         const NormGrad gq, const NormGrad gk, float eps,
-                                                        const int32_t* __restrict__ pos, int rows, NormLanes ln,
-                                                        float* __restrict__ parts) {
-    constexpr int CH = kChunks<V>, U = V >= 4 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
+                                                        const int32_t* __restrict__ pos, int rows, NormLanes lq,
+                                                        NormLanes lk, int q_wgs, float* __restrict__ parts) {
+    __shared__ __attribute__((aligned(16))) float gain[kGainWords];
     __shared__ float sums[256];
-    const int width = CH * ln.run * 2 * V;
-    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    const bool is_q = (int)blockIdx.x < q_wgs;
+    const NormSet s = is_q ? q : k;
+    const NormGrad g = is_q ? gq : gk;
+    const NormLanes ln = is_q ? lq : lk;
+    const int wg = is_q ? blockIdx.x : blockIdx.x - q_wgs, wgs = is_q ? q_wgs : gridDim.x - q_wgs;
+    stage_gain<V, INTER>(gain, CH * ln.run * 2 * V, s.gain, s.gain_dtype, ln, rope.rot_dim);
+    __syncthreads();
     const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
-    const bool busy = slot < ln.slots * ln.rows;
     const float inv_n = 1.f / (float)rope.head_dim;
-    const uint32_t n_all = (uint32_t)q.heads + (uint32_t)k.heads;
-    float acc[2][CH][2 * V];
+    float acc[CH][2 * V];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int j = 0; j < CH; ++j)
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
+        for (int i = 0; i < 2 * V; ++i) acc[j][i] = 0.f;
+    int64_t r = (int64_t)wg * ln.rows + slot / ln.slots;
+    const int64_t stride = (int64_t)wgs * ln.rows;
+    if (slot >= ln.slots * ln.rows) r = rows;
+    const int h0 = slot % ln.slots;
+    int h = h0;
+    Raw<T, V, INTER> nx[CH], ny[CH];
+    auto ask = [&](int64_t row, int head) {
+        const T *x = (const T*)s.x + row * s.x_row + head * s.x_head, *y = (const T*)g.dy + row * g.dy_row + head * g.dy_head;
 #pragma unroll
-            for (int i = 0; i < 2 * V; ++i) acc[s][j][i] = 0.f;
-    for (int64_t r = (int64_t)blockIdx.x * ln.rows + slot / ln.slots; busy && r < rows; r += (int64_t)gridDim.x * ln.rows) {
-        float co[CH][V], si[CH][V];
-        const int64_t p = pos[r];
+        for (int j = 0; j < CH; ++j) {
+            nx[j] = load_chunk<T, V, INTER, STREAM>(x, lane + j * ln.run, ln, rope.rot_dim);
+            ny[j] = load_chunk<T, V, INTER, STREAM>(y, lane + j * ln.run, ln, rope.rot_dim);
+        }
+    };
+    int p = 0;
+    if (r < rows) {
+        p = pos[r];
+        ask(r, h);
+    }
+    float co[CH][V], si[CH][V];
+    while (r < rows) {
+        float a[CH][2 * V], b[CH][2 * V];
 #pragma unroll
-        for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, true, co[j], si[j]);
-        const T *xq = (const T*)q.x + r * q.x_row, *xk = (const T*)k.x + r * k.x_row;
-        const T *yq = (const T*)gq.dy + r * gq.dy_row, *yk = (const T*)gk.dy + r * gk.dy_row;
-        T *oq = (T*)gq.dx + r * gq.dx_row, *ok = (T*)gk.dx + r * gk.dx_row;
-        for (uint32_t h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
-            float a[U][CH][2 * V], b[U][CH][2 * V];
+        for (int j = 0; j < CH; ++j) {
+            widen_chunk<T, V, INTER>(nx[j], lane + j * ln.run, ln, a[j]);
+            widen_chunk<T, V, INTER>(ny[j], lane + j * ln.run, ln, b[j]);
+        }
+        if (h == h0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t h = h0 + u * ln.slots;
-                if (h >= n_all) continue;
-                const bool is_q = h < (uint32_t)q.heads;
-                const T* x = is_q ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
-                const T* y = is_q ? yq + h * gq.dy_head : yk + (h - q.heads) * gk.dy_head;
+            for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, true, co[j], si[j]);
+            if (r + stride < rows) p = pos[r + stride];
+        }
+        T* dst = (T*)g.dx + r * g.dx_row + h * g.dx_head;
+        h += ln.slots;
+        if (h >= s.heads) {
+            h = h0;
+            r += stride;
+        }
+        if (r < rows) ask(r, h);
+        float ss = 0.f;
 #pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    load_chunk<T, V, INTER, STREAM>(x, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
-                    load_chunk<T, V, INTER, STREAM>(y, lane + j * ln.run, ln, rope.rot_dim, b[u][j]);
-                }
-            }
+        for (int j = 0; j < CH; ++j) {
+            turn<V>(b[j], co[j], si[j]);                      // u = R^T dy
+            ss += sum_squares<V>(a[j]);
+        }
+        const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
+        float dot = 0.f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t h = h0 + u * ln.slots;
-                if (h >= n_all) continue;
-                const bool is_q = h < (uint32_t)q.heads;
-                T* dst = is_q ? oq + h * gq.dx_head : ok + (h - q.heads) * gk.dx_head;
-                const float* g = gains + (is_q ? 0 : width);
-                float ss = 0.f;
+        for (int j = 0; j < CH; ++j) {
+            const float* gc = gain + (lane + j * ln.run) * 2 * V;
 #pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    turn<V>(b[u][j], co[j], si[j]);           // u = R^T dy
-                    ss += sum_squares<V>(a[u][j]);
-                }
-                const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
-                float dot = 0.f;
-#pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    const float* gc = g + (lane + j * ln.run) * 2 * V;
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        a[u][j][i] *= rs;                     // x r
-                        const float t = b[u][j][i] * a[u][j][i];
-                        if (is_q) acc[0][j][i] += t;
-                        else acc[1][j][i] += t;
-                        dot = fmaf(t, gc[i], dot);
-                    }
-                }
-                dot = run_sum(dot, ln.run) * inv_n;
-#pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    const float* gc = g + (lane + j * ln.run) * 2 * V;
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) a[u][j][i] = rs * (b[u][j][i] * gc[i] - a[u][j][i] * dot);
-                    store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
-                }
+            for (int i = 0; i < 2 * V; ++i) {
+                a[j][i] *= rs;                                // x r
+                const float t = b[j][i] * a[j][i];
+                acc[j][i] += t;
+                dot = fmaf(t, gc[i], dot);
             }
         }
+        dot = run_sum(dot, ln.run) * inv_n;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const float* gc = gain + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) a[j][i] = rs * (b[j][i] * gc[i] - a[j][i] * dot);
+            store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
+        }
     }
+    if (!parts) return;
     // Over the runs of the workgroup, value by value.
     const int runs = ln.slots * ln.rows;
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int j = 0; j < CH; ++j)
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) {
-                __syncthreads();
-                sums[threadIdx.x] = acc[s][j][i];
-                __syncthreads();
-                if ((int)threadIdx.x < ln.run) {
-                    float t = 0.f;
-                    for (int x = 0; x < runs; ++x) t += sums[x * ln.run + threadIdx.x];
-                    const int at = value_at<V, INTER>(threadIdx.x + j * ln.run, i, ln, rope.rot_dim);
-                    if (at >= 0) parts[((int64_t)blockIdx.x * 2 + s) * rope.head_dim + at] = t;
-                }
+        for (int i = 0; i < 2 * V; ++i) {
+            __syncthreads();
+            sums[threadIdx.x] = acc[j][i];
+            __syncthreads();
+            if ((int)threadIdx.x < ln.run) {
+                float t = 0.f;
+                for (int x = 0; x < runs; ++x) t += sums[x * ln.run + threadIdx.x];
+                const int at = value_at<V, INTER>(threadIdx.x + j * ln.run, i, ln, rope.rot_dim);
+                if (at >= 0) parts[(int64_t)blockIdx.x * rope.head_dim + at] = t;
             }
+        }
 }
 
-// The parts added in order: blockIdx.x takes 16 values of one gain, 16 runs of parts each.
-__global__ __launch_bounds__(256) void gain_sum_kernel(const float* __restrict__ parts, int n_parts, int head_dim,
-                                                       void* out_q, int type_q, void* out_k, int type_k) {
-    __shared__ float run[16][17];
+// The parts added in order: blockIdx.x takes 16 values of one gain, 64 runs of parts each.
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* __restrict__ parts, int q_parts, int k_parts,
+                                                        int head_dim, void* out_q, int type_q, void* out_k, int type_k) {
+    __shared__ float run[64][17];
     const int v = threadIdx.x & 15, at = threadIdx.x >> 4;
     const int per = (head_dim + 15) / 16, set = blockIdx.x / per, i = blockIdx.x % per * 16 + v;
-    const int each = (n_parts + 15) / 16;
+    const int n = set ? k_parts : q_parts, first = set ? q_parts : 0;
+    const int each = (n + 63) / 64, p1 = min(n, (at + 1) * each);
     float t = 0.f;
     if (i < head_dim)
-        for (int p = at * each; p < min(n_parts, (at + 1) * each); ++p) t += parts[((int64_t)p * 2 + set) * head_dim + i];
+#pragma unroll 16
+        for (int p = at * each; p < p1; ++p) t += parts[(int64_t)(first + p) * head_dim + i];
     run[at][v] = t;
     __syncthreads();
     void* out = set ? out_k : out_q;
     if (at || i >= head_dim || !out) return;
-    for (int x = 1; x < 16; ++x) t += run[x][v];
+#pragma unroll 16
+    for (int x = 1; x < 64; ++x) t += run[x][v];
     const int type = set ? type_k : type_q;
     if (type == DLM_F32) reinterpret_cast<float*>(out)[i] = t;
     else if (type == DLM_BF16) reinterpret_cast<__bf16*>(out)[i] = (__bf16)t;
@@ -365,20 +408,22 @@ __global__ __launch_bounds__(256) void gain_sum_kernel(const float* __restrict__
 
 // As append_kernel of rope.hip, keys and queries normalised.  Head indexes run over the
 // keys, the values, then the queries.
-template <typename S, typename D, int V, bool INTER, bool STREAM>
+template <typename S, typename D, int V, bool INTER, bool STREAM, int CH>
 __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, CacheArgs c, int64_t layer_base,
                                                           const int32_t* __restrict__ row_start, int total_rows,
                                                           int max_rows, const NormSet q, const NormSet k, const S* v,
                                                           int64_t v_stride, float eps, const int32_t* __restrict__ pos,
                                                           NormLanes ln) {
-    constexpr int CH = kChunks<V>, U = kFlight<V>;
+    constexpr int U = kFlight<CH>;
     __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
     const int width = CH * ln.run * 2 * V;
     const int b = blockIdx.y;
     const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
     const int i = (int)(blockIdx.z * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;    // max_rows <= 2^24
     const int start = row_start[b], end = min(row_start[b + 1], total_rows), len = c.len[b];
-    stage_gains<V, INTER>(gains, width, q.gain, q.gain_dtype, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    stage_gain<V, INTER>(gains, width, q.gain, q.gain_dtype, ln, rope.rot_dim);
+    stage_gain<V, INTER>(gains + width, width, k.gain, k.gain_dtype, ln, rope.rot_dim);
+    __syncthreads();
     if (slot >= ln.slots * ln.rows || start < 0 || i >= max_rows || start >= end || i >= end - start) return;
     const int64_t r = (int64_t)start + i;
     const int64_t t = (int64_t)len + i;                       // the row's token
@@ -402,7 +447,7 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
     if (refs > 1 && counted_elsewhere(c, b, t, page)) held = false;
     const float inv_n = 1.f / (float)hd;
     for (int h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
-        float a[U][CH][2 * V];
+        Raw<S, V, INTER> raw[U][CH];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * ln.slots;
@@ -412,7 +457,7 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
                                             : (const S*)q.x + r * q.x_row + (h - 2 * c.n_kv) * hd;
 #pragma unroll
             for (int j = 0; j < CH; ++j)
-                load_chunk<S, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                raw[u][j] = load_chunk<S, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -422,23 +467,26 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
             D* dst = is_k   ? reinterpret_cast<D*>(c.k) + base + h * head_stride
                      : is_v ? reinterpret_cast<D*>(c.v) + base + (h - c.n_kv) * head_stride
                             : (D*)q.y + r * q.y_row + (h - 2 * c.n_kv) * hd;
-            if (!is_v) {
-                float ss = 0.f;
+            float a[CH][2 * V], ss = 0.f;
 #pragma unroll
-                for (int j = 0; j < CH; ++j) ss += sum_squares<V>(a[u][j]);
+            for (int j = 0; j < CH; ++j) {
+                widen_chunk<S, V, INTER>(raw[u][j], lane + j * ln.run, ln, a[j]);
+                ss += sum_squares<V>(a[j]);
+            }
+            if (!is_v) {
                 const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
                 const float* g = gains + (is_k ? width : 0);
 #pragma unroll
                 for (int j = 0; j < CH; ++j) {
                     const float* gc = g + (lane + j * ln.run) * 2 * V;
 #pragma unroll
-                    for (int x = 0; x < 2 * V; ++x) a[u][j][x] *= rs * gc[x];
-                    turn<V>(a[u][j], co[j], si[j]);
+                    for (int x = 0; x < 2 * V; ++x) a[j][x] *= rs * gc[x];
+                    turn<V>(a[j], co[j], si[j]);
                 }
             }
 #pragma unroll
             for (int j = 0; j < CH; ++j)
-                store_chunk<D, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[u][j]);
+                store_chunk<D, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
         }
     }
 }
@@ -448,7 +496,8 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
 // Runs of a power of two of lanes; how many heads a workgroup takes at a time: the number
 // that leaves the fewest lanes and turns idle, the largest of those.
 NormLanes lay_out(const dlm_rope& r, int V, int64_t rows, int64_t heads) {
-    NormLanes ln{r.rot_dim / 2 / V, (r.head_dim - r.rot_dim) / V, 1, 1, 1};
+    const int pass = r.interleaved && V > 1 ? 2 * V : V;
+    NormLanes ln{r.rot_dim / 2 / V, (r.head_dim - r.rot_dim) / pass, 1, 1, 1};
     while (ln.run < ln.turn + ln.pass && ln.run < 64) ln.run *= 2;
     const int most = 256 / ln.run;
     double best_use = 0.;
@@ -464,6 +513,28 @@ NormLanes lay_out(const dlm_rope& r, int V, int64_t rows, int64_t heads) {
     return ln;
 }
 
+// pairs_per_access, with values behind the rotated ones in accesses as wide as a pair's.
+template <typename F>
+int pairs_per_chunk(const dlm_rope& r, int elem, F aligned) {
+    int V = pairs_per_access(r, elem, aligned);
+    if (r.interleaved)
+        while (V > 1 && (r.head_dim - r.rot_dim) % (2 * V)) V /= 2;
+    return V;
+}
+// Chunks of a lane: more than one only where a head of up to 256 values is taken in
+// pieces so small that a wave has too few lanes for it.
+template <int V, typename S, typename F>
+hipError_t with_chunks(const dlm_rope& r, const NormLanes& ln, F launch) {
+    auto with_layout = [&](auto ch) {
+        if constexpr (2 * V * sizeof(S) <= 16)                // pairs_per_access
+            if (r.interleaved) return launch(ch, std::true_type{});
+        return launch(ch, std::false_type{});
+    };
+    if constexpr (V <= 2)
+        if (ln.turn + ln.pass > 64) return with_layout(std::integral_constant<int, V == 2 ? 2 : 4>{});
+    return with_layout(std::integral_constant<int, 1>{});
+}
+
 struct NormCall {
     const dlm_rope& rope;
     int rows;
@@ -473,24 +544,35 @@ struct NormCall {
     hipStream_t st;
     const NormGrad *gq = nullptr, *gk = nullptr;
     float* parts = nullptr;
-    int* n_parts = nullptr;
+    int* q_parts = nullptr;
+    int* k_parts = nullptr;
 };
 template <typename T, int V, bool STREAM = false>
 hipError_t norm_layout(const NormCall& a) {
+    if (a.gq) {
+        // Workgroups by the heads of the two sets, at least one for a set that has heads.
+        const NormLanes lq = lay_out(a.rope, V, a.rows, a.q.heads), lk = lay_out(a.rope, V, a.rows, a.k.heads);
+        auto groups = [&](const NormLanes& ln, int heads, int64_t most) {
+            return heads ? (int)std::min<int64_t>(((int64_t)a.rows + ln.rows - 1) / ln.rows, std::max<int64_t>(most, 1)) : 0;
+        };
+        const int64_t all = (int64_t)a.q.heads + a.k.heads;
+        const int nk = groups(lk, a.k.heads, kGradWgsOf<V> * (int64_t)a.k.heads / all);
+        const int nq = groups(lq, a.q.heads, kGradWgsOf<V> - nk);
+        *a.q_parts = nq;
+        *a.k_parts = nk;
+        return with_chunks<V, T>(a.rope, a.q.heads ? lq : lk, [&](auto ch, auto inter) {
+            hipLaunchKernelGGL((norm_grad_kernel<T, V, decltype(inter)::value, STREAM, decltype(ch)::value>), dim3((unsigned)(nq + nk)), dim3(256), 0, a.st, a.rope, a.q, a.k, *a.gq, *a.gk, a.eps,
+                               a.pos, a.rows, lq, lk, nq, a.parts);
+            return hipGetLastError();
+        });
+    }
     const NormLanes ln = lay_out(a.rope, V, a.rows, (int64_t)a.q.heads + a.k.heads);
     const int64_t wgs = ((int64_t)a.rows + ln.rows - 1) / ln.rows;
-    if (a.gq) {
-        const int n = (int)std::min<int64_t>(wgs, kGradWgs);
-        *a.n_parts = n;
-        auto kernel = a.rope.interleaved ? norm_grad_kernel<T, V, true, STREAM> : norm_grad_kernel<T, V, false, STREAM>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, a.st, a.rope, a.q, a.k, *a.gq, *a.gk, a.eps, a.pos,
-                           a.rows, ln, a.parts);
-    } else {
-        const dim3 grid((unsigned)std::min(wgs, kWgsAcross), (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
-        auto kernel = a.rope.interleaved ? norm_kernel<T, V, true, STREAM> : norm_kernel<T, V, false, STREAM>;
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.st, a.rope, a.q, a.k, a.eps, a.pos, a.rows, ln);
-    }
-    return hipGetLastError();
+    const dim3 grid((unsigned)std::min(wgs, kWgsAcross), (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
+    return with_chunks<V, T>(a.rope, ln, [&](auto ch, auto inter) {
+        hipLaunchKernelGGL((norm_kernel<T, V, decltype(inter)::value, STREAM, decltype(ch)::value>), grid, dim3(256), 0, a.st, a.rope, a.q, a.k, a.eps, a.pos, a.rows, ln);
+        return hipGetLastError();
+    });
 }
 template <typename T>
 hipError_t norm_type(const NormCall& a) {
@@ -501,7 +583,7 @@ hipError_t norm_type(const NormCall& a) {
         if (!one(s.x, s.x_row, s.x_head)) return false;
         return g ? one(g->dy, g->dy_row, g->dy_head) && one(g->dx, g->dx_row, g->dx_head) : one(s.y, s.y_row, s.y_head);
     };
-    const int V = pairs_per_access(a.rope, sizeof(T), [&](int n) { return set_fits(a.q, a.gq, n) && set_fits(a.k, a.gk, n); });
+    const int V = pairs_per_chunk(a.rope, sizeof(T), [&](int n) { return set_fits(a.q, a.gq, n) && set_fits(a.k, a.gk, n); });
     constexpr int W = 16 / sizeof(T);
     const bool stream = streams((a.gq ? 3 : 2) * (int64_t)a.rows * ((int64_t)a.q.heads + a.k.heads) * a.rope.head_dim * sizeof(T));
     if (V == W && stream) return norm_layout<T, W, true>(a);
@@ -550,14 +632,15 @@ hipError_t append_layout(const AppendNormCall& a) {
     const int64_t wgs = ((int64_t)a.max_rows + ln.rows - 1) / ln.rows;
     const dim3 grid((unsigned)std::min(wgs, kWgsAcross), a.c.n_seqs, (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
     const int64_t layer_base = (int64_t)a.layer * a.c.n_pages * a.c.n_kv * a.c.page_len * a.c.head_dim;
-    auto kernel = a.rope.interleaved ? append_norm_kernel<S, D, V, true, STREAM> : append_norm_kernel<S, D, V, false, STREAM>;
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, a.st, a.rope, a.c, layer_base, a.row_start, a.total_rows, a.max_rows,
-                       a.q, a.k, (const S*)a.v, a.v_stride, a.eps, a.pos, ln);
-    return hipGetLastError();
+    return with_chunks<V, S>(a.rope, ln, [&](auto ch, auto inter) {
+        hipLaunchKernelGGL((append_norm_kernel<S, D, V, decltype(inter)::value, STREAM, decltype(ch)::value>), grid, dim3(256), 0, a.st, a.rope, a.c, layer_base, a.row_start, a.total_rows, a.max_rows,
+                           a.q, a.k, (const S*)a.v, a.v_stride, a.eps, a.pos, ln);
+        return hipGetLastError();
+    });
 }
 template <typename S, typename D>
 hipError_t append_type(const AppendNormCall& a) {
-    const int V = pairs_per_access(a.rope, sizeof(S), [&](int n) {
+    const int V = pairs_per_chunk(a.rope, sizeof(S), [&](int n) {
         return fits(a.k.x, sizeof(S), n, a.k.x_row) && fits(a.v, sizeof(S), n, a.v_stride) &&
                (!a.q.heads || (fits(a.q.x, sizeof(S), n, a.q.x_row) && fits(a.q.y, sizeof(D), n, a.q.y_row)));
     });
@@ -580,26 +663,27 @@ hipError_t launch_rope_norm(const dlm_rope& rope, int dtype, int rows, const dlm
     return norm_any(NormCall{rope, rows, norm_set(q), norm_set(k), eps, pos, st}, dtype);
 }
 
-size_t norm_grad_workspace_bytes(int head_dim) { return (size_t)kGradWgs * 2 * head_dim * sizeof(float); }
+size_t norm_grad_workspace_bytes(int head_dim) { return (size_t)kGradWgs * head_dim * sizeof(float); }
 
 hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q,
                                  const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
                                  const int32_t* pos, void* ws, hipStream_t st) {
     NormCall a{rope, rows, norm_set(q), norm_set(k), eps, pos, st};
     const NormGrad gq = norm_grad(q, dq), gk = norm_grad(k, dk);
-    int n_parts = 0;
+    int q_parts = 0, k_parts = 0;
+    void* out_q = q && dq && q->n_heads ? dq->d_dgain : nullptr;
+    void* out_k = k && dk && k->n_heads ? dk->d_dgain : nullptr;
     a.gq = &gq;
     a.gk = &gk;
-    a.parts = (float*)ws;
-    a.n_parts = &n_parts;
+    a.parts = out_q || out_k ? (float*)ws : nullptr;
+    a.q_parts = &q_parts;
+    a.k_parts = &k_parts;
     if (rows > 0 && a.q.heads + (int64_t)a.k.heads > 0) {
         const hipError_t e = norm_any(a, dtype);
         if (e != hipSuccess) return e;
     }
-    void* out_q = q && dq && q->n_heads ? dq->d_dgain : nullptr;
-    void* out_k = k && dk && k->n_heads ? dk->d_dgain : nullptr;
-    if (!out_q && !out_k) return hipSuccess;
-    hipLaunchKernelGGL(gain_sum_kernel, dim3(2 * ((rope.head_dim + 15) / 16)), dim3(256), 0, st, (const float*)ws, n_parts,
+    if (!a.parts) return hipSuccess;
+    hipLaunchKernelGGL(gain_sum_kernel, dim3(2 * ((rope.head_dim + 15) / 16)), dim3(1024), 0, st, a.parts, q_parts, k_parts,
                        rope.head_dim, out_q, q ? q->gain_dtype : 0, out_k, k ? k->gain_dtype : 0);
     return hipGetLastError();
 }
