@@ -147,6 +147,34 @@ __device__ __forceinline__ void chunk_angles(const dlm_rope& rope, int64_t pos, 
     }
     if (c < ln.turn) angles<V>(rope.phase, rope.scale, pos, c * V, back, co, si);
 }
+// Cosines and sines of a workgroup's rows: worked out once, a pair per thread, into LDS
+// ([rows][pairs]; `pos` tells the position of a row, -1 past the last one's), and from
+// there to the lanes; 1 and 0 for the values behind the rotated ones, so that every lane
+// turns what it holds.
+template <int N>
+struct Angles {
+    float co[N], si[N];
+};
+template <int N, typename F>
+__device__ __forceinline__ void stage_angles(Angles<N>& lds, const dlm_rope& rope, int rows, bool back, F pos) {
+    const int half = rope.rot_dim / 2;
+    for (int x = threadIdx.x; x < rows * half; x += blockDim.x) {
+        const int row = x / half, i = x - row * half;
+        float c[1], s[1];
+        angles<1>(rope.phase, rope.scale, pos(row), i, back, c, s);
+        lds.co[x] = c[0];
+        lds.si[x] = s[0];
+    }
+}
+template <int V, int N>
+__device__ __forceinline__ void read_angles(const Angles<N>& lds, int row, int half, int c, bool turns, float (&co)[V],
+                                            float (&si)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        co[i] = turns ? lds.co[row * half + (turns ? c * V + i : 0)] : 1.f;
+        si[i] = turns ? lds.si[row * half + (turns ? c * V + i : 0)] : 0.f;
+    }
+}
 template <int V>
 __device__ __forceinline__ void turn(float (&a)[2 * V], const float (&co)[V], const float (&si)[V]) {
 #pragma unroll
@@ -192,63 +220,59 @@ struct NormSet {
     int64_t y_row, y_head;
 };
 
-// Heads that a lane has in flight.
-template <int CH>
-constexpr int kFlight = CH == 1 ? 4 : 1;
+// Pairs of a workgroup's rows: its lanes hold V per chunk.
+template <int V, int CH>
+constexpr int kRowPairs = 256 * V * CH;
 
+// A lane asks for its next head before it works on the one at hand.
 template <typename T, int V, bool INTER, bool STREAM, int CH>
 __global__ __launch_bounds__(256) void norm_kernel(const dlm_rope rope, const NormSet q, const NormSet k, float eps,
                                                    const int32_t* __restrict__ pos, int rows, NormLanes ln) {
-    constexpr int U = kFlight<CH>;
     __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
     const int width = CH * ln.run * 2 * V;
+    const int64_t r0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows;
     stage_gain<V, INTER>(gains, width, q.gain, q.gain_dtype, ln, rope.rot_dim);
     stage_gain<V, INTER>(gains + width, width, k.gain, k.gain_dtype, ln, rope.rot_dim);
     __syncthreads();
-    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
-    const int64_t r = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;
+    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run, row = slot / ln.slots;
+    const int64_t r = r0 + row;
     if (slot >= ln.slots * ln.rows || r >= rows) return;      // whole runs
-    float co[CH][V], si[CH][V];
-    const int64_t p = pos[r];
-#pragma unroll
-    for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, false, co[j], si[j]);
     const T *xq = (const T*)q.x + r * q.x_row, *xk = (const T*)k.x + r * k.x_row;
     T *yq = (T*)q.y + r * q.y_row, *yk = (T*)k.y + r * k.y_row;
     const float inv_n = 1.f / (float)rope.head_dim;
     const uint32_t n_all = (uint32_t)q.heads + (uint32_t)k.heads;
-    for (uint32_t h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
-        Raw<T, V, INTER> raw[U][CH];
+    float co[CH][V], si[CH][V];
+    const int64_t p = pos[r];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = h0 + u * ln.slots;
-            if (h >= n_all) continue;
-            const T* src = h < (uint32_t)q.heads ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
+    for (int j = 0; j < CH; ++j) chunk_angles<V>(rope, p, lane + j * ln.run, ln, false, co[j], si[j]);
+    Raw<T, V, INTER> raw[CH];
+    auto ask = [&](uint32_t h) {
+        const T* src = h < (uint32_t)q.heads ? xq + h * q.x_head : xk + (h - q.heads) * k.x_head;
 #pragma unroll
-            for (int j = 0; j < CH; ++j)
-                raw[u][j] = load_chunk<T, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
+        for (int j = 0; j < CH; ++j) raw[j] = load_chunk<T, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
+    };
+    uint32_t h = slot % ln.slots;
+    if (h < n_all) ask(h);
+    while (h < n_all) {
+        const bool is_q = h < (uint32_t)q.heads;
+        T* dst = is_q ? yq + h * q.y_head : yk + (h - q.heads) * k.y_head;
+        float a[CH][2 * V], ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            widen_chunk<T, V, INTER>(raw[j], lane + j * ln.run, ln, a[j]);
+            ss += sum_squares<V>(a[j]);
         }
+        h += ln.slots;
+        if (h < n_all) ask(h);
+        const float rs = rsqrtf(run_sum(ss, ln.run) * inv_n + eps);
+        const float* g = gains + (is_q ? 0 : width);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t h = h0 + u * ln.slots;
-            if (h >= n_all) continue;
-            const bool is_q = h < (uint32_t)q.heads;
-            T* dst = is_q ? yq + h * q.y_head : yk + (h - q.heads) * k.y_head;
-            float a[CH][2 * V], ss = 0.f;
+        for (int j = 0; j < CH; ++j) {
+            const float* gc = g + (lane + j * ln.run) * 2 * V;
 #pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                widen_chunk<T, V, INTER>(raw[u][j], lane + j * ln.run, ln, a[j]);
-                ss += sum_squares<V>(a[j]);
-            }
-            const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
-            const float* g = gains + (is_q ? 0 : width);
-#pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                const float* gc = g + (lane + j * ln.run) * 2 * V;
-#pragma unroll
-                for (int i = 0; i < 2 * V; ++i) a[j][i] *= rs * gc[i];
-                turn<V>(a[j], co[j], si[j]);
-                store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
-            }
+            for (int i = 0; i < 2 * V; ++i) a[j][i] *= rs * gc[i];
+            turn<V>(a[j], co[j], si[j]);
+            store_chunk<T, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
         }
     }
 }
@@ -339,7 +363,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, con
             turn<V>(b[j], co[j], si[j]);                      // u = R^T dy
             ss += sum_squares<V>(a[j]);
         }
-        const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
+        const float rs = rsqrtf(run_sum(ss, ln.run) * inv_n + eps);
         float dot = 0.f;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
@@ -414,80 +438,79 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
                                                           int max_rows, const NormSet q, const NormSet k, const S* v,
                                                           int64_t v_stride, float eps, const int32_t* __restrict__ pos,
                                                           NormLanes ln) {
-    constexpr int U = kFlight<CH>;
     __shared__ __attribute__((aligned(16))) float gains[2 * kGainWords];
+    __shared__ __attribute__((aligned(16))) Angles<kRowPairs<V, CH>> ang;
     const int width = CH * ln.run * 2 * V;
     const int b = blockIdx.y;
-    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run;
-    const int i = (int)(blockIdx.z * gridDim.x + blockIdx.x) * ln.rows + slot / ln.slots;    // max_rows <= 2^24
+    const int lane = threadIdx.x & (ln.run - 1), slot = threadIdx.x / ln.run, row = slot / ln.slots;
+    const int i0 = (int)(blockIdx.z * gridDim.x + blockIdx.x) * ln.rows, i = i0 + row;       // max_rows <= 2^24
     const int start = row_start[b], end = min(row_start[b + 1], total_rows), len = c.len[b];
+    if (start < 0 || start >= end || i0 >= max_rows || i0 >= end - start) return;            // the whole workgroup
+    const bool rotate = rope.scale != 0.f;                    // 0: no rotation asked for
+    if (rotate)
+        stage_angles(ang, rope, ln.rows, false, [&](int x) {
+            const int64_t at = min((int64_t)start + i0 + x, (int64_t)end - 1);
+            return pos ? (int64_t)pos[at] : (int64_t)len + i0 + x;
+        });
     stage_gain<V, INTER>(gains, width, q.gain, q.gain_dtype, ln, rope.rot_dim);
     stage_gain<V, INTER>(gains + width, width, k.gain, k.gain_dtype, ln, rope.rot_dim);
-    __syncthreads();
-    if (slot >= ln.slots * ln.rows || start < 0 || i >= max_rows || start >= end || i >= end - start) return;
     const int64_t r = (int64_t)start + i;
     const int64_t t = (int64_t)len + i;                       // the row's token
+    const bool mine = slot < ln.slots * ln.rows && i < max_rows && i < end - start;
     const int64_t entry = t >> c.page_log2;
     int page = -1;
-    if (len >= 0 && entry < c.max_pages) page = c.table[(int64_t)b * c.max_pages + entry];
+    if (mine && len >= 0 && entry < c.max_pages) page = c.table[(int64_t)b * c.max_pages + entry];
     bool held = page >= 0 && page < c.n_pages;                // else the row's keys and values are dropped
     const int refs = held ? c.ref[page] : 0;
-    const int hd = c.head_dim;
+    __syncthreads();
+    if (!mine) return;                                        // whole runs
+    const int hd = c.head_dim, n_all = 2 * c.n_kv + q.heads;
     const int64_t head_stride = (int64_t)c.page_len * hd;     // within a page
     const int64_t base = layer_base + (int64_t)(held ? page : 0) * c.n_kv * head_stride + (t & (c.page_len - 1)) * hd;
-    const int n_all = 2 * c.n_kv + q.heads;
-    float co[CH][V], si[CH][V];
-    const bool rotate = rope.scale != 0.f;                    // 0: no rotation asked for
-    const int64_t p = pos ? pos[r] : t;
+    Raw<S, V, INTER> raw[CH];
+    auto ask = [&](int h) {
+        const S* src = h < c.n_kv       ? (const S*)k.x + r * k.x_row + h * hd
+                       : h < 2 * c.n_kv ? v + r * v_stride + (h - c.n_kv) * hd
+                                        : (const S*)q.x + r * q.x_row + (h - 2 * c.n_kv) * hd;
 #pragma unroll
-    for (int j = 0; j < CH; ++j) {
-        const int chunk = rotate ? lane + j * ln.run : ln.turn;           // chunk ln.turn: cosine 1
-        chunk_angles<V>(rope, p, chunk, ln, false, co[j], si[j]);
-    }
+        for (int j = 0; j < CH; ++j) raw[j] = load_chunk<S, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
+    };
+    int h = slot % ln.slots;
+    if (h < n_all) ask(h);
+    float co[CH][V], si[CH][V];
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+        read_angles<V>(ang, row, rope.rot_dim / 2, lane + j * ln.run, rotate && lane + j * ln.run < ln.turn, co[j], si[j]);
     if (refs > 1 && counted_elsewhere(c, b, t, page)) held = false;
     const float inv_n = 1.f / (float)hd;
-    for (int h0 = slot % ln.slots; h0 < n_all; h0 += U * ln.slots) {
-        Raw<S, V, INTER> raw[U][CH];
+    while (h < n_all) {
+        const bool is_k = h < c.n_kv, is_v = !is_k && h < 2 * c.n_kv, drop = h < 2 * c.n_kv && !held;
+        D* dst = is_k   ? reinterpret_cast<D*>(c.k) + base + h * head_stride
+                 : is_v ? reinterpret_cast<D*>(c.v) + base + (h - c.n_kv) * head_stride
+                        : (D*)q.y + r * q.y_row + (h - 2 * c.n_kv) * hd;
+        float a[CH][2 * V], ss = 0.f;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * ln.slots;
-            if (h >= n_all || (h < 2 * c.n_kv && !held)) continue;
-            const S* src = h < c.n_kv       ? (const S*)k.x + r * k.x_row + h * hd
-                           : h < 2 * c.n_kv ? v + r * v_stride + (h - c.n_kv) * hd
-                                            : (const S*)q.x + r * q.x_row + (h - 2 * c.n_kv) * hd;
-#pragma unroll
-            for (int j = 0; j < CH; ++j)
-                raw[u][j] = load_chunk<S, V, INTER, STREAM>(src, lane + j * ln.run, ln, rope.rot_dim);
+        for (int j = 0; j < CH; ++j) {
+            widen_chunk<S, V, INTER>(raw[j], lane + j * ln.run, ln, a[j]);
+            ss += sum_squares<V>(a[j]);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * ln.slots;
-            if (h >= n_all || (h < 2 * c.n_kv && !held)) continue;
-            const bool is_k = h < c.n_kv, is_v = !is_k && h < 2 * c.n_kv;
-            D* dst = is_k   ? reinterpret_cast<D*>(c.k) + base + h * head_stride
-                     : is_v ? reinterpret_cast<D*>(c.v) + base + (h - c.n_kv) * head_stride
-                            : (D*)q.y + r * q.y_row + (h - 2 * c.n_kv) * hd;
-            float a[CH][2 * V], ss = 0.f;
+        h += ln.slots;
+        if (h < n_all) ask(h);
+        if (drop) continue;
+        if (!is_v) {
+            const float rs = rsqrtf(run_sum(ss, ln.run) * inv_n + eps);
+            const float* g = gains + (is_k ? width : 0);
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                widen_chunk<S, V, INTER>(raw[u][j], lane + j * ln.run, ln, a[j]);
-                ss += sum_squares<V>(a[j]);
+                const float* gc = g + (lane + j * ln.run) * 2 * V;
+#pragma unroll
+                for (int x = 0; x < 2 * V; ++x) a[j][x] *= rs * gc[x];
+                turn<V>(a[j], co[j], si[j]);
             }
-            if (!is_v) {
-                const float rs = 1.f / sqrtf(run_sum(ss, ln.run) * inv_n + eps);
-                const float* g = gains + (is_k ? width : 0);
-#pragma unroll
-                for (int j = 0; j < CH; ++j) {
-                    const float* gc = g + (lane + j * ln.run) * 2 * V;
-#pragma unroll
-                    for (int x = 0; x < 2 * V; ++x) a[j][x] *= rs * gc[x];
-                    turn<V>(a[j], co[j], si[j]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < CH; ++j)
-                store_chunk<D, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
         }
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+            store_chunk<D, V, INTER, STREAM>(dst, lane + j * ln.run, ln, rope.rot_dim, a[j]);
     }
 }
 
@@ -495,13 +518,13 @@ __global__ __launch_bounds__(256) void append_norm_kernel(const dlm_rope rope, C
 
 // Runs of a power of two of lanes; how many heads a workgroup takes at a time: the number
 // that leaves the fewest lanes and turns idle, the largest of those.
-NormLanes lay_out(const dlm_rope& r, int V, int64_t rows, int64_t heads) {
+NormLanes lay_out(const dlm_rope& r, int V, int64_t rows, int64_t heads, int64_t most_slots = 256) {
     const int pass = r.interleaved && V > 1 ? 2 * V : V;
     NormLanes ln{r.rot_dim / 2 / V, (r.head_dim - r.rot_dim) / pass, 1, 1, 1};
     while (ln.run < ln.turn + ln.pass && ln.run < 64) ln.run *= 2;
     const int most = 256 / ln.run;
     double best_use = 0.;
-    for (int s = 1; s <= heads && s <= most; ++s) {
+    for (int s = 1; s <= heads && s <= most && s <= most_slots; ++s) {
         const int at_once = (int)std::min<int64_t>(most / s, rows);
         const double use = (double)(s * at_once) / most * heads / (s * ((heads + s - 1) / s));
         if (use >= best_use) {
@@ -535,6 +558,8 @@ hipError_t with_chunks(const dlm_rope& r, const NormLanes& ln, F launch) {
     return with_layout(std::integral_constant<int, 1>{});
 }
 
+constexpr int kWalk = 4;
+
 struct NormCall {
     const dlm_rope& rope;
     int rows;
@@ -551,7 +576,8 @@ template <typename T, int V, bool STREAM = false>
 hipError_t norm_layout(const NormCall& a) {
     if (a.gq) {
         // Workgroups by the heads of the two sets, at least one for a set that has heads.
-        const NormLanes lq = lay_out(a.rope, V, a.rows, a.q.heads), lk = lay_out(a.rope, V, a.rows, a.k.heads);
+        const NormLanes lq = lay_out(a.rope, V, a.rows, a.q.heads, std::max(a.q.heads / kWalk, 1)),
+                        lk = lay_out(a.rope, V, a.rows, a.k.heads, std::max(a.k.heads / kWalk, 1));
         auto groups = [&](const NormLanes& ln, int heads, int64_t most) {
             return heads ? (int)std::min<int64_t>(((int64_t)a.rows + ln.rows - 1) / ln.rows, std::max<int64_t>(most, 1)) : 0;
         };

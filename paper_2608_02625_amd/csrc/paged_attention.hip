@@ -1548,7 +1548,8 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
     p.mask = nullptr;
     p.mask_words = 0;
     const Shape sp = prefix_shape(c.n_seqs, c.n_kv, total_rows, max_group_rows, a.group, max_keys);
-    const Shape sa = own_shape(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, max_keys);
+    Shape sa = own_shape(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, max_keys);
+    if (may_split(sp, max_keys)) sa.min_steps = std::min(sa.min_steps, 2);    // the join is there
     char* at = (char*)ws;
     auto carve = [&](AttnArgs& x, const Shape& s) {
         x.info = (int4*)at;
