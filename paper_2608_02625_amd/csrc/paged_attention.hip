@@ -42,6 +42,7 @@
 // workspace, and a second kernel joins them in order: results do not depend on
 // timing.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "cache.h"
@@ -182,8 +183,6 @@ struct AttnArgs {
     const int32_t* rows;                      // [total_rows]: the groups' rows
     float* row_o;                             // this launch's (kPrefix; kSuffix behind a prefix)
     float2* row_ml;
-    const float* pre_o;                       // kSuffix: the prefix's, taken in here; NULL: by join_rows_kernel
-    const float2* pre_ml;
     int4* info;                               // [n_seqs]: first slot, parts, row tiles of an item
 };
 
@@ -263,22 +262,25 @@ __device__ __forceinline__ int from_lane(int v, int l) {
 #endif
 }
 
+// Row tiles and steps of a sequence or a group.
+__device__ __forceinline__ void seq_shape(const AttnArgs& a, const Seq& s, int& tiles, int& steps) {
+    tiles = (s.n * a.group + a.rows_per_wg - 1) >> a.rows_log2;
+    steps = max((s.keys - s.first + a.step - 1) >> a.step_log2, 1);
+}
+
 // The index-th unit (or, with `items`, the index-th item of several parts) in the
 // order sequence, key head, part, row tile; false if there are fewer.  A lane
-// looks after a sequence, 64 at a time.
+// looks after a sequence, 64 at a time.  given: most steps of a unit (0: worked out here).
 template <bool ITEMS, int MODE>
-__device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u) {
+__device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u, int given = 0) {
     const int lane = threadIdx.x & 63;
-    auto shape = [&](const Seq& s, int& tiles, int& steps) {
-        tiles = (s.n * a.group + a.rows_per_wg - 1) >> a.rows_log2;
-        steps = max((s.keys - s.first + a.step - 1) >> a.step_log2, 1);
-    };
+    auto shape = [&](const Seq& s, int& tiles, int& steps) { seq_shape(a, s, tiles, steps); };
     const Seq first = sequence<MODE>(a, lane);
     // Steps of all items: float32, since row starts that overlap may make more of them
     // than an int holds, and what follows needs no more than its bound (max_slots).
     float sum = 0.f;
     int items = 0;
-    for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
+    for (int b0 = 0; given == 0 && b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
         shape(b0 ? sequence<MODE>(a, b0 + lane) : first, tiles, steps);
         sum += wave_sum_dpp((float)tiles * (float)steps * (float)a.c.n_kv);
@@ -287,7 +289,7 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
     // Cut into runs of sum / n steps an item's last one is half empty on average, so
     // this aims at `units` of them together.
     const int n = max(a.units - items / 2, a.units / 2);
-    const int most = max(a.min_steps, (int)fminf(ceilf(sum / (float)n), 0x1p30f));
+    const int most = given ? given : max(a.min_steps, (int)fminf(ceilf(sum / (float)n), 0x1p30f));
     int before = 0, slots_before = 0;
     for (int b0 = 0; b0 < a.c.n_seqs; b0 += 64) {
         int tiles, steps;
@@ -332,6 +334,37 @@ __device__ __forceinline__ bool find_unit(const AttnArgs& a, int index, Unit& u)
         slots_before = from_lane(slot_end, 63);
     }
     return false;
+}
+
+// Prefixes and own keys in one launch: units of about as many keys each, so many that all of
+// them together make what the chip holds at once (a tile of keys costs a workgroup about as
+// much against 128 rows, by its products, as against a few, by its bytes).
+struct Balance {
+    int most_pre, most_own, pre_units;
+};
+__device__ __forceinline__ Balance balance(const AttnArgs& pre, const AttnArgs& own) {
+    const int lane = threadIdx.x & 63;
+    float keys = 0.f;
+    int items = 0;
+    for (int b0 = 0; b0 < own.c.n_seqs; b0 += 64) {
+        const Seq p = sequence<kPrefix>(pre, b0 + lane), s = sequence<kSuffix>(own, b0 + lane);
+        int tp, ts, steps;
+        seq_shape(pre, p, tp, steps);
+        seq_shape(own, s, ts, steps);
+        keys += wave_sum_dpp(((float)tp * (float)p.keys + (float)ts * (float)(s.keys - s.first)) * (float)own.c.n_kv);
+        items += from_lane(wave_scan((tp + ts) * own.c.n_kv), 63);
+    }
+    const int n = max(own.units - items / 2, own.units / 2);
+    const float each = keys / (float)n;
+    Balance r{max(pre.min_steps, (int)fminf(ceilf(each / (float)pre.step), 0x1p30f)),
+              max(own.min_steps, (int)fminf(ceilf(each / (float)own.step), 0x1p30f)), 0};
+    for (int b0 = 0; b0 < own.c.n_seqs; b0 += 64) {
+        int tiles, steps;
+        seq_shape(pre, sequence<kPrefix>(pre, b0 + lane), tiles, steps);
+        const int parts = (int)((uint32_t)(steps + r.most_pre - 1) / (uint32_t)r.most_pre);
+        r.pre_units += from_lane(wave_scan(tiles * pre.c.n_kv * parts), 63);
+    }
+    return r;
 }
 
 // Where join_rows_kernel finds the parts of a sequence or a group, from its first unit.
@@ -672,25 +705,24 @@ __device__ __forceinline__ int k_turn(int row) {          // of a chunk's number
     return HD == 128 ? row & 3 : (row >> 1) & 3;
 }
 
+// LDS of a workgroup.
+template <int HD, int WK>
+constexpr int kManyLds = WK * kManyStages * (kTile / Dims<HD>::ROWS_PER_COPY * kCopyStep + Dims<HD>::HALF);
+
+// Workgroup `wg` of a launch.  smem: the kernel's only LDS variable: with a second one the
+// compiler tells the two apart, takes a fragment read to depend on every copy in flight into
+// this one, and waits for them all.
 template <bool F16, int HD, bool ONCE, int WK, int MODE>
-__global__ __launch_bounds__(256 * WK) __attribute__((amdgpu_waves_per_eu(WK == 1 ? 3 : 2))) void
-attend_many_kernel(const AttnArgs a) {
+__device__ __forceinline__ void attend_many(const AttnArgs& a, int wg, char* smem, int given = 0) {
     using D = Dims<HD>;
     constexpr int K_TILE = kTile / D::ROWS_PER_COPY * kCopyStep;
     constexpr int NS = kManyStages, STAGE = K_TILE + D::HALF;
     constexpr int COPIES = D::HALF / 1024 / 4;            // 1 KB copies per wave of a K or V tile
-    // The kernel's only LDS variable: with a second one the compiler tells the two
-    // apart, takes a fragment read to depend on every copy in flight into this one,
-    // and waits for them all.
-    __shared__ __attribute__((aligned(16))) char smem[WK * NS * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform((tid >> 6) & 3), wk = uniform(tid >> 8);
     const int g = lane >> 5, j = lane & 31;
     Unit u;
-    // Neighbouring units share their keys (row tiles): workgroups go to the 8 XCDs
-    // in turn, so each XCD takes runs of 8 units.
-    const int wg = blockIdx.x;
-    if (!find_unit<false, MODE>(a, (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7), u)) return;
+    if (!find_unit<false, MODE>(a, wg, u, given)) return;
     note_item<MODE>(a, u);
     const int rows = min(u.s.n * a.group - u.row_tile * kManyRows, kManyRows);           // of this workgroup
     const bool busy = wave * 32 < rows;                   // this wave has rows
@@ -836,24 +868,8 @@ attend_many_kernel(const AttnArgs a) {
         m = mn;
     }
     if (!busy) return;
-    if constexpr (MODE == kSuffix)
-        if (a.pre_o && u.s.first > 0) {                   // not split: the prefix is taken in here
-            const float2 pre = a.pre_ml[t * a.n_heads + head];
-            const Two w = together(a, m, pre.x);
-            const float* p = a.pre_o + (t * a.n_heads + head) * HD + 4 * g;
-#pragma unroll
-            for (int nb = 0; nb < D::NB; ++nb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x4 v = *reinterpret_cast<const f32x4*>(p + nb * 32 + 8 * e);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nb][4 * e + i] = o[nb][4 * e + i] * w.f0 + v[i] * w.f1;
-                }
-            l = l * w.f0 + pre.y * w.f1;
-            m = w.m;
-        }
     const bool split = u.parts > 1;
-    if (split || MODE == kPrefix || (MODE == kSuffix && !a.pre_o && u.s.first > 0)) {                       // what is left of a row until its parts are joined
+    if (split || MODE == kPrefix || (MODE == kSuffix && u.s.first > 0)) {                       // what is left of a row until its parts are joined
         if (row < rows) {
             const int64_t at = split ? (int64_t)u.slot * kManyRows + row : t * a.n_heads + head;
             float* p = (split ? a.part_o : a.row_o) + at * HD + 4 * g;
@@ -888,6 +904,17 @@ attend_many_kernel(const AttnArgs a) {
     if (a.lse && g == 0 && row < rows) a.lse[t * a.n_heads + head] = log_sum<F16>(a, m, l);
 }
 
+// Neighbouring units share their keys (row tiles): workgroups go to the 8 XCDs in turn, so
+// each XCD takes runs of 8 units.
+__device__ __forceinline__ int xcd_order(int wg) { return (wg & ~63) + (wg & 7) * 8 + ((wg >> 3) & 7); }
+
+template <bool F16, int HD, bool ONCE, int WK, int MODE>
+__global__ __launch_bounds__(256 * WK) __attribute__((amdgpu_waves_per_eu(WK == 1 ? 3 : 2))) void
+attend_many_kernel(const AttnArgs a) {
+    __shared__ __attribute__((aligned(16))) char smem[kManyLds<HD, WK>];
+    attend_many<F16, HD, ONCE, WK, MODE>(a, xcd_order(blockIdx.x), smem);
+}
+
 // ------------------------------------------------------------------ few rows
 
 // Up to 64 packed rows (RT row tiles per wave): bound by the bytes of K and V, each
@@ -902,22 +929,27 @@ attend_many_kernel(const AttnArgs a) {
 // 5.8 TB/s; 13 rows of 32 heads on 8 behind 131072 tokens (537 MB): 92 us, 5.8 TB/s; 641
 // keys of 64: 8.2 us, of which 5.3 are there for a single key (a launch, four loads that
 // need each other, the end).
+constexpr int kFewWaves = 4;
+template <int HD, int RT, int S>
+struct FewLds {
+    static constexpr int RING = 2 * S * Dims<HD>::HALF;   // a wave's stages: S tiles of K, then of V
+    static constexpr int OUT = 32 * RT * HD * 4;          // a wave's outputs in the end, then maxima and sums
+    static constexpr int OWN = RING > OUT + 32 * RT * 8 ? RING : OUT + 32 * RT * 8;
+    static constexpr int ALL = kFewWaves * OWN;
+};
+
 template <bool F16, int HD, int RT, int S, int MODE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 && RT == 1 ? 4 : RT == 1 ? 2 : 1))) void
-attend_few_kernel(const AttnArgs a) {
+__device__ __forceinline__ void attend_few(const AttnArgs& a, int wg, char* smem, int given = 0) {
     using D = Dims<HD>;
-    constexpr int WAVES = 4, TERMS = RT == 1 ? 2 : 1;
+    constexpr int WAVES = kFewWaves, TERMS = RT == 1 ? 2 : 1;
     constexpr int COPIES = D::HALF / 1024;                // 1 KB copies of a V tile
     constexpr int C4 = HD / 4;
-    constexpr int RING = 2 * S * D::HALF;                 // a wave's stages: S tiles of K, then of V
-    constexpr int OUT = 32 * RT * HD * 4;                 // a wave's outputs in the end, then maxima and sums
-    constexpr int OWN = RING > OUT + 32 * RT * 8 ? RING : OUT + 32 * RT * 8;
-    __shared__ __attribute__((aligned(16))) char smem[WAVES * OWN];   // the only LDS variable, as above
+    constexpr int OUT = FewLds<HD, RT, S>::OUT, OWN = FewLds<HD, RT, S>::OWN;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int g = lane >> 5, j = lane & 31;
     Unit u;
-    if (!find_unit<false, MODE>(a, blockIdx.x, u)) return;
+    if (!find_unit<false, MODE>(a, wg, u, given)) return;
     note_item<MODE>(a, u);
     const int rows = u.s.n * a.group;                     // one row tile: all rows of (sequence, key head)
     Keys<HD> keys(a, u);
@@ -1090,24 +1122,40 @@ attend_few_kernel(const AttnArgs a) {
         }
         const int64_t t = packed_row<MODE>(a, u.s, (uint32_t)row / (uint32_t)a.group);
         const int h = u.kvh * a.group + (int)((uint32_t)row % (uint32_t)a.group);
-        if constexpr (MODE == kSuffix)
-            if (a.pre_o && u.s.first > 0) {               // not split: the prefix is taken in here
-                const float2 pre = a.pre_ml[t * a.n_heads + h];
-                const Two w = together(a, m, pre.x);
-                o = o * w.f0 + *reinterpret_cast<const f32x4*>(a.pre_o + (t * a.n_heads + h) * HD + c4 * 4) * w.f1;
-                l = l * w.f0 + pre.y * w.f1;
-                m = w.m;
-            }
         if (u.parts > 1) {
             *reinterpret_cast<f32x4*>(a.part_o + ((int64_t)u.slot * a.rows_per_wg + row) * HD + c4 * 4) = o;
             if (c4 == 0) a.part_ml[(int64_t)u.slot * a.rows_per_wg + row] = float2{m, l};
-        } else if (MODE == kPrefix || (MODE == kSuffix && !a.pre_o && u.s.first > 0)) {
+        } else if (MODE == kPrefix || (MODE == kSuffix && u.s.first > 0)) {
             *reinterpret_cast<f32x4*>(a.row_o + (t * a.n_heads + h) * HD + c4 * 4) = o;
             if (c4 == 0) a.row_ml[t * a.n_heads + h] = float2{m, l};
         } else {
             store_out<F16>(a, t, h, c4 * 4, HD, o, l == 0.f ? 0.f : 1.f / l);
             if (a.lse && c4 == 0) a.lse[t * a.n_heads + h] = log_sum<F16>(a, m, l);
         }
+    }
+}
+
+template <bool F16, int HD, int RT, int S, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 && RT == 1 ? 4 : RT == 1 ? 2 : 1))) void
+attend_few_kernel(const AttnArgs a) {
+    __shared__ __attribute__((aligned(16))) char smem[FewLds<HD, RT, S>::ALL];
+    attend_few<F16, HD, RT, S, MODE>(a, blockIdx.x, smem);
+}
+
+// Prefixes and up to 32 packed rows' own keys in one launch, so that neither waits for the
+// other's start and end: units of the prefixes first.
+template <bool F16, int HD, bool MANY>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void
+attend_both_kernel(const AttnArgs pre, const AttnArgs own) {
+    constexpr int FEW = FewLds<HD, 1, 1>::ALL, ALL = MANY && kManyLds<HD, 1> > FEW ? kManyLds<HD, 1> : FEW;
+    __shared__ __attribute__((aligned(16))) char smem[ALL];
+    const Balance l = balance(pre, own);
+    const int wg = blockIdx.x;
+    if (wg < l.pre_units) {
+        if constexpr (MANY) attend_many<F16, HD, false, 1, kPrefix>(pre, wg < (l.pre_units & ~63) ? xcd_order(wg) : wg, smem, l.most_pre);
+        else attend_few<F16, HD, 1, 1, kPrefix>(pre, wg, smem, l.most_pre);
+    } else {
+        attend_few<F16, HD, 1, 1, kSuffix>(own, wg - l.pre_units, smem, l.most_own);
     }
 }
 
@@ -1281,9 +1329,10 @@ int64_t item_bound(int n_seqs, int n_kv, int total_rows, int max_rows, int group
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+int64_t round64(int64_t n) { return (n + 63) / 64 * 64; }
 template <bool F16, int HD, int MODE>
 hipError_t launch(const AttnArgs& a, int64_t items, bool may_split, hipStream_t st) {
-    const int64_t wgs = (items + (may_split ? a.units : 0) + 63) / 64 * 64;
+    const int64_t wgs = round64(items + (may_split ? a.units : 0));
     if (wgs > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)wgs), block(256);
     if (a.rows_per_wg == 32)
@@ -1332,13 +1381,18 @@ void take_shape(AttnArgs& a, const Shape& s, void* ws) {
     a.part_ml = (float2*)((char*)ws + round256((size_t)a.max_slots * s.rows_per_wg * a.c.head_dim * 4));
 }
 // n_items: sequences or groups at most.
+int64_t items_of(const AttnArgs& a, int n_items) {
+    return item_bound(n_items, a.c.n_kv, a.total_rows, a.max_rows, a.group, a.rows_per_wg);
+}
+// The list's counts are 32-bit, whatever the row starts.
+bool countable(const AttnArgs& a) {
+    return (int64_t)a.c.n_seqs * a.c.n_kv * (((int64_t)a.max_rows * a.group + a.rows_per_wg - 1) / a.rows_per_wg) <= (1 << 29);
+}
 template <int MODE>
 hipError_t attend(const AttnArgs& a, int dtype, int n_items, bool split, hipStream_t st) {
     const CacheArgs& c = a.c;
-    const int64_t items = item_bound(n_items, c.n_kv, a.total_rows, a.max_rows, a.group, a.rows_per_wg);
-    // The list's counts are 32-bit, whatever the row starts.
-    if ((int64_t)c.n_seqs * c.n_kv * (((int64_t)a.max_rows * a.group + a.rows_per_wg - 1) / a.rows_per_wg) > (1 << 29))
-        return hipErrorInvalidValue;
+    const int64_t items = items_of(a, n_items);
+    if (!countable(a)) return hipErrorInvalidValue;
     if (dtype == DLM_F16)
         return c.head_dim == 128 ? launch<true, 128, MODE>(a, items, split, st) : launch<true, 64, MODE>(a, items, split, st);
     return c.head_dim == 128 ? launch<false, 128, MODE>(a, items, split, st) : launch<false, 64, MODE>(a, items, split, st);
@@ -1483,9 +1537,15 @@ __global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t*
         for (int i = 0; in && i < n; ++i) out[w.rows + list + off + i] = start + i;
 }
 
+// Units aimed at where prefixes and own keys share a launch: the workgroups that the chip holds.
+constexpr int kBothUnits = 512;
 // A group has at least two sequences.
 int most_groups(int n_seqs) { return std::max(n_seqs / 2, 1); }
-Shape prefix_shape(int n_seqs, int n_kv, int total_rows, int max_group_rows, int group, int max_keys) {
+Shape prefix_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int max_group_rows, int group, int max_keys) {
+    if ((int64_t)max_rows * group <= 32) {                // beside the sequences' own keys
+        if ((int64_t)max_group_rows * group <= 32) return {32, 4 * kTile, kBothUnits, 2};
+        return {kManyRows, kTile, kBothUnits, 8};
+    }
     return shape_for(max_group_rows, group, item_bound(most_groups(n_seqs), n_kv, total_rows, max_group_rows, group, kManyRows),
                      max_keys);
 }
@@ -1528,7 +1588,7 @@ size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int tot
                                      int group) {
     const size_t own = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_rows, group);
     if (!shares(max_rows, max_group_rows, group, 0x7fffffff)) return own;
-    return own + parts_bytes(prefix_shape(n_seqs, n_kv, total_rows, max_group_rows, group, 0), head_dim) +
+    return own + parts_bytes(prefix_shape(n_seqs, n_kv, total_rows, max_rows, max_group_rows, group, 0), head_dim) +
            2 * (row_bytes(total_rows, n_kv * group, head_dim) + round256((size_t)n_seqs * sizeof(int4)));
 }
 
@@ -1547,9 +1607,13 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
     p.max_rows = max_group_rows;
     p.mask = nullptr;
     p.mask_words = 0;
-    const Shape sp = prefix_shape(c.n_seqs, c.n_kv, total_rows, max_group_rows, a.group, max_keys);
+    const bool both = (int64_t)max_rows * a.group <= 32;
+    const Shape sp = prefix_shape(c.n_seqs, c.n_kv, total_rows, max_rows, max_group_rows, a.group, max_keys);
     Shape sa = own_shape(c.n_seqs, c.n_kv, total_rows, max_rows, a.group, max_keys);
-    if (may_split(sp, max_keys)) sa.min_steps = std::min(sa.min_steps, 2);    // the join is there
+    if (both) {                                           // few rows either way: 256 keys at least
+        sa.units = kBothUnits;
+        sa.min_steps = 2;
+    }
     char* at = (char*)ws;
     auto carve = [&](AttnArgs& x, const Shape& s) {
         x.info = (int4*)at;
@@ -1562,14 +1626,28 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
     };
     carve(p, sp);
     carve(a, sa);
-    const bool split = may_split(sp, max_keys) || may_split(sa, max_keys);
-    if (!split) {                                         // nothing to join: the second launch takes the prefix in
-        a.pre_o = p.row_o;
-        a.pre_ml = p.row_ml;
+    hipError_t e;
+    if (both) {
+        if (!countable(p) || !countable(a)) return hipErrorInvalidValue;
+        // Split items make at most a unit more than their keys, and all together `units` of those.
+        const int64_t wgs = items_of(p, most_groups(c.n_seqs)) + items_of(a, c.n_seqs) + 2 * kBothUnits;
+        if (wgs > 0x7fffffff) return hipErrorInvalidValue;
+        const bool many = sp.rows_per_wg == kManyRows;
+        auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, st, p, a);
+            return hipGetLastError();
+        };
+        auto pick = [&](auto f16) {
+            constexpr bool F = decltype(f16)::value;
+            if (c.head_dim == 128) return many ? go(attend_both_kernel<F, 128, true>) : go(attend_both_kernel<F, 128, false>);
+            return many ? go(attend_both_kernel<F, 64, true>) : go(attend_both_kernel<F, 64, false>);
+        };
+        e = dtype == DLM_F16 ? pick(std::true_type{}) : pick(std::false_type{});
+    } else {
+        e = attend<kPrefix>(p, dtype, most_groups(c.n_seqs), may_split(sp, max_keys), st);
+        if (e == hipSuccess) e = attend<kSuffix>(a, dtype, c.n_seqs, may_split(sa, max_keys), st);
     }
-    hipError_t e = attend<kPrefix>(p, dtype, most_groups(c.n_seqs), may_split(sp, max_keys), st);
-    if (e == hipSuccess) e = attend<kSuffix>(a, dtype, c.n_seqs, may_split(sa, max_keys), st);
-    if (e != hipSuccess || !split) return e;
+    if (e != hipSuccess) return e;
     const int per = 256 / (c.head_dim / 4 * kJoinRuns);
     const dim3 grid((unsigned)total_rows, (unsigned)((n_heads + per - 1) / per));
     auto kernel = dtype == DLM_F16 ? (c.head_dim == 128 ? join_rows_kernel<true, 128> : join_rows_kernel<true, 64>)
