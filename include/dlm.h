@@ -600,7 +600,9 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
  * found.  It holds for these row starts as long as lengths and tables stay as they are, that
  * is for all layers of a pass: make it after reserve.
  * dlm_cache_attend_shared: dlm_cache_attend with d_share, in the same total_rows, max_rows and
- * max_group_rows; the results are the same but for the order of sums.
+ * max_group_rows; the results are the same but for the order of sums.  Where sharing would
+ * cost more than it saves (short prefixes, long windows: by max_keys and the sizes, which
+ * max_keys should therefore tell) it does what dlm_cache_attend does.
  */
 size_t dlm_cache_share_bytes(const dlm_cache* cache, int32_t total_rows);
 dlm_status dlm_cache_share(const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows, int32_t max_rows,

@@ -1552,8 +1552,25 @@ Shape prefix_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int max_g
 Shape own_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int max_keys) {
     return shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), max_keys);
 }
-bool shares(int max_rows, int max_group_rows, int group, int max_keys) {
-    return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows && max_keys > kTile;
+// Whether a call could share at all: windows of more packed rows fill their workgroups' tiles
+// by themselves.
+bool may_share(int max_rows, int max_group_rows, int group) {
+    return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows;
+}
+// Whether it pays.  What it saves are bytes: without it every sequence reads its keys, most
+// of them from the caches.  What it costs are a join that is always there, and each row's
+// values out and in again.  So: the keys of as many sequences as there are windows of
+// max_rows, against 48 MB and 1000 bytes for each value of the result.  Plain / shared, us,
+// bf16, a group of n sequences with 40 tokens of their own.  16 heads of 128 on 4, a row
+// each: n 4, 2048 shared tokens 10.6 / 12.4, 16384 22.3 / 18.1; n 16, 2048 13.5 / 15.2, 4096
+// 18.5 / 15.6; n 64, 1024 16.6 / 18.0, 2048 22.8 / 18.9, 4096 35.6 / 21.6; 4 rows each, n
+// 16, 4096 19.2 / 21.2, 16384 43.1 / 34.0; 12 rows each, 4096 30.2 / 38.0, 16384 68.4 / 55.4.
+// 16 heads of 64: n 16, 512 8.1 / 11.7, 1024 13.2 / 12.1, 2048 17.3 / 12.3.
+bool shares(const AttnArgs& a, int max_group_rows) {
+    if (!may_share(a.max_rows, max_group_rows, a.group)) return false;
+    const double values = (double)a.total_rows * a.n_heads * a.c.head_dim;
+    const double windows = ((double)a.total_rows + a.max_rows - 1) / a.max_rows;
+    return windows * a.max_keys * (4. * a.c.n_kv * a.c.head_dim) >= 48e6 + 1000. * values;
 }
 size_t row_bytes(int total_rows, int n_heads, int head_dim) {
     const size_t n = (size_t)total_rows * n_heads;
@@ -1587,7 +1604,7 @@ hipError_t launch_share(const CacheArgs& c, const int32_t* row_start, int total_
 size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int max_group_rows,
                                      int group) {
     const size_t own = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_rows, group);
-    if (!shares(max_rows, max_group_rows, group, 0x7fffffff)) return own;
+    if (!may_share(max_rows, max_group_rows, group)) return own;
     return own + parts_bytes(prefix_shape(n_seqs, n_kv, total_rows, max_rows, max_group_rows, group, 0), head_dim) +
            2 * (row_bytes(total_rows, n_kv * group, head_dim) + round256((size_t)n_seqs * sizeof(int4)));
 }
@@ -1598,7 +1615,7 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
                                 int64_t o_stride, float* lse, void* ws, hipStream_t st) {
     AttnArgs a = attend_args(c, dtype, layer, row_start, total_rows, max_rows, max_keys, n_heads, q, q_stride, mask, mask_words,
                              scale, o, o_stride, lse);
-    if (!shares(max_rows, max_group_rows, a.group, max_keys)) return attend_plain(a, dtype, ws, st);
+    if (!shares(a, max_group_rows)) return attend_plain(a, dtype, ws, st);
     const ShareWords w = share_words(c.n_seqs, total_rows);
     a.groups = (const int4*)(share + w.groups);
     a.members = (const int4*)(share + w.members);
@@ -1629,8 +1646,9 @@ hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const 
     hipError_t e;
     if (both) {
         if (!countable(p) || !countable(a)) return hipErrorInvalidValue;
-        // Split items make at most a unit more than their keys, and all together `units` of those.
-        const int64_t wgs = items_of(p, most_groups(c.n_seqs)) + items_of(a, c.n_seqs) + 2 * kBothUnits;
+        // An item makes less than one unit more than its share of `units` (balance): a few over
+        // for the rounding of their sum.
+        const int64_t wgs = items_of(p, most_groups(c.n_seqs)) + items_of(a, c.n_seqs) + kBothUnits + 8;
         if (wgs > 0x7fffffff) return hipErrorInvalidValue;
         const bool many = sp.rows_per_wg == kManyRows;
         auto go = [&](auto kernel) {

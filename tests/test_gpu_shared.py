@@ -30,7 +30,8 @@ def _gpu():
 
 class Case:
     """Sequences of groups (numbers; -1: by itself) with `whole` pages in common, their
-    tokens on the CPU and in the pool, places without a token NaN."""
+    tokens on the CPU and in the pool, places without a token NaN.  Tables are so wide that
+    a call without a bound on the keys shares, whatever the lengths."""
 
     def __init__(self, dtype, H, KV, hd, page, group, whole, lens, rows, kind="full", seed=0, width=0, layers=1):
         from paper_2608_02625_amd import PagedCache
@@ -38,7 +39,8 @@ class Case:
         self.dtype, self.H, self.KV, self.hd, self.page, self.rows, self.lens = dtype, H, KV, hd, page, rows, lens
         B = len(lens)
         need = [-(-(n + r) // page) for n, r in zip(lens, rows)]
-        width = max(max(need), 1) + width
+        values = sum(rows) * H * hd
+        width = max(max(need), 1) + width + int((48e6 + 1000 * values) / (4 * KV * hd)) // page + 1
         n_pages = sum(need) + 4
         order = list(range(n_pages))
         rng.shuffle(order)
@@ -78,12 +80,12 @@ class Case:
         self.mask = None if kind == "full" else ref.pack_mask(self.sees, words).cuda()
         self.kind = kind
 
-    def run(self, max_group_rows=None, max_keys=None, check=True, gone=()):
+    def run(self, max_group_rows=None, max_keys=0, check=True, gone=()):
         c, T, top = self.c, self.T, max(self.rows)
         share = c.share(self.starts, self.group, T, top, max_group_rows)
         out = torch.full((T + 2, self.H, self.hd), 5.0, dtype=self.dtype, device="cuda")
         lse = torch.full((T, self.H), 5.0, device="cuda")
-        most = max(n + r for n, r in zip(self.lens, self.rows)) if max_keys is None else max_keys
+        most = max_keys
         got = c.attend(0, self.q.cuda(), self.starts, top, mask=self.mask, max_keys=most, out=out[1:T + 1], lse=lse, share=share)
         assert (out[0] == 5.0).all() and (out[T + 1] == 5.0).all()
         if check:
@@ -155,6 +157,7 @@ def test_groups(dtype, H, KV, hd, page, groups, members, tokens, tail, rows, kin
     again, lse2, _ = case.run(max(by_group), check=False)
     assert torch.equal(got, again) and torch.equal(lse, lse2)
     case.run()                                        # no bound but the rows
+    case.run(max(by_group), max(a + b for a, b in zip(lens, n)))      # as it pays
     _, _, skip = case.run(max(by_group) - 1)          # the largest group has more rows than it says
     assert any(skip) == any(s for s, g in zip(case.run(max(by_group), check=False)[2], group)
                             if g >= 0 and by_group[g] < max(by_group))
@@ -198,6 +201,11 @@ def test_bounds_on_keys_and_row_starts():
     case = Case(**base)
     for most in (0, 353, 345, 330, 100, 33, 32, 5, 1):
         case.run(max_keys=most)
+    # as many sequences as it takes to share under a bound below the prefix
+    n, t = 60, 3000
+    many = Case(BF, 16, 16, 64, 64, [0] * n, {0: 46}, [t + b for b in range(n)], [1] * n, seed=2)
+    for most in (t + n + 1, 2999, 1985, 1024, 1000):
+        many.run(max_keys=most)
     # Row starts that fall or overlap are not allowed; they reach no memory of others.
     guard = torch.full((400, 8, 128), 5.0, dtype=BF, device="cuda")
     q = torch.randn(200, 8, 128, device="cuda").to(BF)
@@ -251,7 +259,7 @@ def test_forks_as_they_are_used():
     from paper_2608_02625_amd import PagedCache
     g = torch.Generator().manual_seed(9)
     H, KV, hd, page, L, B = 8, 2, 64, 16, 3, 4
-    c = PagedCache(L, 64, page, KV, hd, B, 12)
+    c = PagedCache(L, 64, page, KV, hd, B, 9000)      # so wide that a call without a bound on its keys shares
     groups = _ints([0] * B)
     keys, values = [[] for _ in range(B)], [[] for _ in range(B)]
 
@@ -314,14 +322,14 @@ def test_captured_and_on_another_stream():
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         share = c.share(case.starts, case.group, T, 2)
-        got = c.attend(0, q, case.starts, 2, max_keys=2702, share=share)
+        got = c.attend(0, q, case.starts, 2, share=share)
     side.synchronize()
     assert torch.equal(got, want)
     out = torch.empty_like(q)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         share = c.share(case.starts, case.group, T, 2)
-        c.attend(0, q, case.starts, 2, max_keys=2702, out=out, share=share)
+        c.attend(0, q, case.starts, 2, out=out, share=share)
     for k in range(3):
         out.fill_(0)
         q.copy_(case.q.roll(k, 0))
@@ -329,5 +337,5 @@ def test_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         share = c.share(case.starts, case.group, T, 2)
-        assert torch.equal(out, c.attend(0, q, case.starts, 2, max_keys=2702, share=share)), k
+        assert torch.equal(out, c.attend(0, q, case.starts, 2, share=share)), k
         log(f"[replay {k}] {share.data.view(torch.int32)[24:48:4].tolist()}")
