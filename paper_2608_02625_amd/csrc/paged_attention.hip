@@ -712,7 +712,7 @@ constexpr int kManyLds = WK * kManyStages * (kTile / Dims<HD>::ROWS_PER_COPY * k
 // Workgroup `wg` of a launch.  smem: the kernel's only LDS variable: with a second one the
 // compiler tells the two apart, takes a fragment read to depend on every copy in flight into
 // this one, and waits for them all.
-template <bool F16, int HD, bool ONCE, int WK, int MODE>
+template <bool F16, int HD, bool ONCE, int WK, int MODE, int TERMS = 1>
 __device__ __forceinline__ void attend_many(const AttnArgs& a, int wg, char* smem, int given = 0) {
     using D = Dims<HD>;
     constexpr int K_TILE = kTile / D::ROWS_PER_COPY * kCopyStep;
@@ -829,9 +829,9 @@ __device__ __forceinline__ void attend_many(const AttnArgs& a, int wg, char* sme
             sched_fence();
             if (__builtin_expect(masked, 0)) rt[0].hide(st, seen_keys(a, u.s, lo, hi, k0, (uint32_t)gone), g);
             if (a.mask) words(tile_at(i + 1));
-            s16x8 pf[1][1][2];
+            s16x8 pf[1][TERMS][2];
             rt[0].softmax(st, a.scale_log2, a.lim, pf[0]);
-            wild |= add_values<F16, HD, 1, 1>(rt, pf, vf, lds, sb + K_TILE, lane, vfrag, masked);
+            wild |= add_values<F16, HD, 1, TERMS>(rt, pf, vf, lds, sb + K_TILE, lane, vfrag, masked);
         }
     }
 
@@ -1143,7 +1143,8 @@ attend_few_kernel(const AttnArgs a) {
 }
 
 // Prefixes and up to 32 packed rows' own keys in one launch, so that neither waits for the
-// other's start and end: units of the prefixes first.
+// other's start and end: units of the prefixes first.  Both take two terms of a probability, as
+// the same windows do without a shared prefix.
 template <bool F16, int HD, bool MANY>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2))) void
 attend_both_kernel(const AttnArgs pre, const AttnArgs own) {
@@ -1152,7 +1153,7 @@ attend_both_kernel(const AttnArgs pre, const AttnArgs own) {
     const Balance l = balance(pre, own);
     const int wg = blockIdx.x;
     if (wg < l.pre_units) {
-        if constexpr (MANY) attend_many<F16, HD, false, 1, kPrefix>(pre, wg < (l.pre_units & ~63) ? xcd_order(wg) : wg, smem, l.most_pre);
+        if constexpr (MANY) attend_many<F16, HD, false, 1, kPrefix, 2>(pre, wg < (l.pre_units & ~63) ? xcd_order(wg) : wg, smem, l.most_pre);
         else attend_few<F16, HD, 1, 1, kPrefix>(pre, wg, smem, l.most_pre);
     } else {
         attend_few<F16, HD, 1, 1, kSuffix>(own, wg - l.pre_units, smem, l.most_own);
