@@ -327,12 +327,16 @@ class PagedCache:
         """Workspace of calls with these sizes; kept, so that captured graphs stay valid."""
         return self._workspace((total_rows, max_rows, n_heads), self.lib.dlm_cache_workspace_bytes)
 
-    def _workspace(self, key: tuple, size) -> torch.Tensor:
+    def _workspace(self, key: tuple, size, rounded: bool = False) -> torch.Tensor:
+        """rounded: sizes that follow the rows go up to powers of two, so that all of them
+        together stay below four times the largest need."""
         ws = self._ws.get(key)
         if ws is None:
             n = size(self._ref, *key)
             if n == 0:
                 raise ValueError(f"invalid sizes: {key[0]} rows, {key[1]} at most, {key[-1]} heads")
+            if rounded:
+                n = 1 << (n - 1).bit_length()
             ws = self._by_size.get(n)
             if ws is None:
                 ws = self._by_size[n] = torch.empty(n, dtype=torch.uint8, device=self.device)
@@ -492,7 +496,7 @@ class PagedCache:
                 raise ValueError("lengths or tables have changed since share was made")
             if T:
                 most = share.max_group_rows
-                ws = self._workspace((T, max_rows, most, heads), self.lib.dlm_cache_shared_workspace_bytes)
+                ws = self._workspace((T, max_rows, most, heads), self.lib.dlm_cache_shared_workspace_bytes, rounded=True)
                 self._call("dlm_cache_attend_shared", layer, starts, T, max_rows, most, max_keys, share.data.data_ptr(),
                            share.data.numel(), heads, q.data_ptr(), qs, bits, words, scale, out.data_ptr(), os,
                            None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel())

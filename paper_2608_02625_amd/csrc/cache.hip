@@ -308,6 +308,7 @@ dlm_status dlm_rope_norm(const dlm_rope* rope, int32_t dtype, int32_t rows, cons
         TRY(check_norm_set(q, nullptr, false, dtype, rows, rope->head_dim));
         TRY(check_norm_set(k, nullptr, false, dtype, rows, rope->head_dim));
         if (norm_idle(rows, q, k)) return DLM_OK;
+        if (k && q->n_heads && k->n_heads && q->d_y == k->d_y) return fail(DLM_ERR_INVALID_ARG, "the sets' results overlap");
         return launched(launch_rope_norm(*rope, dtype, rows, q, k, eps, d_pos, (hipStream_t)hip_stream), "rope_norm");
     } catch (...) {
         return dlm_internal_caught();
@@ -331,6 +332,10 @@ dlm_status dlm_rope_norm_grad(const dlm_rope* rope, int32_t dtype, int32_t rows,
         TRY(check_norm(rope, dtype, rows, eps, q, k, d_pos));
         TRY(check_norm_set(q, dq, true, dtype, rows, rope->head_dim));
         TRY(check_norm_set(k, dk, true, dtype, rows, rope->head_dim));
+        if (!norm_idle(rows, q, k) && k && q->n_heads && k->n_heads && dq->d_dx == dk->d_dx)
+            return fail(DLM_ERR_INVALID_ARG, "the sets' results overlap");
+        if (k && q->n_heads && k->n_heads && dq->d_dgain && dq->d_dgain == dk->d_dgain)
+            return fail(DLM_ERR_INVALID_ARG, "the gains' gradients overlap");
         TRY(check_workspace(d_workspace, workspace_bytes, norm_grad_workspace_bytes(rope->head_dim)));
         return launched(launch_rope_norm_grad(*rope, dtype, rows, q, k, dq, dk, eps, d_pos, d_workspace,
                                               (hipStream_t)hip_stream), "rope_norm_grad");
@@ -573,8 +578,8 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
         const int rows = std::min(max_rows, total_rows);
         if (rows > kVerifyMaxRows) return fail(DLM_ERR_INVALID_ARG, "max_rows must be at most 1024");
         if (dtype != DLM_BF16 && dtype != DLM_F16 && dtype != DLM_F32) return fail(DLM_ERR_INVALID_ARG, "unknown dtype");
-        if (!(temperature >= 0.) || !std::isfinite(temperature))
-            return fail(DLM_ERR_INVALID_ARG, "temperature must be finite and >= 0");
+        if (!(temperature == 0. || temperature >= 1e-30) || !std::isfinite(temperature))
+            return fail(DLM_ERR_INVALID_ARG, "temperature must be finite, and 0 or at least 1e-30");
         if (d_draft && d_parent) return fail(DLM_ERR_INVALID_ARG, "with the draft's logits windows are chains: parent must be NULL");
         if (!d_next || !d_keep_start || !d_u_next) return fail(DLM_ERR_INVALID_ARG, "next, keep_start or u_next is NULL");
         if (total_rows > 0 && (!d_tokens || !d_target || !d_u || !d_keep))
@@ -600,7 +605,7 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
         a.draft = drafts ? d_draft : nullptr;
         a.target_stride = target_stride;
         a.draft_stride = draft_stride;
-        a.c = temperature > 0. ? std::min(1.4426950408889634 / temperature, 1e250) : 0.;
+        a.c = temperature > 0. ? 1.4426950408889634 / temperature : 0.;
         a.u = d_u;
         a.u_next = d_u_next;
         a.next = d_next;

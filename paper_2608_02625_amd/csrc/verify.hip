@@ -677,7 +677,7 @@ hipError_t launch_verify(VerifyArgs a, int dtype, void* ws, hipStream_t st) {
     a.sums = (double*)(at += z.verdicts);
     a.rest = (double*)(at += z.sums);
     a.inverse = (double*)(at + round256((size_t)a.n_seqs * row_chunks(a.vocab) * 8));
-    a.cf = (float)std::min(a.c, 3e38);
+    a.cf = (float)a.c;
     if (dtype == DLM_BF16) return verify_type<__bf16>(a, st);
     if (dtype == DLM_F16) return verify_type<_Float16>(a, st);
     return verify_type<float>(a, st);

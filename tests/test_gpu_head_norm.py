@@ -339,3 +339,28 @@ def test_append_normalises_keys_and_queries(dtype, hd, page, src):
     want = {(int(table[s, (lens[s] + i) // page]), (lens[s] + i) % page) for s, i in [(3, 0)] + [(2, i) for i in range(17)]
             if not (s == 2 and (31 + i) // page == 31 // page)}
     assert {tuple(x) for x in changed.nonzero().tolist()} == want
+
+
+@pytest.mark.parametrize("dtype,src", [(BF, BF), (BF, F32), (HF, HF)])
+@pytest.mark.parametrize("hd,rot,interleaved", [(64, 32, True), (128, 48, False), (128, 98, False), (64, 62, True), (64, 2, False)])
+def test_append_of_partly_rotated_heads(hd, rot, interleaved, dtype, src):
+    P = _lib()
+    g = torch.Generator().manual_seed(rot)
+    kw = dict(scaling="yarn", factor=4.0, original_len=512) if rot >= 32 else {}
+    rope, r = _rope(P, hd, rot, interleaved, **kw)
+    heads, kv, page, T = 3, 2, 32, 70
+    c = P.PagedCache(1, 8, page, kv, hd, 2, 4, dtype=dtype)
+    starts = torch.tensor([0, 40, 70], dtype=torch.int32, device="cuda")
+    assert bool(c.reserve(starts).all())
+    for off in (0, 1):                                # aligned, and at odd addresses
+        t = torch.randn(T * (heads + 2 * kv) * hd + off, generator=g).to(src).cuda()[off:].view(T, -1)
+        q, k, v = [t[:, a * hd:b * hd].view(T, b - a, hd) for a, b in ((0, heads), (heads, heads + kv), (heads + kv, heads + 2 * kv))]
+        gains = [(1 + 0.2 * torch.randn(hd, generator=g)).cuda() for _ in range(2)]
+        pos = torch.randint(0, 9000, (T,), generator=g, dtype=torch.int32)
+        got = c.append(0, k, v, starts, 40, q=q, rope=rope, positions=pos.cuda(), q_gain=gains[0], k_gain=gains[1], norm_eps=1e-5)
+        table = c.table.cpu()
+        place = [(int(table[s, i // page]), i % page) for s, n in ((0, 40), (1, 30)) for i in range(n)]
+        for x, gain, have in ((q, gains[0], got), (k, gains[1], torch.stack([c.k[0].cpu()[p, :, o] for p, o in place]))):
+            y, tol = _forward(x.cpu(), gain.cpu().double(), pos, r, 1e-5)
+            _within(have, y, tol + _rounding(y, dtype), f"append {hd} {rot} {dtype} {off}")
+        assert torch.equal(torch.stack([c.v[0].cpu()[p, :, o] for p, o in place]), v.cpu().to(dtype))

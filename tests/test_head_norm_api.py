@@ -81,6 +81,12 @@ def test_other_refusals():
     _refused(lib, lib.dlm_rope_norm_grad(rp, 0, 3, qp, None, gp, None, 1e-6, FAKE, None, n, None), "workspace")
     _refused(lib, lib.dlm_rope_norm_grad(rp, 0, 3, qp, None, gp, None, 1e-6, FAKE, FAKE + 64, n, None), "256-byte")
     _refused(lib, lib.dlm_rope_norm_grad(rp, 0, 3, qp, None, gp, None, 1e-6, FAKE, FAKE, n - 1, None), "small", -5)
+    # results of both sets in one place
+    far = _heads(L, d_y=3 * FAKE)
+    _refused(lib, lib.dlm_rope_norm(rp, 0, 3, qp, qp, 1e-6, FAKE, None), "overlap")
+    _refused(lib, lib.dlm_rope_norm_grad(rp, 0, 3, qp, ctypes.byref(far), gp, gp, 1e-6, FAKE, FAKE, n, None), "overlap")
+    other = _grads(L, d_dx=5 * FAKE)
+    _refused(lib, lib.dlm_rope_norm_grad(rp, 0, 3, qp, qp, gp, ctypes.byref(other), 1e-6, FAKE, FAKE, n, None), "overlap")
     # nothing to do
     assert lib.dlm_rope_norm(rp, 0, 0, qp, None, 1e-6, None, None) == 0
     none = _heads(L, n_heads=0, d_x=None, d_y=None)
