@@ -296,12 +296,12 @@ constexpr int kGradWgsOf = V == 8 ? 768 : kGradWgs;
 // The first q_wgs workgroups take the queries, the others the keys, each every q_wgs-th (or
 // other) group of rows.  A lane asks for its next head before it works on the one at hand.
 // The gain's sums stay in registers over all of them, are added over the workgroup's runs in
-// order, and leave one part per workgroup; the second kernel adds the parts in order.
+// order, in float64, and leave one part per workgroup; the second kernel adds the parts in order.
 template <typename T, int V, bool INTER, bool STREAM, int CH>
 __global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, const NormSet q, const NormSet k,
                                                         const NormGrad gq, const NormGrad gk, float eps,
                                                         const int32_t* __restrict__ pos, int rows, NormLanes lq,
-                                                        NormLanes lk, int q_wgs, float* __restrict__ parts) {
+                                                        NormLanes lk, int q_wgs, double* __restrict__ parts) {
     __shared__ __attribute__((aligned(16))) float gain[kGainWords];
     __shared__ float sums[256];
     const bool is_q = (int)blockIdx.x < q_wgs;
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, con
             sums[threadIdx.x] = acc[j][i];
             __syncthreads();
             if ((int)threadIdx.x < ln.run) {
-                float t = 0.f;
+                double t = 0.0;
                 for (int x = 0; x < runs; ++x) t += sums[x * ln.run + threadIdx.x];
                 const int at = value_at<V, INTER>(threadIdx.x + j * ln.run, i, ln, rope.rot_dim);
                 if (at >= 0) parts[(int64_t)blockIdx.x * rope.head_dim + at] = t;
@@ -405,14 +405,14 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(const dlm_rope rope, con
 }
 
 // The parts added in order: blockIdx.x takes 16 values of one gain, 64 runs of parts each.
-__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* __restrict__ parts, int q_parts, int k_parts,
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const double* __restrict__ parts, int q_parts, int k_parts,
                                                         int head_dim, void* out_q, int type_q, void* out_k, int type_k) {
-    __shared__ float run[64][17];
+    __shared__ double run[64][17];
     const int v = threadIdx.x & 15, at = threadIdx.x >> 4;
     const int per = (head_dim + 15) / 16, set = blockIdx.x / per, i = blockIdx.x % per * 16 + v;
     const int n = set ? k_parts : q_parts, first = set ? q_parts : 0;
     const int each = (n + 63) / 64, p1 = min(n, (at + 1) * each);
-    float t = 0.f;
+    double t = 0.0;
     if (i < head_dim)
 #pragma unroll 16
         for (int p = at * each; p < p1; ++p) t += parts[(int64_t)(first + p) * head_dim + i];
@@ -423,9 +423,9 @@ __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* __restrict_
 #pragma unroll 16
     for (int x = 1; x < 64; ++x) t += run[x][v];
     const int type = set ? type_k : type_q;
-    if (type == DLM_F32) reinterpret_cast<float*>(out)[i] = t;
-    else if (type == DLM_BF16) reinterpret_cast<__bf16*>(out)[i] = (__bf16)t;
-    else reinterpret_cast<_Float16*>(out)[i] = (_Float16)t;
+    if (type == DLM_F32) reinterpret_cast<float*>(out)[i] = (float)t;
+    else if (type == DLM_BF16) reinterpret_cast<__bf16*>(out)[i] = (__bf16)(float)t;
+    else reinterpret_cast<_Float16*>(out)[i] = (_Float16)(float)t;
 }
 
 // ------------------------------------------------------------------ into pages
@@ -568,7 +568,7 @@ struct NormCall {
     const int32_t* pos;
     hipStream_t st;
     const NormGrad *gq = nullptr, *gk = nullptr;
-    float* parts = nullptr;
+    double* parts = nullptr;
     int* q_parts = nullptr;
     int* k_parts = nullptr;
 };
@@ -689,7 +689,7 @@ hipError_t launch_rope_norm(const dlm_rope& rope, int dtype, int rows, const dlm
     return norm_any(NormCall{rope, rows, norm_set(q), norm_set(k), eps, pos, st}, dtype);
 }
 
-size_t norm_grad_workspace_bytes(int head_dim) { return (size_t)kGradWgs * head_dim * sizeof(float); }
+size_t norm_grad_workspace_bytes(int head_dim) { return (size_t)kGradWgs * head_dim * sizeof(double); }
 
 hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, const dlm_norm_heads* q,
                                  const dlm_norm_heads* k, const dlm_norm_grads* dq, const dlm_norm_grads* dk, float eps,
@@ -701,7 +701,7 @@ hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, cons
     void* out_k = k && dk && k->n_heads ? dk->d_dgain : nullptr;
     a.gq = &gq;
     a.gk = &gk;
-    a.parts = out_q || out_k ? (float*)ws : nullptr;
+    a.parts = out_q || out_k ? (double*)ws : nullptr;
     a.q_parts = &q_parts;
     a.k_parts = &k_parts;
     if (rows > 0 && a.q.heads + (int64_t)a.k.heads > 0) {
