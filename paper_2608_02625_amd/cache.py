@@ -175,7 +175,7 @@ class Rope:
         for c, x, y, name in ((sets[0], q, out, "out"), (sets[1], k, k_out, "k_out")):
             if x is not None:
                 if y is None:
-                    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                    y = torch.empty_like(x, memory_format=torch.contiguous_format)
                 elif y.shape != x.shape or y.dtype is not x.dtype or y.device != x.device or y.stride(2) != 1:
                     raise ValueError(f"{name} must have its input's shape, type and device, a head's values next to each other")
                 c.d_y = y.data_ptr()
@@ -200,13 +200,13 @@ class Rope:
             if dy.stride(2) != 1:                     # a head's values lie next to each other
                 dy = dy.clone(memory_format=torch.contiguous_format)
             sets.append(self._norm_set(x, gain, q, name))
-            dx = torch.empty(x.shape, dtype=kind, device=device)
+            dx = torch.empty_like(x, memory_format=torch.contiguous_format)
             dg = torch.empty_like(gain) if gain is not None and need else None
             grads.append(DlmNormGrads(dy.data_ptr(), dy.stride(0), dy.stride(1), dx.data_ptr(), dx.stride(0), dx.stride(1),
                                       None if dg is None else dg.data_ptr()))
             got.append((dx, dg, dy))
         n = self.lib.dlm_rope_norm_grad_workspace_bytes(self._ref)
-        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        ws = positions.new_empty(n // 4)
         _launch(self.lib.dlm_rope_norm_grad, "dlm_rope_norm_grad", device.index, self._ref, _DTYPES[kind], rows,
                 ctypes.byref(sets[0]), ctypes.byref(sets[1]), ctypes.byref(grads[0]), ctypes.byref(grads[1]), eps,
                 positions.data_ptr(), ws.data_ptr(), n)
@@ -462,7 +462,7 @@ class PagedCache:
         n = self.lib.dlm_cache_share_bytes(self._ref, rows)
         if n == 0:
             raise ValueError(f"invalid number of rows: {rows}")
-        data = torch.empty(n, dtype=torch.uint8, device=self.device)
+        data = groups.new_empty(n // 4)
         self._call("dlm_cache_share", starts, rows, max_rows, group, most, data.data_ptr(), n)
         return Share(self, rows, max_rows, most, data)
 
@@ -498,7 +498,7 @@ class PagedCache:
                 most = share.max_group_rows
                 ws = self._workspace((T, max_rows, most, heads), self.lib.dlm_cache_shared_workspace_bytes, rounded=True)
                 self._call("dlm_cache_attend_shared", layer, starts, T, max_rows, most, max_keys, share.data.data_ptr(),
-                           share.data.numel(), heads, q.data_ptr(), qs, bits, words, scale, out.data_ptr(), os,
+                           4 * share.data.numel(), heads, q.data_ptr(), qs, bits, words, scale, out.data_ptr(), os,
                            None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel())
             return out
         if T:

@@ -71,8 +71,8 @@ def verify(row_start: torch.Tensor, tokens: torch.Tensor, target: torch.Tensor, 
     n = lib.dlm_verify_workspace_bytes(n_seqs, rows, vocab, 0 if draft is None else 1)
     if n == 0:
         raise ValueError(f"invalid sizes: {n_seqs} sequences, {rows} rows of {vocab} logits")
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
-    out = torch.empty(2 * n_seqs + 1 + rows, dtype=torch.int32, device=device)
+    ws = row_start.new_empty((n + 3) // 4)
+    out = row_start.new_empty(2 * n_seqs + 1 + rows)
     nxt, keep_start, keep = out[:n_seqs], out[n_seqs:2 * n_seqs + 1], out[2 * n_seqs + 1:]
     _launch(lib.dlm_verify, "dlm_verify", device.index, n_seqs, starts, rows,
             min(1024, rows) if max_rows is None else int(max_rows), toks, up_ptr, _DTYPES[target.dtype], vocab,

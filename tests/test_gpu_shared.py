@@ -90,7 +90,7 @@ class Case:
         assert (out[0] == 5.0).all() and (out[T + 1] == 5.0).all()
         if check:
             self.check(got, lse, most, gone)
-        skip = share.data.view(torch.int32)[4 * c.n_seqs:8 * c.n_seqs:4].tolist()
+        skip = share.data[4 * c.n_seqs:8 * c.n_seqs:4].tolist()
         return got, lse, skip
 
     def check(self, got, lse, most, gone):
@@ -214,11 +214,11 @@ def test_bounds_on_keys_and_row_starts():
             s = case.c.share(_ints(starts), case.group, 200, top)
             case.c.attend(0, q, _ints(starts), top, out=guard[100:300], share=s)
     # what another pass left in a share reaches no memory of others either
-    s.data.view(torch.int32).fill_(1 << 30)
+    s.data.fill_(1 << 30)
     case.c.attend(0, q, _ints([0, 2, 3, 6]), 200, out=guard[100:300], share=s)
     s = case.c.share(_ints([0, 2, 3, 6]), case.group, 200, 3)
     for word in (-1, 7, 1 << 30, -(1 << 31)):
-        s.data.view(torch.int32).fill_(word)
+        s.data.fill_(word)
         case.c.attend(0, q, _ints([0, 2, 3, 6]), 3, out=guard[100:300], share=s)
     assert (guard[:100] == 5).all() and (guard[300:] == 5).all()
 
@@ -285,7 +285,7 @@ def test_forks_as_they_are_used():
     for rows in ([1, 1, 1, 1], [2, 1, 0, 5], [30, 1, 1, 2]):
         starts, T = append(rows)
         share = c.share(starts, groups, T, max(rows))
-        assert share.data.view(torch.int32)[4 * B:8 * B:4].tolist() == [64 if n else 0 for n in rows]
+        assert share.data[4 * B:8 * B:4].tolist() == [64 if n else 0 for n in rows]
         q = torch.randn(L, T, H, hd, generator=g).to(BF)
         for layer in range(L):
             x = q[layer].cuda()
@@ -338,4 +338,4 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         share = c.share(case.starts, case.group, T, 2)
         assert torch.equal(out, c.attend(0, q, case.starts, 2, share=share)), k
-        log(f"[replay {k}] {share.data.view(torch.int32)[24:48:4].tolist()}")
+        log(f"[replay {k}] {share.data[24:48:4].tolist()}")
