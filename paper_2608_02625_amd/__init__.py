@@ -5,7 +5,8 @@ fused per-position top-1/confidence reduction over the vocabulary, and the
 threshold edit/unmask rule -- all in hand-written HIP kernels behind the C ABI
 of include/dlm.h (libdlm.so); also block-AR drafting, the two-model
 draft-then-refine cascade, and a paged key/value cache with rotary positions
-and attention of windows (tokens, trees and blocks of drafted tokens) over it.  PyTorch supplies device memory and streams.
+(and norms of heads in the same pass), attention of windows (tokens, trees and blocks of drafted tokens, prefixes shared
+by sequences read once) over it, and the verification of drafted tokens.  PyTorch supplies device memory and streams.
 """
 
 from ._lib import DlmConfig, DlmError, DlmStats, LIB_PATH, load  # noqa: F401

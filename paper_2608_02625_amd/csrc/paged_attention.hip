@@ -33,6 +33,13 @@
 // values; where there are any they are taken out of the product and put back, as
 // infinities or NaN, into the rows that see them.
 //
+// Shared prefixes.  Sequences of a group that begin with the same pages have their rows
+// packed together against those pages (kPrefix), each sequence's rows against what follows
+// (kSuffix), and join_rows_kernel joins what the two left.  share_kernel finds the pages
+// from the tables, once for all layers of a pass.  A token of 64 sequences behind 16384
+// shared ones, 16 heads of 128 on 4, 16 to 1024 tokens of their own (101 MB, without
+// sharing 2.3 GB): 31.5 + 5.8 us a layer, without sharing 139.
+//
 // Work.  What bounds the kernel depends on the rows: bytes for a few, products
 // for many.  Either way the chip is filled by units of at most C steps of keys,
 // C such that all sequences' steps make about as many as the chip holds: a long sequence is
