@@ -705,8 +705,8 @@ dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int
  * over its sum; p_r as it is where less than 2^-43 is left, which is rounding).  When no child is left, d_next[s] is
  * drawn from p_r: the first v at which the running sum passes d_u_next[s] times the whole.
  * d_u float [total_rows] and d_u_next float [n_seqs] hold numbers in [0, 1) (others are read
- * as if cut off to it); entries of rows 0 are not read.  temperature >= 1e-30, or 0: p_r is 1 for the
- * largest logit (the lowest such v), and d_draft is not read.  A token outside [0, vocab) is
+ * as if cut off to it); entries of rows 0 are not read.  temperature is
+ * from 1e-30 to 1e30, or 0: p_r is 1 for the largest logit (the lowest such v), and d_draft is not read.  A token outside [0, vocab) is
  * never kept.  Logits: -infinity and NaN are chances of 0, +infinity counts as the largest
  * float32.  Where a row has no chance above 0, d_next is -1, as for a sequence without rows.
  *

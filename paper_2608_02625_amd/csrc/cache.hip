@@ -578,8 +578,9 @@ dlm_status dlm_verify(int32_t n_seqs, const int32_t* d_row_start, int32_t total_
         const int rows = std::min(max_rows, total_rows);
         if (rows > kVerifyMaxRows) return fail(DLM_ERR_INVALID_ARG, "max_rows must be at most 1024");
         if (dtype != DLM_BF16 && dtype != DLM_F16 && dtype != DLM_F32) return fail(DLM_ERR_INVALID_ARG, "unknown dtype");
-        if (!(temperature == 0. || temperature >= 1e-30) || !std::isfinite(temperature))
-            return fail(DLM_ERR_INVALID_ARG, "temperature must be finite, and 0 or at least 1e-30");
+        // float32 holds log2(e) / temperature, and its product with an infinity is one.
+        if (!(temperature == 0. || (temperature >= 1e-30 && temperature <= 1e30)))
+            return fail(DLM_ERR_INVALID_ARG, "temperature must be 0 or from 1e-30 to 1e30");
         if (d_draft && d_parent) return fail(DLM_ERR_INVALID_ARG, "with the draft's logits windows are chains: parent must be NULL");
         if (!d_next || !d_keep_start || !d_u_next) return fail(DLM_ERR_INVALID_ARG, "next, keep_start or u_next is NULL");
         if (total_rows > 0 && (!d_tokens || !d_target || !d_u || !d_keep))

@@ -49,7 +49,7 @@ def verify(row_start: torch.Tensor, tokens: torch.Tensor, target: torch.Tensor, 
     [rows, vocab]: the target's logits after each row; draft: those that each row's child
     was drawn from (chains only), None for drafted tokens that are certain.  u float32
     [rows], u_next float32 [n_seqs]: random numbers in [0, 1), one per drafted token and one
-    per sequence.  temperature divides the logits; 0: the largest decides.  max_rows: rows
+    per sequence.  temperature divides the logits (1e-30 to 1e30; 0: the largest decides).  max_rows: rows
     of the longest window (default and at most 1024).  No gradient passes through it.
     """
     lib, device = _lib.load(), target.device

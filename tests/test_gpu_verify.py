@@ -195,6 +195,22 @@ def test_greedy(shape):
         _same(_run(c), _want(c))                                                  # the draft is not read
 
 
+@pytest.mark.parametrize("shape", ["chain", "certain", "tree"])
+@pytest.mark.parametrize("temperature", [1e-30, 1e-3, 0.9, 1e6, 1e30])
+@pytest.mark.parametrize("offset", [0.0, 3000.0, -4.0e6, 2.0 ** 100])
+def test_temperatures_and_offsets(offset, temperature, shape):
+    """Chunks whose exponents float32 holds in one step and others, beside masked tokens and infinities."""
+    c = _case(21, [5, 3, 9, 1], 5000, F32, shape)
+    for name in ("target", "draft"):
+        if c[name] is not None:
+            c[name] = c[name] + offset                # few distinct logits where it is large
+            c[name][:, 5::7] = -math.inf
+            c[name][1, 2100] = math.nan               # one chunk of the row
+    c["target"][6, 4200] = math.inf
+    c["temperature"] = temperature
+    _same(_run(c, "odd"), _want(c))
+
+
 def test_rows_without_chances_and_wild_logits():
     inf, nan = math.inf, math.nan
     for shape in ("chain", "certain"):

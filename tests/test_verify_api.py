@@ -17,7 +17,7 @@ BAD = [(dict(n_seqs=0), "n_seqs"), (dict(n_seqs=65536), "n_seqs"), (dict(total_r
        (dict(total_rows=2000, max_rows=1025), "max_rows"), (dict(vocab=0), "vocab"), (dict(vocab=(1 << 24) + 1), "vocab"),
        (dict(total_rows=1 << 20, vocab=1 << 24, target_stride=1 << 24), "2^31"), (dict(dtype=3), "dtype"),
        (dict(dtype=-1), "dtype"), (dict(temperature=-0.5), "temperature"), (dict(temperature=math.nan), "temperature"),
-       (dict(temperature=math.inf), "temperature"), (dict(temperature=1e-31), "temperature"), (dict(d_row_start=None), "NULL"), (dict(d_tokens=None), "NULL"),
+       (dict(temperature=math.inf), "temperature"), (dict(temperature=1e-31), "temperature"), (dict(temperature=1.1e30), "temperature"), (dict(d_row_start=None), "NULL"), (dict(d_tokens=None), "NULL"),
        (dict(d_target=None), "NULL"), (dict(d_u=None), "NULL"), (dict(d_u_next=None), "NULL"), (dict(d_next=None), "NULL"),
        (dict(d_keep=None), "NULL"), (dict(d_keep_start=None), "NULL"), (dict(d_parent=FAKE, d_draft=FAKE, draft_stride=50), "parent"),
        (dict(target_stride=49), "stride"), (dict(d_draft=FAKE, draft_stride=49), "stride"), (dict(d_target=FAKE + 2), "aligned"),
