@@ -15,9 +15,9 @@
 //
 // Bound by the bytes.  32768 rows of 20 heads of 128, bf16 (336 MB): 64 us, 5.25 TB/s, as
 // the rotation alone.  32 prompts of up to 1024 rows, float32 to pages of bf16 (377 MB): 65
-// us, 5.8 TB/s.  Gradient of 16384 rows of 20 heads, bf16 (252 MB): 61 us, 4.1 TB/s with 11
-// waves per CU (146 registers).  The vector units are busy 73 % of the time in the norms and
-// 66 % in the gradient.  A row of each of 32 sequences: 5.9 us, four loads that need each other.
+// us, 5.8 TB/s.  The vector units are busy 73 % of the time in the norms.  Gradient of 16384
+// rows of 20 heads, bf16 (252 MB): 52 us, 4.9 TB/s; there they are busy 85 % of it, and are
+// what bounds it.  A row of each of 32 sequences: 5.9 us, four loads that need each other.
 #include <algorithm>
 #include <type_traits>
 
@@ -293,13 +293,13 @@ struct NormGrad {
     void* dx;
     int64_t dx_row, dx_head;
 };
-// Workgroups of the gradient, each with a part of one gain's gradient: at most what the chip
-// holds at once (3 per CU where a lane holds 16 values, 146 VGPRs, else 4), so that the parts
-// are few and no second turn of workgroups runs half empty (16384 rows of 20 heads of 128,
-// bf16: 1024 workgroups 83 us).
-constexpr int kGradWgs = 1024;
-template <int V>
-constexpr int kGradWgsOf = V == 8 ? 768 : kGradWgs;
+// Pairs of a lane in the gradient, and its workgroups, each with a part of one gain's
+// gradient: as many as the chip holds at once (5 per CU at 86 VGPRs), so that the parts are
+// few and no second turn of workgroups runs half empty.  16384 rows of 20 heads of 128, bf16:
+// 8 pairs (146 VGPRs) and 768 workgroups 65 us, 1024 83; 4 pairs and 768, 1024, 1280, 1536
+// workgroups 63, 61, 54, 67.
+constexpr int kGradPairs = 4;
+constexpr int kGradWgs = 1280;
 
 // The first q_wgs workgroups take the queries, the others the keys, each every q_wgs-th (or
 // other) group of rows.  A lane asks for its next head before it works on the one at hand.
@@ -566,9 +566,11 @@ hipError_t with_chunks(const dlm_rope& r, const NormLanes& ln, F launch) {
     return with_layout(std::integral_constant<int, 1>{});
 }
 
-// Heads of a row that a run of lanes walks in the gradient, so that its angles, as much
+// Heads of a row that a run of lanes walks in the gradient at most, so that its angles, as much
 // arithmetic as a head, are worked out once for them: a training step of 16384 rows of 20 heads
-// with 1, 2, 4 and 8 of them 119, 106, 103, 109 us.
+// with 2, 4 and 8 of them 107, 95, 97 us.  Fewer where that would leave workgroups idle
+// (grad_layout): a row of 20 heads with 1 and 4 of them 9.7 and 11.3 us, 256 rows of 40 heads
+// 12.3 and 13.3; 1024 rows of 20 heads, float32, 17.3 and 16.5.
 constexpr int kWalk = 4;
 
 struct NormCall {
@@ -584,25 +586,29 @@ struct NormCall {
     int* k_parts = nullptr;
 };
 template <typename T, int V, bool STREAM = false>
+hipError_t grad_layout(const NormCall& a) {
+    // Workgroups by the heads of the two sets, at least one for a set that has heads.
+    const int64_t all = (int64_t)a.q.heads + a.k.heads;
+    // Times that half of the workgroups are full with a head per run.
+    const int64_t full = (int64_t)a.rows * all / (kGradWgs / 2 * (256 / lay_out(a.rope, V, 1, 1, 1).run));
+    const int walk = (int)std::clamp<int64_t>(full, 1, kWalk);
+    const NormLanes lq = lay_out(a.rope, V, a.rows, a.q.heads, std::max(a.q.heads / walk, 1)),
+                    lk = lay_out(a.rope, V, a.rows, a.k.heads, std::max(a.k.heads / walk, 1));
+    auto groups = [&](const NormLanes& ln, int heads, int64_t most) {
+        return heads ? (int)std::min<int64_t>(((int64_t)a.rows + ln.rows - 1) / ln.rows, std::max<int64_t>(most, 1)) : 0;
+    };
+    const int nk = groups(lk, a.k.heads, kGradWgs * (int64_t)a.k.heads / all);
+    const int nq = groups(lq, a.q.heads, kGradWgs - nk);
+    *a.q_parts = nq;
+    *a.k_parts = nk;
+    return with_chunks<V, T>(a.rope, a.q.heads ? lq : lk, [&](auto ch, auto inter) {
+        hipLaunchKernelGGL((norm_grad_kernel<T, V, decltype(inter)::value, STREAM, decltype(ch)::value>), dim3((unsigned)(nq + nk)), dim3(256), 0, a.st, a.rope, a.q, a.k, *a.gq, *a.gk, a.eps,
+                           a.pos, a.rows, lq, lk, nq, a.parts);
+        return hipGetLastError();
+    });
+}
+template <typename T, int V, bool STREAM = false>
 hipError_t norm_layout(const NormCall& a) {
-    if (a.gq) {
-        // Workgroups by the heads of the two sets, at least one for a set that has heads.
-        const NormLanes lq = lay_out(a.rope, V, a.rows, a.q.heads, std::max(a.q.heads / kWalk, 1)),
-                        lk = lay_out(a.rope, V, a.rows, a.k.heads, std::max(a.k.heads / kWalk, 1));
-        auto groups = [&](const NormLanes& ln, int heads, int64_t most) {
-            return heads ? (int)std::min<int64_t>(((int64_t)a.rows + ln.rows - 1) / ln.rows, std::max<int64_t>(most, 1)) : 0;
-        };
-        const int64_t all = (int64_t)a.q.heads + a.k.heads;
-        const int nk = groups(lk, a.k.heads, kGradWgsOf<V> * (int64_t)a.k.heads / all);
-        const int nq = groups(lq, a.q.heads, kGradWgsOf<V> - nk);
-        *a.q_parts = nq;
-        *a.k_parts = nk;
-        return with_chunks<V, T>(a.rope, a.q.heads ? lq : lk, [&](auto ch, auto inter) {
-            hipLaunchKernelGGL((norm_grad_kernel<T, V, decltype(inter)::value, STREAM, decltype(ch)::value>), dim3((unsigned)(nq + nk)), dim3(256), 0, a.st, a.rope, a.q, a.k, *a.gq, *a.gk, a.eps,
-                               a.pos, a.rows, lq, lk, nq, a.parts);
-            return hipGetLastError();
-        });
-    }
     const NormLanes ln = lay_out(a.rope, V, a.rows, (int64_t)a.q.heads + a.k.heads);
     const int64_t wgs = ((int64_t)a.rows + ln.rows - 1) / ln.rows;
     const dim3 grid((unsigned)std::min(wgs, kWgsAcross), (unsigned)((wgs + kWgsAcross - 1) / kWgsAcross));
@@ -623,6 +629,13 @@ hipError_t norm_type(const NormCall& a) {
     const int V = pairs_per_chunk(a.rope, sizeof(T), [&](int n) { return set_fits(a.q, a.gq, n) && set_fits(a.k, a.gk, n); });
     constexpr int W = 16 / sizeof(T);
     const bool stream = streams((a.gq ? 3 : 2) * (int64_t)a.rows * ((int64_t)a.q.heads + a.k.heads) * a.rope.head_dim * sizeof(T));
+    if (a.gq) {
+        if (V >= kGradPairs) return stream ? grad_layout<T, kGradPairs, true>(a) : grad_layout<T, kGradPairs>(a);
+        if constexpr (sizeof(T) == 4)
+            if (a.rope.interleaved && V == W / 2 && stream) return grad_layout<T, W / 2, true>(a);
+        if (V == 2) return grad_layout<T, 2>(a);
+        return grad_layout<T, 1>(a);
+    }
     if (V == W && stream) return norm_layout<T, W, true>(a);
     if (a.rope.interleaved && V == W / 2 && stream) return norm_layout<T, W / 2, true>(a);
     if constexpr (sizeof(T) == 2)
