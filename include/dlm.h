@@ -429,8 +429,8 @@ dlm_status dlm_rope_apply(const dlm_rope* rope, int32_t dtype, int32_t rows, int
  *
  * dlm_rope_norm_grad: gradients of a loss with respect to x (d_dx, of `dtype`) and the
  * gain (d_dgain, of gain_dtype, may be NULL; the sum over rows and heads, in the same
- * order on every call), given that with respect to y (d_dy, of `dtype`).  d_y of the
- * sets is not read.  d_dx may be d_dy with the same strides.
+ * order on every call: zeros where there are none), given that with respect to y (d_dy,
+ * of `dtype`).  d_y of the sets is not read.  d_dx may be d_dy with the same strides.
  * d_workspace: dlm_rope_norm_grad_workspace_bytes(rope), 256-byte aligned; it keeps
  * nothing between calls, and calls that share it must be ordered.
  */

@@ -98,7 +98,8 @@ dlm_status check_gain(int dtype, int gain_dtype, const void* gain, const void* d
 }
 // A set of heads of dlm_rope_norm or, with `grad`, of its gradient.
 dlm_status check_norm_set(const dlm_norm_heads* s, const dlm_norm_grads* g, bool grad, int dtype, int64_t rows, int64_t hd) {
-    if (!s || s->n_heads == 0) return DLM_OK;
+    if (!s) return DLM_OK;
+    if (s->n_heads == 0) return grad && g && g->d_dgain ? check_gain(dtype, s->gain_dtype, nullptr, g->d_dgain) : DLM_OK;
     if (s->n_heads < 0 || s->n_heads > (1 << 24)) return fail(DLM_ERR_INVALID_ARG, "n_heads must be in [0, 2^24]");
     if (grad && !g) return fail(DLM_ERR_INVALID_ARG, "a set of heads without its gradients");
     TRY(check_gain(dtype, s->gain_dtype, s->d_gain, grad ? g->d_dgain : nullptr));
@@ -334,7 +335,7 @@ dlm_status dlm_rope_norm_grad(const dlm_rope* rope, int32_t dtype, int32_t rows,
         TRY(check_norm_set(k, dk, true, dtype, rows, rope->head_dim));
         if (!norm_idle(rows, q, k) && k && q->n_heads && k->n_heads && dq->d_dx == dk->d_dx)
             return fail(DLM_ERR_INVALID_ARG, "the sets' results overlap");
-        if (k && q->n_heads && k->n_heads && dq->d_dgain && dq->d_dgain == dk->d_dgain)
+        if (dq && k && dk && dq->d_dgain && dq->d_dgain == dk->d_dgain)
             return fail(DLM_ERR_INVALID_ARG, "the gains' gradients overlap");
         TRY(check_workspace(d_workspace, workspace_bytes, norm_grad_workspace_bytes(rope->head_dim)));
         return launched(launch_rope_norm_grad(*rope, dtype, rows, q, k, dq, dk, eps, d_pos, d_workspace,

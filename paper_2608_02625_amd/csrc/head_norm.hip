@@ -721,8 +721,9 @@ hipError_t launch_rope_norm_grad(const dlm_rope& rope, int dtype, int rows, cons
     NormCall a{rope, rows, norm_set(q), norm_set(k), eps, pos, st};
     const NormGrad gq = norm_grad(q, dq), gk = norm_grad(k, dk);
     int q_parts = 0, k_parts = 0;
-    void* out_q = q && dq && q->n_heads ? dq->d_dgain : nullptr;
-    void* out_k = k && dk && k->n_heads ? dk->d_dgain : nullptr;
+    // A set without heads leaves no parts, and a gain's gradient of zeros.
+    void* out_q = q && dq ? dq->d_dgain : nullptr;
+    void* out_k = k && dk ? dk->d_dgain : nullptr;
     a.gq = &gq;
     a.gk = &gk;
     a.parts = out_q || out_k ? (double*)ws : nullptr;
