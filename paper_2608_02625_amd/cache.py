@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import DlmCache, DlmNormGrads, DlmNormHeads, DlmRope, DlmRopeSpec, check
@@ -76,6 +77,15 @@ def _gain(t: torch.Tensor | None, name: str, head_dim: int, dtype: torch.dtype, 
     return t.data_ptr(), _DTYPES[t.dtype]
 
 
+def _no_tangents(*tensors: torch.Tensor | None):
+    """Refuse dual tensors of forward-mode differentiation: a kernel reads their values alone,
+    and the result would say that its derivative is zero."""
+    if forward_ad._current_level >= 0:                    # else nothing carries a tangent
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("no forward-mode derivative (tangent) passes through a rotation")
+
+
 class Rope:
     """Frequencies of rotary positions; a plain host structure, no device memory.
 
@@ -109,7 +119,9 @@ class Rope:
         """x [rows, heads, head_dim] (any row and head strides) rotated to `positions`
         (int32 [rows]); into `out` (may be x).  transpose: the gradient with respect
         to x, given the gradient x of a rotation's result; autograd takes it by itself
-        where x requires a gradient (`out` cannot be part of that)."""
+        where x requires a gradient (`out` cannot be part of that; tangents of forward-mode
+        differentiation are refused)."""
+        _no_tangents(x, out)
         if torch.is_grad_enabled() and (x.requires_grad or (out is not None and out.requires_grad)):
             if out is not None:
                 raise ValueError("a result in `out` carries no gradient: detach x and out, or leave out away")
@@ -142,7 +154,9 @@ class Rope:
         [head_dim] (their type or float32; None: ones), rotated to `positions`, in one
         launch: (queries, keys).  k None: queries alone.  out, k_out: results of queries and
         keys (may be q and k).  Gradients of q, k and the gains come by autograd (`out` and
-        `k_out` cannot be part of that, nor a gradient of the gradient)."""
+        `k_out` cannot be part of that, nor a gradient of the gradient; tangents of forward-mode
+        differentiation are refused)."""
+        _no_tangents(q, k, q_gain, k_gain, out, k_out)
         given = [t for t in (out, k_out) if t is not None]
         if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, q_gain, k_gain, *given)):
             if given:
@@ -234,6 +248,7 @@ class _NormRotation(torch.autograd.Function):
         q, k, positions, q_gain, k_gain = ctx.saved_tensors
         if dq is None and dk is None:
             return (None,) * 7
+        _no_tangents(dq, dk)
         need = ctx.needs_input_grad
         gq, gk, gqg, gkg = ctx.rope._norm_grad(q, k, positions, q_gain, k_gain, ctx.eps, dq, dk,
                                                (need[0], need[1], need[3], need[4]))

@@ -35,3 +35,21 @@ def test_a_gain_without_heads_has_a_gradient_of_zeros(heads, kv, gain_dtype):
     for count, dx, dg in zip((heads, kv), got[:n], got[n:]):
         assert dx.shape == (rows, count, hd)
         assert bool(dg.isfinite().all()) and bool(dg.any()) == (count > 0)
+
+
+def test_tangents_are_refused_forwards_and_backwards():
+    from torch.autograd import forward_ad
+    from paper_2608_02625_amd import Rope
+    rope = Rope(64)
+    x = torch.randn(5, 2, 64, device="cuda", requires_grad=True)
+    pos = torch.arange(5, dtype=torch.int32, device="cuda")
+    for f in (lambda t: rope.norm_apply(t, None, pos)[0], lambda t: rope.apply(t, pos)):
+        with forward_ad.dual_level():
+            with pytest.raises(ValueError, match="tangent"):
+                f(forward_ad.make_dual(x.detach(), torch.ones_like(x)))
+            y = f(x)
+            seed = forward_ad.make_dual(torch.ones_like(y), torch.ones_like(y))
+            with pytest.raises(ValueError, match="tangent"):
+                torch.autograd.grad(y, x, seed)
+        y = f(x)
+        assert torch.autograd.grad(y, x, torch.ones_like(y))[0].shape == x.shape

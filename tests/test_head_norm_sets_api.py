@@ -36,3 +36,30 @@ def test_the_gains_gradients_of_two_sets_have_places_of_their_own():
     for q, k in ((empty, full), (full, empty), (empty, empty)):
         _refused(lib, lib.dlm_rope_norm_grad(ctypes.byref(r), 0, 3, ctypes.byref(q), ctypes.byref(k), ctypes.byref(a),
                                              ctypes.byref(b), 1e-6, FAKE, FAKE, n, None), "overlap")
+
+
+@pytest.mark.parametrize("which", ["q", "k", "q_gain", "k_gain", "out", "k_out"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_tangents_are_refused(which, grad):
+    """A dual tensor's address leads to its values alone: the derivative would be lost."""
+    import torch
+    from torch.autograd import forward_ad
+    from paper_2608_02625_amd import Rope
+    rope = Rope(64)
+    t = dict(q=torch.randn(3, 2, 64), k=torch.randn(3, 2, 64), q_gain=torch.ones(64), k_gain=torch.ones(64),
+             out=torch.empty(3, 2, 64), k_out=torch.empty(3, 2, 64))
+    if which not in ("out", "k_out"):
+        t["out"] = t["k_out"] = None
+    if grad:
+        t["q"].requires_grad_()
+    pos = torch.arange(3, dtype=torch.int32)
+    with forward_ad.dual_level():
+        t[which] = forward_ad.make_dual(t[which], torch.ones_like(t[which]))
+        with pytest.raises(ValueError, match="tangent"):
+            rope.norm_apply(t["q"], t["k"], pos, t["q_gain"], t["k_gain"], out=t["out"], k_out=t["k_out"])
+        if which in ("q", "out"):
+            with pytest.raises(ValueError, match="tangent"):
+                rope.apply(t["q"], pos, out=t["out"])
+        # without one the refusal is that of a tensor on the host
+        with pytest.raises(ValueError, match="device tensor"):
+            rope.norm_apply(torch.randn(3, 2, 64), None, pos)
