@@ -72,7 +72,8 @@ __device__ __forceinline__ Raw<S, V, INTER> load_chunk(const S* src, int c, cons
     Raw<S, V, INTER> r{};
     if (c < ln.turn) {
         if constexpr (INTER) {
-            r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + 2 * V * c);
+            if constexpr (V == 1) r.x = __builtin_bit_cast(typename Raw<S, V, INTER>::X, load<STREAM, Pairs<S, V>>(src + 2 * V * c));
+            else r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + 2 * V * c);
         } else {
             r.x = load<STREAM, typename Raw<S, V, INTER>::X>(src + V * c);
             r.y = load<STREAM, typename Raw<S, V, INTER>::Y>(src + V * c + rot_dim / 2);
@@ -107,7 +108,7 @@ __device__ __forceinline__ void store_chunk(D* dst, int c, const NormLanes& ln, 
     constexpr int P = kPass<V, INTER>;
     if (c < ln.turn) {
         if constexpr (INTER) {
-            Vec<D, 2 * V> x;
+            Pairs<D, V> x;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 x.v[2 * i] = (D)a[i];

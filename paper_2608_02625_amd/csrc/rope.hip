@@ -28,7 +28,7 @@ __device__ __forceinline__ void turn_pairs(const S* src, D* dst, int o, int half
                                            const float (&s)[V], bool rotate) {
     float a[V], b[V];
     if constexpr (INTER) {
-        const auto x = load<STREAM, Vec<S, 2 * V>>(src + 2 * o);
+        const auto x = load<STREAM, Pairs<S, V>>(src + 2 * o);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             a[i] = to_f32(x.v[2 * i]);
@@ -51,7 +51,7 @@ __device__ __forceinline__ void turn_pairs(const S* src, D* dst, int o, int half
         }
     }
     if constexpr (INTER) {
-        Vec<D, 2 * V> x;
+        Pairs<D, V> x;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             x.v[2 * i] = (D)a[i];

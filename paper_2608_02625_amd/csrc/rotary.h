@@ -33,6 +33,14 @@ template <typename T, int N>
 struct alignas(sizeof(T) * N) Vec {
     T v[N];
 };
+// V neighbouring pairs.  A single one (V = 1) is what is left where rows lie anywhere, so it
+// asks for no more than its elements' alignment (pairs_per_access has checked wider ones).
+template <typename T, int V>
+struct alignas(sizeof(T) * (V == 1 ? 1 : 2 * V)) Pairs {
+    T v[2 * V];
+};
+static_assert(alignof(Pairs<__bf16, 1>) == 2 && alignof(Pairs<float, 1>) == 4, "a pair at an odd element");
+static_assert(alignof(Pairs<__bf16, 2>) == 8 && alignof(Pairs<float, 2>) == 16, "whole accesses");
 // One access; STREAM: past the caches' replacement.
 template <bool STREAM, typename V>
 __device__ __forceinline__ V load(const void* p) {
