@@ -211,7 +211,7 @@ std::string check_verify_sizes(int n_seqs, int total_rows, int vocab) {
     if (n_seqs < 1 || n_seqs > 65535) return "n_seqs must be in [1, 65535]";
     if (total_rows < 0 || total_rows > (1 << 20)) return "total_rows must be in [0, 2^20]";
     if (vocab < 1 || vocab > (1 << 24)) return "vocab must be in [1, 2^24]";
-    if (verify_workgroups(total_rows, vocab) > 0x7fffffff) return "total_rows * (vocab / 8192 + 2) must be below 2^31";
+    if (verify_workgroups(total_rows, vocab) > kVerifyMaxWorkgroups) return "total_rows * (vocab / 8192 + 2) must be below 2^31";
     return "";
 }
 

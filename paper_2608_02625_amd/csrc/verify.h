@@ -24,6 +24,19 @@ struct VerifyArgs {
     void* verdicts;
     double *sums, *rest, *inverse;
 };
+// A grid for n workgroups, counted along x first, the last ones idle: an axis takes fewer
+// than 2^32 threads, the second one at most 65535 workgroups.
+constexpr int kVerifyThreads = 256;
+struct VerifyGrid {
+    unsigned x, y;
+};
+constexpr VerifyGrid verify_grid(int64_t n) {
+    constexpr int64_t across = 1 << 16;
+    return {(unsigned)(n < across ? n : across), (unsigned)((n + across - 1) / across)};
+}
+constexpr int64_t kVerifyMaxWorkgroups = 0x7fffffff;
+static_assert((int64_t)verify_grid(kVerifyMaxWorkgroups).x * kVerifyThreads < (int64_t)1 << 32 &&
+              verify_grid(kVerifyMaxWorkgroups).y <= 65535, "every size that is taken can be launched");
 int64_t verify_workgroups(int total_rows, int vocab);
 size_t verify_workspace_bytes(int n_seqs, int total_rows, int vocab, bool draft);
 hipError_t launch_verify(VerifyArgs a, int dtype, void* ws, hipStream_t st);

@@ -35,7 +35,7 @@
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = kVerifyThreads, kWaves = kThreads / 64;
 constexpr int kChunk = 2048;                      // tokens of a chunk: 32 per lane of a wave, 8 per thread of a workgroup
 constexpr int kPer = kChunk / 64;
 
@@ -145,16 +145,17 @@ __device__ __forceinline__ int chunk_token(int v0, int i) {
 // m c would leave more than 2^(1/16) to correct.
 constexpr float kPlainExponent = 0x1p20f;
 
-// Four chunks of row blockIdx.x / groups, a wave each; blockIdx.y: target or draft.
+// Four chunks of a row, a wave each (verify_grid); blockIdx.z: target or draft.
 // A chunk is first taken as if its logits were ordinary.  A NaN among them makes the sum
 // one, +infinity the maximum, and then they are cleaned and summed again; -infinity needs
 // nothing (94 MB of bf16: 24.7 us where every value is cleaned first, 21.2 so).
 template <typename T, bool GREEDY>
 __global__ __launch_bounds__(kThreads) void stats_kernel(const VerifyArgs a, int chunks, int groups) {
-    const bool draft = blockIdx.y;
-    const int64_t r = blockIdx.x / (unsigned)groups;
-    const int ch = uniform((int)(blockIdx.x % (unsigned)groups) * kWaves + (int)(threadIdx.x >> 6));
-    if (ch >= chunks) return;
+    const bool draft = blockIdx.z;
+    const unsigned wg = blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t r = wg / (unsigned)groups;
+    const int ch = uniform((int)(wg % (unsigned)groups) * kWaves + (int)(threadIdx.x >> 6));
+    if (ch >= chunks || r >= a.total_rows) return;
     const T* row = (const T*)(draft ? a.draft : a.target) + r * (draft ? a.draft_stride : a.target_stride);
     const int v0 = ch * kChunk - row_offset(row);
     float z[kPer];
@@ -667,16 +668,22 @@ template <typename T>
 hipError_t verify_type(const VerifyArgs& a, hipStream_t st) {
     const int chunks = (int)row_chunks(a.vocab), groups = (int)row_groups(a.vocab), sets = a.draft ? 2 : 1;
     const bool greedy = a.c == 0.0;
+    // Each reads what those before it left: none runs behind one that was not launched.
+    hipError_t e = hipSuccess;
+    auto go = [&](auto kernel, dim3 grid, int threads, auto... more) {
+        if (e != hipSuccess) return;
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, st, a, chunks, more...);
+        e = hipGetLastError();
+    };
     if (a.total_rows > 0) {
-        const dim3 grid((unsigned)((int64_t)a.total_rows * groups), sets);
-        if (greedy) hipLaunchKernelGGL((stats_kernel<T, true>), grid, dim3(kThreads), 0, st, a, chunks, groups);
-        else hipLaunchKernelGGL((stats_kernel<T, false>), grid, dim3(kThreads), 0, st, a, chunks, groups);
+        const VerifyGrid g = verify_grid(verify_workgroups(a.total_rows, a.vocab));
+        go(greedy ? stats_kernel<T, true> : stats_kernel<T, false>, dim3(g.x, g.y, sets), kThreads, groups);
     }
-    hipLaunchKernelGGL((walk_kernel<T>), dim3(a.n_seqs), dim3(kWalkThreads), 0, st, a, chunks);
-    if (!greedy) hipLaunchKernelGGL((sums_kernel<T>), dim3(chunks, a.n_seqs, sets), dim3(kThreads), 0, st, a, chunks);
-    if (a.draft) hipLaunchKernelGGL((rest_kernel<T>), dim3(chunks, a.n_seqs), dim3(kThreads), 0, st, a, chunks);
-    hipLaunchKernelGGL((pick_kernel<T>), dim3(a.n_seqs), dim3(kThreads), 0, st, a, chunks);
-    return hipGetLastError();
+    go(walk_kernel<T>, dim3(a.n_seqs), kWalkThreads);
+    if (!greedy) go(sums_kernel<T>, dim3(chunks, a.n_seqs, sets), kThreads);
+    if (a.draft) go(rest_kernel<T>, dim3(chunks, a.n_seqs), kThreads);
+    go(pick_kernel<T>, dim3(a.n_seqs), kThreads);
+    return e;
 }
 // Workspace in order: parts, path, removed, verdicts, sums, rest and inverses.
 struct Sizes {
