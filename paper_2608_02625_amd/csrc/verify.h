@@ -8,6 +8,7 @@
 #include "../../include/dlm.h"
 
 constexpr int kVerifyMaxRows = 1024;     // a sequence's rows stand in one workgroup's LDS
+constexpr int kVerifyRowWords = kVerifyMaxRows / 32;
 
 struct VerifyArgs {
     int n_seqs, total_rows, max_rows, vocab;
@@ -20,7 +21,7 @@ struct VerifyArgs {
     int32_t *next, *keep, *keep_start;
     // workspace
     void* parts;
-    int32_t *path, *removed;
+    uint32_t *kept, *removed;            // a bit per row of a window, kVerifyRowWords per sequence
     void* verdicts;
     double *sums, *rest, *inverse;
 };

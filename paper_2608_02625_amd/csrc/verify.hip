@@ -50,7 +50,7 @@ struct Verdict {
     float mp, mq;                                 // maxima of the node's rows; mp -inf: nothing to draw from
     int32_t count, node, best;                    // kept rows; node; greedy's token
     int32_t rest;                                 // its child was rejected, with a draft
-    int32_t removed;                              // rejected certain tokens, from VerifyArgs::removed[start] on
+    int32_t removed;                              // certain tokens were rejected: VerifyArgs::removed
     int32_t unused;
 };
 
@@ -219,8 +219,10 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
     __shared__ double sum[2][kVerifyMaxRows], p[kVerifyMaxRows], q[kVerifyMaxRows];
     __shared__ float top[2][kVerifyMaxRows], zp[kVerifyMaxRows], zq[kVerifyMaxRows];
     __shared__ int best[kVerifyMaxRows], parent[kVerifyMaxRows], token[kVerifyMaxRows];
+    __shared__ uint32_t kept[kVerifyRowWords];
     __shared__ double lds[kWalkWaves];
     __shared__ int doubt;                         // the row at which the walk waits for exact sums (-1: it is done)
+    __shared__ int last;                          // the node that it has come to
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const Window w = window(a, b);
     const bool greedy = a.c == 0.0;
@@ -243,6 +245,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
         zp[tid] = known ? logit(target + (int64_t)up * a.target_stride, x) : -INFINITY;
         zq[tid] = known && a.draft ? logit(draft + (int64_t)up * a.draft_stride, x) : -INFINITY;
     }
+    if (tid < kVerifyRowWords) kept[tid] = tid == 0;      // row 0
     const int sets = a.draft ? 2 : 1;
     for (int x = wave; x < sets * w.n; x += kWalkWaves) {
         const int d = x >= w.n, i = d ? x - w.n : x;
@@ -294,12 +297,9 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
     chances(-1);
     // The first wave walks, a lane per row, 64 rows at a time: of the rows below the node at
     // hand the next one is tried, until there is none.
-    int* path = a.path + w.start;
-    int* removed = a.removed + w.start;
-    int at = 0, count = 1, rejected = 0, n_removed = 0, exact = -1, from = 1;           // exact: the node of float64 sums
+    int at = 0, count = 1, rejected = 0, exact = -1, from = 1;     // exact: the node of float64 sums
     double mass = 1.0;                            // what is left of the node's p
     bool done = false;
-    if (tid == 0) path[0] = 0;
     for (;;) {
         if (wave == 0) {
             int stop = -1;
@@ -321,9 +321,9 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
                     from = i0 + l + 1;
                     if ((__ballot(lhs < r) >> l) & 1) {
                         at = i0 + l;
-                        if (lane == 0) path[count] = at;
+                        if (lane == 0) kept[at >> 5] |= 1u << (at & 31);
                         ++count;
-                        rejected = n_removed = 0;
+                        rejected = 0;
                         mass = 1.0;
                         continue;
                     }
@@ -333,15 +333,13 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
                         break;
                     }
                     mass = fmax(mass - __shfl(r, l, 64), 0.0);
-                    const int x_l = token[i0 + l];
-                    if ((unsigned)x_l < (unsigned)a.vocab) {
-                        if (lane == 0) removed[n_removed] = x_l;
-                        ++n_removed;
-                    }
                 }
                 from = max(from, i0 + 64 < w.n && stop < 0 && !done ? i0 + 64 : from);
             }
-            if (lane == 0) doubt = stop;
+            if (lane == 0) {
+                doubt = stop;
+                last = at;
+            }
             if (stop >= 0) from = stop;
         }
         __syncthreads();
@@ -371,9 +369,15 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
                 if (parent[i] == node) mass = fmax(mass - p[i], 0.0);
         }
     }
+    // Without a draft every child of the last node has been rejected.
+    const bool gone = !a.draft && tid < w.n && parent[tid] == last && (unsigned)token[tid] < (unsigned)a.vocab;
+    const uint64_t votes = __ballot(gone);
+    if (lane < 2) a.removed[b * kVerifyRowWords + 2 * wave + lane] = (uint32_t)(votes >> (32 * lane));
+    if (tid < kVerifyRowWords) a.kept[b * kVerifyRowWords + tid] = kept[tid];
+    const int removed = __syncthreads_or(gone);
     if (tid) return;
     const bool any = sum[0][at] > 0.0;
-    *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, n_removed, 0};
+    *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, removed, 0};
 }
 
 // ------------------------------------------------------------------ sums, rest
@@ -387,19 +391,20 @@ __device__ __forceinline__ const T* node_row(const VerifyArgs& a, const Verdict&
 // A workgroup's thread of a chunk: kDraw tokens from v on, those that are gone at -infinity.
 constexpr int kDraw = kChunk / kThreads;
 template <typename T>
-__device__ __forceinline__ void load_target(const VerifyArgs& a, const Verdict& d, int start, const T* row, int v,
+__device__ __forceinline__ void load_target(const VerifyArgs& a, const Verdict& d, int b, const Window& w, const T* row, int v,
                                             float (&z)[kDraw]) {
     constexpr int E = Elems<T>::N;
 #pragma unroll
     for (int k = 0; k < kDraw / E; ++k) load_vector<T, false>(row, v + k * E, a.vocab, z + k * E);
 #pragma unroll
     for (int i = 0; i < kDraw; ++i) z[i] = clean(z[i]);
-    for (int j = 0; j < d.removed; ++j) {
-        const int x = a.removed[start + j];
+    for (int j = 0; d.removed && j < w.n; j += 32)
+        for (uint32_t bits = a.removed[b * kVerifyRowWords + (j >> 5)]; bits; bits &= bits - 1) {
+            const int x = a.tokens[w.start + j + __builtin_ctz(bits)];
 #pragma unroll
-        for (int i = 0; i < kDraw; ++i)
-            if (v + i == x) z[i] = -INFINITY;
-    }
+            for (int i = 0; i < kDraw; ++i)
+                if (v + i == x) z[i] = -INFINITY;
+        }
 }
 // The same tokens of the draft's row, whose vectors may lie otherwise.
 template <typename T>
@@ -437,7 +442,7 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs a, int 
     double s = 0.0;
     if (m > -INFINITY) {
         float z[kDraw];
-        load_target(a, d, w.start, row, v, z);            // with a draft nothing is gone
+        load_target(a, d, b, w, row, v, z);            // with a draft nothing is gone
 #pragma unroll
         for (int i = 0; i < kDraw; ++i) s += weight(z[i], m, a.c);
     }
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void rest_kernel(const VerifyArgs a, int 
     const T* prow = node_row<T>(a, d, w.start, false);
     const int v = ch * kChunk - row_offset(prow) + (int)threadIdx.x * kDraw;
     float z[kDraw], y[kDraw];
-    load_target(a, d, w.start, prow, v, z);
+    load_target(a, d, b, w, prow, v, z);
     load_draft(a, node_row<T>(a, d, w.start, true), v, y);
     const double ip = wave_inverse(a.sums + (int64_t)b * chunks, chunks);
     const double iq = wave_inverse(a.sums + ((int64_t)a.n_seqs + b) * chunks, chunks);
@@ -580,8 +585,14 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int 
         rest_total += part_total[i];
     }
     total_keep = min(total_keep, a.total_rows);
-    for (int i = tid; i < d.count; i += kThreads)
-        if (base + i < a.total_rows) a.keep[base + i] = a.path[w.start + i];
+    for (int i = tid; i < w.n; i += kThreads) {           // a kept row behind those before it
+        const uint32_t* kept = a.kept + b * kVerifyRowWords;
+        const uint32_t bits = kept[i >> 5];
+        if (!((bits >> (i & 31)) & 1)) continue;
+        int at = base + __popc(bits & ((1u << (i & 31)) - 1));
+        for (int x = 0; x < i >> 5; ++x) at += __popc(kept[x]);
+        if (at < a.total_rows) a.keep[at] = i;
+    }
     for (int64_t i = total_keep + (int64_t)b * kThreads + tid; i < a.total_rows; i += (int64_t)a.n_seqs * kThreads) a.keep[i] = -1;
     if (tid == 0) {
         a.keep_start[b] = min(base, a.total_rows);
@@ -626,7 +637,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int 
     for (int tries = 0; ch >= 0 && token < 0 && tries < chunks; ++tries, ch = ch + 1 == chunks ? 0 : ch + 1) {
         const int v = ch * kChunk - row_offset(prow) + tid * kDraw;
         float z[kDraw], y[kDraw];
-        load_target(a, d, w.start, prow, v, z);
+        load_target(a, d, b, w, prow, v, z);
         if (qrow) load_draft(a, qrow, v, y);
         double x[kDraw];
         own = 0.0;
@@ -685,13 +696,13 @@ hipError_t verify_type(const VerifyArgs& a, hipStream_t st) {
     go(pick_kernel<T>, dim3(a.n_seqs), kThreads);
     return e;
 }
-// Workspace in order: parts, path, removed, verdicts, sums, rest and inverses.
+// Workspace in order: parts, kept, removed, verdicts, sums, rest and inverses.
 struct Sizes {
     size_t parts, rows, verdicts, sums, rest;
     Sizes(int n_seqs, int total_rows, int vocab, bool draft) {
         const size_t chunks = row_chunks(vocab), sets = draft ? 2 : 1;
         parts = round256(sets * total_rows * chunks * sizeof(Part));
-        rows = round256((size_t)total_rows * 4);
+        rows = round256((size_t)n_seqs * kVerifyRowWords * 4);
         verdicts = round256((size_t)n_seqs * sizeof(Verdict));
         sums = round256(sets * n_seqs * chunks * 8);
         rest = draft ? round256((size_t)n_seqs * chunks * 8) + round256((size_t)n_seqs * 16) : 0;
@@ -711,8 +722,8 @@ hipError_t launch_verify(VerifyArgs a, int dtype, void* ws, hipStream_t st) {
     const Sizes z(a.n_seqs, a.total_rows, a.vocab, a.draft != nullptr);
     char* at = (char*)ws;
     a.parts = at;
-    a.path = (int32_t*)(at += z.parts);
-    a.removed = (int32_t*)(at += z.rows);
+    a.kept = (uint32_t*)(at += z.parts);
+    a.removed = (uint32_t*)(at += z.rows);
     a.verdicts = at += z.rows;
     a.sums = (double*)(at += z.verdicts);
     a.rest = (double*)(at += z.sums);
