@@ -50,8 +50,7 @@ struct Verdict {
     float mp, mq;                                 // maxima of the node's rows; mp -inf: nothing to draw from
     int32_t count, node, best;                    // kept rows; node; greedy's token
     int32_t rest;                                 // its child was rejected, with a draft
-    int32_t removed;                              // certain tokens were rejected: VerifyArgs::removed
-    int32_t unused;
+    int32_t unused[2];
 };
 
 template <typename T>
@@ -228,7 +227,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
     const bool greedy = a.c == 0.0;
     Verdict* out = (Verdict*)a.verdicts + b;
     if (w.n == 0) {
-        if (tid == 0) *out = Verdict{-INFINITY, 0.f, 0, 0, -1, 0, 0, 0};
+        if (tid == 0) *out = Verdict{-INFINITY, 0.f, 0, 0, -1, 0, {}};
         return;
     }
     const T *target = (const T*)a.target + (int64_t)w.start * a.target_stride;
@@ -369,15 +368,14 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
                 if (parent[i] == node) mass = fmax(mass - p[i], 0.0);
         }
     }
-    // Without a draft every child of the last node has been rejected.
-    const bool gone = !a.draft && tid < w.n && parent[tid] == last && (unsigned)token[tid] < (unsigned)a.vocab;
-    const uint64_t votes = __ballot(gone);
-    if (lane < 2) a.removed[b * kVerifyRowWords + 2 * wave + lane] = (uint32_t)(votes >> (32 * lane));
-    if (tid < kVerifyRowWords) a.kept[b * kVerifyRowWords + tid] = kept[tid];
-    const int removed = __syncthreads_or(gone);
+    if (!a.draft) {                               // every child of the last node has been rejected
+        const uint64_t gone = __ballot(tid < w.n && parent[tid] == last && (unsigned)token[tid] < (unsigned)a.vocab);
+        if (wave * 64 < w.n && lane < 2) a.removed[b * kVerifyRowWords + 2 * wave + lane] = (uint32_t)(gone >> (32 * lane));
+    }
+    if (tid * 32 < w.n) a.kept[b * kVerifyRowWords + tid] = kept[tid];
     if (tid) return;
     const bool any = sum[0][at] > 0.0;
-    *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, removed, 0};
+    *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, {}};
 }
 
 // ------------------------------------------------------------------ sums, rest
@@ -391,14 +389,14 @@ __device__ __forceinline__ const T* node_row(const VerifyArgs& a, const Verdict&
 // A workgroup's thread of a chunk: kDraw tokens from v on, those that are gone at -infinity.
 constexpr int kDraw = kChunk / kThreads;
 template <typename T>
-__device__ __forceinline__ void load_target(const VerifyArgs& a, const Verdict& d, int b, const Window& w, const T* row, int v,
+__device__ __forceinline__ void load_target(const VerifyArgs& a, int b, const Window& w, const T* row, int v,
                                             float (&z)[kDraw]) {
     constexpr int E = Elems<T>::N;
 #pragma unroll
     for (int k = 0; k < kDraw / E; ++k) load_vector<T, false>(row, v + k * E, a.vocab, z + k * E);
 #pragma unroll
     for (int i = 0; i < kDraw; ++i) z[i] = clean(z[i]);
-    for (int j = 0; d.removed && j < w.n; j += 32)
+    for (int j = 0; !a.draft && j < w.n; j += 32)
         for (uint32_t bits = a.removed[b * kVerifyRowWords + (j >> 5)]; bits; bits &= bits - 1) {
             const int x = a.tokens[w.start + j + __builtin_ctz(bits)];
 #pragma unroll
@@ -442,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(const VerifyArgs a, int 
     double s = 0.0;
     if (m > -INFINITY) {
         float z[kDraw];
-        load_target(a, d, b, w, row, v, z);            // with a draft nothing is gone
+        load_target(a, b, w, row, v, z);            // with a draft nothing is gone
 #pragma unroll
         for (int i = 0; i < kDraw; ++i) s += weight(z[i], m, a.c);
     }
@@ -468,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void rest_kernel(const VerifyArgs a, int 
     const T* prow = node_row<T>(a, d, w.start, false);
     const int v = ch * kChunk - row_offset(prow) + (int)threadIdx.x * kDraw;
     float z[kDraw], y[kDraw];
-    load_target(a, d, b, w, prow, v, z);
+    load_target(a, b, w, prow, v, z);
     load_draft(a, node_row<T>(a, d, w.start, true), v, y);
     const double ip = wave_inverse(a.sums + (int64_t)b * chunks, chunks);
     const double iq = wave_inverse(a.sums + ((int64_t)a.n_seqs + b) * chunks, chunks);
@@ -637,7 +635,7 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(const VerifyArgs a, int 
     for (int tries = 0; ch >= 0 && token < 0 && tries < chunks; ++tries, ch = ch + 1 == chunks ? 0 : ch + 1) {
         const int v = ch * kChunk - row_offset(prow) + tid * kDraw;
         float z[kDraw], y[kDraw];
-        load_target(a, d, b, w, prow, v, z);
+        load_target(a, b, w, prow, v, z);
         if (qrow) load_draft(a, qrow, v, y);
         double x[kDraw];
         own = 0.0;
