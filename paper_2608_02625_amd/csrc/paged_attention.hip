@@ -1576,8 +1576,12 @@ bool may_share(int max_rows, int max_group_rows, int group) {
 // 16 heads of 64: n 16, 512 8.1 / 11.7, 1024 13.2 / 12.1, 2048 17.3 / 12.3.
 bool shares(const AttnArgs& a, int max_group_rows) {
     if (!may_share(a.max_rows, max_group_rows, a.group)) return false;
+    // join_rows_kernel has a workgroup per row and some of its heads; an axis takes fewer than
+    // 2^32 threads.
+    if (a.total_rows >= (1 << 24)) return false;
     const double values = (double)a.total_rows * a.n_heads * a.c.head_dim;
-    const double windows = ((double)a.total_rows + a.max_rows - 1) / a.max_rows;
+    // Rows may be more than the windows have: no more of them than sequences.
+    const double windows = std::min(((double)a.total_rows + a.max_rows - 1) / a.max_rows, (double)a.c.n_seqs);
     return windows * a.max_keys * (4. * a.c.n_kv * a.c.head_dim) >= 48e6 + 1000. * values;
 }
 size_t row_bytes(int total_rows, int n_heads, int head_dim) {
