@@ -596,6 +596,8 @@ dlm_status dlm_cache_attend(const dlm_cache* cache, int32_t layer, const int32_t
  * is found in their tables: the pages at the front that all of them name and count whole,
  * in multiples of 32 tokens.  max_group_rows: an upper bound of the rows of a group that the
  * caller vouches for; a group of more rows shares nothing, nor does one with a single member.
+ * Where windows can share (max_rows times query heads per key head up to 128), n_seqs * n_heads *
+ * max_group_rows <= 2^33.
  * d_share (dlm_cache_share_bytes(cache, total_rows) bytes, 256-byte aligned) takes what was
  * found.  It holds for these row starts as long as lengths and tables stay as they are, that
  * is for all layers of a pass: make it after reserve.

@@ -72,6 +72,9 @@ hipError_t launch_attend(const CacheArgs& c, int dtype, int layer, const int32_t
 size_t share_bytes(int n_seqs, int total_rows);
 hipError_t launch_share(const CacheArgs& c, const int32_t* row_start, int total_rows, int max_rows, const int32_t* group,
                         int max_group_rows, int32_t* share, hipStream_t st);
+// Whether a call could share at all: windows of more packed rows fill their workgroups' tiles
+// by themselves.
+bool attend_may_share(int max_rows, int max_group_rows, int group);
 size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int max_group_rows,
                                      int group);
 hipError_t launch_attend_shared(const CacheArgs& c, int dtype, int layer, const int32_t* row_start, int total_rows,

@@ -495,7 +495,9 @@ dlm_status dlm_cache_attend_shared(const dlm_cache* cache, int32_t layer, const 
         const int rows = std::min(max_rows, total_rows), group = n_heads / cache->n_kv_heads;
         TRY(check_share(*cache, total_rows, max_group_rows, d_share, bytes));
         const int group_rows = std::min(max_group_rows, total_rows);
-        const std::string bad = dlm_internal_check_windows(*cache, n_heads, group_rows);
+        // A group's rows are counted together where they could share: as a window of so many.
+        const std::string bad = attend_may_share(rows, group_rows, group)
+                                    ? dlm_internal_check_windows(*cache, n_heads, group_rows) : "";
         if (!bad.empty()) return fail(DLM_ERR_INVALID_ARG, bad);
         TRY(check_workspace(d_workspace, workspace_bytes,
                             attend_shared_workspace_bytes(cache->n_seqs, cache->n_kv_heads, cache->head_dim, total_rows, rows,

@@ -1560,11 +1560,6 @@ Shape prefix_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int max_g
 Shape own_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int group, int max_keys) {
     return shape_for(max_rows, group, item_bound(n_seqs, n_kv, total_rows, max_rows, group, kManyRows), max_keys);
 }
-// Whether a call could share at all: windows of more packed rows fill their workgroups' tiles
-// by themselves.
-bool may_share(int max_rows, int max_group_rows, int group) {
-    return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows;
-}
 // Whether it pays.  What it saves are bytes: without it every sequence reads its keys, most
 // of them from the caches.  What it costs are a join that is always there, and each row's
 // values out and in again.  So: the keys of as many sequences as there are windows of
@@ -1575,7 +1570,7 @@ bool may_share(int max_rows, int max_group_rows, int group) {
 // 16, 4096 19.2 / 21.2, 16384 43.1 / 34.0; 12 rows each, 4096 30.2 / 38.0, 16384 68.4 / 55.4.
 // 16 heads of 64: n 16, 512 8.1 / 11.7, 1024 13.2 / 12.1, 2048 17.3 / 12.3.
 bool shares(const AttnArgs& a, int max_group_rows) {
-    if (!may_share(a.max_rows, max_group_rows, a.group)) return false;
+    if (!attend_may_share(a.max_rows, max_group_rows, a.group)) return false;
     // join_rows_kernel has a workgroup per row and some of its heads; an axis takes fewer than
     // 2^32 threads.
     if (a.total_rows >= (1 << 24)) return false;
@@ -1613,10 +1608,14 @@ hipError_t launch_share(const CacheArgs& c, const int32_t* row_start, int total_
     return hipGetLastError();
 }
 
+bool attend_may_share(int max_rows, int max_group_rows, int group) {
+    return max_group_rows > max_rows && (int64_t)max_rows * group <= kManyRows;
+}
+
 size_t attend_shared_workspace_bytes(int n_seqs, int n_kv, int head_dim, int total_rows, int max_rows, int max_group_rows,
                                      int group) {
     const size_t own = attend_workspace_bytes(n_seqs, n_kv, head_dim, total_rows, max_rows, group);
-    if (!may_share(max_rows, max_group_rows, group)) return own;
+    if (!attend_may_share(max_rows, max_group_rows, group)) return own;
     return own + parts_bytes(prefix_shape(n_seqs, n_kv, total_rows, max_rows, max_group_rows, group, 0), head_dim) +
            2 * (row_bytes(total_rows, n_kv * group, head_dim) + round256((size_t)n_seqs * sizeof(int4)));
 }
