@@ -7,7 +7,8 @@
 //
 //   stats    every row of target and draft in chunks of kChunk tokens, a wave each:
 //            maximum and float32 sum
-//   walk     a workgroup per sequence: rows' totals, drafted tokens' p and q, the path
+//   walk     a workgroup per sequence: rows' totals, drafted tokens' p and q, the path (kept and
+//            rejected rows as bits of the sequence: windows may lie over each other)
 //   sums     float64 sums by chunk of the rows that the next token is drawn from
 //   rest     with a draft: float64 sums of max(p - q, 0) by chunk, where one was rejected
 //   pick     a workgroup per sequence: the next token from chunk sums and one chunk; the
@@ -16,7 +17,8 @@
 // A token is drawn where a running sum over the vocabulary passes a border, and float32
 // sums over 157184 tokens move the borders by more than many tokens weigh: so the sums of
 // the one row (or pair) that a sequence draws from are float64, of float64 powers (2^t
-// reduced to half around the nearest integer, its series to the 11th power, off by 6e-15).
+// reduced to half around the nearest integer, its series to the 11th power, off by at most 9e-15
+// of it).
 // Whether a drafted token is kept is a single comparison, which float32 sums decide but
 // for one in 10^5: when both sides are that near the walk works the row's sum out in
 // float64 itself.  Float64 for every row would be bound by its arithmetic (32 chains of up
@@ -218,7 +220,6 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
     __shared__ double sum[2][kVerifyMaxRows], p[kVerifyMaxRows], q[kVerifyMaxRows];
     __shared__ float top[2][kVerifyMaxRows], zp[kVerifyMaxRows], zq[kVerifyMaxRows];
     __shared__ int best[kVerifyMaxRows], parent[kVerifyMaxRows], token[kVerifyMaxRows];
-    __shared__ uint32_t kept[kVerifyRowWords];
     __shared__ double lds[kWalkWaves];
     __shared__ int doubt;                         // the row at which the walk waits for exact sums (-1: it is done)
     __shared__ int last;                          // the node that it has come to
@@ -244,7 +245,6 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
         zp[tid] = known ? logit(target + (int64_t)up * a.target_stride, x) : -INFINITY;
         zq[tid] = known && a.draft ? logit(draft + (int64_t)up * a.draft_stride, x) : -INFINITY;
     }
-    if (tid < kVerifyRowWords) kept[tid] = tid == 0;      // row 0
     const int sets = a.draft ? 2 : 1;
     for (int x = wave; x < sets * w.n; x += kWalkWaves) {
         const int d = x >= w.n, i = d ? x - w.n : x;
@@ -298,6 +298,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
     // hand the next one is tried, until there is none.
     int at = 0, count = 1, rejected = 0, exact = -1, from = 1;     // exact: the node of float64 sums
     double mass = 1.0;                            // what is left of the node's p
+    uint32_t kept = tid == 0;                     // of rows 32 lane .. 32 lane + 31, row 0 among them
     bool done = false;
     for (;;) {
         if (wave == 0) {
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
                     from = i0 + l + 1;
                     if ((__ballot(lhs < r) >> l) & 1) {
                         at = i0 + l;
-                        if (lane == 0) kept[at >> 5] |= 1u << (at & 31);
+                        kept |= lane == at >> 5 ? 1u << (at & 31) : 0u;
                         ++count;
                         rejected = 0;
                         mass = 1.0;
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(const VerifyArgs a, 
         const uint64_t gone = __ballot(tid < w.n && parent[tid] == last && (unsigned)token[tid] < (unsigned)a.vocab);
         if (wave * 64 < w.n && lane < 2) a.removed[b * kVerifyRowWords + 2 * wave + lane] = (uint32_t)(gone >> (32 * lane));
     }
-    if (tid * 32 < w.n) a.kept[b * kVerifyRowWords + tid] = kept[tid];
+    if (tid * 32 < w.n) a.kept[b * kVerifyRowWords + tid] = kept;
     if (tid) return;
     const bool any = sum[0][at] > 0.0;
     *out = Verdict{any ? top[0][at] : -INFINITY, a.draft ? top[1][at] : 0.f, count, at, best[at], a.draft && rejected, {}};
