@@ -679,7 +679,9 @@ dlm_status dlm_cache_step(dlm_model* m, const dlm_cache* cache, const int32_t* d
 
 /*
  * dlm_cache_step with every row's logits, float [total_rows][vocab] in d_logits (not
- * NULL), for what the vocabulary reduction does not answer: verification, sampling.
+ * NULL), for what the vocabulary reduction does not answer: verification, sampling.  They are
+ * a second product of the same sums in the same order: d_max_logit is the largest of a row's
+ * logits bit for bit, and d_top1 the first token that has it.
  */
 dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int32_t* d_row_start, int32_t total_rows,
                                  int32_t max_rows, int32_t max_keys, const int32_t* d_tokens, const int32_t* d_pos,
@@ -703,18 +705,22 @@ dlm_status dlm_cache_step_logits(dlm_model* m, const dlm_cache* cache, const int
  *
  * From row 0 on, the children of the row r at hand are tried in order of their rows.  Child
  * i with token x = d_tokens[..i] is kept if d_u[..i] q_r(x) < p_r(x), and then is the row at
- * hand; if not, p_r becomes max(p_r - q_r, 0) over its sum (certain drafts: p_r without x,
- * over its sum; p_r as it is where less than 2^-43 is left, which is rounding).  When no child is left, d_next[s] is
- * drawn from p_r: the first v at which the running sum passes d_u_next[s] times the whole.
+ * hand; if not, p_r becomes max(p_r - q_r, 0) over its sum, or stays as it is where less than
+ * 2^-43 of that is left, which is rounding (certain drafts: p_r without x, over its sum).  When
+ * no child is left, d_next[s] is drawn from p_r: the first v at which the running sum passes
+ * d_u_next[s] times the whole.
  * d_u float [total_rows] and d_u_next float [n_seqs] hold numbers in [0, 1) (others are read
- * as if cut off to it); entries of rows 0 are not read.  temperature is
- * from 1e-30 to 1e30, or 0: p_r is 1 for the largest logit (the lowest such v), and d_draft is not read.  A token outside [0, vocab) is
- * never kept.  Logits: -infinity and NaN are chances of 0, +infinity counts as the largest
+ * as if cut off to it); entries of rows 0 are not read.  temperature is from 1e-30 to 1e30, or
+ * 0: p_r is 1 for the largest logit (the lowest such v), and d_draft is not read.  A token
+ * outside [0, vocab) is never kept.  Logits: -infinity and NaN are chances of 0, +infinity counts as the largest
  * float32.  Where a row has no chance above 0, d_next is -1, as for a sequence without rows.
  *
  * d_keep int32 [total_rows]: the kept rows of each window, row 0 among them, sequence after
  * sequence, -1 behind them; d_keep_start int32 [n_seqs + 1]: where each begins.  Both are
- * what dlm_cache_commit takes.  Sums are float64.
+ * what dlm_cache_commit takes.  Windows over each other are verified each as if it stood alone;
+ * if they keep more than total_rows rows together, the list ends there.
+ * The next token is drawn by float64 sums of float64 powers.  Whether a token is kept is
+ * decided by float32 sums, and by float64 ones where both sides are within 1e-5 of each other.
  * Limits: n_seqs <= 65535; total_rows <= 2^20; max_rows <= 1024 (later rows of a window are
  * not read); vocab <= 2^24; total_rows * (vocab / 8192 + 2) < 2^31.  d_workspace:
  * dlm_verify_workspace_bytes, 256-byte aligned; it keeps nothing between calls, and calls

@@ -1545,7 +1545,9 @@ __global__ __launch_bounds__(1024) void share_kernel(CacheArgs c, const int32_t*
         for (int i = 0; in && i < n; ++i) out[w.rows + list + off + i] = start + i;
 }
 
-// Units aimed at where prefixes and own keys share a launch: the workgroups that the chip holds.
+// Units aimed at where prefixes and own keys share a launch: two per CU, the workgroups that the
+// chip holds with heads of 128 (64 sequences behind 16384 shared tokens: 384 to 640 cost the
+// same); with heads of 64 it holds four per CU.
 constexpr int kBothUnits = 512;
 // A group has at least two sequences.
 int most_groups(int n_seqs) { return std::max(n_seqs / 2, 1); }
@@ -1565,7 +1567,8 @@ Shape own_shape(int n_seqs, int n_kv, int total_rows, int max_rows, int group, i
 // values out and in again.  So: the keys of as many sequences as there are windows of
 // max_rows, against 48 MB and 1000 bytes for each value of the result.  Plain / shared, us,
 // bf16, a group of n sequences with 40 tokens of their own.  16 heads of 128 on 4, a row
-// each: n 4, 2048 shared tokens 10.6 / 12.4, 16384 22.3 / 18.1; n 16, 2048 13.5 / 15.2, 4096
+// each: n 4, 2048 shared tokens 10.2 / 11.8, 4096 13.4 / 12.6, 6144 16.0 / 13.0 (not shared: the
+// line is too high for so few), 8192 15.1 / 14.0, 16384 22.3 / 18.1; n 16, 2048 13.5 / 15.2, 4096
 // 18.5 / 15.6; n 64, 1024 16.6 / 18.0, 2048 22.8 / 18.9, 4096 35.6 / 21.6; 4 rows each, n
 // 16, 4096 19.2 / 21.2, 16384 43.1 / 34.0; 12 rows each, 4096 30.2 / 38.0, 16384 68.4 / 55.4.
 // 16 heads of 64: n 16, 512 8.1 / 11.7, 1024 13.2 / 12.1, 2048 17.3 / 12.3.

@@ -253,7 +253,7 @@ class Refiner:
         the window rows that a row sees (default: all of its window's).  Returns (top-1
         int32, confidence float, max logit float), each [rows]; at most 65536 rows, none is
         a pass with nothing to do.  logits: float32 [rows, vocab], takes every row's logits
-        (what verify asks for).  Calls of one model share workspaces (kept, so that
+        (what verify asks for), by a second product with the vocabulary.  Calls of one model share workspaces (kept, so that
         captured graphs stay valid): order them on one stream."""
         T = tokens.numel()
         if cache.device.index != (self.device.index if self.device.index is not None else torch.cuda.current_device()):
